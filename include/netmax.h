@@ -275,6 +275,81 @@ int netmax_consensus_dist(netmax_ctx *ctx, double *out_host);
 #define NETMAX_STATIC_MAX_LD ((int64_t)NETMAX_STATIC_PARTIALS * 1024)
 int netmax_consensus_dist_static(int32_t M, int64_t D, int64_t ld, const float *x_dev, double *cd_dev, void *stream);
 
+/* ---- Operators for language models --------------------------------------------------------------------------
+ * What a worker's local step on a language model needs beside the perceptron of netmax_local_step: linear layers with an
+ * epilogue, losses on the log probabilities of sampled tokens, and an orthogonalised update that netmax_mix can take as its
+ * gradient.  These calls need no context and allocate nothing: the caller passes the stream (NULL = the null stream) of the
+ * current device and a workspace, device memory, 256-byte aligned, of the size that the call's ..._workspace function gives (a host
+ * function; -1 if the arguments are refused; 0: work may be NULL).  A workspace holds nothing between calls and may be used again by
+ * the next call on the same stream.  Every call enqueues its kernels and returns without waiting.  Texts of errors:
+ * netmax_last_error(NULL).  Matrices are row-major with rows `ld` elements apart and, in a batch, `s` elements from one matrix to the
+ * next (0: the same one for all, for inputs); vectors of a batch lie `s` apart.  Sums are held in float or more and the results rounded once. */
+typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NETMAX_ACT_SILU = 3 } netmax_act; /* GELU: the error function's */
+
+typedef struct {
+    int64_t batch;          /* layers, e.g. one per worker: 0 .. 65535 */
+    int64_t rows;           /* tokens per layer, >= 0 */
+    int64_t d_in, d_out;    /* >= 1 */
+    int32_t dtype;          /* netmax_dtype of all matrices and vectors */
+    int32_t act;            /* netmax_act */
+    int64_t ldx, ldw, ldr, ldy, ldz;            /* rows of x, w, residual, y (and dy), z */
+    int64_t sx, sw, sb, sr, sy, sz;             /* x, w, bias, residual, y (and dy), z of a batch */
+    int64_t lddx, lddw, sdx, sdw, sdb;          /* gradients: rows of dx, dw; dx, dw, db of a batch */
+} netmax_linear_shape;
+
+/* y = act(z) + residual, z = x w + bias, for every layer of the batch: x [rows][d_in], w [d_in][d_out] (the layout of a perceptron's W),
+ * bias [d_out], residual and y [rows][d_out].  bias and residual may be NULL; z may be NULL or receives z, which netmax_linear_grad needs.
+ * y may be the residual's memory with the residual's strides. */
+int64_t netmax_linear_workspace(const netmax_linear_shape *shape);
+int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w, const void *bias, const void *residual, void *y, void *z,
+                  void *work, int64_t work_bytes, void *stream);
+
+/* The gradients of that layer from dy = dl/dy (which is the residual's gradient, too): with dz = dy act'(z) (ReLU's derivative at 0 is 0),
+ * dx = dz w^T, dw = x^T dz, db = the sum of dz over the rows; each may be NULL.  z as netmax_linear left it, NULL for NETMAX_ACT_NONE.
+ * bfloat16: dz is rounded to bfloat16 for the products, as the errors of a perceptron are; db sums it before that.  rows = 0 gives dw = 0 and db = 0.
+ * Results of the same call are the same bits every time. */
+int64_t netmax_linear_grad_workspace(const netmax_linear_shape *shape);
+int netmax_linear_grad(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w, const void *z, void *dx, void *dw, void *db,
+                       void *work, int64_t work_bytes, void *stream);
+
+typedef struct {
+    int64_t batch;          /* matrices, e.g. one per worker: 0 .. 65535 */
+    int64_t rows, cols;     /* >= 1 */
+    int32_t dtype;          /* netmax_dtype of g and out; the momentum is float */
+    int32_t steps;          /* Newton-Schulz products, 1 .. 64 */
+    int32_t nesterov;
+    float mu, a, b, c, eps, scale;              /* eps > 0 */
+    int64_t ldg, sg, ldm, sm, ldo, so;          /* g, m (and m_out), out */
+} netmax_orth_shape;
+
+/* An orthogonalised momentum step for every matrix of the batch: m_out = mu m + g, u = g + mu m_out (nesterov) or m_out,
+ * X = u / max(||u||_F, eps), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X, out = scale X.  With (3.4445, -4.7750, 2.0315) and five
+ * steps the singular values end near 1.  m and m_out may be the same memory; both NULL: u = g.  out may be g's memory with g's strides.
+ * To mix such updates: write them to g (tile layout, netmax_pack) of a context with momentum 0 and call netmax_mix. */
+int64_t netmax_orthogonalize_workspace(const netmax_orth_shape *shape);
+int netmax_orthogonalize(const netmax_orth_shape *shape, const void *g, const float *m, float *m_out, void *out, void *work, int64_t work_bytes, void *stream);
+
+/* The clipped policy loss with a KL term on the logits of sampled tokens, and the gradient of the sum of all losses by the logits.
+ * For a token with logits z, label y, log p = z_y - log sum exp z and r = exp(log p - old_logp):
+ *     loss = weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(d) - d - 1)),   d = ref_logp - log p
+ * (where both terms of the minimum are equal, the gradient is the unclipped one's).  logits [tokens][vocab], dtype, rows ld apart; labels int32,
+ * all others float [tokens].  weight may be NULL (all 1); a token whose weight is 0 or whose label is outside 0 .. vocab - 1 has loss, logp and
+ * gradient 0, and its logits are not looked at.  Logits of -inf have probability 0; so has all of a row that holds nothing else.  ref_logp may be NULL if
+ * kl is 0.  logp [tokens] and grad [tokens][vocab] (dtype, rows ldg apart) may be NULL; grad may be the logits' memory.  All on the device. */
+int netmax_policy_loss(int64_t tokens, int64_t vocab, int32_t dtype, const void *logits, int64_t ld, const int32_t *labels, const float *old_logp,
+                       const float *ref_logp, const float *advantage, const float *weight, float clip_low, float clip_high, float kl, float *loss,
+                       float *logp, void *grad, int64_t ldg, void *stream);
+
+/* The loss of paired log ratios: sequence q holds tokens offsets[q] .. offsets[q + 1] - 1 (offsets: device int32 [2 pairs + 1], not decreasing),
+ * sequence 2 p is the chosen one of pair p and 2 p + 1 the rejected one.  With R_q = sum over its tokens of weight (log p - ref_logp) and
+ * h = beta (R_2p - R_2p+1):   loss[p] = scale (-(1 - smoothing) log sigma(h) - smoothing log sigma(-h)),   ratio[q] = R_q.
+ * Logits, labels, weight and grad as for netmax_policy_loss (the gradient of the sum of loss[p]); tokens outside of all sequences have gradient 0;
+ * an empty sequence has R_q = 0.  The sums over a sequence are taken in double, in a fixed order. */
+int64_t netmax_preference_workspace(int64_t tokens, int64_t pairs);
+int netmax_preference_loss(int64_t tokens, int64_t vocab, int32_t dtype, const void *logits, int64_t ld, const int32_t *labels, int64_t pairs,
+                           const int32_t *offsets, const float *ref_logp, const float *weight, float beta, float smoothing, float scale, float *loss,
+                           float *ratio, void *grad, int64_t ldg, void *work, int64_t work_bytes, void *stream);
+
 /* Device pointer of the current parameters x^t (one of x_a, x_b; tile layout), NULL if nothing is bound. */
 const float *netmax_params(const netmax_ctx *ctx);
 

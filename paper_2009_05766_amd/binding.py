@@ -21,12 +21,15 @@ NETMAX_OK, NETMAX_EINVAL, NETMAX_EINFEASIBLE, NETMAX_ESTATE, NETMAX_EDEVICE, NET
 NETMAX_FLAT, NETMAX_MLP = 0, 1
 NETMAX_F32, NETMAX_BF16 = 0, 1
 NETMAX_MIX_POLICY, NETMAX_MIX_FIXED = 0, 1
+NETMAX_ACT_NONE, NETMAX_ACT_RELU, NETMAX_ACT_GELU, NETMAX_ACT_SILU = range(4)
 
 EXPORTS = (
     "netmax_init", "netmax_build_tables", "netmax_generate_policy", "netmax_set_policy", "netmax_set_lr", "netmax_bind_state",
     "netmax_bind_data", "netmax_pack", "netmax_unpack", "netmax_unpack_zeroed", "netmax_sample_peers", "netmax_sample_batch", "netmax_local_step", "netmax_mix", "netmax_run", "netmax_update_times", "netmax_update_times_async", "netmax_activity", "netmax_mean_times", "netmax_set_activity", "netmax_async_run", "netmax_set_fusion", "netmax_set_barrier_patience",
     "netmax_consensus_dist", "netmax_consensus_dist_static", "netmax_params", "netmax_losses", "netmax_read_losses", "netmax_read_hidden", "netmax_iteration", "netmax_get_tables",
     "netmax_last_error", "netmax_destroy",
+    "netmax_linear_workspace", "netmax_linear", "netmax_linear_grad_workspace", "netmax_linear_grad", "netmax_orthogonalize_workspace",
+    "netmax_orthogonalize", "netmax_policy_loss", "netmax_preference_workspace", "netmax_preference_loss",
 )
 
 
@@ -47,6 +50,18 @@ class netmax_config(C.Structure):
         ("P", C.c_void_p), ("adj", C.c_void_p), ("stream", C.c_void_p),
         ("mix_mode", C.c_int32), ("fixed_weight", C.c_float),
     ]
+
+
+class netmax_linear_shape(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("batch", "rows", "d_in", "d_out")] + [("dtype", C.c_int32), ("act", C.c_int32)] +
+                [(n, C.c_int64) for n in ("ldx", "ldw", "ldr", "ldy", "ldz", "sx", "sw", "sb", "sr", "sy", "sz",
+                                          "lddx", "lddw", "sdx", "sdw", "sdb")])
+
+
+class netmax_orth_shape(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("batch", "rows", "cols")] + [(n, C.c_int32) for n in ("dtype", "steps", "nesterov")] +
+                [(n, C.c_float) for n in ("mu", "a", "b", "c", "eps", "scale")] +
+                [(n, C.c_int64) for n in ("ldg", "sg", "ldm", "sm", "ldo", "so")])
 
 
 _lib = None
@@ -99,6 +114,15 @@ def load():
         "netmax_get_tables": (C.c_int, [vp, vp, vp, vp]),
         "netmax_last_error": (C.c_char_p, [vp]),
         "netmax_destroy": (C.c_int, [vp]),
+        "netmax_linear_workspace": (i64, [C.POINTER(netmax_linear_shape)]),
+        "netmax_linear": (C.c_int, [C.POINTER(netmax_linear_shape)] + [vp] * 7 + [i64, vp]),
+        "netmax_linear_grad_workspace": (i64, [C.POINTER(netmax_linear_shape)]),
+        "netmax_linear_grad": (C.c_int, [C.POINTER(netmax_linear_shape)] + [vp] * 8 + [i64, vp]),
+        "netmax_orthogonalize_workspace": (i64, [C.POINTER(netmax_orth_shape)]),
+        "netmax_orthogonalize": (C.c_int, [C.POINTER(netmax_orth_shape)] + [vp] * 5 + [i64, vp]),
+        "netmax_policy_loss": (C.c_int, [i64, i64, i32, vp, i64, vp, vp, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp]),
+        "netmax_preference_workspace": (i64, [i64, i64]),
+        "netmax_preference_loss": (C.c_int, [i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)

@@ -1,0 +1,114 @@
+// Matrix products C = A B of the operators for language models: operands, epilogues and launchers.
+//
+// A is [M][K] and B [K][N]; either may be stored with its contraction index K next to each other in memory ("k_near") or
+// with M (of A), N (of B) next to each other.  ld: elements from one stored row to the next; step: from one matrix of the
+// batch to the next.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "bf16.h"
+#include "vec.h"
+
+namespace netmax {
+
+struct Operand { const void *p; int64_t ld, step; bool k_near; };
+
+enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+// act(z); the exact (error function) form of GELU.
+__device__ __forceinline__ float act_of(int act, float z)
+{
+    if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;                // a NaN stays one
+    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (act == ACT_SILU) return z / (1.0f + expf(-z));
+    return z;
+}
+
+// act'(z); ReLU's is 0 at 0.  SiLU's factor 1 - s of a large z times a vanishing s would be inf * 0: s is 0 there first.
+__device__ __forceinline__ float act_slope(int act, float z)
+{
+    if (act == ACT_RELU) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+    if (act == ACT_GELU) {
+        const float bell = expf(-0.5f * z * z) * 0.39894228040143268f;
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + (bell == 0.0f ? 0.0f : z * bell);
+    }
+    if (act == ACT_SILU) {
+        const float s = 1.0f / (1.0f + expf(-z));
+        return s == 0.0f ? 0.0f : s * (1.0f + z * (1.0f - s));
+    }
+    return 1.0f;
+}
+
+// ---- values in memory: float or bfloat16 (as its 16 bits) ------------------------------------------------------------
+
+__device__ __forceinline__ float load_value(const float *p) { return *p; }
+__device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bits_to_float(*p); }
+__device__ __forceinline__ void store_value(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = (uint16_t)bf16_bits(v); }
+__device__ __forceinline__ f32x4 load_four(const float *p) { return load4(p); }
+__device__ __forceinline__ f32x4 load_four(const uint16_t *p)
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u)};
+}
+__device__ __forceinline__ void store_four(float *p, f32x4 v) { store4(p, v); }
+__device__ __forceinline__ void store_four(uint16_t *p, f32x4 v)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+// Four values from column n of `cols`; `whole`: rows start at multiples of four values in aligned memory.
+template <typename T> __device__ __forceinline__ f32x4 load_up_to_four(const T *row, int64_t n, int64_t cols, bool whole)
+{
+    if (whole && n + 4 <= cols) return load_four(row + n);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < cols) v[e] = load_value(row + n + e);
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_up_to_four(T *row, int64_t n, int64_t cols, bool whole, f32x4 v)
+{
+    if (whole && n + 4 <= cols) { store_four(row + n, v); return; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < cols) store_value(row + n + e, v[e]);
+}
+
+// ---- epilogues: told of four neighbouring columns n .. n + 3 of row m of matrix g of the batch -----------------------
+
+// y = act(acc + bias) + residual, z = acc + bias; bias, residual and z may be null.
+template <typename T> struct LinearEpilogue {
+    int64_t M, N;
+    const T *bias, *residual; T *y, *z;
+    int64_t ldr, ldy, ldz, sb, sr, sy, sz;
+    int act; bool whole;
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m >= M || n >= N) return;
+        if (bias) v += load_up_to_four(bias + g * sb, n, N, whole);
+        if (z) store_up_to_four(z + g * sz + m * ldz, n, N, whole, v);
+        if (act != ACT_NONE)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = act_of(act, v[e]);
+        if (residual) v += load_up_to_four(residual + g * sr + m * ldr, n, N, whole);
+        store_up_to_four(y + g * sy + m * ldy, n, N, whole, v);
+    }
+};
+
+// out = alpha acc + beta own, all [M][N] next to each other; own may be null.
+template <typename T> struct SumEpilogue {
+    int64_t M, N;
+    float alpha, beta;
+    const float *own; T *out;
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m >= M || n >= N) return;
+        const int64_t row = (g * M + m) * N;
+        v *= alpha;
+        if (own) v += beta * load_up_to_four(own + row, n, N, false);
+        store_up_to_four(out + row, n, N, false, v);
+    }
+};
+
+}  // namespace netmax

@@ -2,6 +2,7 @@
 // kernel launches.  Everything that touches model data runs in the kernels of this directory.
 #include "../../include/netmax.h"
 #include "async_plan.h"
+#include "errors.h"
 #include "kernels.h"
 #include "layout.h"
 #include "philox.h"
@@ -108,6 +109,13 @@ static thread_local std::string g_init_error;
 static int fail(netmax_ctx *ctx, int code, const std::string &msg)
 {
     if (ctx) ctx->err = msg; else g_init_error = msg;
+    return code;
+}
+
+// No exception leaves through the C entry points of the context-free operators: a text that cannot be kept is dropped.
+int netmax_fail(int code, const char *msg) noexcept
+{
+    try { g_init_error = msg; } catch (...) { }
     return code;
 }
 
