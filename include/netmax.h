@@ -289,7 +289,7 @@ typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NE
 typedef struct {
     int64_t batch;          /* layers, e.g. one per worker: 0 .. 65535 */
     int64_t rows;           /* tokens per layer, >= 0 */
-    int64_t d_in, d_out;    /* >= 1 */
+    int64_t d_in, d_out;    /* 1 .. 2^22 - 1 */
     int32_t dtype;          /* netmax_dtype of all matrices and vectors */
     int32_t act;            /* netmax_act */
     int64_t ldx, ldw, ldr, ldy, ldz;            /* rows of x, w, residual, y (and dy), z */
@@ -299,8 +299,9 @@ typedef struct {
 
 /* y = act(z) + residual, z = x w + bias, for every layer of the batch: x [rows][d_in], w [d_in][d_out] (the layout of a perceptron's W),
  * bias [d_out], residual and y [rows][d_out].  bias and residual may be NULL; z may be NULL or receives z, which netmax_linear_grad needs.
- * y may be the residual's memory with the residual's strides. */
-int64_t netmax_linear_workspace(const netmax_linear_shape *shape);
+ * y may be the residual's memory with the residual's strides.  The workspace depends on the alignment of x and w (bfloat16 rows that do not start at multiples of
+ * 16 bytes are laid out anew): pass the pointers of the call. */
+int64_t netmax_linear_workspace(const netmax_linear_shape *shape, const void *x, const void *w);
 int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w, const void *bias, const void *residual, void *y, void *z,
                   void *work, int64_t work_bytes, void *stream);
 
@@ -308,7 +309,7 @@ int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w
  * dx = dz w^T, dw = x^T dz, db = the sum of dz over the rows; each may be NULL.  z as netmax_linear left it, NULL for NETMAX_ACT_NONE.
  * bfloat16: dz is rounded to bfloat16 for the products, as the errors of a perceptron are; db sums it before that.  rows = 0 gives dw = 0 and db = 0.
  * Results of the same call are the same bits every time. */
-int64_t netmax_linear_grad_workspace(const netmax_linear_shape *shape);
+int64_t netmax_linear_grad_workspace(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w);
 int netmax_linear_grad(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w, const void *z, void *dx, void *dw, void *db,
                        void *work, int64_t work_bytes, void *stream);
 

@@ -114,9 +114,9 @@ def load():
         "netmax_get_tables": (C.c_int, [vp, vp, vp, vp]),
         "netmax_last_error": (C.c_char_p, [vp]),
         "netmax_destroy": (C.c_int, [vp]),
-        "netmax_linear_workspace": (i64, [C.POINTER(netmax_linear_shape)]),
+        "netmax_linear_workspace": (i64, [C.POINTER(netmax_linear_shape), vp, vp]),
         "netmax_linear": (C.c_int, [C.POINTER(netmax_linear_shape)] + [vp] * 7 + [i64, vp]),
-        "netmax_linear_grad_workspace": (i64, [C.POINTER(netmax_linear_shape)]),
+        "netmax_linear_grad_workspace": (i64, [C.POINTER(netmax_linear_shape), vp, vp, vp]),
         "netmax_linear_grad": (C.c_int, [C.POINTER(netmax_linear_shape)] + [vp] * 8 + [i64, vp]),
         "netmax_orthogonalize_workspace": (i64, [C.POINTER(netmax_orth_shape)]),
         "netmax_orthogonalize": (C.c_int, [C.POINTER(netmax_orth_shape)] + [vp] * 5 + [i64, vp]),

@@ -1,0 +1,229 @@
+// C = A B for operands of 16 bits (bfloat16 or half) on v_mfma_f32_32x32x16, accumulated in float.
+//
+// A workgroup has a block of BM x BN results.  A step of 64 contraction indices of both operands goes from memory straight into LDS
+// (16 bytes per lane and request), two steps in turn: while one is multiplied the next one arrives, one barrier per step.
+// Each operand lies in LDS as it lies in memory:
+//   contraction index near   [rows][64]: lanes read 16 bytes of a row; the 16-byte units of a row are permuted by (row / 2) % 8, so that
+//                            sixteen rows at one index lie in different banks
+//   row index near           [64][rows]: ds_read_b64_tr_b16 hands each lane four contraction indices of its row; groups of 64 bytes are permuted by
+//                            k % 4 (rows of 128 bytes: k / 2 % 2), so that the four stored rows that one such read touches lie in different banks
+// The permutations are applied to the memory addresses, since a request to LDS fills consecutive units.
+// B goes in as the instruction's first operand, so that a lane ends with four neighbouring columns of a row.
+//
+// Memory: 16-byte aligned, ld and step multiples of 8, extents along memory rounded up to 8 readable; where the contraction index is near and K is
+// no multiple of 8, zeros from K to the next multiple.  Rows past the end are read as the last ones (their results are not kept); contraction
+// indices past the end as zeros.
+#pragma once
+#include "gemm.h"
+
+namespace netmax {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int G16_STEP = 64;
+
+__device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma16(half8 a, half8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+static __device__ const uint4 g16_zeros = {0, 0, 0, 0};
+
+// 16 bytes of every lane to LDS, from `unit` of the wave on.  Restrict: what is requested is never what is read before the next barrier.
+__device__ __forceinline__ void to_lds(const char *__restrict__ from, char *__restrict__ to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+__device__ __forceinline__ s16x4 read_turned(const char *__restrict__ p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+}
+template <typename V> __device__ __forceinline__ V read_unit(const char *__restrict__ p) { return *reinterpret_cast<const V *>(p); }
+
+template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 64 ? (k >> 1) & 1 : k & 3; }
+
+// One operand's step: ROWS results' rows x 64 contraction indices, brought by THREADS threads.
+template <int ROWS, bool K_NEAR, int THREADS> struct Step16 {
+    static constexpr int BYTES = ROWS * G16_STEP * 2, PIECES = BYTES / 16 / THREADS, ROW_UNITS = ROWS / 8;
+    uint32_t offset[PIECES];                                        // of this lane's piece from the step's first byte
+    int first_k[PIECES];
+
+    __device__ __forceinline__ void place(int64_t row0, int64_t rows, int64_t ld)
+    {
+        // rows past the end are the last ones, so an offset stays below ROWS (64) rows of ld; ld < 2^22
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+            const int q = u * THREADS + (int)threadIdx.x;
+            if (K_NEAR) {
+                const int r = q / 8, c = (q % 8) ^ ((r >> 1) & 7);
+                const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
+                first_k[u] = c * 8;
+                offset[u] = (uint32_t)((row - row0) * ld * 2 + c * 16);
+            } else {
+                const int k = q / ROW_UNITS, c = (q % ROW_UNITS) ^ (turned_group<ROWS>(k) << 2);
+                const int64_t last = (rows + 7) / 8 - 1, unit = row0 / 8 + c < last ? row0 / 8 + c : last;
+                first_k[u] = k;
+                offset[u] = (uint32_t)((int64_t)k * ld * 2 + (unit - row0 / 8) * 16);
+            }
+        }
+    }
+    // `from`: the step's first byte (row row0, first index of the step); a wave's units lie next to each other
+    __device__ __forceinline__ void request(const char *from, char *lds) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) to_lds(from + offset[u], lds + u * THREADS * 16 + wave * 1024);
+    }
+    // the last step: indices from `left` on are zeros
+    __device__ __forceinline__ void request_tail(const char *from, char *lds, int left) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u)
+            to_lds(first_k[u] < left ? from + offset[u] : (const char *)&g16_zeros, lds + u * THREADS * 16 + wave * 1024);
+    }
+};
+
+// Where a lane reads its part of 32 rows from `first` (a multiple of 32) on.
+template <int ROWS, bool K_NEAR> struct Fragment16 {
+    int base[4];                                                     // K_NEAR: one for each 16 indices of the step; else base[0]
+    __device__ __forceinline__ void place(int first)
+    {
+        const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
+        if (K_NEAR) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) base[kk] = (first + at) * 128 + ((kk * 2 + half) ^ ((at >> 1) & 7)) * 16;
+        } else {
+            const int group = (lane >> 4) & 1, t = lane & 15;
+            base[0] = (half * 8 + t / 4) * (ROWS * 2) + ((first / 32) ^ turned_group<ROWS>(t / 4)) * 64 + group * 32 + (t & 3) * 8;
+        }
+    }
+    template <typename V> __device__ __forceinline__ V read(const char *lds, int kk) const
+    {
+        if (K_NEAR) return read_unit<V>(lds + base[kk]);
+        const s16x4 lo = read_turned(lds + base[0] + kk * 16 * (ROWS * 2)), hi = read_turned(lds + base[0] + (kk * 16 + 4) * (ROWS * 2));
+        return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Numbers workgroups so that those of one L2 (every eighth) have neighbouring blocks, and blocks in columns of eight rows of blocks.
+__device__ __forceinline__ void block_place(uint32_t id, uint32_t all, uint32_t mblocks, uint32_t nblocks, uint32_t &g, uint32_t &mb, uint32_t &nb)
+{
+    const uint32_t each = all / 8, more = all % 8, part = id % 8;
+    id = part * each + (part < more ? part : more) + id / 8;
+    const uint32_t per = mblocks * nblocks;
+    g = id / per;
+    id -= g * per;
+    const uint32_t band = id / (8 * nblocks), high = mblocks - band * 8 < 8 ? mblocks - band * 8 : 8, in = id - band * 8 * nblocks;
+    nb = in / high;
+    mb = band * 8 + in % high;
+}
+
+// Products of planes: with SPLIT an operand is two planes, hi + lo 2^-11; lo hi + hi lo are added up first and scaled, then hi hi.  The
+// product of the two low planes is below 2^-22 of the result's terms and left out.
+struct Planes16 { const char *hi, *lo; int64_t ld, step; };          // ld, step in elements
+
+template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, bool AK, bool BK, bool SPLIT, class Epilogue>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64)
+gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
+{
+    constexpr int THREADS = WAVES_M * WAVES_N * 64, TM = BM / WAVES_M / 32, TN = BN / WAVES_N / 32;
+    typedef Step16<BM, AK, THREADS> StepA;
+    typedef Step16<BN, BK, THREADS> StepB;
+    __shared__ __align__(16) char lds[2][StepA::BYTES + StepB::BYTES];
+    uint32_t g, mb, nb;
+    const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
+    block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
+    const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
+    const int64_t kstepA = AK ? G16_STEP * 2 : A.ld * (G16_STEP * 2), kstepB = BK ? G16_STEP * 2 : B.ld * (G16_STEP * 2);
+    const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
+    const int wave = threadIdx.x >> 6, wm = wave / WAVES_N * (TM * 32), wn = wave % WAVES_N * (TN * 32);
+    StepA sa;
+    StepB sb;
+    sa.place(m0, M, A.ld);
+    sb.place(n0, N, B.ld);
+    Fragment16<BM, AK> fa[TM];
+    Fragment16<BN, BK> fb[TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[i].place(wm + i * 32);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[j].place(wn + j * 32);
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+    const int64_t whole = (K + G16_STEP - 1) / G16_STEP;
+    const int first = (int)(whole * split / splits), steps = (int)(whole * (split + 1) / splits) - first, total = SPLIT ? 3 * steps : steps;
+    auto bring = [&](int s, char *to) {
+        const int part = !SPLIT || s >= 2 * steps ? 2 : s >= steps ? 1 : 0, k = first + (SPLIT ? s - part * steps : s);
+        const char *a = (SPLIT && part == 0 ? A.lo : A.hi) + from_a + k * kstepA, *b = (SPLIT && part == 1 ? B.lo : B.hi) + from_b + k * kstepB;
+        const int64_t left = K - (int64_t)k * G16_STEP;
+        if (left >= G16_STEP) {
+            sa.request(a, to);
+            sb.request(b, to + StepA::BYTES);
+        } else {
+            sa.request_tail(a, to, (int)left);
+            sb.request_tail(b, to + StepA::BYTES, (int)left);
+        }
+    };
+    if (total > 0) bring(0, lds[0]);
+    __syncthreads();
+    for (int s = 0; s < total; ++s) {
+        if (s + 1 < total) bring(s + 1, lds[(s + 1) & 1]);
+        if (SPLIT && s == 2 * steps)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] *= 0x1p-11f;
+        const char *ca = lds[s & 1], *cb = ca + StepA::BYTES;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            V a[TM], b[TN];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[i] = fa[i].template read<V>(ca, kk);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[j] = fb[j].template read<V>(cb, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(b[j], a[i], acc[i][j]);
+        }
+        __syncthreads();
+    }
+    const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
+    const int64_t where = splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                epilogue(where, m0 + wm + i * 32 + at, n0 + wn + j * 32 + e * 8 + half * 4,
+                         f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+}
+
+// Whether a matrix can be multiplied where it lies (see the top); `stored`: its extent along memory.
+inline bool fits16(const void *p, int64_t ld, int64_t step, int64_t stored)
+{
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && step % 8 == 0 && stored % 8 == 0 && ld < (1 << 22);
+}
+
+template <typename V, int BM, int BN, int WM, int WN, bool SPLIT, class Epilogue>
+void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, uint32_t splits,
+                          const Epilogue &e)
+{
+    const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
+    const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64);
+    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, true, true, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, true, false, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, false, true, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, false, false, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+}
+
+}  // namespace netmax

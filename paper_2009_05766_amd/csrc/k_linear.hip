@@ -1,11 +1,114 @@
 // y = act(x w + b) + r for a batch of layers, and its gradients:
 //     dz = dy act'(z),  dx = dz w^T,  dw = x^T dz,  db = sum over the rows of dz.
+// float is multiplied in float (gemm_f32.h), bfloat16 as it is (gemm16.h); bfloat16 operands whose rows the latter cannot take where they lie
+// are laid out anew first.
+#include "gemm16.h"
 #include "gemm_f32.h"
 #include "linear.h"
 
 namespace netmax {
 
 static inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// ---- operands of 16 bits laid out anew -------------------------------------------------------------------------------
+
+// out [batch][rows][wide] = in [batch][rows][cols] (rows ld, matrices step apart) with zeros behind each row; wide a multiple of 8.
+__global__ void __launch_bounds__(256) lay_out_kernel(int64_t rows, int64_t cols, int64_t wide, const uint16_t *__restrict__ in, int64_t ld, int64_t step, uint16_t *__restrict__ out)
+{
+    const int64_t units = wide / 8, all = rows * units, g = blockIdx.y;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
+        const int64_t r = q / units, c = (q - r * units) * 8;
+        const uint16_t *p = in + g * step + r * ld + c;
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = (c + 2 * e < cols ? p[2 * e] : 0u) | (uint32_t)(c + 2 * e + 1 < cols ? p[2 * e + 1] : 0u) << 16;
+        *reinterpret_cast<uint4 *>(out + (g * all + q) * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+
+// A matrix [rows][cols] of a batch as an operand; `copy`: it has to be laid out anew.
+struct Source {
+    const void *p; int64_t ld, step, rows, cols; bool copy;
+    Source(const void *p_, int64_t ld_, int64_t step_, int64_t rows_, int64_t cols_) : p(p_), ld(ld_), step(step_), rows(rows_), cols(cols_), copy(!fits16(p_, ld_, step_, cols_)) { }
+    int64_t bytes(int64_t batch) const { return copy ? round_up((step || batch == 0 ? batch : 1) * rows * round_up(cols, 8) * 2, 256) : 0; }
+    // The operand, after a copy to `work` (advanced) where one is needed.
+    Planes16 take(hipStream_t s, int64_t batch, char *&work) const
+    {
+        if (!copy || rows == 0) return Planes16{(const char *)p, nullptr, ld, step};
+        const int64_t wide = round_up(cols, 8), own = step ? batch : 1, want = (rows * wide / 8 + 255) / 256;
+        char *to = work;
+        work += bytes(batch);
+        lay_out_kernel<<<dim3((uint32_t)(want < 4096 ? want : 4096), (uint32_t)own), 256, 0, s>>>(rows, cols, wide, (const uint16_t *)p, ld, step, (uint16_t *)to);
+        return Planes16{to, nullptr, wide, step ? rows * wide : 0};
+    }
+};
+
+// ---- products whose contraction is shared out ------------------------------------------------------------------------
+
+// Partial results of one share of the contraction: [splits][batch][M][wide], float.
+struct PartEpilogue {
+    int64_t M, N, wide; float *p;
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m < M && n < N) store4(p + (g * M + m) * wide + n, v);
+    }
+};
+
+// The partial results added up in order, then the epilogue.
+template <class Epilogue>
+__global__ void __launch_bounds__(256) join_parts_kernel(int64_t batch, int64_t M, int64_t wide, int splits, const float *__restrict__ parts, Epilogue epilogue)
+{
+    const int64_t quads = wide / 4, all = batch * M * quads;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
+        f32x4 v = load4(parts + q * 4);
+        for (int k = 1; k < splits; ++k) v += load4(parts + ((int64_t)k * all + q) * 4);
+        const int64_t row = q / quads, g = row / M;
+        epilogue(g, row - g * M, (q - row * quads) * 4, v);
+    }
+}
+
+// Blocks and shares of a product: large blocks where they fill the card, smaller ones otherwise, and the contraction shared out where even
+// those are few.
+struct Plan16 { int block; int splits; };
+static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
+{
+    const auto blocks = [&](int64_t b) { return batch * ((M + b - 1) / b) * ((N + b - 1) / b); };
+    const int64_t steps = (K + G16_STEP - 1) / G16_STEP;
+    if (blocks(256) >= 192) return {256, 1};
+    const int block = blocks(128) >= 128 && M > 64 && N > 64 ? 128 : 64;
+    const int64_t want = 512 / (blocks(block) > 0 ? blocks(block) : 1), most = steps / 4;
+    const int64_t splits = want < most ? want : most;
+    return {block, (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits)};
+}
+static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K)
+{
+    const Plan16 p = plan16(batch, M, N, K);
+    return p.splits > 1 ? round_up(p.splits * batch * M * round_up(N, 4) * 4, 256) : 0;
+}
+
+template <class Epilogue>
+static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, int splits,
+                            const Epilogue &e)
+{
+    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+}
+
+// `work`: part_bytes() of it.
+template <class Epilogue>
+static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, const Epilogue &e, char *work)
+{
+    const Plan16 p = plan16(batch, M, N, K);
+    if (p.splits == 1) {
+        launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, 1, e);
+        return;
+    }
+    const int64_t wide = round_up(N, 4), quads = batch * M * wide / 4;
+    launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, p.splits, PartEpilogue{M, N, wide, (float *)work});
+    join_parts_kernel<<<(uint32_t)((quads + 255) / 256 < 2048 ? (quads + 255) / 256 : 2048), 256, 0, s>>>(batch, M, wide, p.splits, (const float *)work, e);
+}
 
 // ---- dz and db -------------------------------------------------------------------------------------------------------
 
@@ -15,8 +118,9 @@ constexpr int SLOPE_ROWS = 64;
 template <typename T>
 __global__ void __launch_bounds__(256)
 slope_kernel(int64_t rows, int64_t cols, const T *__restrict__ dy, int64_t lddy, int64_t sdy, const T *__restrict__ z, int64_t ldz, int64_t sz, int act,
-             T *__restrict__ dz, float *__restrict__ sums)
+             T *__restrict__ dz, int64_t wide, float *__restrict__ sums)
 {
+    // dz has rows of `wide` values, zeros behind the columns: what the product's contraction over them needs
     __shared__ float part[4][64];
     const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), r0 = (int64_t)blockIdx.y * SLOPE_ROWS;
     float sum = 0.0f;
@@ -25,8 +129,10 @@ slope_kernel(int64_t rows, int64_t cols, const T *__restrict__ dy, int64_t lddy,
             float v = load_value(dy + g * sdy + r * lddy + n);
             if (act != ACT_NONE) v *= act_slope(act, load_value(z + g * sz + r * ldz + n));
             sum += v;
-            if (dz) store_value(dz + (g * rows + r) * cols + n, v);
+            if (dz) store_value(dz + (g * rows + r) * wide + n, v);
         }
+    else if (dz && n < wide)
+        for (int64_t r = r0 + (threadIdx.x >> 6); r < r0 + SLOPE_ROWS && r < rows; r += 4) dz[(g * rows + r) * wide + n] = T(0);
     part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
     __syncthreads();
     if (sums && threadIdx.x < 64 && n < cols)
@@ -45,54 +151,88 @@ __global__ void __launch_bounds__(256) bias_sum_kernel(int64_t cols, int64_t par
 
 // ---- launchers -------------------------------------------------------------------------------------------------------
 
-int64_t linear_workspace(const LinearArgs &) { return 0; }
-
-template <typename T> static void linear_of(hipStream_t s, const LinearArgs &a)
+template <typename T> static LinearEpilogue<T> forward_epilogue(const LinearArgs &a)
 {
     const bool whole = whole_pieces(a.y, a.ldy, a.sy, sizeof(T)) && (!a.z || whole_pieces(a.z, a.ldz, a.sz, sizeof(T))) &&
                        (!a.residual || whole_pieces(a.residual, a.ldr, a.sr, sizeof(T))) && (!a.bias || whole_pieces(a.bias, 0, a.sb, sizeof(T)));
-    const LinearEpilogue<T> e{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz,
-                              a.sb, a.sr, a.sy, a.sz, a.act, whole};
-    launch_gemm_f32<T>(s, a.batch, a.rows, a.dout, a.din, Operand{a.x, a.ldx, a.sx, true}, Operand{a.w, a.ldw, a.sw, false}, e);
+    return LinearEpilogue<T>{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz, a.sb, a.sr, a.sy, a.sz, a.act, whole};
+}
+// out [rows][cols] alone
+template <typename T> static LinearEpilogue<T> plain_epilogue(int64_t rows, int64_t cols, void *out, int64_t ld, int64_t step)
+{
+    return LinearEpilogue<T>{rows, cols, nullptr, nullptr, (T *)out, nullptr, 0, ld, 0, 0, 0, step, 0, ACT_NONE, whole_pieces(out, ld, step, sizeof(T))};
 }
 
-void launch_linear(hipStream_t s, const LinearArgs &a, void *)
+int64_t linear_workspace(const LinearArgs &a)
 {
-    if (a.bf16) linear_of<uint16_t>(s, a); else linear_of<float>(s, a);
+    if (!a.bf16) return 0;
+    return Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + part_bytes(a.batch, a.rows, a.dout, a.din);
 }
 
-static int64_t dz_bytes(const LinearGradArgs &a)
+void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
 {
-    return a.act == ACT_NONE ? 0 : round_up(a.batch * a.rows * a.dout * (a.bf16 ? 2 : 4), 256);
+    if (!a.bf16) {
+        launch_gemm_f32<float>(s, a.batch, a.rows, a.dout, a.din, Operand{a.x, a.ldx, a.sx, true}, Operand{a.w, a.ldw, a.sw, false}, forward_epilogue<float>(a));
+        return;
+    }
+    char *at = (char *)work;
+    const Planes16 x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(s, a.batch, at), w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(s, a.batch, at);
+    launch_product16(s, a.batch, a.rows, a.dout, a.din, x, true, w, false, forward_epilogue<uint16_t>(a), at);
 }
+
 static int64_t sum_parts(const LinearGradArgs &a) { return (a.rows + SLOPE_ROWS - 1) / SLOPE_ROWS; }
-int64_t linear_grad_workspace(const LinearGradArgs &a) { return dz_bytes(a) + round_up(a.batch * sum_parts(a) * a.dout * 4, 256); }
+static int64_t sum_bytes(const LinearGradArgs &a) { return round_up(a.batch * sum_parts(a) * a.dout * 4, 256); }
+static int64_t dz_wide(const LinearGradArgs &a) { return a.bf16 ? round_up(a.dout, 8) : a.dout; }
 
-template <typename T> static void linear_grad_of(hipStream_t s, const LinearGradArgs &a, char *work)
+int64_t linear_grad_workspace(const LinearGradArgs &a)
 {
-    T *dz = a.act == ACT_NONE ? nullptr : (T *)work;
-    float *sums = a.db ? (float *)(work + dz_bytes(a)) : nullptr;
-    if ((dz || sums) && a.rows > 0)
-        slope_kernel<T><<<dim3((uint32_t)((a.dout + 63) / 64), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
-            a.rows, a.dout, (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz, sums);
+    int64_t n = sum_bytes(a);
+    if (a.act != ACT_NONE) n += round_up(a.batch * a.rows * dz_wide(a) * (a.bf16 ? 2 : 4), 256);
+    else if (a.bf16) n += Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).bytes(a.batch);
+    if (!a.bf16) return n;
+    const int64_t dx = part_bytes(a.batch, a.rows, a.din, a.dout), dw = part_bytes(a.batch, a.din, a.dout, a.rows);
+    return n + Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + (dx > dw ? dx : dw);
+}
+
+template <typename T> static void launch_slopes(hipStream_t s, const LinearGradArgs &a, T *dz, float *sums)
+{
+    if ((dz || a.db) && a.rows > 0)
+        slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + 63) / 64), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
+            a.rows, a.dout, (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz, dz_wide(a), a.db ? sums : nullptr);
     if (a.db)
         bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 255) / 256), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
-    const Operand d = dz ? Operand{dz, a.dout, a.rows * a.dout, true} : Operand{a.dy, a.lddy, a.sdy, true};
-    if (a.dx && a.rows > 0) {
-        const LinearEpilogue<T> e{a.rows, a.din, nullptr, nullptr, (T *)a.dx, nullptr, 0, a.lddx, 0, 0, 0, a.sdx, 0, ACT_NONE,
-                                  whole_pieces(a.dx, a.lddx, a.sdx, sizeof(T))};
-        launch_gemm_f32<T>(s, a.batch, a.rows, a.din, a.dout, d, Operand{a.w, a.ldw, a.sw, true}, e);
-    }
-    if (a.dw) {
-        const LinearEpilogue<T> e{a.din, a.dout, nullptr, nullptr, (T *)a.dw, nullptr, 0, a.lddw, 0, 0, 0, a.sdw, 0, ACT_NONE,
-                                  whole_pieces(a.dw, a.lddw, a.sdw, sizeof(T))};
-        launch_gemm_f32<T>(s, a.batch, a.din, a.dout, a.rows, Operand{a.x, a.ldx, a.sx, false}, Operand{d.p, d.ld, d.step, false}, e);
-    }
 }
 
 void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
 {
-    if (a.bf16) linear_grad_of<uint16_t>(s, a, (char *)work); else linear_grad_of<float>(s, a, (char *)work);
+    char *at = (char *)work;
+    float *sums = (float *)at;
+    at += sum_bytes(a);
+    void *dz = nullptr;
+    if (a.act != ACT_NONE) {
+        dz = at;
+        at += round_up(a.batch * a.rows * dz_wide(a) * (a.bf16 ? 2 : 4), 256);
+    }
+    if (!a.bf16) {
+        launch_slopes<float>(s, a, (float *)dz, sums);
+        const Operand d = dz ? Operand{dz, a.dout, a.rows * a.dout, true} : Operand{a.dy, a.lddy, a.sdy, true};
+        if (a.dx && a.rows > 0)
+            launch_gemm_f32<float>(s, a.batch, a.rows, a.din, a.dout, d, Operand{a.w, a.ldw, a.sw, true}, plain_epilogue<float>(a.rows, a.din, a.dx, a.lddx, a.sdx));
+        if (a.dw)
+            launch_gemm_f32<float>(s, a.batch, a.din, a.dout, a.rows, Operand{a.x, a.ldx, a.sx, false}, Operand{d.p, d.ld, d.step, false},
+                                   plain_epilogue<float>(a.din, a.dout, a.dw, a.lddw, a.sdw));
+        return;
+    }
+    launch_slopes<uint16_t>(s, a, (uint16_t *)dz, sums);
+    const Planes16 d = dz ? Planes16{(const char *)dz, nullptr, dz_wide(a), a.rows * dz_wide(a)} : Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).take(s, a.batch, at);
+    if (a.dx && a.rows > 0) {
+        const Planes16 w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(s, a.batch, at);
+        launch_product16(s, a.batch, a.rows, a.din, a.dout, d, true, w, true, plain_epilogue<uint16_t>(a.rows, a.din, a.dx, a.lddx, a.sdx), at);
+    }
+    if (a.dw) {
+        const Planes16 x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(s, a.batch, at);
+        launch_product16(s, a.batch, a.din, a.dout, a.rows, x, false, d, false, plain_epilogue<uint16_t>(a.din, a.dout, a.dw, a.lddw, a.sdw), at);
+    }
 }
 
 }  // namespace netmax

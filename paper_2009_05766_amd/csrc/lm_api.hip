@@ -37,8 +37,8 @@ static bool strides_ok(int64_t batch, int64_t rows, int64_t cols, int64_t ld, in
 static int check_linear(const netmax_linear_shape *s)
 {
     if (!s) return netmax_fail(NETMAX_EINVAL, "shape is NULL");
-    if (s->batch < 0 || s->batch > 65535 || s->rows < 0 || s->d_in < 1 || s->d_out < 1)
-        return netmax_fail(NETMAX_EINVAL, "need 0 <= batch <= 65535, rows >= 0, d_in >= 1 and d_out >= 1");
+    if (s->batch < 0 || s->batch > 65535 || s->rows < 0 || s->d_in < 1 || s->d_out < 1 || s->d_in >= 1 << 22 || s->d_out >= 1 << 22)
+        return netmax_fail(NETMAX_EINVAL, "need 0 <= batch <= 65535, rows >= 0, 1 <= d_in < 2^22 and 1 <= d_out < 2^22");
     if (!product_fits(s->batch, s->rows, s->d_in) || !product_fits(s->batch, s->rows, s->d_out) || !product_fits(s->batch, s->d_in, s->d_out) ||
         !blocks_fit(s->batch, s->rows, s->d_in) || !blocks_fit(s->batch, s->rows, s->d_out) || !blocks_fit(s->batch, s->d_in, s->d_out) || s->rows > (int64_t)65535 * 64)
         return netmax_fail(NETMAX_EINVAL, "the layer is too large");
@@ -79,10 +79,12 @@ static int check_work(const void *work, int64_t have, int64_t need)
     return netmax_fail(NETMAX_EINVAL, buf);
 }
 
-extern "C" int64_t netmax_linear_workspace(const netmax_linear_shape *s)
+extern "C" int64_t netmax_linear_workspace(const netmax_linear_shape *s, const void *x, const void *w)
 {
     if (check_linear(s) != NETMAX_OK) return -1;
-    return linear_workspace(linear_args(s));
+    LinearArgs a = linear_args(s);
+    a.x = x; a.w = w;
+    return linear_workspace(a);
 }
 
 extern "C" int netmax_linear(const netmax_linear_shape *s, const void *x, const void *w, const void *bias, const void *residual, void *y, void *z,
@@ -113,10 +115,12 @@ static LinearGradArgs linear_grad_args(const netmax_linear_shape *s)
     return a;
 }
 
-extern "C" int64_t netmax_linear_grad_workspace(const netmax_linear_shape *s)
+extern "C" int64_t netmax_linear_grad_workspace(const netmax_linear_shape *s, const void *dy, const void *x, const void *w)
 {
     if (check_linear(s) != NETMAX_OK) return -1;
-    return linear_grad_workspace(linear_grad_args(s));
+    LinearGradArgs a = linear_grad_args(s);
+    a.dy = dy; a.x = x; a.w = w;
+    return linear_grad_workspace(a);
 }
 
 extern "C" int netmax_linear_grad(const netmax_linear_shape *s, const void *dy, const void *x, const void *w, const void *z, void *dx, void *dw, void *db,

@@ -117,7 +117,7 @@ def netmax_linear(x, w, bias=None, residual=None, *, act: str = "none", keep_pre
     sb = bias.stride(0) if bias is not None and lead else 0
     shape = netmax_linear_shape(lead[0] if lead else 1, rows, d_in, d_out, _DTYPES[dt], kind, ldx, ldw, ldr, ldy, ldz, sx, sw, sb, sr, sy, sz)
     lib, ref = load(), C.byref(shape)
-    work = _workspace(lib.netmax_linear_workspace(ref), x.device)
+    work = _workspace(lib.netmax_linear_workspace(ref, _p(x), _p(w)), x.device)
     _call(lib.netmax_linear, x.device, ref, _p(x), _p(w), _p(bias), _p(residual), _p(y), _p(z), _p(work), 0 if work is None else work.numel())
     return (y, z) if keep_preact or z is not None else y
 
@@ -157,7 +157,7 @@ def netmax_linear_grad(dy, x, w, z=None, *, act: str = "none", need_input: bool 
     shape = netmax_linear_shape(lead[0] if lead else 1, rows, d_in, d_out, _DTYPES[dt], kind, ldx, ldw, 0, ldy, ldz, sx, sw, 0, 0, sy, sz, lddx, lddw,
                                 sdx, sdw, sdb)
     lib, ref = load(), C.byref(shape)
-    work = _workspace(lib.netmax_linear_grad_workspace(ref), dev)
+    work = _workspace(lib.netmax_linear_grad_workspace(ref, _p(dy), _p(x), _p(w)), dev)
     _call(lib.netmax_linear_grad, dev, ref, _p(dy), _p(x), _p(w), _p(z), _p(dx), _p(dw), _p(db), _p(work), 0 if work is None else work.numel())
     return dx, dw, db
 
