@@ -315,7 +315,7 @@ int netmax_linear_grad(const netmax_linear_shape *shape, const void *dy, const v
 
 typedef struct {
     int64_t batch;          /* matrices, e.g. one per worker: 0 .. 65535 */
-    int64_t rows, cols;     /* >= 1 */
+    int64_t rows, cols;     /* 1 .. 2^22 - 1 */
     int32_t dtype;          /* netmax_dtype of g and out; the momentum is float */
     int32_t steps;          /* Newton-Schulz products, 1 .. 64 */
     int32_t nesterov;

@@ -57,6 +57,12 @@ __device__ __forceinline__ void store_four(uint16_t *p, f32x4 v)
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
 }
+// Whether pieces of four values can be taken whole: rows and matrices start at multiples of four values in aligned memory.
+inline bool whole_pieces(const void *p, int64_t ld, int64_t step, int value_bytes)
+{
+    return (uintptr_t)p % (4 * value_bytes) == 0 && ld % 4 == 0 && step % 4 == 0;
+}
+
 // Four values from column n of `cols`; `whole`: rows start at multiples of four values in aligned memory.
 template <typename T> __device__ __forceinline__ f32x4 load_up_to_four(const T *row, int64_t n, int64_t cols, bool whole)
 {

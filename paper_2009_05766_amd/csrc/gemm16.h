@@ -121,11 +121,25 @@ __device__ __forceinline__ void block_place(uint32_t id, uint32_t all, uint32_t 
     mb = band * 8 + in % high;
 }
 
+// The same for the lower triangle of a square of `side` x `side` blocks.
+__device__ __forceinline__ void triangle_place(uint32_t id, uint32_t all, uint32_t side, uint32_t &g, uint32_t &mb, uint32_t &nb)
+{
+    const uint32_t each = all / 8, more = all % 8, part = id % 8;
+    id = part * each + (part < more ? part : more) + id / 8;
+    const uint32_t per = side * (side + 1) / 2;
+    g = id / per;
+    id -= g * per;
+    mb = (uint32_t)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
+    while ((mb + 1) * (mb + 2) / 2 <= id) ++mb;                     // the root is rounded
+    while (mb * (mb + 1) / 2 > id) --mb;
+    nb = id - mb * (mb + 1) / 2;
+}
+
 // Products of planes: with SPLIT an operand is two planes, hi + lo 2^-11; lo hi + hi lo are added up first and scaled, then hi hi.  The
 // product of the two low planes is below 2^-22 of the result's terms and left out.
 struct Planes16 { const char *hi, *lo; int64_t ld, step; };          // ld, step in elements
 
-template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, bool AK, bool BK, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * 64)
 gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
 {
@@ -135,7 +149,8 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     __shared__ __align__(16) char lds[2][StepA::BYTES + StepB::BYTES];
     uint32_t g, mb, nb;
     const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
-    block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
+    if (TRIANGLE) triangle_place(blockIdx.x % all, all, mblocks, g, mb, nb);
+    else block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
     const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
     const int64_t kstepA = AK ? G16_STEP * 2 : A.ld * (G16_STEP * 2), kstepB = BK ? G16_STEP * 2 : B.ld * (G16_STEP * 2);
     const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
@@ -220,10 +235,20 @@ void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, in
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64);
-    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, true, true, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, true, false, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, false, true, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, false, false, SPLIT><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+}
+
+// The lower triangle of blocks of a symmetric product, A B with B = A transposed as stored: both operands have the same orientation.
+template <typename V, int BM, int WM, int WN, bool SPLIT, class Epilogue>
+void launch_gemm16_triangle(hipStream_t s, int64_t batch, int64_t M, int64_t K, const Planes16 &a, bool near, const Epilogue &e)
+{
+    const uint32_t side = (uint32_t)((M + BM - 1) / BM);
+    const dim3 grid((uint32_t)(batch * side * (side + 1) / 2)), block(WM * WN * 64);
+    if (near) gemm16_kernel<V, BM, BM, WM, WN, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    else gemm16_kernel<V, BM, BM, WM, WN, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
 }
 
 }  // namespace netmax

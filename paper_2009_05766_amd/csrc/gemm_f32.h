@@ -109,12 +109,6 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
                          f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
 }
 
-// Whether pieces of four values can be taken whole: rows and matrices start at multiples of four values in aligned memory.
-inline bool whole_pieces(const void *p, int64_t ld, int64_t step, int value_bytes)
-{
-    return (uintptr_t)p % (4 * value_bytes) == 0 && ld % 4 == 0 && step % 4 == 0;
-}
-
 template <typename T, int BM, int BN, class Epilogue>
 void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {

@@ -4,12 +4,125 @@
 // The polynomial a s + b s^3 + c s^5 drives the singular values of X towards 1 and leaves the singular vectors alone.  Matrices with
 // more rows than columns are multiplied from the other side, A = X^T X and X <- a X + X B, which is the same polynomial on the smaller
 // square.
-#include "gemm_f32.h"
+//
+// X is held as two planes of halves, s X = hi + lo 2^-11, which carry 22 bits: |X| <= 1 at the start and every singular value stays below
+// 1.3, so that halves reach, and s, a power of two near the root of the longer side, keeps small entries away from the subnormal ones.
+//   float        all products of planes but lo lo (SPLIT): as exact as float products, at three times the cost of one product of halves
+//                instead of sixteen times
+//   bfloat16     products of hi planes (11 bits), the term a X from both planes.  B's diagonal, its large part near the end, is kept in float and
+//                joins a X: the rounding of B then halves the result's error, to 0.6e-3 where the rounding of the result itself is 1.7e-3
+// A and B are symmetric: their blocks on and below the diagonal are computed and written to both sides.
+#include "gemm16.h"
 #include "orth.h"
 
 namespace netmax {
 
 constexpr int NORM_BLOCKS = 64;       // partial sums of squares of one matrix
+
+__device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
+
+// v = hi + lo 2^-11
+struct TwoHalves {
+    _Float16 hi, lo;
+    __device__ __forceinline__ explicit TwoHalves(float v)
+    {
+        hi = (_Float16)v;
+        lo = (_Float16)((v - (float)hi) * 2048.0f);
+    }
+};
+__device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return fmaf((float)__builtin_bit_cast(_Float16, lo), 0x1p-11f, (float)__builtin_bit_cast(_Float16, hi)); }
+
+// Four neighbours of a row of planes; the planes' rows are padded to multiples of 8.
+__device__ __forceinline__ f32x4 load_planes(const uint16_t *hi, const uint16_t *lo)
+{
+    const uint2 h = *reinterpret_cast<const uint2 *>(hi), l = *reinterpret_cast<const uint2 *>(lo);
+    return f32x4{joined((uint16_t)h.x, (uint16_t)l.x), joined((uint16_t)(h.x >> 16), (uint16_t)(l.x >> 16)), joined((uint16_t)h.y, (uint16_t)l.y),
+                 joined((uint16_t)(h.y >> 16), (uint16_t)(l.y >> 16))};
+}
+__device__ __forceinline__ f32x4 load_plane(const uint16_t *hi)
+{
+    const uint2 h = *reinterpret_cast<const uint2 *>(hi);
+    return f32x4{joined((uint16_t)h.x, 0), joined((uint16_t)(h.x >> 16), 0), joined((uint16_t)h.y, 0), joined((uint16_t)(h.y >> 16), 0)};
+}
+__device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v)
+{
+    const TwoHalves a(v[0]), b(v[1]), c(v[2]), d(v[3]);
+    *reinterpret_cast<uint2 *>(hi) = make_uint2(half_bits(a.hi) | half_bits(b.hi) << 16, half_bits(c.hi) | half_bits(d.hi) << 16);
+    if (lo) *reinterpret_cast<uint2 *>(lo) = make_uint2(half_bits(a.lo) | half_bits(b.lo) << 16, half_bits(c.lo) | half_bits(d.lo) << 16);
+}
+
+// A symmetric result alpha acc + beta own as planes [batch][side][wide], zeros behind each row; lo may be null.  With `diagonal` its diagonal goes
+// there and is 0 in the planes.
+struct SquareEpilogue {
+    int64_t side, wide; float alpha, beta;
+    const uint16_t *own_hi, *own_lo; uint16_t *hi, *lo; float *diagonal;
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        // squares of 64 x 64 on the diagonal lie whole inside computed blocks and are written as they come; of all others the lower ones
+        const int64_t lower = m / 64 - n / 64, base = g * side * wide;
+        if (m >= wide || n >= wide || lower < 0) return;
+        if (m < side) {
+            const int64_t at = base + m * wide + n;
+            v *= alpha;
+            if (own_hi) v += beta * (own_lo ? load_planes(own_hi + at, own_lo + at) : load_plane(own_hi + at));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (n + e >= side) v[e] = 0.0f;
+                if (diagonal && n + e == m) { diagonal[g * side + m] = v[e]; v[e] = 0.0f; }
+            }
+            store_planes(hi + at, lo ? lo + at : nullptr, v);
+        } else {
+            v = f32x4{0, 0, 0, 0};                                  // the mirror image lies behind the rows
+        }
+        if (lower == 0) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const TwoHalves h(v[e]);                                // n + e < side: a lower square's columns all exist
+            hi[base + (n + e) * wide + m] = __builtin_bit_cast(uint16_t, h.hi);
+            if (lo) lo[base + (n + e) * wide + m] = __builtin_bit_cast(uint16_t, h.lo);
+        }
+    }
+};
+
+// X <- acc + (a + diagonal) X as planes [batch][rows][wide]; the diagonal goes by rows or, `tall`, by columns.
+struct StepEpilogue {
+    int64_t rows, cols, wide; float a; bool tall;
+    const uint16_t *own_hi, *own_lo; uint16_t *hi, *lo; const float *diagonal;
+    __device__ __forceinline__ f32x4 value(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        const int64_t at = (g * rows + m) * wide + n;
+        f32x4 f = {a, a, a, a};
+        if (diagonal) {
+            if (tall) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n + e < cols) f[e] += diagonal[g * cols + n + e];
+            } else {
+                f += diagonal[g * rows + m];
+            }
+        }
+        const f32x4 x = load_planes(own_hi + at, own_lo + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? fmaf(f[e], x[e], v[e]) : 0.0f;
+        return v;
+    }
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m >= rows || n >= wide) return;
+        const int64_t at = (g * rows + m) * wide + n;
+        store_planes(hi + at, lo + at, value(g, m, n, v));
+    }
+};
+
+// The last step: scale X to the caller's memory.
+template <typename T> struct LastEpilogue {
+    StepEpilogue step; float scale; T *out; int64_t ldo, so; bool whole;
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m >= step.rows || n >= step.cols) return;
+        store_up_to_four(out + g * so + m * ldo, n, step.cols, whole, scale * step.value(g, m, n, v));
+    }
+};
 
 // m' and a part of the sum of squares of u (double; the parts are added in order by whoever needs the norm).
 template <typename T>
@@ -38,62 +151,99 @@ __global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, double *__res
     if (threadIdx.x == 0) parts[g * NORM_BLOCKS + blockIdx.x] = part[0];
 }
 
+// The planes of s u / max(||u||, eps).
 template <typename T>
-__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, const double *__restrict__ parts, float *__restrict__ X)
+__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, const double *__restrict__ parts, float s, int64_t wide, uint16_t *__restrict__ hi, uint16_t *__restrict__ lo)
 {
-    const int64_t g = blockIdx.y, count = a.rows * a.cols;
+    const int64_t g = blockIdx.y, count = a.rows * wide;
     double sum = 0.0;
     for (int k = 0; k < NORM_BLOCKS; ++k) sum += parts[g * NORM_BLOCKS + k];
-    const double norm = sqrt(sum);
-    const float inv = (float)(1.0 / (norm > (double)a.eps || norm != norm ? norm : (double)a.eps));
+    const double norm = sqrt(sum), factor = (double)s / (norm > (double)a.eps || norm != norm ? norm : (double)a.eps);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < count; q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / a.cols, c = q % a.cols;
-        float u = load_value((const T *)a.g + g * a.sg + r * a.ldg + c);
-        if (a.m) {
-            const float m = a.m_out[g * a.sm + r * a.ldm + c];
-            u = a.nesterov ? fmaf(a.mu, m, u) : m;
+        const int64_t r = q / wide, c = q % wide;
+        float u = 0.0f;
+        if (c < a.cols) {
+            u = load_value((const T *)a.g + g * a.sg + r * a.ldg + c);
+            if (a.m) {
+                const float m = a.m_out[g * a.sm + r * a.ldm + c];
+                u = a.nesterov ? fmaf(a.mu, m, u) : m;
+            }
         }
-        X[g * count + q] = u * inv;
+        const TwoHalves h((float)((double)u * factor));
+        hi[g * count + q] = __builtin_bit_cast(uint16_t, h.hi);
+        lo[g * count + q] = __builtin_bit_cast(uint16_t, h.lo);
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) result_kernel(OrthArgs a, const float *__restrict__ X)
+static int64_t side_of(const OrthArgs &a) { return a.rows < a.cols ? a.rows : a.cols; }
+static int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+static int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+static int64_t x_bytes(const OrthArgs &a) { return up256(a.batch * a.rows * up8(a.cols) * 2); }               // one plane
+static int64_t square_bytes(const OrthArgs &a) { return up256(a.batch * side_of(a) * up8(side_of(a)) * 2); }
+
+int64_t orth_workspace(const OrthArgs &a)
 {
-    const int64_t g = blockIdx.y, count = a.rows * a.cols;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < count; q += (int64_t)gridDim.x * 256)
-        store_value((T *)a.out + g * a.so + q / a.cols * a.ldo + q % a.cols, a.scale * X[g * count + q]);
+    return 4 * x_bytes(a) + (a.bf16 ? 2 : 4) * square_bytes(a) + up256(a.batch * side_of(a) * 4) + up256(8 * a.batch * NORM_BLOCKS);
 }
 
-static int64_t side(const OrthArgs &a) { return a.rows < a.cols ? a.rows : a.cols; }
-static int64_t x_floats(const OrthArgs &a) { return (a.batch * a.rows * a.cols + 63) / 64 * 64; }
-static int64_t a_floats(const OrthArgs &a) { return (a.batch * side(a) * side(a) + 63) / 64 * 64; }
+// Blocks of 256, 128 or 64: the largest that still give most compute units one.
+static int block_of(int64_t blocks256, int64_t blocks128) { return blocks256 >= 192 ? 256 : blocks128 >= 192 ? 128 : 64; }
 
-int64_t orth_workspace(const OrthArgs &a) { return 4 * (2 * x_floats(a) + 2 * a_floats(a)) + 8 * a.batch * NORM_BLOCKS; }
-
-template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, float *work)
+template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
 {
-    float *X = work, *Y = X + x_floats(a), *A = Y + x_floats(a), *B = A + a_floats(a);
-    double *parts = (double *)(B + a_floats(a));
-    const int64_t k = side(a), xs = a.rows * a.cols;
+    const auto blocks = [&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; };
+    const int block = block_of(blocks(256), blocks(128));
+    if (block == 256) launch_gemm16_triangle<half8, 256, 2, 4, SPLIT>(s, batch, side, K, x, near, e);
+    else if (block == 128) launch_gemm16_triangle<half8, 128, 2, 2, SPLIT>(s, batch, side, K, x, near, e);
+    else launch_gemm16_triangle<half8, 64, 2, 2, SPLIT>(s, batch, side, K, x, near, e);
+}
+
+template <bool SPLIT, class Epilogue>
+static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, const Planes16 &b, const Epilogue &e)
+{
+    const bool tall = a.rows > a.cols;
+    const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
+    const int block = block_of(blocks(256), blocks(128));
+    const int64_t k = side_of(a);
+    const Planes16 &l = tall ? x : b, &r = tall ? b : x;            // B is symmetric: its rows are its columns
+    if (block == 256) launch_gemm16_blocks<half8, 256, 256, 2, 4, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
+    else if (block == 128) launch_gemm16_blocks<half8, 128, 128, 2, 2, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
+    else launch_gemm16_blocks<half8, 64, 64, 2, 2, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
+}
+
+template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char *work)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;
+    const auto take = [&](int64_t n) { char *p = work; work += n; return (uint16_t *)p; };
+    uint16_t *xh = take(x_bytes(a)), *xl = take(x_bytes(a)), *yh = take(x_bytes(a)), *yl = take(x_bytes(a));
+    uint16_t *ah = take(square_bytes(a)), *bh = take(square_bytes(a)), *al = SPLIT ? take(square_bytes(a)) : nullptr, *bl = SPLIT ? take(square_bytes(a)) : nullptr;
+    float *diagonal = (float *)take(up256(a.batch * side_of(a) * 4));
+    double *parts = (double *)work;
+    const int64_t side = side_of(a), wide = up8(a.cols), swide = up8(side), longer = a.rows > a.cols ? a.rows : a.cols;
+    const bool tall = a.rows > a.cols;
+    float sx = 1.0f;
+    while ((double)sx * sx * 2.0 < (double)longer) sx *= 2.0f;       // near the root of the longer side
     const dim3 grid(NORM_BLOCKS, (uint32_t)a.batch);
     momentum_kernel<T><<<grid, 256, 0, s>>>(a, parts);
-    normalise_kernel<T><<<grid, 256, 0, s>>>(a, parts, X);
-    const bool tall = a.rows > a.cols;
+    normalise_kernel<T><<<grid, 256, 0, s>>>(a, parts, sx, wide, xh, xl);
+    const auto planes = [](const uint16_t *h, const uint16_t *l, int64_t ld, int64_t rows) { return Planes16{(const char *)h, (const char *)l, ld, rows * ld}; };
     for (int i = 0; i < a.steps; ++i) {
-        launch_gemm_f32<float>(s, a.batch, k, k, tall ? a.rows : a.cols, Operand{X, a.cols, xs, !tall}, Operand{X, a.cols, xs, !tall},
-                               SumEpilogue<float>{k, k, 1.0f, 0.0f, nullptr, A});
-        launch_gemm_f32<float>(s, a.batch, k, k, k, Operand{A, k, k * k, true}, Operand{A, k, k * k, true}, SumEpilogue<float>{k, k, a.c, a.b, A, B});
-        const Operand x{X, a.cols, xs, tall}, p{B, k, k * k, true};
-        launch_gemm_f32<float>(s, a.batch, a.rows, a.cols, k, tall ? x : p, tall ? p : x, SumEpilogue<float>{a.rows, a.cols, 1.0f, a.a, X, Y});
-        float *t = X; X = Y; Y = t;
+        launch_square<SPLIT>(s, a.batch, side, tall ? a.rows : a.cols, planes(xh, xl, wide, a.rows), !tall,
+                             SquareEpilogue{side, swide, 1.0f / (sx * sx), 0.0f, nullptr, nullptr, ah, al, nullptr});
+        launch_square<SPLIT>(s, a.batch, side, side, planes(ah, al, swide, side), true,
+                             SquareEpilogue{side, swide, a.c, a.b, ah, al, bh, bl, SPLIT ? nullptr : diagonal});
+        const StepEpilogue step{a.rows, a.cols, wide, a.a, tall, xh, xl, yh, yl, SPLIT ? nullptr : diagonal};
+        const Planes16 x = planes(xh, xl, wide, a.rows), b = planes(bh, bl, swide, side);
+        if (i + 1 < a.steps) launch_step<SPLIT>(s, a, x, b, step);
+        else launch_step<SPLIT>(s, a, x, b, LastEpilogue<T>{step, a.scale / sx, (T *)a.out, a.ldo, a.so, whole_pieces(a.out, a.ldo, a.so, sizeof(T))});
+        uint16_t *t = xh; xh = yh; yh = t;
+        t = xl; xl = yl; yl = t;
     }
-    result_kernel<T><<<grid, 256, 0, s>>>(a, X);
 }
 
 void launch_orth(hipStream_t s, const OrthArgs &a, void *work)
 {
-    if (a.bf16) orth_of<uint16_t>(s, a, (float *)work); else orth_of<float>(s, a, (float *)work);
+    if (a.bf16) orth_of<uint16_t>(s, a, (char *)work); else orth_of<float>(s, a, (char *)work);
 }
 
 }  // namespace netmax

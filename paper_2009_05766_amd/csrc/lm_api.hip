@@ -149,7 +149,8 @@ extern "C" int netmax_linear_grad(const netmax_linear_shape *s, const void *dy, 
 static int check_orth(const netmax_orth_shape *s)
 {
     if (!s) return netmax_fail(NETMAX_EINVAL, "shape is NULL");
-    if (s->batch < 0 || s->batch > 65535 || s->rows < 1 || s->cols < 1) return netmax_fail(NETMAX_EINVAL, "need 0 <= batch <= 65535, rows >= 1 and cols >= 1");
+    if (s->batch < 0 || s->batch > 65535 || s->rows < 1 || s->cols < 1 || s->rows >= 1 << 22 || s->cols >= 1 << 22)
+        return netmax_fail(NETMAX_EINVAL, "need 0 <= batch <= 65535, 1 <= rows < 2^22 and 1 <= cols < 2^22");
     if (!product_fits(s->batch, s->rows, s->cols) || !blocks_fit(s->batch, s->rows, s->cols)) return netmax_fail(NETMAX_EINVAL, "the matrices are too large");
     if (!dtype_known(s->dtype)) return netmax_fail(NETMAX_EINVAL, "dtype must be NETMAX_F32 or NETMAX_BF16");
     if (s->steps < 1 || s->steps > 64) return netmax_fail(NETMAX_EINVAL, "steps must be in 1..64");
