@@ -42,6 +42,14 @@ __device__ __forceinline__ s16x4 read_turned(const char *__restrict__ p)
 }
 template <typename V> __device__ __forceinline__ V read_unit(const char *__restrict__ p) { return *reinterpret_cast<const V *>(p); }
 
+// LDS that lanes of one wave exchange values through: what is written before is read behind.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 64 ? (k >> 1) & 1 : k & 3; }
 
 // One operand's step: ROWS results' rows x 64 contraction indices, brought by THREADS threads.
@@ -211,16 +219,34 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
         }
         __syncthreads();
     }
+    // Results leave by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes have neighbouring columns of a row: straight from the
+    // instruction's layout a request would touch 32 rows, 16 bytes in each.
+    constexpr int COLS = TN * 32, PITCH = COLS + 4;
     const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
+    float *stage = (float *)lds + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
     const int64_t where = splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                epilogue(where, m0 + wm + i * 32 + at, n0 + wn + j * 32 + e * 8 + half * 4,
-                         f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+                store4(stage + at * PITCH + j * 32 + e * 8 + half * 4, f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+        wave_order();
+#pragma unroll
+        for (int r = 0; r < 32; r += 256 / COLS) {
+            const int row = r + lane / (COLS / 4), col = lane % (COLS / 4) * 4;
+            epilogue(where, m0 + wm + i * 32 + row, n0 + wn + col, load4(stage + row * PITCH + col));
+        }
+        if constexpr (TRIANGLE)                                     // the mirror image: rows are columns
+#pragma unroll
+            for (int c = 0; c < COLS; c += 8) {
+                const int row = c + lane / 8, col = lane % 8 * 4;
+                const float *p = stage + col * PITCH + row;
+                epilogue.mirror(where, n0 + wn + row, m0 + wm + i * 32 + col, f32x4{p[0], p[PITCH], p[2 * PITCH], p[3 * PITCH]});
+            }
+        wave_order();
+    }
 }
 
 // Whether a matrix can be multiplied where it lies (see the top); `stored`: its extent along memory.

@@ -112,41 +112,57 @@ static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N,
 
 // ---- dz and db -------------------------------------------------------------------------------------------------------
 
-// A workgroup takes SLOPE_ROWS rows of 64 columns: dz, and the column sums of dz over these rows (float, rows in order).
-constexpr int SLOPE_ROWS = 64;
+// A workgroup takes SLOPE_ROWS rows of 256 columns, a wave every fourth row, a lane four columns: dz, and the column sums of dz (before its rounding) over
+// these rows, in float, in a fixed order.  Bound by memory: dy and z in, dz out.
+constexpr int SLOPE_ROWS = 64, SLOPE_COLS = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(256)
-slope_kernel(int64_t rows, int64_t cols, const T *__restrict__ dy, int64_t lddy, int64_t sdy, const T *__restrict__ z, int64_t ldz, int64_t sz, int act,
-             T *__restrict__ dz, int64_t wide, float *__restrict__ sums)
+slope_kernel(int64_t rows, int64_t cols, const T *__restrict__ dy, int64_t lddy, int64_t sdy, bool wdy, const T *__restrict__ z, int64_t ldz, int64_t sz, bool wz, int act,
+             T *__restrict__ dz, int64_t wide, bool wdz, float *__restrict__ sums)
 {
     // dz has rows of `wide` values, zeros behind the columns: what the product's contraction over them needs
-    __shared__ float part[4][64];
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), r0 = (int64_t)blockIdx.y * SLOPE_ROWS;
-    float sum = 0.0f;
-    if (n < cols)
-        for (int64_t r = r0 + (threadIdx.x >> 6); r < r0 + SLOPE_ROWS && r < rows; r += 4) {
-            float v = load_value(dy + g * sdy + r * lddy + n);
-            if (act != ACT_NONE) v *= act_slope(act, load_value(z + g * sz + r * ldz + n));
+    __shared__ __align__(16) float part[4][SLOPE_COLS];
+    const int wave = threadIdx.x >> 6, at = (threadIdx.x & 63) * 4;
+    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * SLOPE_COLS + at, r0 = (int64_t)blockIdx.y * SLOPE_ROWS + wave;
+    const int64_t end = (int64_t)(blockIdx.y + 1) * SLOPE_ROWS < rows ? (int64_t)(blockIdx.y + 1) * SLOPE_ROWS : rows;
+    dy += g * sdy;
+    z += g * sz;
+    f32x4 sum = {0, 0, 0, 0};
+    if (n < wide)
+#pragma unroll 4
+        for (int64_t r = r0; r < end; r += 4) {
+            f32x4 v = load_up_to_four(dy + r * lddy, n, cols, wdy);
+            if (act != ACT_NONE) {
+                const f32x4 pre = load_up_to_four(z + r * ldz, n, cols, wz);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? v[e] * act_slope(act, pre[e]) : 0.0f;
+            }
             sum += v;
-            if (dz) store_value(dz + (g * rows + r) * wide + n, v);
+            if (dz) store_up_to_four(dz + (g * rows + r) * wide, n, wide, wdz, v);
         }
-    else if (dz && n < wide)
-        for (int64_t r = r0 + (threadIdx.x >> 6); r < r0 + SLOPE_ROWS && r < rows; r += 4) dz[(g * rows + r) * wide + n] = T(0);
-    part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+    if (!sums) return;
+    store4(&part[wave][at], sum);
     __syncthreads();
-    if (sums && threadIdx.x < 64 && n < cols)
-        sums[((int64_t)g * gridDim.y + blockIdx.y) * cols + n] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+    const int64_t col = (int64_t)blockIdx.x * SLOPE_COLS + threadIdx.x;
+    if (col < cols)
+        sums[((int64_t)g * gridDim.y + blockIdx.y) * cols + col] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
 }
 
+// 64 columns per workgroup; four waves take the parts in turn, then their sums are added in order.
 template <typename T>
 __global__ void __launch_bounds__(256) bias_sum_kernel(int64_t cols, int64_t parts, const float *__restrict__ sums, T *__restrict__ db, int64_t sdb)
 {
-    const int64_t g = blockIdx.y, n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= cols) return;
+    __shared__ float part[4][64];
+    const int wave = threadIdx.x >> 6, at = threadIdx.x & 63;
+    const int64_t g = blockIdx.y, n = (int64_t)blockIdx.x * 64 + at;
     float sum = 0.0f;
-    for (int64_t k = 0; k < parts; ++k) sum += sums[(g * parts + k) * cols + n];
-    store_value(db + g * sdb + n, sum);
+    if (n < cols)
+#pragma unroll 8
+        for (int64_t k = wave; k < parts; k += 4) sum += sums[(g * parts + k) * cols + n];
+    part[wave][at] = sum;
+    __syncthreads();
+    if (wave == 0 && n < cols) store_value(db + g * sdb + n, (part[0][at] + part[1][at]) + (part[2][at] + part[3][at]));
 }
 
 // ---- launchers -------------------------------------------------------------------------------------------------------
@@ -197,10 +213,11 @@ int64_t linear_grad_workspace(const LinearGradArgs &a)
 template <typename T> static void launch_slopes(hipStream_t s, const LinearGradArgs &a, T *dz, float *sums)
 {
     if ((dz || a.db) && a.rows > 0)
-        slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + 63) / 64), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
-            a.rows, a.dout, (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz, dz_wide(a), a.db ? sums : nullptr);
+        slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
+            a.rows, a.dout, (const T *)a.dy, a.lddy, a.sdy, whole_pieces(a.dy, a.lddy, a.sdy, sizeof(T)), (const T *)a.z, a.ldz, a.sz,
+            whole_pieces(a.z, a.ldz, a.sz, sizeof(T)), a.act, dz, dz_wide(a), dz_wide(a) % 4 == 0, a.db ? sums : nullptr);
     if (a.db)
-        bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 255) / 256), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
+        bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 63) / 64), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
 }
 
 void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)

@@ -17,7 +17,7 @@
 
 namespace netmax {
 
-constexpr int NORM_BLOCKS = 64;       // partial sums of squares of one matrix
+constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, at most
 
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
 
@@ -52,35 +52,30 @@ __device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v
 }
 
 // A symmetric result alpha acc + beta own as planes [batch][side][wide], zeros behind each row; lo may be null.  With `diagonal` its diagonal goes
-// there and is 0 in the planes.
+// there and is 0 in the planes.  Squares of 64 x 64 on the diagonal lie whole inside computed blocks and are kept as they come; of all others those
+// below it are, and their mirror images.
 struct SquareEpilogue {
     int64_t side, wide; float alpha, beta;
     const uint16_t *own_hi, *own_lo; uint16_t *hi, *lo; float *diagonal;
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    __device__ __forceinline__ void keep(int64_t g, int64_t m, int64_t n, f32x4 v) const
     {
-        // squares of 64 x 64 on the diagonal lie whole inside computed blocks and are written as they come; of all others the lower ones
-        const int64_t lower = m / 64 - n / 64, base = g * side * wide;
-        if (m >= wide || n >= wide || lower < 0) return;
-        if (m < side) {
-            const int64_t at = base + m * wide + n;
-            v *= alpha;
-            if (own_hi) v += beta * (own_lo ? load_planes(own_hi + at, own_lo + at) : load_plane(own_hi + at));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (n + e >= side) v[e] = 0.0f;
-                if (diagonal && n + e == m) { diagonal[g * side + m] = v[e]; v[e] = 0.0f; }
-            }
-            store_planes(hi + at, lo ? lo + at : nullptr, v);
-        } else {
-            v = f32x4{0, 0, 0, 0};                                  // the mirror image lies behind the rows
-        }
-        if (lower == 0) return;
+        const int64_t at = (g * side + m) * wide + n;
+        v *= alpha;
+        if (own_hi) v += beta * (own_lo ? load_planes(own_hi + at, own_lo + at) : load_plane(own_hi + at));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const TwoHalves h(v[e]);                                // n + e < side: a lower square's columns all exist
-            hi[base + (n + e) * wide + m] = __builtin_bit_cast(uint16_t, h.hi);
-            if (lo) lo[base + (n + e) * wide + m] = __builtin_bit_cast(uint16_t, h.lo);
+            if (n + e >= side) v[e] = 0.0f;
+            if (diagonal && n + e == m) { diagonal[g * side + m] = v[e]; v[e] = 0.0f; }
         }
+        store_planes(hi + at, lo ? lo + at : nullptr, v);
+    }
+    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m < side && n < wide && m / 64 >= n / 64) keep(g, m, n, v);
+    }
+    __device__ __forceinline__ void mirror(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    {
+        if (m < side && n < wide && n / 64 > m / 64) keep(g, m, n, v);
     }
 };
 
@@ -124,23 +119,48 @@ template <typename T> struct LastEpilogue {
     }
 };
 
-// m' and a part of the sum of squares of u (double; the parts are added in order by whoever needs the norm).
+// Four neighbours q of a matrix, in units of four of rows padded to `wide`: their row and column.
+__device__ __forceinline__ void unit_place(int64_t q, uint32_t units, int64_t &r, int64_t &c)
+{
+    if (q <= 0xFFFFFFFF) { const uint32_t row = (uint32_t)q / units; r = row; c = ((uint32_t)q - row * units) * 4; }
+    else { r = q / units; c = (q - r * units) * 4; }
+}
+
+// Two kernels with the same workgroups: a workgroup takes every NORM_BLOCKS-th run of 256 units, four of them in flight per thread.
+constexpr int NORM_AHEAD = 4;
+
+// m' and a part of the sum of squares of u (in double; the parts are added in order by whoever needs the norm).
 template <typename T>
-__global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, double *__restrict__ parts)
+__global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, bool wg, bool wm, double *__restrict__ parts)
 {
     __shared__ double part[256];
-    const int64_t g = blockIdx.y, count = a.rows * a.cols;
+    const int64_t g = blockIdx.y;
+    const uint32_t units = (uint32_t)((a.cols + 3) / 4);
+    const int64_t count = a.rows * units, stride = (int64_t)gridDim.x * 256;
+    const T *from = (const T *)a.g + g * a.sg;
     double sum = 0.0;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < count; q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / a.cols, c = q % a.cols;
-        float u = load_value((const T *)a.g + g * a.sg + r * a.ldg + c);
-        if (a.m) {
-            const int64_t at = g * a.sm + r * a.ldm + c;
-            const float m = fmaf(a.mu, a.m[at], u);
-            a.m_out[at] = m;
-            u = a.nesterov ? fmaf(a.mu, m, u) : m;
+    for (int64_t q0 = (int64_t)blockIdx.x * 256 + threadIdx.x; q0 < count; q0 += NORM_AHEAD * stride) {
+        f32x4 u[NORM_AHEAD], m[NORM_AHEAD];
+        int64_t r[NORM_AHEAD], c[NORM_AHEAD];
+#pragma unroll
+        for (int k = 0; k < NORM_AHEAD; ++k) {
+            const int64_t q = q0 + k * stride;
+            if (q >= count) { u[k] = m[k] = f32x4{0, 0, 0, 0}; continue; }
+            unit_place(q, units, r[k], c[k]);
+            u[k] = load_up_to_four(from + r[k] * a.ldg, c[k], a.cols, wg);
+            if (a.m) m[k] = load_up_to_four(a.m + g * a.sm + r[k] * a.ldm, c[k], a.cols, wm);
         }
-        sum += (double)u * (double)u;
+#pragma unroll
+        for (int k = 0; k < NORM_AHEAD; ++k) {
+            if (q0 + k * stride >= count) continue;
+            if (a.m) {
+                m[k] = fma4(a.mu, m[k], u[k]);
+                store_up_to_four(a.m_out + g * a.sm + r[k] * a.ldm, c[k], a.cols, wm, m[k]);
+                u[k] = a.nesterov ? fma4(a.mu, m[k], u[k]) : m[k];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += (double)u[k][e] * (double)u[k][e];
+        }
     }
     part[threadIdx.x] = sum;
     __syncthreads();
@@ -148,31 +168,51 @@ __global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, double *__res
         if ((int)threadIdx.x < d) part[threadIdx.x] += part[threadIdx.x + d];
         __syncthreads();
     }
-    if (threadIdx.x == 0) parts[g * NORM_BLOCKS + blockIdx.x] = part[0];
+    if (threadIdx.x == 0) parts[g * gridDim.x + blockIdx.x] = part[0];
 }
 
 // The planes of s u / max(||u||, eps).
 template <typename T>
-__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, const double *__restrict__ parts, float s, int64_t wide, uint16_t *__restrict__ hi, uint16_t *__restrict__ lo)
+__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, bool wg, bool wm, const double *__restrict__ parts, float s, int64_t wide, uint16_t *__restrict__ hi,
+                                                        uint16_t *__restrict__ lo)
 {
-    const int64_t g = blockIdx.y, count = a.rows * wide;
+    const int64_t g = blockIdx.y;
+    const uint32_t units = (uint32_t)(wide / 4);
+    const int64_t count = a.rows * units, stride = (int64_t)gridDim.x * 256;
     double sum = 0.0;
-    for (int k = 0; k < NORM_BLOCKS; ++k) sum += parts[g * NORM_BLOCKS + k];
+    for (uint32_t k = 0; k < gridDim.x; ++k) sum += parts[g * gridDim.x + k];
     const double norm = sqrt(sum), factor = (double)s / (norm > (double)a.eps || norm != norm ? norm : (double)a.eps);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < count; q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / wide, c = q % wide;
-        float u = 0.0f;
-        if (c < a.cols) {
-            u = load_value((const T *)a.g + g * a.sg + r * a.ldg + c);
-            if (a.m) {
-                const float m = a.m_out[g * a.sm + r * a.ldm + c];
-                u = a.nesterov ? fmaf(a.mu, m, u) : m;
-            }
+    const T *from = (const T *)a.g + g * a.sg;
+    for (int64_t q0 = (int64_t)blockIdx.x * 256 + threadIdx.x; q0 < count; q0 += NORM_AHEAD * stride) {
+        f32x4 u[NORM_AHEAD], m[NORM_AHEAD];
+#pragma unroll
+        for (int k = 0; k < NORM_AHEAD; ++k) {
+            const int64_t q = q0 + k * stride;
+            u[k] = m[k] = f32x4{0, 0, 0, 0};
+            if (q >= count) continue;
+            int64_t r, c;
+            unit_place(q, units, r, c);
+            if (!a.m || a.nesterov) u[k] = load_up_to_four(from + r * a.ldg, c, a.cols, wg);
+            if (a.m) m[k] = load_up_to_four(a.m_out + g * a.sm + r * a.ldm, c, a.cols, wm);
         }
-        const TwoHalves h((float)((double)u * factor));
-        hi[g * count + q] = __builtin_bit_cast(uint16_t, h.hi);
-        lo[g * count + q] = __builtin_bit_cast(uint16_t, h.lo);
+#pragma unroll
+        for (int k = 0; k < NORM_AHEAD; ++k) {
+            const int64_t q = q0 + k * stride;
+            if (q >= count) continue;
+            if (a.m) u[k] = a.nesterov ? fma4(a.mu, m[k], u[k]) : m[k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[k][e] = (float)((double)u[k][e] * factor);
+            store_planes(hi + (g * count + q) * 4, lo + (g * count + q) * 4, u[k]);
+        }
     }
+}
+
+// Workgroups for one matrix: enough for the card, and not more than have something to do.
+static uint32_t norm_blocks(const OrthArgs &a)
+{
+    const int64_t work = (a.rows * ((a.cols + 3) / 4) + 256 * NORM_AHEAD - 1) / (256 * NORM_AHEAD), fill = (2048 + a.batch - 1) / a.batch;
+    const int64_t n = work < fill ? work : fill;
+    return (uint32_t)(n < 1 ? 1 : n > NORM_BLOCKS ? NORM_BLOCKS : n);
 }
 
 static int64_t side_of(const OrthArgs &a) { return a.rows < a.cols ? a.rows : a.cols; }
@@ -223,9 +263,10 @@ template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char
     const bool tall = a.rows > a.cols;
     float sx = 1.0f;
     while ((double)sx * sx * 2.0 < (double)longer) sx *= 2.0f;       // near the root of the longer side
-    const dim3 grid(NORM_BLOCKS, (uint32_t)a.batch);
-    momentum_kernel<T><<<grid, 256, 0, s>>>(a, parts);
-    normalise_kernel<T><<<grid, 256, 0, s>>>(a, parts, sx, wide, xh, xl);
+    const dim3 grid(norm_blocks(a), (uint32_t)a.batch);
+    const bool wg = whole_pieces(a.g, a.ldg, a.sg, sizeof(T)), wm = !a.m || (whole_pieces(a.m, a.ldm, a.sm, 4) && whole_pieces(a.m_out, a.ldm, a.sm, 4));
+    momentum_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts);
+    normalise_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts, sx, wide, xh, xl);
     const auto planes = [](const uint16_t *h, const uint16_t *l, int64_t ld, int64_t rows) { return Planes16{(const char *)h, (const char *)l, ld, rows * ld}; };
     for (int i = 0; i < a.steps; ++i) {
         launch_square<SPLIT>(s, a.batch, side, tall ? a.rows : a.cols, planes(xh, xl, wide, a.rows), !tall,
