@@ -24,7 +24,8 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int G16_STEP = 64;
+// Where a unit of 16 bytes of row r lies in a row of STEP indices: sixteen rows at one index in different banks.
+template <int STEP> __device__ __forceinline__ int near_unit(int r, int c) { return STEP == 32 ? c ^ ((r >> 2) & 3) : c ^ ((r >> 1) & 7); }
 
 __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma16(half8 a, half8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -53,8 +54,8 @@ __device__ __forceinline__ void wave_order()
 template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 64 ? (k >> 1) & 1 : k & 3; }
 
 // One operand's step: ROWS results' rows x 64 contraction indices, brought by THREADS threads.
-template <int ROWS, bool K_NEAR, int THREADS> struct Step16 {
-    static constexpr int BYTES = ROWS * G16_STEP * 2, PIECES = BYTES / 16 / THREADS, ROW_UNITS = ROWS / 8;
+template <int ROWS, bool K_NEAR, int STEP, int THREADS> struct Step16 {
+    static constexpr int BYTES = ROWS * STEP * 2, PIECES = BYTES / 16 / THREADS, ROW_UNITS = ROWS / 8;
     uint32_t offset[PIECES];                                        // of this lane's piece from the step's first byte
     int first_k[PIECES];
 
@@ -65,7 +66,7 @@ template <int ROWS, bool K_NEAR, int THREADS> struct Step16 {
         for (int u = 0; u < PIECES; ++u) {
             const int q = u * THREADS + (int)threadIdx.x;
             if (K_NEAR) {
-                const int r = q / 8, c = (q % 8) ^ ((r >> 1) & 7);
+                const int r = q / (STEP / 8), c = near_unit<STEP>(r, q % (STEP / 8));
                 const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
                 first_k[u] = c * 8;
                 offset[u] = (uint32_t)((row - row0) * ld * 2 + c * 16);
@@ -77,32 +78,23 @@ template <int ROWS, bool K_NEAR, int THREADS> struct Step16 {
             }
         }
     }
-    // `from`: the step's first byte (row row0, first index of the step); a wave's units lie next to each other
-    __device__ __forceinline__ void request(const char *from, char *lds) const
+    // Piece u of the step that starts at `from` (row row0, first index of the step) and has `left` indices (fewer than a step's: zeros behind them); a wave's units lie next to each other.
+    __device__ __forceinline__ void request(int u, const char *from, char *lds, int left) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int u = 0; u < PIECES; ++u) to_lds(from + offset[u], lds + u * THREADS * 16 + wave * 1024);
-    }
-    // the last step: indices from `left` on are zeros
-    __device__ __forceinline__ void request_tail(const char *from, char *lds, int left) const
-    {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-        for (int u = 0; u < PIECES; ++u)
-            to_lds(first_k[u] < left ? from + offset[u] : (const char *)&g16_zeros, lds + u * THREADS * 16 + wave * 1024);
+        to_lds(first_k[u] < left ? from + offset[u] : (const char *)&g16_zeros, lds + u * THREADS * 16 + wave * 1024);
     }
 };
 
 // Where a lane reads its part of 32 rows from `first` (a multiple of 32) on.
-template <int ROWS, bool K_NEAR> struct Fragment16 {
-    int base[4];                                                     // K_NEAR: one for each 16 indices of the step; else base[0]
+template <int ROWS, bool K_NEAR, int STEP> struct Fragment16 {
+    int base[STEP / 16];                                                     // K_NEAR: one for each 16 indices of the step; else base[0]
     __device__ __forceinline__ void place(int first)
     {
         const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
         if (K_NEAR) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) base[kk] = (first + at) * 128 + ((kk * 2 + half) ^ ((at >> 1) & 7)) * 16;
+            for (int kk = 0; kk < STEP / 16; ++kk) base[kk] = (first + at) * (STEP * 2) + near_unit<STEP>(at, kk * 2 + half) * 16;
         } else {
             const int group = (lane >> 4) & 1, t = lane & 15;
             base[0] = (half * 8 + t / 4) * (ROWS * 2) + ((first / 32) ^ turned_group<ROWS>(t / 4)) * 64 + group * 32 + (t & 3) * 8;
@@ -143,32 +135,33 @@ __device__ __forceinline__ void triangle_place(uint32_t id, uint32_t all, uint32
     nb = id - mb * (mb + 1) / 2;
 }
 
-// Products of planes: with SPLIT an operand is two planes, hi + lo 2^-11; lo hi + hi lo are added up first and scaled, then hi hi.  The
-// product of the two low planes is below 2^-22 of the result's terms and left out.
+// With SPLIT an operand is two planes, hi + lo: both planes of both operands come to LDS, and hi hi, hi lo and lo hi are added up; lo lo, below 2^-22 of
+// the terms, is left out.
 struct Planes16 { const char *hi, *lo; int64_t ld, step; };          // ld, step in elements
 
-template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
+template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, int STEP, int STAGES, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * 64)
 gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, TM = BM / WAVES_M / 32, TN = BN / WAVES_N / 32;
-    typedef Step16<BM, AK, THREADS> StepA;
-    typedef Step16<BN, BK, THREADS> StepB;
-    __shared__ __align__(16) char lds[2][StepA::BYTES + StepB::BYTES];
+    typedef Step16<BM, AK, STEP, THREADS> StepA;
+    typedef Step16<BN, BK, STEP, THREADS> StepB;
+    constexpr int PLANES = SPLIT ? 2 : 1, STAGE = PLANES * (StepA::BYTES + StepB::BYTES), REQUESTS = PLANES * (StepA::PIECES + StepB::PIECES);
+    __shared__ __align__(16) char lds[STAGES][STAGE];
     uint32_t g, mb, nb;
     const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
     if (TRIANGLE) triangle_place(blockIdx.x % all, all, mblocks, g, mb, nb);
     else block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
     const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
-    const int64_t kstepA = AK ? G16_STEP * 2 : A.ld * (G16_STEP * 2), kstepB = BK ? G16_STEP * 2 : B.ld * (G16_STEP * 2);
+    const int64_t kstepA = AK ? STEP * 2 : A.ld * (STEP * 2), kstepB = BK ? STEP * 2 : B.ld * (STEP * 2);
     const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
     const int wave = threadIdx.x >> 6, wm = wave / WAVES_N * (TM * 32), wn = wave % WAVES_N * (TN * 32);
     StepA sa;
     StepB sb;
     sa.place(m0, M, A.ld);
     sb.place(n0, N, B.ld);
-    Fragment16<BM, AK> fa[TM];
-    Fragment16<BN, BK> fb[TN];
+    Fragment16<BM, AK, STEP> fa[TM];
+    Fragment16<BN, BK, STEP> fb[TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i) fa[i].place(wm + i * 32);
 #pragma unroll
@@ -181,44 +174,82 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
-    const int64_t whole = (K + G16_STEP - 1) / G16_STEP;
-    const int first = (int)(whole * split / splits), steps = (int)(whole * (split + 1) / splits) - first, total = SPLIT ? 3 * steps : steps;
-    auto bring = [&](int s, char *to) {
-        const int part = !SPLIT || s >= 2 * steps ? 2 : s >= steps ? 1 : 0, k = first + (SPLIT ? s - part * steps : s);
-        const char *a = (SPLIT && part == 0 ? A.lo : A.hi) + from_a + k * kstepA, *b = (SPLIT && part == 1 ? B.lo : B.hi) + from_b + k * kstepB;
-        const int64_t left = K - (int64_t)k * G16_STEP;
-        if (left >= G16_STEP) {
-            sa.request(a, to);
-            sb.request(b, to + StepA::BYTES);
-        } else {
-            sa.request_tail(a, to, (int)left);
-            sb.request_tail(b, to + StepA::BYTES, (int)left);
+    const int64_t whole = (K + STEP - 1) / STEP;
+    const int first = (int)(whole * split / splits), total = (int)(whole * (split + 1) / splits) - first;
+    // A step on its way to LDS: its pieces are requested one by one.  Steps behind the last one are requested, too, as zeros that nobody reads, so that the
+    // loop below has no branches.
+    int64_t next_a, next_b;
+    char *next_to;
+    int next_left;
+    const auto aim = [&](int s) {
+        const int64_t k = first + s, left = K - k * STEP;
+        next_a = from_a + k * kstepA;
+        next_b = from_b + k * kstepB;
+        next_to = lds[s % STAGES];
+        next_left = s >= total ? 0 : left < STEP ? (int)left : STEP;
+    };
+    const auto request = [&](int u) {                               // pieces of A, of B, then those of the low planes
+        const bool low = u >= StepA::PIECES + StepB::PIECES;
+        char *to = next_to + (low ? StepA::BYTES + StepB::BYTES : 0);
+        if (low) u -= StepA::PIECES + StepB::PIECES;
+        if (u < StepA::PIECES) sa.request(u, (low ? A.lo : A.hi) + next_a, to, next_left);
+        else sb.request(u - StepA::PIECES, (low ? B.lo : B.hi) + next_b, to + StepA::BYTES, next_left);
+    };
+    // While 16 indices are multiplied the next 16 come from LDS into registers.  Before the last 16 of step s are multiplied, step s + 1 has arrived and all
+    // waves hold the rest of step s: the barrier and the first reads behind it are covered by those products, and step s + STAGES may fill the space of
+    // step s.  Its requests are spread over the products that follow (a wave waits at each one while the others' are taken, and so would its
+    // products behind them).  STAGES - 2 steps are under way at every wait.
+    constexpr int PARTS = STEP / 16, HALF = (REQUESTS + 1) / 2;      // half of the requests go with the step's last products, the others with the next step's first
+    V a[2][PLANES][TM], b[2][PLANES][TN];
+    const auto read = [&](int set, const char *from, int kk) {
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) {
+            const char *plane = from + p * (StepA::BYTES + StepB::BYTES);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) a[set][p][i] = fa[i].template read<V>(plane, kk);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) b[set][p][j] = fb[j].template read<V>(plane + StepA::BYTES, kk);
         }
     };
-    if (total > 0) bring(0, lds[0]);
-    __syncthreads();
-    for (int s = 0; s < total; ++s) {
-        if (s + 1 < total) bring(s + 1, lds[(s + 1) & 1]);
-        if (SPLIT && s == 2 * steps)
+    const auto multiply = [&](int set, int first_piece, int end_piece) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] *= 0x1p-11f;
-        const char *ca = lds[s & 1], *cb = ca + StepA::BYTES;
+            for (int j = 0; j < TN; ++j) {
+                const int at = i * TN + j, before = at * HALF / (TM * TN), here = (at + 1) * HALF / (TM * TN);
+                if constexpr (SPLIT) {
+                    acc[i][j] = mfma16(b[set][0][j], a[set][1][i], acc[i][j]);
+                    acc[i][j] = mfma16(b[set][1][j], a[set][0][i], acc[i][j]);
+                }
+                acc[i][j] = mfma16(b[set][0][j], a[set][0][i], acc[i][j]);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            V a[TM], b[TN];
+                for (int u = before; u < here; ++u)
+                    if (first_piece + u < end_piece) request(first_piece + u);
+            }
+    };
+    for (int s = 0; s < STAGES - 1; ++s) {
+        aim(s);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = fa[i].template read<V>(ca, kk);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = fb[j].template read<V>(cb, kk);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(b[j], a[i], acc[i][j]);
-        }
-        __syncthreads();
+        for (int u = 0; u < REQUESTS; ++u) request(u);
     }
+    aim(STAGES - 1);
+#pragma unroll
+    for (int u = 0; u < HALF; ++u) request(u);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * REQUESTS + HALF) : "memory");
+    read(0, lds[0], 0);
+    for (int s = 0; s < total; ++s) {
+#pragma unroll
+        for (int kk = 0; kk < PARTS - 1; ++kk) {
+            read((kk + 1) & 1, lds[s % STAGES], kk + 1);
+            if (kk == 0) multiply(0, HALF, REQUESTS);
+            else multiply(kk & 1, 0, 0);
+        }
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * REQUESTS) : "memory");
+        read(0, lds[(s + 1) % STAGES], 0);
+        aim(s + STAGES);
+        multiply(1, 0, HALF);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     // Results leave by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes have neighbouring columns of a row: straight from the
     // instruction's layout a request would touch 32 rows, 16 bytes in each.
     constexpr int COLS = TN * 32, PITCH = COLS + 4;
@@ -255,26 +286,36 @@ inline bool fits16(const void *p, int64_t ld, int64_t step, int64_t stored)
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && step % 8 == 0 && stored % 8 == 0 && ld < (1 << 22);
 }
 
-template <typename V, int BM, int BN, int WM, int WN, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
 void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, uint32_t splits,
                           const Epilogue &e)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64);
-    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
 }
 
 // The lower triangle of blocks of a symmetric product, A B with B = A transposed as stored: both operands have the same orientation.
-template <typename V, int BM, int WM, int WN, bool SPLIT, class Epilogue>
+template <typename V, int BM, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
 void launch_gemm16_triangle(hipStream_t s, int64_t batch, int64_t M, int64_t K, const Planes16 &a, bool near, const Epilogue &e)
 {
     const uint32_t side = (uint32_t)((M + BM - 1) / BM);
     const dim3 grid((uint32_t)(batch * side * (side + 1) / 2)), block(WM * WN * 64);
-    if (near) gemm16_kernel<V, BM, BM, WM, WN, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
-    else gemm16_kernel<V, BM, BM, WM, WN, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    if (near) gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    else gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+}
+
+// C = A B with A's contraction index near and B's as `bk` says, in blocks of BM x BM.
+template <typename V, int BM, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+void launch_gemm16_step(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, const Planes16 &b, bool bk, const Epilogue &e)
+{
+    const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BM - 1) / BM);
+    const dim3 grid((uint32_t)(batch * mb * nb)), block(WM * WN * 64);
+    if (bk) gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
+    else gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
 }
 
 }  // namespace netmax

@@ -74,7 +74,7 @@ struct Plan16 { int block; int splits; };
 static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
 {
     const auto blocks = [&](int64_t b) { return batch * ((M + b - 1) / b) * ((N + b - 1) / b); };
-    const int64_t steps = (K + G16_STEP - 1) / G16_STEP;
+    const int64_t steps = (K + 64 - 1) / 64;
     if (blocks(256) >= 192) return {256, 1};
     const int block = blocks(128) >= 128 && M > 64 && N > 64 ? 128 : 64;
     const int64_t want = 512 / (blocks(block) > 0 ? blocks(block) : 1), most = steps / 4;
@@ -91,9 +91,11 @@ template <class Epilogue>
 static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, int splits,
                             const Epilogue &e)
 {
-    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block) * splits;
+    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
 }
 
 // `work`: part_bytes() of it.

@@ -5,10 +5,11 @@
 // more rows than columns are multiplied from the other side, A = X^T X and X <- a X + X B, which is the same polynomial on the smaller
 // square.
 //
-// X is held as two planes of halves, s X = hi + lo 2^-11, which carry 22 bits: |X| <= 1 at the start and every singular value stays below
-// 1.3, so that halves reach, and s, a power of two near the root of the longer side, keeps small entries away from the subnormal ones.
-//   float        all products of planes but lo lo (SPLIT): as exact as float products, at three times the cost of one product of halves
-//                instead of sixteen times
+// X, A and B are held as two planes of halves, scaled by powers of two: 2^11 X = hi + lo, 2^8 A, 2^8 B.  hi carries 11 bits and lo the next ones, down to
+// the halves' smallest step, 2^-24: 2^-35 of X, whose entries are about one over the root of the longer side in the end and smaller by the root
+// of the other side at the start, 2^-32 of A and B.  Halves reach to 65504: |X| <= 1 at the start, and singular values stay below 1.3 with the
+// usual coefficients (a polynomial that lets X grow past 32, or A or B past 255, is not for this operator).
+//   float        hi hi + hi lo + lo hi (SPLIT): as exact as float products, at three times the cost of one product of halves instead of sixteen times
 //   bfloat16     products of hi planes (11 bits), the term a X from both planes.  B's diagonal, its large part near the end, is kept in float and
 //                joins a X: the rounding of B then halves the result's error, to 0.6e-3 where the rounding of the result itself is 1.7e-3
 // A and B are symmetric: their blocks on and below the diagonal are computed and written to both sides.
@@ -21,16 +22,18 @@ constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, 
 
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
 
-// v = hi + lo 2^-11
+constexpr float X_SCALE = 0x1p11f, SQUARE_SCALE = 0x1p8f;
+
+// v = hi + lo
 struct TwoHalves {
     _Float16 hi, lo;
     __device__ __forceinline__ explicit TwoHalves(float v)
     {
         hi = (_Float16)v;
-        lo = (_Float16)((v - (float)hi) * 2048.0f);
+        lo = (_Float16)(v - (float)hi);
     }
 };
-__device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return fmaf((float)__builtin_bit_cast(_Float16, lo), 0x1p-11f, (float)__builtin_bit_cast(_Float16, hi)); }
+__device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return (float)__builtin_bit_cast(_Float16, lo) + (float)__builtin_bit_cast(_Float16, hi); }
 
 // Four neighbours of a row of planes; the planes' rows are padded to multiples of 8.
 __device__ __forceinline__ f32x4 load_planes(const uint16_t *hi, const uint16_t *lo)
@@ -65,7 +68,7 @@ struct SquareEpilogue {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (n + e >= side) v[e] = 0.0f;
-            if (diagonal && n + e == m) { diagonal[g * side + m] = v[e]; v[e] = 0.0f; }
+            if (diagonal && n + e == m) { diagonal[g * side + m] = v[e] * (1.0f / SQUARE_SCALE); v[e] = 0.0f; }
         }
         store_planes(hi + at, lo ? lo + at : nullptr, v);
     }
@@ -97,6 +100,7 @@ struct StepEpilogue {
             }
         }
         const f32x4 x = load_planes(own_hi + at, own_lo + at);
+        v *= 1.0f / SQUARE_SCALE;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? fmaf(f[e], x[e], v[e]) : 0.0f;
         return v;
@@ -226,29 +230,34 @@ int64_t orth_workspace(const OrthArgs &a)
     return 4 * x_bytes(a) + (a.bf16 ? 2 : 4) * square_bytes(a) + up256(a.batch * side_of(a) * 4) + up256(8 * a.batch * NORM_BLOCKS);
 }
 
-// Blocks of 256, 128 or 64: the largest that still give most compute units one.
-static int block_of(int64_t blocks256, int64_t blocks128) { return blocks256 >= 192 ? 256 : blocks128 >= 192 ? 128 : 64; }
+// One launch for every block shape: `go` gets it as BM, waves, step and stages of gemm16_kernel.
+template <int BM_, int WM_, int WN_, int STEP_, int STAGES_> struct Shape { static constexpr int BM = BM_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_; };
+template <bool SPLIT, class Blocks, class Go> static void with_shape(const Blocks &blocks, const Go &go)
+{
+    // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has
+    if constexpr (!SPLIT)
+        if (blocks(256) >= 192) { go(Shape<256, 2, 4, 64, 2>()); return; }
+    if (blocks(128) >= 512) go(Shape<128, 2, 2, SPLIT ? 32 : 64, 2>());
+    else if (blocks(128) >= 128) go(Shape<128, 2, 4, SPLIT ? 32 : 64, 4>());
+    else go(Shape<64, 2, 2, SPLIT ? 32 : 64, 4>());
+}
 
 template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
 {
-    const auto blocks = [&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; };
-    const int block = block_of(blocks(256), blocks(128));
-    if (block == 256) launch_gemm16_triangle<half8, 256, 2, 4, SPLIT>(s, batch, side, K, x, near, e);
-    else if (block == 128) launch_gemm16_triangle<half8, 128, 2, 2, SPLIT>(s, batch, side, K, x, near, e);
-    else launch_gemm16_triangle<half8, 64, 2, 2, SPLIT>(s, batch, side, K, x, near, e);
+    with_shape<SPLIT>([&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; }, [&](auto f) {
+        launch_gemm16_triangle<half8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, batch, side, K, x, near, e);
+    });
 }
 
 template <bool SPLIT, class Epilogue>
 static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, const Planes16 &b, const Epilogue &e)
 {
     const bool tall = a.rows > a.cols;
-    const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
-    const int block = block_of(blocks(256), blocks(128));
     const int64_t k = side_of(a);
     const Planes16 &l = tall ? x : b, &r = tall ? b : x;            // B is symmetric: its rows are its columns
-    if (block == 256) launch_gemm16_blocks<half8, 256, 256, 2, 4, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
-    else if (block == 128) launch_gemm16_blocks<half8, 128, 128, 2, 2, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
-    else launch_gemm16_blocks<half8, 64, 64, 2, 2, SPLIT>(s, a.batch, a.rows, a.cols, k, l, true, r, tall, 1, e);
+    with_shape<SPLIT>([&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); }, [&](auto f) {
+        launch_gemm16_step<half8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e);
+    });
 }
 
 template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char *work)
@@ -259,24 +268,22 @@ template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char
     uint16_t *ah = take(square_bytes(a)), *bh = take(square_bytes(a)), *al = SPLIT ? take(square_bytes(a)) : nullptr, *bl = SPLIT ? take(square_bytes(a)) : nullptr;
     float *diagonal = (float *)take(up256(a.batch * side_of(a) * 4));
     double *parts = (double *)work;
-    const int64_t side = side_of(a), wide = up8(a.cols), swide = up8(side), longer = a.rows > a.cols ? a.rows : a.cols;
+    const int64_t side = side_of(a), wide = up8(a.cols), swide = up8(side);
     const bool tall = a.rows > a.cols;
-    float sx = 1.0f;
-    while ((double)sx * sx * 2.0 < (double)longer) sx *= 2.0f;       // near the root of the longer side
     const dim3 grid(norm_blocks(a), (uint32_t)a.batch);
     const bool wg = whole_pieces(a.g, a.ldg, a.sg, sizeof(T)), wm = !a.m || (whole_pieces(a.m, a.ldm, a.sm, 4) && whole_pieces(a.m_out, a.ldm, a.sm, 4));
     momentum_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts);
-    normalise_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts, sx, wide, xh, xl);
+    normalise_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts, X_SCALE, wide, xh, xl);
     const auto planes = [](const uint16_t *h, const uint16_t *l, int64_t ld, int64_t rows) { return Planes16{(const char *)h, (const char *)l, ld, rows * ld}; };
     for (int i = 0; i < a.steps; ++i) {
         launch_square<SPLIT>(s, a.batch, side, tall ? a.rows : a.cols, planes(xh, xl, wide, a.rows), !tall,
-                             SquareEpilogue{side, swide, 1.0f / (sx * sx), 0.0f, nullptr, nullptr, ah, al, nullptr});
+                             SquareEpilogue{side, swide, SQUARE_SCALE / (X_SCALE * X_SCALE), 0.0f, nullptr, nullptr, ah, al, nullptr});
         launch_square<SPLIT>(s, a.batch, side, side, planes(ah, al, swide, side), true,
-                             SquareEpilogue{side, swide, a.c, a.b, ah, al, bh, bl, SPLIT ? nullptr : diagonal});
+                             SquareEpilogue{side, swide, a.c / SQUARE_SCALE, a.b, ah, al, bh, bl, SPLIT ? nullptr : diagonal});
         const StepEpilogue step{a.rows, a.cols, wide, a.a, tall, xh, xl, yh, yl, SPLIT ? nullptr : diagonal};
         const Planes16 x = planes(xh, xl, wide, a.rows), b = planes(bh, bl, swide, side);
         if (i + 1 < a.steps) launch_step<SPLIT>(s, a, x, b, step);
-        else launch_step<SPLIT>(s, a, x, b, LastEpilogue<T>{step, a.scale / sx, (T *)a.out, a.ldo, a.so, whole_pieces(a.out, a.ldo, a.so, sizeof(T))});
+        else launch_step<SPLIT>(s, a, x, b, LastEpilogue<T>{step, a.scale / X_SCALE, (T *)a.out, a.ldo, a.so, whole_pieces(a.out, a.ldo, a.so, sizeof(T))});
         uint16_t *t = xh; xh = yh; yh = t;
         t = xl; xl = yl; yl = t;
     }
