@@ -16,25 +16,39 @@ struct Operand { const void *p; int64_t ld, step; bool k_near; };
 
 enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
-// act(z); the exact (error function) form of GELU.
+// The normal distribution function as 0.5 (1 + erf(z / sqrt 2)) and the bell exp(-z^2 / 2), which its approximation needs anyway: formula 7.1.26 of
+// Abramowitz and Stegun's handbook, erf x = 1 - (a1 t + .. + a5 t^5) exp(-x^2) with t = 1 / (1 + p x) for x >= 0, to 1.5e-7.  (The library's erff took as
+// long as all other work of an epilogue.)
+__device__ __forceinline__ float normal_distribution(float z, float &bell)
+{
+    const float x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+    bell = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+    const float tail = 0.5f * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * bell;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+__device__ __forceinline__ float sigmoid_of(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
+
+// act(z); GELU with the normal distribution function (not its tanh form).
 __device__ __forceinline__ float act_of(int act, float z)
 {
+    float bell;
     if (act == ACT_RELU) return z < 0.0f ? 0.0f : z;                // a NaN stays one
-    if (act == ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (act == ACT_SILU) return z / (1.0f + expf(-z));
+    if (act == ACT_GELU) return z * normal_distribution(z, bell);
+    if (act == ACT_SILU) return z * sigmoid_of(z);
     return z;
 }
 
-// act'(z); ReLU's is 0 at 0.  SiLU's factor 1 - s of a large z times a vanishing s would be inf * 0: s is 0 there first.
+// act'(z); ReLU's is 0 at 0.  Far out a factor that grows with z meets one that has vanished: such products are 0.
 __device__ __forceinline__ float act_slope(int act, float z)
 {
     if (act == ACT_RELU) return z > 0.0f ? 1.0f : z != z ? z : 0.0f;
     if (act == ACT_GELU) {
-        const float bell = expf(-0.5f * z * z) * 0.39894228040143268f;
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + (bell == 0.0f ? 0.0f : z * bell);
+        float bell;
+        const float below = normal_distribution(z, bell);
+        return below + (bell == 0.0f ? 0.0f : z * (bell * 0.39894228f));
     }
     if (act == ACT_SILU) {
-        const float s = 1.0f / (1.0f + expf(-z));
+        const float s = sigmoid_of(z);
         return s == 0.0f ? 0.0f : s * (1.0f + z * (1.0f - s));
     }
     return 1.0f;

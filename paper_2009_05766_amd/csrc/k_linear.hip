@@ -114,20 +114,20 @@ static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N,
 
 // ---- dz and db -------------------------------------------------------------------------------------------------------
 
-// A workgroup takes SLOPE_ROWS rows of 256 columns, a wave every fourth row, a lane four columns: dz, and the column sums of dz (before its rounding) over
+// A workgroup takes `run` rows of 256 columns, a wave every fourth row, a lane four columns: dz, and the column sums of dz (before its rounding) over
 // these rows, in float, in a fixed order.  Bound by memory: dy and z in, dz out.
-constexpr int SLOPE_ROWS = 64, SLOPE_COLS = 256;
+constexpr int SLOPE_COLS = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(256)
-slope_kernel(int64_t rows, int64_t cols, const T *__restrict__ dy, int64_t lddy, int64_t sdy, bool wdy, const T *__restrict__ z, int64_t ldz, int64_t sz, bool wz, int act,
+slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int64_t lddy, int64_t sdy, bool wdy, const T *__restrict__ z, int64_t ldz, int64_t sz, bool wz, int act,
              T *__restrict__ dz, int64_t wide, bool wdz, float *__restrict__ sums)
 {
     // dz has rows of `wide` values, zeros behind the columns: what the product's contraction over them needs
     __shared__ __align__(16) float part[4][SLOPE_COLS];
     const int wave = threadIdx.x >> 6, at = (threadIdx.x & 63) * 4;
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * SLOPE_COLS + at, r0 = (int64_t)blockIdx.y * SLOPE_ROWS + wave;
-    const int64_t end = (int64_t)(blockIdx.y + 1) * SLOPE_ROWS < rows ? (int64_t)(blockIdx.y + 1) * SLOPE_ROWS : rows;
+    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * SLOPE_COLS + at, r0 = (int64_t)blockIdx.y * run + wave;
+    const int64_t end = (int64_t)(blockIdx.y + 1) * run < rows ? (int64_t)(blockIdx.y + 1) * run : rows;
     dy += g * sdy;
     z += g * sz;
     f32x4 sum = {0, 0, 0, 0};
@@ -198,9 +198,17 @@ void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
     launch_product16(s, a.batch, a.rows, a.dout, a.din, x, true, w, false, forward_epilogue<uint16_t>(a), at);
 }
 
-static int64_t sum_parts(const LinearGradArgs &a) { return (a.rows + SLOPE_ROWS - 1) / SLOPE_ROWS; }
-static int64_t sum_bytes(const LinearGradArgs &a) { return round_up(a.batch * sum_parts(a) * a.dout * 4, 256); }
 static int64_t dz_wide(const LinearGradArgs &a) { return a.bf16 ? round_up(a.dout, 8) : a.dout; }
+// Rows of a workgroup of slope_kernel: 64, or fewer where that leaves compute units without work (at 1111 x 2049, rows at odd places, 64: 35 us).
+static int slope_run(const LinearGradArgs &a)
+{
+    const int64_t across = a.batch * ((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS);
+    int run = 64;
+    while (run > 8 && across * ((a.rows + run - 1) / run) < 1024) run /= 2;
+    return run;
+}
+static int64_t sum_parts(const LinearGradArgs &a) { return (a.rows + slope_run(a) - 1) / slope_run(a); }
+static int64_t sum_bytes(const LinearGradArgs &a) { return round_up(a.batch * sum_parts(a) * a.dout * 4, 256); }
 
 int64_t linear_grad_workspace(const LinearGradArgs &a)
 {
@@ -216,7 +224,7 @@ template <typename T> static void launch_slopes(hipStream_t s, const LinearGradA
 {
     if ((dz || a.db) && a.rows > 0)
         slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
-            a.rows, a.dout, (const T *)a.dy, a.lddy, a.sdy, whole_pieces(a.dy, a.lddy, a.sdy, sizeof(T)), (const T *)a.z, a.ldz, a.sz,
+            a.rows, a.dout, slope_run(a), (const T *)a.dy, a.lddy, a.sdy, whole_pieces(a.dy, a.lddy, a.sdy, sizeof(T)), (const T *)a.z, a.ldz, a.sz,
             whole_pieces(a.z, a.ldz, a.sz, sizeof(T)), a.act, dz, dz_wide(a), dz_wide(a) % 4 == 0, a.db ? sums : nullptr);
     if (a.db)
         bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 63) / 64), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
