@@ -14,6 +14,16 @@ namespace netmax {
 
 struct Operand { const void *p; int64_t ld, step; bool k_near; };
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// LDS that lanes of one wave exchange values through: what is written before is read behind.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 enum Act : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
 // The normal distribution function as 0.5 (1 + erf(z / sqrt 2)) and the bell exp(-z^2 / 2), which its approximation needs anyway: formula 7.1.26 of

@@ -18,7 +18,6 @@
 
 namespace netmax {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -42,14 +41,6 @@ __device__ __forceinline__ s16x4 read_turned(const char *__restrict__ p)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
 template <typename V> __device__ __forceinline__ V read_unit(const char *__restrict__ p) { return *reinterpret_cast<const V *>(p); }
-
-// LDS that lanes of one wave exchange values through: what is written before is read behind.
-__device__ __forceinline__ void wave_order()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 64 ? (k >> 1) & 1 : k & 3; }
 

@@ -1,29 +1,27 @@
 // C = A B for operands of any type, shape, stride and orientation, multiplied in float on v_mfma_f32_32x32x2_f32.
 //
-// A workgroup of four waves has a block of BM x BN results; a step of 16 contraction indices lies in LDS as [k][m] and [k][n], the
-// instruction's own layout (lane l: row l % 32, index l / 32), while the next step is on its way in registers.  B goes in as the
-// instruction's first operand, so that a lane ends with four neighbouring columns of a row.
+// Four waves have a block of BM x BN results; a step of STEP contraction indices lies in LDS as [k][m] and [k][n], the instruction's own layout (lane
+// l: row l % 32, index l / 32), while the next step is on its way in registers.  Where blocks are few, GROUPS groups of four waves share a block's
+// steps in turn and add up their results in LDS: few workgroups are bound by the chain of loads, barrier and products of a step, and four waves
+// by the instruction's 64 cycles (16 x 64 x 784 x 512: 31.6 us in one group and steps of 16).  B goes in as the instruction's first operand, so that a
+// lane ends with four neighbouring columns of a row.
 #pragma once
 #include "gemm.h"
 
 namespace netmax {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
-constexpr int GEMM_STEP = 16;
-
 // The values of one step that a thread brings: pieces of four neighbours in memory.
-template <typename T, int ROWS, bool K_NEAR> struct StepPieces {
-    static constexpr int PIECES = ROWS * GEMM_STEP / 4 / 256;
+template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
+    static constexpr int PIECES = ROWS * STEP / 4 / 256;
     static constexpr int PITCH = ROWS + 4;
     f32x4 v[PIECES];
     __device__ __forceinline__ void request(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K, bool whole)
     {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
-            const int q = u * 256 + (int)threadIdx.x;
+            const int q = u * 256 + (int)(threadIdx.x & 255);
             if (K_NEAR) {
-                const int64_t r = row0 + q / (GEMM_STEP / 4), k = k0 + q % (GEMM_STEP / 4) * 4;
+                const int64_t r = row0 + q / (STEP / 4), k = k0 + q % (STEP / 4) * 4;
                 v[u] = r < rows ? load_up_to_four(p + r * ld, k, K, whole) : f32x4{0, 0, 0, 0};
             } else {
                 const int64_t k = k0 + q / (ROWS / 4), r = row0 + q % (ROWS / 4) * 4;
@@ -35,9 +33,9 @@ template <typename T, int ROWS, bool K_NEAR> struct StepPieces {
     {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
-            const int q = u * 256 + (int)threadIdx.x;
+            const int q = u * 256 + (int)(threadIdx.x & 255);
             if (K_NEAR) {
-                const int r = q / (GEMM_STEP / 4), k = q % (GEMM_STEP / 4) * 4;
+                const int r = q / (STEP / 4), k = q % (STEP / 4) * 4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) lds[(k + e) * PITCH + r] = v[u][e];
             } else {
@@ -48,21 +46,25 @@ template <typename T, int ROWS, bool K_NEAR> struct StepPieces {
     }
 };
 
-template <typename T, int BM, int BN, bool AK, bool BK, class Epilogue>
-__global__ void __launch_bounds__(256)
+template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
+__global__ void __launch_bounds__(256 * GROUPS)
 gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, bool wa, const T *__restrict__ B, int64_t ldb,
                 int64_t sb, bool wb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
 {
-    typedef StepPieces<T, BM, AK> PiecesA;
-    typedef StepPieces<T, BN, BK> PiecesB;
-    constexpr int TM = BM / 64, TN = BN / 64;                       // 32 x 32 results of a wave; the waves lie 2 x 2
-    __shared__ __align__(16) float la[2][GEMM_STEP * PiecesA::PITCH], lb[2][GEMM_STEP * PiecesB::PITCH];
+    typedef StepPieces<T, BM, STEP, AK> PiecesA;
+    typedef StepPieces<T, BN, STEP, BK> PiecesB;
+    // a wave has TM x TN squares of 32 x 32 results; SHARES waves of a group share a square and the indices of a step
+    constexpr int TM = BM >= 128 ? 2 : 1, TN = BN >= 128 ? 2 : 1, ACROSS = BN / 32 / TN, TILES = BM / 32 / TM * ACROSS, SHARES = 4 / TILES, PARTS = GROUPS * SHARES;
+    constexpr int STEP_FLOATS = STEP * (PiecesA::PITCH + PiecesB::PITCH);
+    static_assert(TILES * 32 * 36 <= 2 * GROUPS * STEP_FLOATS, "results leave by way of the steps' space");
+    static_assert((PARTS - 1) * BM * BN <= 2 * GROUPS * STEP_FLOATS, "partial results fit the steps' space");
+    __shared__ __align__(16) float lds[GROUPS][2][STEP_FLOATS];
     const uint32_t per = mblocks * nblocks, g = blockIdx.x / per, b = blockIdx.x % per;
     const int64_t m0 = (int64_t)(b / nblocks) * BM, n0 = (int64_t)(b % nblocks) * BN;
     A += (int64_t)g * sa;
     B += (int64_t)g * sb;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, at = lane & 31;
-    const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) & 3, group = threadIdx.x >> 8, half = lane >> 5, at = lane & 31;
+    const int tile = wave % TILES, share = wave / TILES, wm = tile / ACROSS * (TM * 32), wn = tile % ACROSS * (TN * 32);
     PiecesA pa;
     PiecesB pb;
     f32x16 acc[TM][TN];
@@ -72,22 +74,21 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    const int64_t steps = (K + GEMM_STEP - 1) / GEMM_STEP;
-    if (steps > 0) {
-        pa.request(A, lda, m0, M, 0, K, wa);
-        pb.request(B, ldb, n0, N, 0, K, wb);
-    }
-    for (int64_t s = 0; s < steps; ++s) {
-        float *ca = la[s & 1], *cb = lb[s & 1];
+    const int64_t steps = (K + STEP - 1) / STEP, turns = (steps + GROUPS - 1) / GROUPS;         // a group without a step has zeros
+    pa.request(A, lda, m0, M, (int64_t)group * STEP, K, wa);
+    pb.request(B, ldb, n0, N, (int64_t)group * STEP, K, wb);
+    for (int64_t s = 0; s < turns; ++s) {
+        float *ca = lds[group][s & 1], *cb = ca + STEP * PiecesA::PITCH;
         pa.place(ca);
         pb.place(cb);
         __syncthreads();
-        if (s + 1 < steps) {
-            pa.request(A, lda, m0, M, (s + 1) * GEMM_STEP, K, wa);
-            pb.request(B, ldb, n0, N, (s + 1) * GEMM_STEP, K, wb);
+        if (s + 1 < turns) {
+            pa.request(A, lda, m0, M, ((s + 1) * GROUPS + group) * STEP, K, wa);
+            pb.request(B, ldb, n0, N, ((s + 1) * GROUPS + group) * STEP, K, wb);
         }
 #pragma unroll
-        for (int k = 0; k < GEMM_STEP; k += 2) {
+        for (int q = 0; q < STEP / SHARES; q += 2) {
+            const int k = share * (STEP / SHARES) + q;
             float a[TM], c[TN];
 #pragma unroll
             for (int i = 0; i < TM; ++i) a[i] = ca[(k + half) * PiecesA::PITCH + wm + i * 32 + at];
@@ -99,17 +100,54 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
                 for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(c[j], a[i], acc[i][j], 0, 0, 0);
         }
     }
+    if constexpr (PARTS > 1) {
+        constexpr int STRIDE = TM * TN * 4 * TILES * 64;            // pieces of four of one part
+        const int part = group * SHARES + share;
+        f32x4 *mine = reinterpret_cast<f32x4 *>(&lds[0][0][0]) + tile * 64 + lane;
+        __syncthreads();
+        if (part > 0)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        mine[(part - 1) * STRIDE + ((i * TN + j) * 4 + e) * (TILES * 64)] =
+                            f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int o = 0; o < PARTS - 1 && part == 0; ++o)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x4 v = mine[o * STRIDE + ((i * TN + j) * 4 + e) * (TILES * 64)];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[i][j][4 * e + q] += v[q];
+                    }
+    }
+    // results leave by way of LDS, so that neighbouring lanes have neighbouring columns of a row
+    __syncthreads();
+    if (group * SHARES + share > 0) return;
+    float *stage = &lds[0][0][0] + __builtin_amdgcn_readfirstlane(tile) * (32 * 36);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+        for (int j = 0; j < TN; ++j) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                epilogue(g, m0 + wm + i * 32 + at, n0 + wn + j * 32 + e * 8 + half * 4,
-                         f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+                store4(stage + at * 36 + e * 8 + half * 4, f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
+            wave_order();
+#pragma unroll
+            for (int r = 0; r < 32; r += 8)
+                epilogue(g, m0 + wm + i * 32 + r + lane / 8, n0 + wn + j * 32 + lane % 8 * 4, load4(stage + (r + lane / 8) * 36 + lane % 8 * 4));
+            wave_order();
+        }
 }
 
-template <typename T, int BM, int BN, class Epilogue>
+template <typename T, int BM, int BN, int STEP, int GROUPS, class Epilogue>
 void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
@@ -117,22 +155,24 @@ void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, 
     const T *pa = (const T *)a.p, *pb = (const T *)b.p;
     const bool wa = whole_pieces(a.p, a.ld, a.step, sizeof(T)), wb = whole_pieces(b.p, b.ld, b.step, sizeof(T));
     if (a.k_near && b.k_near)
-        gemm_f32_kernel<T, BM, BN, true, true><<<grid, 256, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
     else if (a.k_near)
-        gemm_f32_kernel<T, BM, BN, true, false><<<grid, 256, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
     else if (b.k_near)
-        gemm_f32_kernel<T, BM, BN, false, true><<<grid, 256, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
     else
-        gemm_f32_kernel<T, BM, BN, false, false><<<grid, 256, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
 }
 
 template <typename T, class Epilogue>
 void launch_gemm_f32(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {
-    if (batch * ((M + 127) / 128) * ((N + 127) / 128) >= 256)
-        launch_gemm_f32_blocks<T, 128, 128>(s, batch, M, N, K, a, b, epilogue);
-    else
-        launch_gemm_f32_blocks<T, 64, 64>(s, batch, M, N, K, a, b, epilogue);
+    const auto blocks = [&](int64_t m, int64_t n) { return batch * ((M + m - 1) / m) * ((N + n - 1) / n); };
+    // blocks of 128 where they are many and the contraction pays for their start; the fewer blocks, the more waves on each
+    if (blocks(128, 128) >= 256 && K >= 256) launch_gemm_f32_blocks<T, 128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
+    else if (blocks(64, 64) >= 512) launch_gemm_f32_blocks<T, 64, 64, 32, 1>(s, batch, M, N, K, a, b, epilogue);
+    else if (blocks(64, 64) > 128) launch_gemm_f32_blocks<T, 64, 64, 32, 4>(s, batch, M, N, K, a, b, epilogue);
+    else launch_gemm_f32_blocks<T, 64, 32, 32, 4>(s, batch, M, N, K, a, b, epilogue);
 }
 
 }  // namespace netmax
