@@ -70,36 +70,34 @@ __device__ __forceinline__ float load_value(const float *p) { return *p; }
 __device__ __forceinline__ float load_value(const uint16_t *p) { return bf16_bits_to_float(*p); }
 __device__ __forceinline__ void store_value(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = (uint16_t)bf16_bits(v); }
-__device__ __forceinline__ f32x4 load_four(const float *p) { return load4(p); }
+// Four neighbours at any address of a value, in one request.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+__device__ __forceinline__ f32x4 load_four(const float *p) { return *reinterpret_cast<const f32x4_any *>(p); }
 __device__ __forceinline__ f32x4 load_four(const uint16_t *p)
 {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u)};
+    const u32x2 u = *reinterpret_cast<const u32x2_any *>(p);
+    return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xFFFF0000u)};
 }
-__device__ __forceinline__ void store_four(float *p, f32x4 v) { store4(p, v); }
+__device__ __forceinline__ void store_four(float *p, f32x4 v) { *reinterpret_cast<f32x4_any *>(p) = v; }
 __device__ __forceinline__ void store_four(uint16_t *p, f32x4 v)
 {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    *reinterpret_cast<u32x2_any *>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
-// Whether pieces of four values can be taken whole: rows and matrices start at multiples of four values in aligned memory.
-inline bool whole_pieces(const void *p, int64_t ld, int64_t step, int value_bytes)
+// Four values from column n of `cols`; those behind the last are 0.
+template <typename T> __device__ __forceinline__ f32x4 load_up_to_four(const T *row, int64_t n, int64_t cols)
 {
-    return (uintptr_t)p % (4 * value_bytes) == 0 && ld % 4 == 0 && step % 4 == 0;
-}
-
-// Four values from column n of `cols`; `whole`: rows start at multiples of four values in aligned memory.
-template <typename T> __device__ __forceinline__ f32x4 load_up_to_four(const T *row, int64_t n, int64_t cols, bool whole)
-{
-    if (whole && n + 4 <= cols) return load_four(row + n);
+    if (n + 4 <= cols) return load_four(row + n);
     f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (n + e < cols) v[e] = load_value(row + n + e);
     return v;
 }
-template <typename T> __device__ __forceinline__ void store_up_to_four(T *row, int64_t n, int64_t cols, bool whole, f32x4 v)
+template <typename T> __device__ __forceinline__ void store_up_to_four(T *row, int64_t n, int64_t cols, f32x4 v)
 {
-    if (whole && n + 4 <= cols) { store_four(row + n, v); return; }
+    if (n + 4 <= cols) { store_four(row + n, v); return; }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (n + e < cols) store_value(row + n + e, v[e]);
@@ -112,32 +110,17 @@ template <typename T> struct LinearEpilogue {
     int64_t M, N;
     const T *bias, *residual; T *y, *z;
     int64_t ldr, ldy, ldz, sb, sr, sy, sz;
-    int act; bool whole;
+    int act;
     __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
     {
         if (m >= M || n >= N) return;
-        if (bias) v += load_up_to_four(bias + g * sb, n, N, whole);
-        if (z) store_up_to_four(z + g * sz + m * ldz, n, N, whole, v);
+        if (bias) v += load_up_to_four(bias + g * sb, n, N);
+        if (z) store_up_to_four(z + g * sz + m * ldz, n, N, v);
         if (act != ACT_NONE)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = act_of(act, v[e]);
-        if (residual) v += load_up_to_four(residual + g * sr + m * ldr, n, N, whole);
-        store_up_to_four(y + g * sy + m * ldy, n, N, whole, v);
-    }
-};
-
-// out = alpha acc + beta own, all [M][N] next to each other; own may be null.
-template <typename T> struct SumEpilogue {
-    int64_t M, N;
-    float alpha, beta;
-    const float *own; T *out;
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
-    {
-        if (m >= M || n >= N) return;
-        const int64_t row = (g * M + m) * N;
-        v *= alpha;
-        if (own) v += beta * load_up_to_four(own + row, n, N, false);
-        store_up_to_four(out + row, n, N, false, v);
+        if (residual) v += load_up_to_four(residual + g * sr + m * ldr, n, N);
+        store_up_to_four(y + g * sy + m * ldy, n, N, v);
     }
 };
 

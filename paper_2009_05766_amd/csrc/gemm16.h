@@ -6,7 +6,7 @@
 //   contraction index near   [rows][64]: lanes read 16 bytes of a row; the 16-byte units of a row are permuted by (row / 2) % 8, so that
 //                            sixteen rows at one index lie in different banks
 //   row index near           [64][rows]: ds_read_b64_tr_b16 hands each lane four contraction indices of its row; groups of 64 bytes are permuted by
-//                            k % 4 (rows of 128 bytes: k / 2 % 2), so that the four stored rows that one such read touches lie in different banks
+//                            k % 4 (rows of 128 bytes: k / 2 % 2, of 64 bytes: not at all), so that the four stored rows that one such read touches lie in different banks
 // The permutations are applied to the memory addresses, since a request to LDS fills consecutive units.
 // B goes in as the instruction's first operand, so that a lane ends with four neighbouring columns of a row.
 //
@@ -42,20 +42,20 @@ __device__ __forceinline__ s16x4 read_turned(const char *__restrict__ p)
 }
 template <typename V> __device__ __forceinline__ V read_unit(const char *__restrict__ p) { return *reinterpret_cast<const V *>(p); }
 
-template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 64 ? (k >> 1) & 1 : k & 3; }
+template <int ROWS> __device__ __forceinline__ int turned_group(int k) { return ROWS == 32 ? 0 : ROWS == 64 ? (k >> 1) & 1 : k & 3; }
 
-// One operand's step: ROWS results' rows x 64 contraction indices, brought by THREADS threads.
+// One operand's step: ROWS results' rows x STEP contraction indices, brought by THREADS threads.
 template <int ROWS, bool K_NEAR, int STEP, int THREADS> struct Step16 {
     static constexpr int BYTES = ROWS * STEP * 2, PIECES = BYTES / 16 / THREADS, ROW_UNITS = ROWS / 8;
     uint32_t offset[PIECES];                                        // of this lane's piece from the step's first byte
     int first_k[PIECES];
 
-    __device__ __forceinline__ void place(int64_t row0, int64_t rows, int64_t ld)
+    __device__ __forceinline__ void place(int thread, int64_t row0, int64_t rows, int64_t ld)
     {
         // rows past the end are the last ones, so an offset stays below ROWS (64) rows of ld; ld < 2^22
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
-            const int q = u * THREADS + (int)threadIdx.x;
+            const int q = u * THREADS + thread;
             if (K_NEAR) {
                 const int r = q / (STEP / 8), c = near_unit<STEP>(r, q % (STEP / 8));
                 const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
@@ -70,9 +70,8 @@ template <int ROWS, bool K_NEAR, int STEP, int THREADS> struct Step16 {
         }
     }
     // Piece u of the step that starts at `from` (row row0, first index of the step) and has `left` indices (fewer than a step's: zeros behind them); a wave's units lie next to each other.
-    __device__ __forceinline__ void request(int u, const char *from, char *lds, int left) const
+    __device__ __forceinline__ void request(int u, int wave, const char *from, char *lds, int left) const
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         to_lds(first_k[u] < left ? from + offset[u] : (const char *)&g16_zeros, lds + u * THREADS * 16 + wave * 1024);
     }
 };
@@ -99,11 +98,17 @@ template <int ROWS, bool K_NEAR, int STEP> struct Fragment16 {
     }
 };
 
+// Renumbers workgroups so that those of one L2 (every eighth) are neighbours.
+__device__ __forceinline__ uint32_t l2_neighbours(uint32_t id, uint32_t all)
+{
+    const uint32_t each = all / 8, more = all % 8, part = id % 8;
+    return part * each + (part < more ? part : more) + id / 8;
+}
+
 // Numbers workgroups so that those of one L2 (every eighth) have neighbouring blocks, and blocks in columns of eight rows of blocks.
 __device__ __forceinline__ void block_place(uint32_t id, uint32_t all, uint32_t mblocks, uint32_t nblocks, uint32_t &g, uint32_t &mb, uint32_t &nb)
 {
-    const uint32_t each = all / 8, more = all % 8, part = id % 8;
-    id = part * each + (part < more ? part : more) + id / 8;
+    id = l2_neighbours(id, all);
     const uint32_t per = mblocks * nblocks;
     g = id / per;
     id -= g * per;
@@ -115,8 +120,7 @@ __device__ __forceinline__ void block_place(uint32_t id, uint32_t all, uint32_t 
 // The same for the lower triangle of a square of `side` x `side` blocks.
 __device__ __forceinline__ void triangle_place(uint32_t id, uint32_t all, uint32_t side, uint32_t &g, uint32_t &mb, uint32_t &nb)
 {
-    const uint32_t each = all / 8, more = all % 8, part = id % 8;
-    id = part * each + (part < more ? part : more) + id / 8;
+    id = l2_neighbours(id, all);
     const uint32_t per = side * (side + 1) / 2;
     g = id / per;
     id -= g * per;
@@ -149,8 +153,8 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     const int wave = threadIdx.x >> 6, wm = wave / WAVES_N * (TM * 32), wn = wave % WAVES_N * (TN * 32);
     StepA sa;
     StepB sb;
-    sa.place(m0, M, A.ld);
-    sb.place(n0, N, B.ld);
+    sa.place(threadIdx.x, m0, M, A.ld);
+    sb.place(threadIdx.x, n0, N, B.ld);
     Fragment16<BM, AK, STEP> fa[TM];
     Fragment16<BN, BK, STEP> fb[TN];
 #pragma unroll
@@ -169,6 +173,7 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     const int first = (int)(whole * split / splits), total = (int)(whole * (split + 1) / splits) - first;
     // A step on its way to LDS: its pieces are requested one by one.  Steps behind the last one are requested, too, as zeros that nobody reads, so that the
     // loop below has no branches.
+    const int mine = __builtin_amdgcn_readfirstlane(wave);
     int64_t next_a, next_b;
     char *next_to;
     int next_left;
@@ -183,8 +188,8 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
         const bool low = u >= StepA::PIECES + StepB::PIECES;
         char *to = next_to + (low ? StepA::BYTES + StepB::BYTES : 0);
         if (low) u -= StepA::PIECES + StepB::PIECES;
-        if (u < StepA::PIECES) sa.request(u, (low ? A.lo : A.hi) + next_a, to, next_left);
-        else sb.request(u - StepA::PIECES, (low ? B.lo : B.hi) + next_b, to + StepA::BYTES, next_left);
+        if (u < StepA::PIECES) sa.request(u, mine, (low ? A.lo : A.hi) + next_a, to, next_left);
+        else sb.request(u - StepA::PIECES, mine, (low ? B.lo : B.hi) + next_b, to + StepA::BYTES, next_left);
     };
     // While 16 indices are multiplied the next 16 come from LDS into registers.  Before the last 16 of step s are multiplied, step s + 1 has arrived and all
     // waves hold the rest of step s: the barrier and the first reads behind it are covered by those products, and step s + STAGES may fill the space of
@@ -268,6 +273,93 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
                 epilogue.mirror(where, n0 + wn + row, m0 + wm + i * 32 + col, f32x4{p[0], p[PITCH], p[2 * PITCH], p[3 * PITCH]});
             }
         wave_order();
+    }
+}
+
+// C = A B for few rows, at most 32 TM: the weights are what has to be read.  A workgroup has 32 columns; its eight waves take steps of 32 indices in turn,
+// each with its own space in LDS for a few steps under way and without a barrier.  The waves' sums are added in LDS in order.  Neighbouring
+// workgroups share an L2, as they share the lines of 128 bytes that 64 bytes of a row of weights lie in.
+constexpr int FEW_WAVES = 8;
+
+template <typename V, int TM, bool BK, class Epilogue>
+__global__ void __launch_bounds__(FEW_WAVES * 64)
+few_rows_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, Epilogue epilogue)
+{
+    constexpr int STEP = 32, STAGES = TM == 1 ? 4 : 3;
+    typedef Step16<32 * TM, true, STEP, 64> StepA;
+    typedef Step16<32, BK, STEP, 64> StepB;
+    constexpr int STAGE = StepA::BYTES + StepB::BYTES, REQUESTS = StepA::PIECES + StepB::PIECES;
+    constexpr int PITCH = 36, SUMS = FEW_WAVES * TM * 32 * PITCH * 4, SPACE = FEW_WAVES * STAGES * STAGE;
+    __shared__ __align__(16) char lds[SPACE > SUMS ? SPACE : SUMS];
+    const int64_t g = blockIdx.y, n0 = (int64_t)l2_neighbours(blockIdx.x, gridDim.x) * 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = lane & 31, half = lane >> 5;
+    const char *from_a = A.hi + g * A.step * 2, *from_b = B.hi + (g * B.step + (BK ? n0 * B.ld : n0)) * 2;
+    char *space = lds + wave * (STAGES * STAGE);
+    const int64_t kstep = BK ? STEP * 2 : B.ld * (STEP * 2);
+    StepA sa;
+    StepB sb;
+    sa.place(lane, 0, M, A.ld);
+    sb.place(lane, n0, N, B.ld);
+    Fragment16<32 * TM, true, STEP> fa[TM];
+    Fragment16<32, BK, STEP> fb;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[i].place(i * 32);
+    fb.place(0);
+    f32x16 acc[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+    const int steps = (int)((K + STEP - 1) / STEP), turns = steps > wave ? (steps - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
+    const auto bring = [&](int s) {                                 // steps behind the last one as zeros that nobody reads
+        const int64_t k = wave + (int64_t)s * FEW_WAVES, all = K - k * STEP;
+        const int left = s >= turns ? 0 : all < STEP ? (int)all : STEP;
+        char *to = space + s % STAGES * STAGE;
+#pragma unroll
+        for (int u = 0; u < StepB::PIECES; ++u) sb.request(u, 0, from_b + k * kstep, to + StepA::BYTES, left);
+#pragma unroll
+        for (int u = 0; u < StepA::PIECES; ++u) sa.request(u, 0, from_a + k * (STEP * 2), to, left);
+    };
+    for (int s = 0; s < STAGES - 1; ++s) bring(s);
+    for (int s = 0; s < turns; ++s) {
+        bring(s + STAGES - 1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * REQUESTS) : "memory");
+        const char *now = space + s % STAGES * STAGE;
+#pragma unroll
+        for (int kk = 0; kk < STEP / 16; ++kk) {
+            const V v = fb.template read<V>(now + StepA::BYTES, kk);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) acc[i] = mfma16(v, fa[i].template read<V>(now, kk), acc[i]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // the step's space is free
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    float *sums = (float *)lds;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            store4(sums + ((wave * TM + i) * 32 + at) * PITCH + e * 8 + half * 4, f32x4{acc[i][4 * e], acc[i][4 * e + 1], acc[i][4 * e + 2], acc[i][4 * e + 3]});
+    __syncthreads();
+    const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 4;     // 64 rows of 8 pieces
+    if (row >= TM * 32) return;
+    f32x4 v = load4(sums + row * PITCH + col);
+#pragma unroll
+    for (int w = 1; w < FEW_WAVES; ++w) v += load4(sums + (w * TM * 32 + row) * PITCH + col);
+    epilogue(g, row, n0 + col, v);
+}
+
+template <typename V, class Epilogue>
+void launch_few_rows(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, const Planes16 &b, bool bk, const Epilogue &e)
+{
+    const dim3 grid((uint32_t)((N + 31) / 32), (uint32_t)batch);
+    if (M <= 32) {
+        if (bk) few_rows_kernel<V, 1, true><<<grid, FEW_WAVES * 64, 0, s>>>(M, N, K, a, b, e);
+        else few_rows_kernel<V, 1, false><<<grid, FEW_WAVES * 64, 0, s>>>(M, N, K, a, b, e);
+    } else {
+        if (bk) few_rows_kernel<V, 2, true><<<grid, FEW_WAVES * 64, 0, s>>>(M, N, K, a, b, e);
+        else few_rows_kernel<V, 2, false><<<grid, FEW_WAVES * 64, 0, s>>>(M, N, K, a, b, e);
     }
 }
 

@@ -15,17 +15,17 @@ template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
     static constexpr int PIECES = ROWS * STEP / 4 / 256;
     static constexpr int PITCH = ROWS + 4;
     f32x4 v[PIECES];
-    __device__ __forceinline__ void request(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K, bool whole)
+    __device__ __forceinline__ void request(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K)
     {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
             const int q = u * 256 + (int)(threadIdx.x & 255);
             if (K_NEAR) {
                 const int64_t r = row0 + q / (STEP / 4), k = k0 + q % (STEP / 4) * 4;
-                v[u] = r < rows ? load_up_to_four(p + r * ld, k, K, whole) : f32x4{0, 0, 0, 0};
+                v[u] = r < rows ? load_up_to_four(p + r * ld, k, K) : f32x4{0, 0, 0, 0};
             } else {
                 const int64_t k = k0 + q / (ROWS / 4), r = row0 + q % (ROWS / 4) * 4;
-                v[u] = k < K ? load_up_to_four(p + k * ld, r, rows, whole) : f32x4{0, 0, 0, 0};
+                v[u] = k < K ? load_up_to_four(p + k * ld, r, rows) : f32x4{0, 0, 0, 0};
             }
         }
     }
@@ -48,8 +48,8 @@ template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
 
 template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
 __global__ void __launch_bounds__(256 * GROUPS)
-gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, bool wa, const T *__restrict__ B, int64_t ldb,
-                int64_t sb, bool wb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
+gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
+                int64_t sb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
 {
     typedef StepPieces<T, BM, STEP, AK> PiecesA;
     typedef StepPieces<T, BN, STEP, BK> PiecesB;
@@ -75,16 +75,16 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     const int64_t steps = (K + STEP - 1) / STEP, turns = (steps + GROUPS - 1) / GROUPS;         // a group without a step has zeros
-    pa.request(A, lda, m0, M, (int64_t)group * STEP, K, wa);
-    pb.request(B, ldb, n0, N, (int64_t)group * STEP, K, wb);
+    pa.request(A, lda, m0, M, (int64_t)group * STEP, K);
+    pb.request(B, ldb, n0, N, (int64_t)group * STEP, K);
     for (int64_t s = 0; s < turns; ++s) {
         float *ca = lds[group][s & 1], *cb = ca + STEP * PiecesA::PITCH;
         pa.place(ca);
         pb.place(cb);
         __syncthreads();
         if (s + 1 < turns) {
-            pa.request(A, lda, m0, M, ((s + 1) * GROUPS + group) * STEP, K, wa);
-            pb.request(B, ldb, n0, N, ((s + 1) * GROUPS + group) * STEP, K, wb);
+            pa.request(A, lda, m0, M, ((s + 1) * GROUPS + group) * STEP, K);
+            pb.request(B, ldb, n0, N, ((s + 1) * GROUPS + group) * STEP, K);
         }
 #pragma unroll
         for (int q = 0; q < STEP / SHARES; q += 2) {
@@ -153,15 +153,14 @@ void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, 
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb));
     const T *pa = (const T *)a.p, *pb = (const T *)b.p;
-    const bool wa = whole_pieces(a.p, a.ld, a.step, sizeof(T)), wb = whole_pieces(b.p, b.ld, b.step, sizeof(T));
     if (a.k_near && b.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
     else if (a.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
     else if (b.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
     else
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, wa, pb, b.ld, b.step, wb, mb, nb, epilogue);
+        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
 }
 
 template <typename T, class Epilogue>

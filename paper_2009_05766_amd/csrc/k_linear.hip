@@ -12,18 +12,26 @@ static inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to
 
 // ---- operands of 16 bits laid out anew -------------------------------------------------------------------------------
 
-// out [batch][rows][wide] = in [batch][rows][cols] (rows ld, matrices step apart) with zeros behind each row; wide a multiple of 8.
-__global__ void __launch_bounds__(256) lay_out_kernel(int64_t rows, int64_t cols, int64_t wide, const uint16_t *__restrict__ in, int64_t ld, int64_t step, uint16_t *__restrict__ out)
+// One matrix [batch][rows][cols] (rows ld, matrices step apart) that goes to [batch][rows][wide] with zeros behind each row; wide a multiple of 8.
+struct Layout { int64_t batch, rows, cols, wide, ld, step; const uint16_t *in; uint16_t *out; };
+constexpr int MOST_LAYOUTS = 3;
+struct Layouts { int n; Layout of[MOST_LAYOUTS]; uint32_t end[MOST_LAYOUTS]; };     // end: workgroups up to and with each
+
+// All matrices that a call lays out anew in one launch.
+__global__ void __launch_bounds__(256) lay_out_kernel(Layouts l)
 {
-    const int64_t units = wide / 8, all = rows * units, g = blockIdx.y;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
-        const int64_t r = q / units, c = (q - r * units) * 8;
-        const uint16_t *p = in + g * step + r * ld + c;
-        uint32_t v[4];
+    int k = 0;
+    while (k + 1 < l.n && blockIdx.x >= l.end[k]) ++k;
+    const Layout m = k == 0 ? l.of[0] : k == 1 ? l.of[1] : l.of[2];
+    const uint32_t before = k == 0 ? 0 : l.end[k - 1], here = l.end[k] - before;
+    const int64_t units = m.wide / 8, all = m.batch * m.rows * units;
+    for (int64_t q = (int64_t)(blockIdx.x - before) * 256 + threadIdx.x; q < all; q += (int64_t)here * 256) {
+        const int64_t row = q / units, g = row / m.rows, c = (q - row * units) * 8;
+        const uint16_t *p = m.in + g * m.step + (row - g * m.rows) * m.ld + c;
+        uint32_t v[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = (c + 2 * e < cols ? p[2 * e] : 0u) | (uint32_t)(c + 2 * e + 1 < cols ? p[2 * e + 1] : 0u) << 16;
-        *reinterpret_cast<uint4 *>(out + (g * all + q) * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+        for (int e = 0; e < 8; ++e) v[e] = c + e < m.cols ? p[e] : 0u;
+        *reinterpret_cast<uint4 *>(m.out + q * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
     }
 }
 
@@ -32,17 +40,23 @@ struct Source {
     const void *p; int64_t ld, step, rows, cols; bool copy;
     Source(const void *p_, int64_t ld_, int64_t step_, int64_t rows_, int64_t cols_) : p(p_), ld(ld_), step(step_), rows(rows_), cols(cols_), copy(!fits16(p_, ld_, step_, cols_)) { }
     int64_t bytes(int64_t batch) const { return copy ? round_up((step || batch == 0 ? batch : 1) * rows * round_up(cols, 8) * 2, 256) : 0; }
-    // The operand, after a copy to `work` (advanced) where one is needed.
-    Planes16 take(hipStream_t s, int64_t batch, char *&work) const
+    // The operand; where a copy is needed, in `work` (advanced), and noted in `l`.
+    Planes16 take(int64_t batch, char *&work, Layouts &l) const
     {
         if (!copy || rows == 0) return Planes16{(const char *)p, nullptr, ld, step};
-        const int64_t wide = round_up(cols, 8), own = step ? batch : 1, want = (rows * wide / 8 + 255) / 256;
+        const int64_t wide = round_up(cols, 8), own = step ? batch : 1, want = (own * rows * wide / 8 + 255) / 256;
         char *to = work;
         work += bytes(batch);
-        lay_out_kernel<<<dim3((uint32_t)(want < 4096 ? want : 4096), (uint32_t)own), 256, 0, s>>>(rows, cols, wide, (const uint16_t *)p, ld, step, (uint16_t *)to);
+        l.of[l.n] = Layout{own, rows, cols, wide, ld, step, (const uint16_t *)p, (uint16_t *)to};
+        l.end[l.n] = (l.n ? l.end[l.n - 1] : 0) + (uint32_t)(want < 4096 ? want : 4096);
+        ++l.n;
         return Planes16{to, nullptr, wide, step ? rows * wide : 0};
     }
 };
+static void lay_out(hipStream_t s, const Layouts &l)
+{
+    if (l.n) lay_out_kernel<<<l.end[l.n - 1], 256, 0, s>>>(l);
+}
 
 // ---- products whose contraction is shared out ------------------------------------------------------------------------
 
@@ -68,21 +82,24 @@ __global__ void __launch_bounds__(256) join_parts_kernel(int64_t batch, int64_t 
     }
 }
 
-// Blocks and shares of a product: large blocks where they fill the card, smaller ones otherwise, and the contraction shared out where even
-// those are few.
+// Blocks and shares of a product: large blocks where they fill the card, smaller ones otherwise, and the contraction shared out where even those are few
+// and long: a share is at least 16 steps (about 8 us, what the join costs; 1111 x 777 x 2049 in two shares of 64 x 64 blocks took 16 + 8 us, in one 17).
 struct Plan16 { int block; int splits; };
 static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
 {
     const auto blocks = [&](int64_t b) { return batch * ((M + b - 1) / b) * ((N + b - 1) / b); };
-    const int64_t steps = (K + 64 - 1) / 64;
+    const int64_t steps = (K + 63) / 64;
     if (blocks(256) >= 192) return {256, 1};
-    const int block = blocks(128) >= 128 && M > 64 && N > 64 ? 128 : 64;
-    const int64_t want = 512 / (blocks(block) > 0 ? blocks(block) : 1), most = steps / 4;
+    const int block = blocks(128) >= 96 && M > 64 && N > 64 ? 128 : 64;
+    const int64_t here = blocks(block) > 0 ? blocks(block) : 1, want = (block == 128 ? 256 : 512) / here, most = steps / 16;
     const int64_t splits = want < most ? want : most;
-    return {block, (int)(splits < 1 ? 1 : splits > 16 ? 16 : splits)};
+    return {block, (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits)};
 }
-static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K)
+// Few rows that lie along the contraction have a kernel of their own (few_rows_kernel).
+constexpr int64_t FEW_ROWS = 64;
+static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, bool ak)
 {
+    if (M <= FEW_ROWS && ak) return 0;
     const Plan16 p = plan16(batch, M, N, K);
     return p.splits > 1 ? round_up(p.splits * batch * M * round_up(N, 4) * 4, 256) : 0;
 }
@@ -102,6 +119,10 @@ static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, 
 template <class Epilogue>
 static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, const Epilogue &e, char *work)
 {
+    if (M <= FEW_ROWS && ak) {
+        launch_few_rows<bf16x8>(s, batch, M, N, K, a, b, bk, e);
+        return;
+    }
     const Plan16 p = plan16(batch, M, N, K);
     if (p.splits == 1) {
         launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, 1, e);
@@ -120,8 +141,8 @@ constexpr int SLOPE_COLS = 256;
 
 template <typename T>
 __global__ void __launch_bounds__(256)
-slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int64_t lddy, int64_t sdy, bool wdy, const T *__restrict__ z, int64_t ldz, int64_t sz, bool wz, int act,
-             T *__restrict__ dz, int64_t wide, bool wdz, float *__restrict__ sums)
+slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int64_t lddy, int64_t sdy, const T *__restrict__ z, int64_t ldz, int64_t sz, int act,
+             T *__restrict__ dz, int64_t wide, float *__restrict__ sums)
 {
     // dz has rows of `wide` values, zeros behind the columns: what the product's contraction over them needs
     __shared__ __align__(16) float part[4][SLOPE_COLS];
@@ -134,14 +155,14 @@ slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int6
     if (n < wide)
 #pragma unroll 4
         for (int64_t r = r0; r < end; r += 4) {
-            f32x4 v = load_up_to_four(dy + r * lddy, n, cols, wdy);
+            f32x4 v = load_up_to_four(dy + r * lddy, n, cols);
             if (act != ACT_NONE) {
-                const f32x4 pre = load_up_to_four(z + r * ldz, n, cols, wz);
+                const f32x4 pre = load_up_to_four(z + r * ldz, n, cols);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? v[e] * act_slope(act, pre[e]) : 0.0f;
             }
             sum += v;
-            if (dz) store_up_to_four(dz + (g * rows + r) * wide, n, wide, wdz, v);
+            if (dz) store_up_to_four(dz + (g * rows + r) * wide, n, wide, v);
         }
     if (!sums) return;
     store4(&part[wave][at], sum);
@@ -171,20 +192,18 @@ __global__ void __launch_bounds__(256) bias_sum_kernel(int64_t cols, int64_t par
 
 template <typename T> static LinearEpilogue<T> forward_epilogue(const LinearArgs &a)
 {
-    const bool whole = whole_pieces(a.y, a.ldy, a.sy, sizeof(T)) && (!a.z || whole_pieces(a.z, a.ldz, a.sz, sizeof(T))) &&
-                       (!a.residual || whole_pieces(a.residual, a.ldr, a.sr, sizeof(T))) && (!a.bias || whole_pieces(a.bias, 0, a.sb, sizeof(T)));
-    return LinearEpilogue<T>{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz, a.sb, a.sr, a.sy, a.sz, a.act, whole};
+    return LinearEpilogue<T>{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz, a.sb, a.sr, a.sy, a.sz, a.act};
 }
 // out [rows][cols] alone
 template <typename T> static LinearEpilogue<T> plain_epilogue(int64_t rows, int64_t cols, void *out, int64_t ld, int64_t step)
 {
-    return LinearEpilogue<T>{rows, cols, nullptr, nullptr, (T *)out, nullptr, 0, ld, 0, 0, 0, step, 0, ACT_NONE, whole_pieces(out, ld, step, sizeof(T))};
+    return LinearEpilogue<T>{rows, cols, nullptr, nullptr, (T *)out, nullptr, 0, ld, 0, 0, 0, step, 0, ACT_NONE};
 }
 
 int64_t linear_workspace(const LinearArgs &a)
 {
     if (!a.bf16) return 0;
-    return Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + part_bytes(a.batch, a.rows, a.dout, a.din);
+    return Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + part_bytes(a.batch, a.rows, a.dout, a.din, true);
 }
 
 void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
@@ -194,7 +213,9 @@ void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
         return;
     }
     char *at = (char *)work;
-    const Planes16 x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(s, a.batch, at), w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(s, a.batch, at);
+    Layouts l{};
+    const Planes16 x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(a.batch, at, l), w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(a.batch, at, l);
+    lay_out(s, l);
     launch_product16(s, a.batch, a.rows, a.dout, a.din, x, true, w, false, forward_epilogue<uint16_t>(a), at);
 }
 
@@ -216,7 +237,7 @@ int64_t linear_grad_workspace(const LinearGradArgs &a)
     if (a.act != ACT_NONE) n += round_up(a.batch * a.rows * dz_wide(a) * (a.bf16 ? 2 : 4), 256);
     else if (a.bf16) n += Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).bytes(a.batch);
     if (!a.bf16) return n;
-    const int64_t dx = part_bytes(a.batch, a.rows, a.din, a.dout), dw = part_bytes(a.batch, a.din, a.dout, a.rows);
+    const int64_t dx = part_bytes(a.batch, a.rows, a.din, a.dout, true), dw = part_bytes(a.batch, a.din, a.dout, a.rows, false);
     return n + Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + (dx > dw ? dx : dw);
 }
 
@@ -224,8 +245,8 @@ template <typename T> static void launch_slopes(hipStream_t s, const LinearGradA
 {
     if ((dz || a.db) && a.rows > 0)
         slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
-            a.rows, a.dout, slope_run(a), (const T *)a.dy, a.lddy, a.sdy, whole_pieces(a.dy, a.lddy, a.sdy, sizeof(T)), (const T *)a.z, a.ldz, a.sz,
-            whole_pieces(a.z, a.ldz, a.sz, sizeof(T)), a.act, dz, dz_wide(a), dz_wide(a) % 4 == 0, a.db ? sums : nullptr);
+            a.rows, a.dout, slope_run(a), (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz,
+            dz_wide(a), a.db ? sums : nullptr);
     if (a.db)
         bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 63) / 64), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
 }
@@ -251,15 +272,16 @@ void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
         return;
     }
     launch_slopes<uint16_t>(s, a, (uint16_t *)dz, sums);
-    const Planes16 d = dz ? Planes16{(const char *)dz, nullptr, dz_wide(a), a.rows * dz_wide(a)} : Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).take(s, a.batch, at);
-    if (a.dx && a.rows > 0) {
-        const Planes16 w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(s, a.batch, at);
+    Layouts l{};
+    const Planes16 d = dz ? Planes16{(const char *)dz, nullptr, dz_wide(a), a.rows * dz_wide(a)} : Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).take(a.batch, at, l);
+    Planes16 w{}, x{};
+    if (a.dx && a.rows > 0) w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(a.batch, at, l);
+    if (a.dw) x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(a.batch, at, l);
+    lay_out(s, l);
+    if (a.dx && a.rows > 0)
         launch_product16(s, a.batch, a.rows, a.din, a.dout, d, true, w, true, plain_epilogue<uint16_t>(a.rows, a.din, a.dx, a.lddx, a.sdx), at);
-    }
-    if (a.dw) {
-        const Planes16 x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(s, a.batch, at);
+    if (a.dw)
         launch_product16(s, a.batch, a.din, a.dout, a.rows, x, false, d, false, plain_epilogue<uint16_t>(a.din, a.dout, a.dw, a.lddw, a.sdw), at);
-    }
 }
 
 }  // namespace netmax

@@ -18,7 +18,7 @@
 
 namespace netmax {
 
-constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, at most
+constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, at most: one for each thread that adds them up
 
 __device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
 
@@ -115,11 +115,11 @@ struct StepEpilogue {
 
 // The last step: scale X to the caller's memory.
 template <typename T> struct LastEpilogue {
-    StepEpilogue step; float scale; T *out; int64_t ldo, so; bool whole;
+    StepEpilogue step; float scale; T *out; int64_t ldo, so;
     __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
     {
         if (m >= step.rows || n >= step.cols) return;
-        store_up_to_four(out + g * so + m * ldo, n, step.cols, whole, scale * step.value(g, m, n, v));
+        store_up_to_four(out + g * so + m * ldo, n, step.cols, scale * step.value(g, m, n, v));
     }
 };
 
@@ -135,7 +135,7 @@ constexpr int NORM_AHEAD = 4;
 
 // m' and a part of the sum of squares of u (in double; the parts are added in order by whoever needs the norm).
 template <typename T>
-__global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, bool wg, bool wm, double *__restrict__ parts)
+__global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, double *__restrict__ parts)
 {
     __shared__ double part[256];
     const int64_t g = blockIdx.y;
@@ -151,15 +151,15 @@ __global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, bool wg, bool
             const int64_t q = q0 + k * stride;
             if (q >= count) { u[k] = m[k] = f32x4{0, 0, 0, 0}; continue; }
             unit_place(q, units, r[k], c[k]);
-            u[k] = load_up_to_four(from + r[k] * a.ldg, c[k], a.cols, wg);
-            if (a.m) m[k] = load_up_to_four(a.m + g * a.sm + r[k] * a.ldm, c[k], a.cols, wm);
+            u[k] = load_up_to_four(from + r[k] * a.ldg, c[k], a.cols);
+            if (a.m) m[k] = load_up_to_four(a.m + g * a.sm + r[k] * a.ldm, c[k], a.cols);
         }
 #pragma unroll
         for (int k = 0; k < NORM_AHEAD; ++k) {
             if (q0 + k * stride >= count) continue;
             if (a.m) {
                 m[k] = fma4(a.mu, m[k], u[k]);
-                store_up_to_four(a.m_out + g * a.sm + r[k] * a.ldm, c[k], a.cols, wm, m[k]);
+                store_up_to_four(a.m_out + g * a.sm + r[k] * a.ldm, c[k], a.cols, m[k]);
                 u[k] = a.nesterov ? fma4(a.mu, m[k], u[k]) : m[k];
             }
 #pragma unroll
@@ -177,14 +177,19 @@ __global__ void __launch_bounds__(256) momentum_kernel(OrthArgs a, bool wg, bool
 
 // The planes of s u / max(||u||, eps).
 template <typename T>
-__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, bool wg, bool wm, const double *__restrict__ parts, float s, int64_t wide, uint16_t *__restrict__ hi,
+__global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, const double *__restrict__ parts, float s, int64_t wide, uint16_t *__restrict__ hi,
                                                         uint16_t *__restrict__ lo)
 {
     const int64_t g = blockIdx.y;
     const uint32_t units = (uint32_t)(wide / 4);
     const int64_t count = a.rows * units, stride = (int64_t)gridDim.x * 256;
-    double sum = 0.0;
-    for (uint32_t k = 0; k < gridDim.x; ++k) sum += parts[g * gridDim.x + k];
+    // every workgroup adds the parts in the same order
+    __shared__ double total[4];
+    double sum = threadIdx.x < gridDim.x ? parts[g * gridDim.x + threadIdx.x] : 0.0;
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) total[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = (total[0] + total[1]) + (total[2] + total[3]);
     const double norm = sqrt(sum), factor = (double)s / (norm > (double)a.eps || norm != norm ? norm : (double)a.eps);
     const T *from = (const T *)a.g + g * a.sg;
     for (int64_t q0 = (int64_t)blockIdx.x * 256 + threadIdx.x; q0 < count; q0 += NORM_AHEAD * stride) {
@@ -196,8 +201,8 @@ __global__ void __launch_bounds__(256) normalise_kernel(OrthArgs a, bool wg, boo
             if (q >= count) continue;
             int64_t r, c;
             unit_place(q, units, r, c);
-            if (!a.m || a.nesterov) u[k] = load_up_to_four(from + r * a.ldg, c, a.cols, wg);
-            if (a.m) m[k] = load_up_to_four(a.m_out + g * a.sm + r * a.ldm, c, a.cols, wm);
+            if (!a.m || a.nesterov) u[k] = load_up_to_four(from + r * a.ldg, c, a.cols);
+            if (a.m) m[k] = load_up_to_four(a.m_out + g * a.sm + r * a.ldm, c, a.cols);
         }
 #pragma unroll
         for (int k = 0; k < NORM_AHEAD; ++k) {
@@ -271,9 +276,8 @@ template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char
     const int64_t side = side_of(a), wide = up8(a.cols), swide = up8(side);
     const bool tall = a.rows > a.cols;
     const dim3 grid(norm_blocks(a), (uint32_t)a.batch);
-    const bool wg = whole_pieces(a.g, a.ldg, a.sg, sizeof(T)), wm = !a.m || (whole_pieces(a.m, a.ldm, a.sm, 4) && whole_pieces(a.m_out, a.ldm, a.sm, 4));
-    momentum_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts);
-    normalise_kernel<T><<<grid, 256, 0, s>>>(a, wg, wm, parts, X_SCALE, wide, xh, xl);
+    momentum_kernel<T><<<grid, 256, 0, s>>>(a, parts);
+    normalise_kernel<T><<<grid, 256, 0, s>>>(a, parts, X_SCALE, wide, xh, xl);
     const auto planes = [](const uint16_t *h, const uint16_t *l, int64_t ld, int64_t rows) { return Planes16{(const char *)h, (const char *)l, ld, rows * ld}; };
     for (int i = 0; i < a.steps; ++i) {
         launch_square<SPLIT>(s, a.batch, side, tall ? a.rows : a.cols, planes(xh, xl, wide, a.rows), !tall,
@@ -283,7 +287,7 @@ template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char
         const StepEpilogue step{a.rows, a.cols, wide, a.a, tall, xh, xl, yh, yl, SPLIT ? nullptr : diagonal};
         const Planes16 x = planes(xh, xl, wide, a.rows), b = planes(bh, bl, swide, side);
         if (i + 1 < a.steps) launch_step<SPLIT>(s, a, x, b, step);
-        else launch_step<SPLIT>(s, a, x, b, LastEpilogue<T>{step, a.scale / X_SCALE, (T *)a.out, a.ldo, a.so, whole_pieces(a.out, a.ldo, a.so, sizeof(T))});
+        else launch_step<SPLIT>(s, a, x, b, LastEpilogue<T>{step, a.scale / X_SCALE, (T *)a.out, a.ldo, a.so});
         uint16_t *t = xh; xh = yh; yh = t;
         t = xl; xl = yl; yl = t;
     }

@@ -21,7 +21,6 @@ namespace netmax {
 constexpr float LOG2E = 1.4426950408889634f;
 
 // 16 bytes of a row, at any address of a value.
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 template <typename T> struct Piece;
