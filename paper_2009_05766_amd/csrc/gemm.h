@@ -74,6 +74,8 @@ __device__ __forceinline__ void store_value(uint16_t *p, float v) { *p = (uint16
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 __device__ __forceinline__ f32x4 load_four(const float *p) { return *reinterpret_cast<const f32x4_any *>(p); }
 __device__ __forceinline__ f32x4 load_four(const uint16_t *p)
 {

@@ -117,17 +117,17 @@ __device__ __forceinline__ void block_place(uint32_t id, uint32_t all, uint32_t 
     mb = band * 8 + in % high;
 }
 
-// The same for the lower triangle of a square of `side` x `side` blocks.
-__device__ __forceinline__ void triangle_place(uint32_t id, uint32_t all, uint32_t side, uint32_t &g, uint32_t &mb, uint32_t &nb)
+// The same for the lower triangle of a square in blocks RATIO times as high as wide: row mb of blocks has RATIO (mb + 1) of them.
+template <int RATIO> __device__ __forceinline__ void triangle_place(uint32_t id, uint32_t all, uint32_t side, uint32_t &g, uint32_t &mb, uint32_t &nb)
 {
     id = l2_neighbours(id, all);
-    const uint32_t per = side * (side + 1) / 2;
+    const uint32_t per = RATIO * side * (side + 1) / 2;
     g = id / per;
     id -= g * per;
-    mb = (uint32_t)((sqrtf(8.0f * (float)id + 1.0f) - 1.0f) * 0.5f);
-    while ((mb + 1) * (mb + 2) / 2 <= id) ++mb;                     // the root is rounded
-    while (mb * (mb + 1) / 2 > id) --mb;
-    nb = id - mb * (mb + 1) / 2;
+    mb = (uint32_t)((sqrtf((8.0f / RATIO) * (float)id + 1.0f) - 1.0f) * 0.5f);
+    while (RATIO * (mb + 1) * (mb + 2) / 2 <= id) ++mb;             // the root is rounded
+    while (RATIO * mb * (mb + 1) / 2 > id) --mb;
+    nb = id - RATIO * mb * (mb + 1) / 2;
 }
 
 // With SPLIT an operand is two planes, hi + lo: both planes of both operands come to LDS, and hi hi, hi lo and lo hi are added up; lo lo, below 2^-22 of
@@ -145,8 +145,10 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     __shared__ __align__(16) char lds[STAGES][STAGE];
     uint32_t g, mb, nb;
     const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
-    if (TRIANGLE) triangle_place(blockIdx.x % all, all, mblocks, g, mb, nb);
-    else block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
+    if (TRIANGLE) {
+        triangle_place<BM / BN>(blockIdx.x % all, all, mblocks, g, mb, nb);
+        if ((int64_t)nb * BN >= N) return;                          // the last row's blocks may reach past the square
+    } else block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
     const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
     const int64_t kstepA = AK ? STEP * 2 : A.ld * (STEP * 2), kstepB = BK ? STEP * 2 : B.ld * (STEP * 2);
     const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
@@ -251,7 +253,7 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     constexpr int COLS = TN * 32, PITCH = COLS + 4;
     const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
     float *stage = (float *)lds + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
-    const int64_t where = splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
+    const int64_t where = !TRIANGLE && splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -382,23 +384,23 @@ void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, in
 }
 
 // The lower triangle of blocks of a symmetric product, A B with B = A transposed as stored: both operands have the same orientation.
-template <typename V, int BM, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
 void launch_gemm16_triangle(hipStream_t s, int64_t batch, int64_t M, int64_t K, const Planes16 &a, bool near, const Epilogue &e)
 {
     const uint32_t side = (uint32_t)((M + BM - 1) / BM);
-    const dim3 grid((uint32_t)(batch * side * (side + 1) / 2)), block(WM * WN * 64);
-    if (near) gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
-    else gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    const dim3 grid((uint32_t)(batch * (BM / BN) * side * (side + 1) / 2)), block(WM * WN * 64);
+    if (near) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
 }
 
-// C = A B with A's contraction index near and B's as `bk` says, in blocks of BM x BM.
-template <typename V, int BM, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+// C = A B with A's contraction index near and B's as `bk` says, in blocks of BM x BN.
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
 void launch_gemm16_step(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, const Planes16 &b, bool bk, const Epilogue &e)
 {
-    const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BM - 1) / BM);
+    const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb)), block(WM * WN * 64);
-    if (bk) gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
-    else gemm16_kernel<V, BM, BM, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
+    if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
 }
 
 }  // namespace netmax

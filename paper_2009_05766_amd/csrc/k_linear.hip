@@ -26,12 +26,19 @@ __global__ void __launch_bounds__(256) lay_out_kernel(Layouts l)
     const uint32_t before = k == 0 ? 0 : l.end[k - 1], here = l.end[k] - before;
     const int64_t units = m.wide / 8, all = m.batch * m.rows * units;
     for (int64_t q = (int64_t)(blockIdx.x - before) * 256 + threadIdx.x; q < all; q += (int64_t)here * 256) {
-        const int64_t row = q / units, g = row / m.rows, c = (q - row * units) * 8;
+        // in 32 bits where they do: a division in 64 takes longer than the copy
+        const int64_t row = all < (int64_t)1 << 32 ? (uint32_t)q / (uint32_t)units : q / units, g = m.batch == 1 ? 0 : row / m.rows, c = (q - row * units) * 8;
         const uint16_t *p = m.in + g * m.step + (row - g * m.rows) * m.ld + c;
-        uint32_t v[8];
+        u32x4 u;
+        if (c + 8 <= m.cols) {
+            u = *reinterpret_cast<const u32x4_any *>(p);
+        } else {
+            uint32_t v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < m.cols ? p[e] : 0u;
-        *reinterpret_cast<uint4 *>(m.out + q * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+            for (int e = 0; e < 8; ++e) v[e] = c + e < m.cols ? p[e] : 0u;
+            u = u32x4{v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16};
+        }
+        *reinterpret_cast<u32x4 *>(m.out + q * 8) = u;
     }
 }
 

@@ -16,6 +16,8 @@
 #include "gemm16.h"
 #include "orth.h"
 
+#include <type_traits>
+
 namespace netmax {
 
 constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, at most: one for each thread that adds them up
@@ -235,23 +237,26 @@ int64_t orth_workspace(const OrthArgs &a)
     return 4 * x_bytes(a) + (a.bf16 ? 2 : 4) * square_bytes(a) + up256(a.batch * side_of(a) * 4) + up256(8 * a.batch * NORM_BLOCKS);
 }
 
-// One launch for every block shape: `go` gets it as BM, waves, step and stages of gemm16_kernel.
-template <int BM_, int WM_, int WN_, int STEP_, int STAGES_> struct Shape { static constexpr int BM = BM_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_; };
-template <bool SPLIT, class Blocks, class Go> static void with_shape(const Blocks &blocks, const Go &go)
+// One launch for every block shape: `go` gets it as BM, BN, waves, step and stages of gemm16_kernel.
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_> struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_; };
+template <bool SPLIT, class Blocks, class Go> static void with_small_shape(const Blocks &blocks, const Go &go)
 {
     // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has
-    if constexpr (!SPLIT)
-        if (blocks(256) >= 192) { go(Shape<256, 2, 4, 64, 2>()); return; }
-    if (blocks(128) >= 512) go(Shape<128, 2, 2, SPLIT ? 32 : 64, 2>());
-    else if (blocks(128) >= 128) go(Shape<128, 2, 4, SPLIT ? 32 : 64, 4>());
-    else go(Shape<64, 2, 2, SPLIT ? 32 : 64, 4>());
+    if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    else if (blocks(128) >= 128) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
+    else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
 }
+// Many blocks: 256 x 128, two workgroups on a compute unit, so that the results of one (planes in and out, as long as half of the products) leave under
+// the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us.
+typedef Shape<256, 128, 4, 2, 32, 3> Paired;
 
 template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
 {
-    with_shape<SPLIT>([&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; }, [&](auto f) {
-        launch_gemm16_triangle<half8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, batch, side, K, x, near, e);
-    });
+    const auto go = [&](auto f) { launch_gemm16_triangle<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, batch, side, K, x, near, e); };
+    const auto blocks = [&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; };
+    if constexpr (!SPLIT)
+        if (blocks(256) >= 192) { go(Paired()); return; }
+    with_small_shape<SPLIT>(blocks, go);
 }
 
 template <bool SPLIT, class Epilogue>
@@ -260,9 +265,15 @@ static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, con
     const bool tall = a.rows > a.cols;
     const int64_t k = side_of(a);
     const Planes16 &l = tall ? x : b, &r = tall ? b : x;            // B is symmetric: its rows are its columns
-    with_shape<SPLIT>([&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); }, [&](auto f) {
-        launch_gemm16_step<half8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e);
-    });
+    const auto go = [&](auto f) { launch_gemm16_step<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e); };
+    const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
+    if constexpr (!SPLIT)
+        if (blocks(256) >= 192) {
+            if constexpr (std::is_same<Epilogue, StepEpilogue>::value) go(Paired());
+            else go(Shape<256, 256, 2, 4, 64, 2>());
+            return;
+        }
+    with_small_shape<SPLIT>(blocks, go);
 }
 
 template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char *work)

@@ -21,8 +21,6 @@ namespace netmax {
 constexpr float LOG2E = 1.4426950408889634f;
 
 // 16 bytes of a row, at any address of a value.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
 template <typename T> struct Piece;
 template <> struct Piece<float> {
     static constexpr int VALUES = 4;

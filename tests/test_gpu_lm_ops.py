@@ -133,6 +133,21 @@ def test_linear_long(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,d_in,d_out", [(4100, 72, 3080), (72, 3500, 4100), (3600, 4001, 99), (5000, 200, 10), (9000, 65, 127)])
+def test_linear_many_blocks(rows, d_in, d_out, dtype):
+    """Results wide enough for the largest blocks in the forward pass, in dw and in dx, with edges; long contractions onto few results."""
+    check_linear(rows, d_in, d_out, dtype, "silu", seed=rows)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [31, 32, 33, 63, 64])
+@pytest.mark.parametrize("d_in,d_out", [(40, 1000), (1000, 40), (4104, 72)])
+def test_linear_few_rows(rows, d_in, d_out, dtype):
+    check_linear(rows, d_in, d_out, dtype, "gelu", seed=rows)
+    check_linear(rows, d_in, d_out, dtype, "none", batch=3, pad=8, seed=rows + 1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_linear_into_given_memory(dtype):
     """Slices of a worker's row of parameters as w, b and their gradients; what lies beside them keeps its values.  In place onto the residual."""
     g = gen(5)
@@ -259,6 +274,17 @@ def test_orthogonalize_sizes(batch, rows, cols, dtype):
     m2 = torch.empty_like(m)
     again = nm.netmax_orthogonalize(a, kept, m_out=m2, mu=0.95)
     assert torch.equal(again, got) and torch.equal(m2, m)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("batch,rows,cols", [(64, 300, 520), (66, 530, 290), (64, 264, 257), (200, 65, 140), (150, 200, 130)])
+def test_orthogonalize_many_matrices(batch, rows, cols, dtype):
+    """Enough blocks for every block shape, with edges."""
+    g = gen(batch)
+    a = gradient_like(g, batch, rows, cols, dtype)
+    want, _ = orth64(a, None, 0.0, False)
+    got = nm.netmax_orthogonalize(a)
+    assert max(off(got[k], want[k]) for k in range(batch)) < ORTH_TOL[dtype]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
