@@ -1,0 +1,48 @@
+// float values as two planes of halves: v = hi + lo, 22 bits and more where v is scaled into the halves' range.
+#pragma once
+#include "gemm16.h"
+
+namespace netmax {
+
+__device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
+
+struct TwoHalves {
+    _Float16 hi, lo;
+    __device__ __forceinline__ explicit TwoHalves(float v)
+    {
+        hi = (_Float16)v;
+        lo = (_Float16)(v - (float)hi);
+    }
+};
+__device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return (float)__builtin_bit_cast(_Float16, lo) + (float)__builtin_bit_cast(_Float16, hi); }
+
+// Four neighbours of a row of planes; the planes' rows are padded to multiples of 8.
+__device__ __forceinline__ f32x4 load_planes(const uint16_t *hi, const uint16_t *lo)
+{
+    const uint2 h = *reinterpret_cast<const uint2 *>(hi), l = *reinterpret_cast<const uint2 *>(lo);
+    return f32x4{joined((uint16_t)h.x, (uint16_t)l.x), joined((uint16_t)(h.x >> 16), (uint16_t)(l.x >> 16)), joined((uint16_t)h.y, (uint16_t)l.y),
+                 joined((uint16_t)(h.y >> 16), (uint16_t)(l.y >> 16))};
+}
+__device__ __forceinline__ f32x4 load_plane(const uint16_t *hi)
+{
+    const uint2 h = *reinterpret_cast<const uint2 *>(hi);
+    return f32x4{joined((uint16_t)h.x, 0), joined((uint16_t)(h.x >> 16), 0), joined((uint16_t)h.y, 0), joined((uint16_t)(h.y >> 16), 0)};
+}
+__device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v)
+{
+    const TwoHalves a(v[0]), b(v[1]), c(v[2]), d(v[3]);
+    *reinterpret_cast<uint2 *>(hi) = make_uint2(half_bits(a.hi) | half_bits(b.hi) << 16, half_bits(c.hi) | half_bits(d.hi) << 16);
+    if (lo) *reinterpret_cast<uint2 *>(lo) = make_uint2(half_bits(a.lo) | half_bits(b.lo) << 16, half_bits(c.lo) | half_bits(d.lo) << 16);
+}
+
+// One launch for every block shape: `go` gets it as BM, BN, waves, step and stages of gemm16_kernel.
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_> struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_; };
+template <bool SPLIT, class Blocks, class Go> static void with_small_shape(const Blocks &blocks, const Go &go)
+{
+    // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has
+    if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    else if (blocks(128) >= 128) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
+    else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
+}
+
+}  // namespace netmax

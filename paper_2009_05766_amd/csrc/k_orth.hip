@@ -13,7 +13,7 @@
 //   bfloat16     products of hi planes (11 bits), the term a X from both planes.  B's diagonal, its large part near the end, is kept in float and
 //                joins a X: the rounding of B then halves the result's error, to 0.6e-3 where the rounding of the result itself is 1.7e-3
 // A and B are symmetric: their blocks on and below the diagonal are computed and written to both sides.
-#include "gemm16.h"
+#include "half_planes.h"
 #include "orth.h"
 
 #include <type_traits>
@@ -22,39 +22,7 @@ namespace netmax {
 
 constexpr int NORM_BLOCKS = 256;      // partial sums of squares of one matrix, at most: one for each thread that adds them up
 
-__device__ __forceinline__ uint32_t half_bits(_Float16 h) { return (uint32_t)__builtin_bit_cast(uint16_t, h); }
-
 constexpr float X_SCALE = 0x1p11f, SQUARE_SCALE = 0x1p8f;
-
-// v = hi + lo
-struct TwoHalves {
-    _Float16 hi, lo;
-    __device__ __forceinline__ explicit TwoHalves(float v)
-    {
-        hi = (_Float16)v;
-        lo = (_Float16)(v - (float)hi);
-    }
-};
-__device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return (float)__builtin_bit_cast(_Float16, lo) + (float)__builtin_bit_cast(_Float16, hi); }
-
-// Four neighbours of a row of planes; the planes' rows are padded to multiples of 8.
-__device__ __forceinline__ f32x4 load_planes(const uint16_t *hi, const uint16_t *lo)
-{
-    const uint2 h = *reinterpret_cast<const uint2 *>(hi), l = *reinterpret_cast<const uint2 *>(lo);
-    return f32x4{joined((uint16_t)h.x, (uint16_t)l.x), joined((uint16_t)(h.x >> 16), (uint16_t)(l.x >> 16)), joined((uint16_t)h.y, (uint16_t)l.y),
-                 joined((uint16_t)(h.y >> 16), (uint16_t)(l.y >> 16))};
-}
-__device__ __forceinline__ f32x4 load_plane(const uint16_t *hi)
-{
-    const uint2 h = *reinterpret_cast<const uint2 *>(hi);
-    return f32x4{joined((uint16_t)h.x, 0), joined((uint16_t)(h.x >> 16), 0), joined((uint16_t)h.y, 0), joined((uint16_t)(h.y >> 16), 0)};
-}
-__device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v)
-{
-    const TwoHalves a(v[0]), b(v[1]), c(v[2]), d(v[3]);
-    *reinterpret_cast<uint2 *>(hi) = make_uint2(half_bits(a.hi) | half_bits(b.hi) << 16, half_bits(c.hi) | half_bits(d.hi) << 16);
-    if (lo) *reinterpret_cast<uint2 *>(lo) = make_uint2(half_bits(a.lo) | half_bits(b.lo) << 16, half_bits(c.lo) | half_bits(d.lo) << 16);
-}
 
 // A symmetric result alpha acc + beta own as planes [batch][side][wide], zeros behind each row; lo may be null.  With `diagonal` its diagonal goes
 // there and is 0 in the planes.  Squares of 64 x 64 on the diagonal lie whole inside computed blocks and are kept as they come; of all others those
@@ -237,15 +205,6 @@ int64_t orth_workspace(const OrthArgs &a)
     return 4 * x_bytes(a) + (a.bf16 ? 2 : 4) * square_bytes(a) + up256(a.batch * side_of(a) * 4) + up256(8 * a.batch * NORM_BLOCKS);
 }
 
-// One launch for every block shape: `go` gets it as BM, BN, waves, step and stages of gemm16_kernel.
-template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_> struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_; };
-template <bool SPLIT, class Blocks, class Go> static void with_small_shape(const Blocks &blocks, const Go &go)
-{
-    // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has
-    if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
-    else if (blocks(128) >= 128) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
-    else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
-}
 // Many blocks: 256 x 128, two workgroups on a compute unit, so that the results of one (planes in and out, as long as half of the products) leave under
 // the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us.
 typedef Shape<256, 128, 4, 2, 32, 3> Paired;

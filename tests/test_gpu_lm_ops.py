@@ -139,6 +139,34 @@ def test_linear_many_blocks(rows, d_in, d_out, dtype):
     check_linear(rows, d_in, d_out, dtype, "silu", seed=rows)
 
 
+@pytest.mark.parametrize("rows,d_in,d_out,batch", [(1600, 1601, 1602, 0), (2048, 1024, 2048, 0), (700, 2304, 2305, 2), (3000, 1500, 1030, 0)])
+def test_linear_large_in_float(rows, d_in, d_out, batch):
+    """Products that are worth planes of halves."""
+    check_linear(rows, d_in, d_out, F32, "gelu", batch=batch, seed=rows)
+    check_linear(rows, d_in, d_out, F32, "none", batch=batch, pad=3, seed=rows + 1)
+
+
+def test_linear_large_in_float_over_many_magnitudes():
+    """Rows of x and columns of w from 1e-30 to 1e+6, an infinity in one row, a NaN in another: every other result as exact as its own magnitudes allow."""
+    g = gen(12)
+    n = 1664
+    x = normal(g, n, n) * 10.0 ** (torch.rand(n, 1, generator=g, device="cuda") * 36 - 30)
+    w = normal(g, n, n) * 10.0 ** (torch.rand(1, n, generator=g, device="cuda") * 16 - 10)
+    x[5] = 0.0
+    w[:, 9] = 0.0
+    keep = x.clone()
+    x[3, 7], x[4, 8], x[6, 0] = float("inf"), float("nan"), 3e38
+    y = nm.netmax_linear(x, w)
+    rows = torch.ones(n, dtype=torch.bool, device="cuda")
+    rows[3] = rows[4] = rows[6] = False
+    X, W = keep.double(), w.double()
+    want, mag = X @ W, X.abs() @ W.abs()
+    within(y[rows], want[rows], ((n + 4) * 2.0 ** -24 * mag + 2.0 ** -24 * want.abs() + 2.0 ** -149)[rows], "y")
+    live = torch.ones(n, dtype=torch.bool, device="cuda")
+    live[9] = False
+    assert not bool(torch.isfinite(y[3:5][:, live]).any())
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("rows", [31, 32, 33, 63, 64])
 @pytest.mark.parametrize("d_in,d_out", [(40, 1000), (1000, 40), (4104, 72)])
