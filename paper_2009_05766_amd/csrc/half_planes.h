@@ -40,7 +40,8 @@ template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_> struct Sha
 template <bool SPLIT, class Blocks, class Go> static void with_small_shape(const Blocks &blocks, const Go &go)
 {
     // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has
-    if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    if (SPLIT && blocks(256) >= 128) go(Shape<256, 128, 4, 2, 32, 3>());
+    else if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
     else if (blocks(128) >= 128) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
     else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
 }

@@ -312,9 +312,36 @@ static void launch_product32(hipStream_t s, int64_t batch, int64_t M, int64_t N,
 
 // ---- dz and db -------------------------------------------------------------------------------------------------------
 
-// A workgroup takes `run` rows of 256 columns, a wave every fourth row, a lane four columns: dz, and the column sums of dz (before its rounding) over
+// A workgroup takes `run` rows of SLOPE_COLS columns, a wave every fourth row, a lane 16 bytes: dz, and the column sums of dz (before its rounding) over
 // these rows, in float, in a fixed order.  Bound by memory: dy and z in, dz out.
-constexpr int SLOPE_COLS = 256;
+template <typename T> constexpr int SLOPE_COLS = 1024 / sizeof(T);
+
+// 16 bytes from column n of `cols` as floats, 0 behind the last; and back.
+template <typename T> __device__ __forceinline__ void load_16_bytes(const T *row, int64_t n, int64_t cols, float (&v)[16 / sizeof(T)])
+{
+    if constexpr (sizeof(T) == 4) {
+        const f32x4 x = load_up_to_four(row, n, cols);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = x[e];
+    } else if (n + 8 <= cols) {
+        const u32x4 x = *reinterpret_cast<const u32x4_any *>(row + n);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = n + e < cols ? load_value(row + n + e) : 0.0f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store_16_bytes(T *row, int64_t n, int64_t cols, const float (&v)[16 / sizeof(T)])
+{
+    if constexpr (sizeof(T) == 4) store_up_to_four(row, n, cols, f32x4{v[0], v[1], v[2], v[3]});
+    else if (n + 8 <= cols)
+        *reinterpret_cast<u32x4_any *>(row + n) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    else
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (n + e < cols) store_value(row + n + e, v[e]);
+}
 
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -322,31 +349,35 @@ slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int6
              T *__restrict__ dz, int64_t wide, float *__restrict__ sums)
 {
     // dz has rows of `wide` values, zeros behind the columns: what the product's contraction over them needs
-    __shared__ __align__(16) float part[4][SLOPE_COLS];
-    const int wave = threadIdx.x >> 6, at = (threadIdx.x & 63) * 4;
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * SLOPE_COLS + at, r0 = (int64_t)blockIdx.y * run + wave;
+    constexpr int VALUES = 16 / sizeof(T), COLS = SLOPE_COLS<T>;
+    __shared__ __align__(16) float part[4][COLS];
+    const int wave = threadIdx.x >> 6, at = (threadIdx.x & 63) * VALUES;
+    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * COLS + at, r0 = (int64_t)blockIdx.y * run + wave;
     const int64_t end = (int64_t)(blockIdx.y + 1) * run < rows ? (int64_t)(blockIdx.y + 1) * run : rows;
     dy += g * sdy;
     z += g * sz;
-    f32x4 sum = {0, 0, 0, 0};
+    float sum[VALUES] = {};
     if (n < wide)
 #pragma unroll 4
         for (int64_t r = r0; r < end; r += 4) {
-            f32x4 v = load_up_to_four(dy + r * lddy, n, cols);
+            float v[VALUES];
+            load_16_bytes(dy + r * lddy, n, cols, v);
             if (act != ACT_NONE) {
-                const f32x4 pre = load_up_to_four(z + r * ldz, n, cols);
+                float pre[VALUES];
+                load_16_bytes(z + r * ldz, n, cols, pre);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? v[e] * act_slope(act, pre[e]) : 0.0f;
+                for (int e = 0; e < VALUES; ++e) v[e] = n + e < cols ? v[e] * act_slope(act, pre[e]) : 0.0f;
             }
-            sum += v;
-            if (dz) store_up_to_four(dz + (g * rows + r) * wide, n, wide, v);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) sum[e] += v[e];
+            if (dz) store_16_bytes(dz + (g * rows + r) * wide, n, wide, v);
         }
     if (!sums) return;
-    store4(&part[wave][at], sum);
+#pragma unroll
+    for (int e = 0; e < VALUES; ++e) part[wave][at + e] = sum[e];
     __syncthreads();
-    const int64_t col = (int64_t)blockIdx.x * SLOPE_COLS + threadIdx.x;
-    if (col < cols)
-        sums[((int64_t)g * gridDim.y + blockIdx.y) * cols + col] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+    for (int c = threadIdx.x; c < COLS && (int64_t)blockIdx.x * COLS + c < cols; c += 256)
+        sums[((int64_t)g * gridDim.y + blockIdx.y) * cols + (int64_t)blockIdx.x * COLS + c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
 }
 
 // 64 columns per workgroup; four waves take the parts in turn, then their sums are added in order.
@@ -404,7 +435,7 @@ static int64_t dz_wide(const LinearGradArgs &a) { return a.bf16 ? round_up(a.dou
 // Rows of a workgroup of slope_kernel: 64, or fewer where that leaves compute units without work (at 1111 x 2049, rows at odd places, 64: 35 us).
 static int slope_run(const LinearGradArgs &a)
 {
-    const int64_t across = a.batch * ((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS);
+    const int64_t across = a.batch * ((dz_wide(a) + 255) / 256);
     int run = 64;
     while (run > 8 && across * ((a.rows + run - 1) / run) < 1024) run /= 2;
     return run;
@@ -431,7 +462,7 @@ int64_t linear_grad_workspace(const LinearGradArgs &a)
 template <typename T> static void launch_slopes(hipStream_t s, const LinearGradArgs &a, T *dz, float *sums)
 {
     if ((dz || a.db) && a.rows > 0)
-        slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS - 1) / SLOPE_COLS), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
+        slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS<T> - 1) / SLOPE_COLS<T>), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
             a.rows, a.dout, slope_run(a), (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz,
             dz_wide(a), a.db ? sums : nullptr);
     if (a.db)

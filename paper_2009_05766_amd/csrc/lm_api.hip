@@ -40,7 +40,7 @@ static int check_linear(const netmax_linear_shape *s)
     if (s->batch < 0 || s->batch > 65535 || s->rows < 0 || s->d_in < 1 || s->d_out < 1 || s->d_in >= 1 << 22 || s->d_out >= 1 << 22)
         return netmax_fail(NETMAX_EINVAL, "need 0 <= batch <= 65535, rows >= 0, 1 <= d_in < 2^22 and 1 <= d_out < 2^22");
     if (!product_fits(s->batch, s->rows, s->d_in) || !product_fits(s->batch, s->rows, s->d_out) || !product_fits(s->batch, s->d_in, s->d_out) ||
-        !blocks_fit(s->batch, s->rows, s->d_in) || !blocks_fit(s->batch, s->rows, s->d_out) || !blocks_fit(s->batch, s->d_in, s->d_out) || s->rows > (int64_t)65535 * 8)
+        !blocks_fit(s->batch, s->rows, s->d_in) || !blocks_fit(s->batch, s->rows, s->d_out) || !blocks_fit(s->batch, s->d_in, s->d_out) || s->rows > (int64_t)65535 * 64)
         return netmax_fail(NETMAX_EINVAL, "the layer is too large");
     if (!dtype_known(s->dtype)) return netmax_fail(NETMAX_EINVAL, "dtype must be NETMAX_F32 or NETMAX_BF16");
     if (s->act < NETMAX_ACT_NONE || s->act > NETMAX_ACT_SILU) return netmax_fail(NETMAX_EINVAL, "unknown activation");
