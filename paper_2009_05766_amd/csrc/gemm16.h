@@ -134,15 +134,19 @@ template <int RATIO> __device__ __forceinline__ void triangle_place(uint32_t id,
 // the terms, is left out.
 struct Planes16 { const char *hi, *lo; int64_t ld, step; };          // ld, step in elements
 
-template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, int STEP, int STAGES, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
-__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64)
+// GROUPS groups of waves take a block's steps in turn, each with its own space, and add up their results in LDS: for few blocks, which are bound by the chain
+// of steps.
+template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, int STEP, int STAGES, int GROUPS, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64 * GROUPS)
 gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, TM = BM / WAVES_M / 32, TN = BN / WAVES_N / 32;
     typedef Step16<BM, AK, STEP, THREADS> StepA;
     typedef Step16<BN, BK, STEP, THREADS> StepB;
     constexpr int PLANES = SPLIT ? 2 : 1, STAGE = PLANES * (StepA::BYTES + StepB::BYTES), REQUESTS = PLANES * (StepA::PIECES + StepB::PIECES);
-    __shared__ __align__(16) char lds[STAGES][STAGE];
+    __shared__ __align__(16) char space[GROUPS][STAGES][STAGE];
+    const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS) : 0, thread = (int)threadIdx.x - group * THREADS;
+    char (&lds)[STAGES][STAGE] = space[group];
     uint32_t g, mb, nb;
     const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
     if (TRIANGLE) {
@@ -152,11 +156,11 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
     const int64_t kstepA = AK ? STEP * 2 : A.ld * (STEP * 2), kstepB = BK ? STEP * 2 : B.ld * (STEP * 2);
     const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
-    const int wave = threadIdx.x >> 6, wm = wave / WAVES_N * (TM * 32), wn = wave % WAVES_N * (TN * 32);
+    const int wave = thread >> 6, wm = wave / WAVES_N * (TM * 32), wn = wave % WAVES_N * (TN * 32);
     StepA sa;
     StepB sb;
-    sa.place(threadIdx.x, m0, M, A.ld);
-    sb.place(threadIdx.x, n0, N, B.ld);
+    sa.place(thread, m0, M, A.ld);
+    sb.place(thread, n0, N, B.ld);
     Fragment16<BM, AK, STEP> fa[TM];
     Fragment16<BN, BK, STEP> fb[TN];
 #pragma unroll
@@ -180,11 +184,11 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     char *next_to;
     int next_left;
     const auto aim = [&](int s) {
-        const int64_t k = first + s, left = K - k * STEP;
+        const int64_t k = first + (int64_t)s * GROUPS + group, left = K - k * STEP;
         next_a = from_a + k * kstepA;
         next_b = from_b + k * kstepB;
         next_to = lds[s % STAGES];
-        next_left = s >= total ? 0 : left < STEP ? (int)left : STEP;
+        next_left = s * GROUPS + group >= total ? 0 : left < STEP ? (int)left : STEP;
     };
     const auto request = [&](int u) {                               // pieces of A, of B, then those of the low planes
         const bool low = u >= StepA::PIECES + StepB::PIECES;
@@ -235,7 +239,8 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     for (int u = 0; u < HALF; ++u) request(u);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * REQUESTS + HALF) : "memory");
     read(0, lds[0], 0);
-    for (int s = 0; s < total; ++s) {
+    const int turns = (total + GROUPS - 1) / GROUPS;                 // a group without a step has zeros
+    for (int s = 0; s < turns; ++s) {
 #pragma unroll
         for (int kk = 0; kk < PARTS - 1; ++kk) {
             read((kk + 1) & 1, lds[s % STAGES], kk + 1);
@@ -248,11 +253,39 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
         multiply(1, 0, HALF);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if constexpr (GROUPS > 1) {
+        // behind the space that results leave by
+        constexpr int OUT = WAVES_M * WAVES_N * 32 * (TN * 32 + 4), QUADS = TM * TN * 4;
+        static_assert(OUT * 4 + (GROUPS - 1) * QUADS * THREADS * 16 <= GROUPS * STAGES * STAGE, "the groups' results fit the steps' space");
+        f32x4 *sums = reinterpret_cast<f32x4 *>((float *)space + OUT) + thread;
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sums[((group - 1) * QUADS + (i * TN + j) * 4 + e) * THREADS] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int o = 0; o < GROUPS - 1; ++o)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x4 v = sums[(o * QUADS + (i * TN + j) * 4 + e) * THREADS];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[i][j][4 * e + q] += v[q];
+                    }
+    }
     // Results leave by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes have neighbouring columns of a row: straight from the
     // instruction's layout a request would touch 32 rows, 16 bytes in each.
     constexpr int COLS = TN * 32, PITCH = COLS + 4;
     const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
-    float *stage = (float *)lds + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
+    float *stage = (float *)space + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
     const int64_t where = !TRIANGLE && splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -371,36 +404,36 @@ inline bool fits16(const void *p, int64_t ld, int64_t step, int64_t stored)
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && step % 8 == 0 && stored % 8 == 0 && ld < (1 << 22);
 }
 
-template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, bool SPLIT, class Epilogue>
 void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, uint32_t splits,
                           const Epilogue &e)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
-    const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64);
-    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64 * GROUPS);
+    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
 }
 
 // The lower triangle of blocks of a symmetric product, A B with B = A transposed as stored: both operands have the same orientation.
-template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, bool SPLIT, class Epilogue>
 void launch_gemm16_triangle(hipStream_t s, int64_t batch, int64_t M, int64_t K, const Planes16 &a, bool near, const Epilogue &e)
 {
     const uint32_t side = (uint32_t)((M + BM - 1) / BM);
-    const dim3 grid((uint32_t)(batch * (BM / BN) * side * (side + 1) / 2)), block(WM * WN * 64);
-    if (near) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    const dim3 grid((uint32_t)(batch * (BM / BN) * side * (side + 1) / 2)), block(WM * WN * 64 * GROUPS);
+    if (near) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, false, SPLIT, true><<<grid, block, 0, s>>>(M, M, K, a, a, side, side, 1, e);
 }
 
 // C = A B with A's contraction index near and B's as `bk` says, in blocks of BM x BN.
-template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, bool SPLIT, class Epilogue>
 void launch_gemm16_step(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, const Planes16 &b, bool bk, const Epilogue &e)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
-    const dim3 grid((uint32_t)(batch * mb * nb)), block(WM * WN * 64);
-    if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
+    const dim3 grid((uint32_t)(batch * mb * nb)), block(WM * WN * 64 * GROUPS);
+    if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, 1, e);
 }
 
 }  // namespace netmax

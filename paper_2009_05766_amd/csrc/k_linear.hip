@@ -98,7 +98,7 @@ static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
     const int64_t steps = (K + 63) / 64;
     if (blocks(256) >= 192) return {256, 1};
     const int block = blocks(128) >= 96 && M > 64 && N > 64 ? 128 : 64;
-    const int64_t here = blocks(block) > 0 ? blocks(block) : 1, want = (block == 128 ? 256 : 512) / here, most = steps / 16;
+    const int64_t here = blocks(block) > 0 ? blocks(block) : 1, want = 256 / here, most = steps / 16;
     const int64_t splits = want < most ? want : most;
     return {block, (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits)};
 }
@@ -116,10 +116,11 @@ static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, 
                             const Epilogue &e)
 {
     const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block) * splits;
-    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (blocks > 256 || K < 512 * splits) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
 }
 
 // `work`: part_bytes() of it.
@@ -216,11 +217,11 @@ column_sizes_kernel(int64_t rows, int64_t cols, int64_t run, const float *__rest
 
 // [batch][rows][cols] with a power for each column, from the sizes of its runs.
 __global__ void __launch_bounds__(256)
-split_columns_kernel(int64_t rows, int64_t cols, int64_t wide, int runs, const float *__restrict__ in, int64_t ld, int64_t step, const float *__restrict__ sizes,
+split_columns_kernel(int64_t rows, int64_t cols, int64_t wide, int run, int runs, const float *__restrict__ in, int64_t ld, int64_t step, const float *__restrict__ sizes,
                      uint16_t *__restrict__ hi, uint16_t *__restrict__ lo, int *__restrict__ powers)
 {
     const int wave = threadIdx.x >> 6;
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 256 + (threadIdx.x & 63) * 4, r0 = (int64_t)blockIdx.y * 64;
+    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 256 + (threadIdx.x & 63) * 4, r0 = (int64_t)blockIdx.y * run;
     if (n >= wide) return;
     f32x4 most = {0, 0, 0, 0};
 #pragma unroll 4
@@ -236,7 +237,7 @@ split_columns_kernel(int64_t rows, int64_t cols, int64_t wide, int runs, const f
         if (blockIdx.y == 0 && wave == 0 && n + e < cols) powers[g * cols + n + e] = -power[e];
     }
 #pragma unroll 4
-    for (int64_t r = r0 + wave; r < r0 + 64 && r < rows; r += 4) {
+    for (int64_t r = r0 + wave; r < r0 + run && r < rows; r += 4) {
         const f32x4 v = load_up_to_four(in + g * step + r * ld, n, cols);
         const int64_t at = (g * rows + r) * wide + n;
         store_split(hi + at, lo + at, f32x4{ldexpf(v[0], power[0]), ldexpf(v[1], power[1]), ldexpf(v[2], power[2]), ldexpf(v[3], power[3])});
@@ -259,7 +260,7 @@ template <class Inner> struct PowerEpilogue {
 
 // Whether a float product is multiplied as planes: where the time that it saves (100 against 300 TFLOP/s) is several times what planes take (reading
 // an operand two or three times and writing it once, and up to five launches).  4096 x 4096 x 4096: 1.37 ms in float, 0.52 ms as planes.
-static bool as_planes(int64_t batch, int64_t M, int64_t N, int64_t K) { return M * N >= 256 * (M + N) && (double)batch * M * N * K >= 4e9; }
+static bool as_planes(int64_t batch, int64_t M, int64_t N, int64_t K) { return M * N >= 256 * (M + N) && (double)batch * M * N * K >= 2.5e9; }
 
 // A float matrix [rows][cols] of a batch as planes, with a power for each row (`near`: the contraction runs along the rows) or each column.
 struct FloatSource {
@@ -281,10 +282,10 @@ struct FloatSource {
         if (near) {
             split_rows_kernel<<<(uint32_t)((all + 3) / 4), 256, 0, s>>>(all, rows, cols, wide, (const float *)p, ld, step, hi, lo, to);
         } else {
-            const int64_t run = round_up((rows + runs() - 1) / runs(), 4);
+            const int64_t run = round_up((rows + runs() - 1) / runs(), 4), each = rows < 4096 ? 16 : 64;     // rows of a workgroup: few leave compute units without work
             const uint32_t across = (uint32_t)((wide + 255) / 256), n = (uint32_t)((rows + run - 1) / run);
             column_sizes_kernel<<<dim3(across, n, (uint32_t)own(batch)), 256, 0, s>>>(rows, cols, run, (const float *)p, ld, step, sizes);
-            split_columns_kernel<<<dim3(across, (uint32_t)((rows + 63) / 64), (uint32_t)own(batch)), 256, 0, s>>>(rows, cols, wide, (int)n, (const float *)p, ld, step, sizes,
+            split_columns_kernel<<<dim3(across, (uint32_t)((rows + each - 1) / each), (uint32_t)own(batch)), 256, 0, s>>>(rows, cols, wide, (int)each, (int)n, (const float *)p, ld, step, sizes,
                                                                                                               hi, lo, to);
         }
         return Planes16{(const char *)hi, (const char *)lo, wide, step ? rows * wide : 0};
@@ -305,8 +306,8 @@ static void launch_product32(hipStream_t s, int64_t batch, int64_t M, int64_t N,
     }
     PowerEpilogue<Epilogue> powers{e, nullptr, nullptr, M, N, 0, 0};
     const Planes16 pa = a.take(s, batch, work, powers.by_row, powers.sr), pb = b.take(s, batch, work + a.bytes(batch), powers.by_column, powers.sc);
-    with_small_shape<true>([&](int64_t n) { return batch * ((M + n - 1) / n) * ((N + n - 1) / n); }, [&](auto f) {
-        launch_gemm16_blocks<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, true>(s, batch, M, N, K, pa, a.near, pb, b.near, 1, powers);
+    with_small_shape<true>(K, [&](int64_t n) { return batch * ((M + n - 1) / n) * ((N + n - 1) / n); }, [&](auto f) {
+        launch_gemm16_blocks<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, true>(s, batch, M, N, K, pa, a.near, pb, b.near, 1, powers);
     });
 }
 

@@ -211,11 +211,11 @@ typedef Shape<256, 128, 4, 2, 32, 3> Paired;
 
 template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
 {
-    const auto go = [&](auto f) { launch_gemm16_triangle<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, batch, side, K, x, near, e); };
+    const auto go = [&](auto f) { launch_gemm16_triangle<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, SPLIT>(s, batch, side, K, x, near, e); };
     const auto blocks = [&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; };
     if constexpr (!SPLIT)
         if (blocks(256) >= 192) { go(Paired()); return; }
-    with_small_shape<SPLIT>(blocks, go);
+    with_small_shape<SPLIT>(K, blocks, go);
 }
 
 template <bool SPLIT, class Epilogue>
@@ -224,7 +224,7 @@ static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, con
     const bool tall = a.rows > a.cols;
     const int64_t k = side_of(a);
     const Planes16 &l = tall ? x : b, &r = tall ? b : x;            // B is symmetric: its rows are its columns
-    const auto go = [&](auto f) { launch_gemm16_step<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e); };
+    const auto go = [&](auto f) { launch_gemm16_step<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e); };
     const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
     if constexpr (!SPLIT)
         if (blocks(256) >= 192) {
@@ -232,7 +232,7 @@ static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, con
             else go(Shape<256, 256, 2, 4, 64, 2>());
             return;
         }
-    with_small_shape<SPLIT>(blocks, go);
+    with_small_shape<SPLIT>(k, blocks, go);
 }
 
 template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char *work)
