@@ -21,7 +21,8 @@ def _refuse(text: str):
 
 
 def _check_tensor(name: str, t, like: torch.Tensor, shape: Tuple[int, ...], dtype: torch.dtype) -> torch.Tensor:
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == like.get_device() and t.shape == shape and (t.stride(-1) == 1 or t.shape[-1] <= 1):
+    # what is right takes one look; what is wrong is looked at closely
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == like.get_device() and t.shape == shape and (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] <= 1):
         return t
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
@@ -103,7 +104,8 @@ def netmax_linear(x, w, bias=None, residual=None, *, act: str = "none", keep_pre
     if not isinstance(w, torch.Tensor) or w.dim() != x.dim():
         _refuse("w must have as many dimensions as x")
     d_out, dt = w.shape[-1], x.dtype
-    _check_tensor("x", x, x, (*lead, rows, d_in), dt)
+    if not x.is_contiguous():
+        _check_tensor("x", x, x, (*lead, rows, d_in), dt)
     _check_tensor("w", w, x, (*lead, d_in, d_out), dt)
     if bias is not None:
         _check_tensor("bias", bias, x, (*lead, d_out), dt)
@@ -203,14 +205,16 @@ def netmax_orthogonalize(g, m=None, *, m_out=None, out=None, mu: float = 0.95, n
 def _token_rows(logits, labels, weight, grad, need_grad):
     _first("logits", logits, (2,))
     tokens, vocab = logits.shape
-    _check_tensor("logits", logits, logits, logits.shape, logits.dtype)
+    dense = logits.is_contiguous()
+    if not dense:
+        _check_tensor("logits", logits, logits, logits.shape, logits.dtype)
     _check_tensor("labels", labels, logits, (tokens,), torch.int32)
     if weight is not None:
         _check_tensor("weight", weight, logits, (tokens,), torch.float32)
     if grad is not None:
         _written("grad", _check_tensor("grad", grad, logits, logits.shape, logits.dtype))
     elif need_grad:
-        grad = torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
+        grad = torch.empty_like(logits) if dense else torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
     return tokens, vocab, grad
 
 
