@@ -137,25 +137,28 @@ template <int RATIO> __device__ __forceinline__ void triangle_place(uint32_t id,
 // the terms, is left out.
 struct Planes16 { const char *hi, *lo; int64_t ld, step; };          // ld, step in elements
 
+template <int BM, int BN, int STEP, int STAGES, int GROUPS, bool SPLIT> constexpr int space16() { return GROUPS * STAGES * (SPLIT ? 2 : 1) * (BM + BN) * STEP * 2; }
+
 // GROUPS groups of waves take a block's steps in turn, each with its own space, and add up their results in LDS: for few blocks, which are bound by the chain
 // of steps.
+// Workgroup `id` of `count`; `space`: space16() bytes of LDS.
 template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, int STEP, int STAGES, int GROUPS, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
-__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64 * GROUPS)
-gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
+__device__ __forceinline__ void gemm16_block(int64_t M, int64_t N, int64_t K, const Planes16 &A, const Planes16 &B, uint32_t mblocks, uint32_t nblocks, uint32_t splits,
+                                             const Epilogue &epilogue, uint32_t id, uint32_t count, char *space_)
 {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, TM = BM / WAVES_M / 32, TN = BN / WAVES_N / 32;
     typedef Step16<BM, AK, STEP, THREADS> StepA;
     typedef Step16<BN, BK, STEP, THREADS> StepB;
     constexpr int PLANES = SPLIT ? 2 : 1, STAGE = PLANES * (StepA::BYTES + StepB::BYTES), REQUESTS = PLANES * (StepA::PIECES + StepB::PIECES);
-    __shared__ __align__(16) char space[GROUPS][STAGES][STAGE];
     const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS) : 0, thread = (int)threadIdx.x - group * THREADS;
-    char (&lds)[STAGES][STAGE] = space[group];
+    static_assert(GROUPS * STAGES * STAGE == space16<BM, BN, STEP, STAGES, GROUPS, SPLIT>(), "the caller's space");
+    char (*lds)[STAGE] = reinterpret_cast<char (*)[STAGE]>(space_ + group * (STAGES * STAGE));
     uint32_t g, mb, nb;
-    const uint32_t all = gridDim.x / splits, split = blockIdx.x / all;
+    const uint32_t all = count / splits, split = id / all;
     if (TRIANGLE) {
-        triangle_place<BM / BN>(blockIdx.x % all, all, mblocks, g, mb, nb);
+        triangle_place<BM / BN>(id % all, all, mblocks, g, mb, nb);
         if ((int64_t)nb * BN >= N) return;                          // the last row's blocks may reach past the square
-    } else block_place(blockIdx.x % all, all, mblocks, nblocks, g, mb, nb);
+    } else block_place(id % all, all, mblocks, nblocks, g, mb, nb);
     const int64_t m0 = (int64_t)mb * BM, n0 = (int64_t)nb * BN;
     const int64_t kstepA = AK ? STEP * 2 : A.ld * (STEP * 2), kstepB = BK ? STEP * 2 : B.ld * (STEP * 2);
     const int64_t from_a = ((int64_t)g * A.step + (AK ? m0 * A.ld : m0)) * 2, from_b = ((int64_t)g * B.step + (BK ? n0 * B.ld : n0)) * 2;
@@ -260,7 +263,7 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
         // behind the space that results leave by
         constexpr int OUT = WAVES_M * WAVES_N * 32 * (TN * 32 + 4), QUADS = TM * TN * 4;
         static_assert(OUT * 4 + (GROUPS - 1) * QUADS * THREADS * 16 <= GROUPS * STAGES * STAGE, "the groups' results fit the steps' space");
-        f32x4 *sums = reinterpret_cast<f32x4 *>((float *)space + OUT) + thread;
+        f32x4 *sums = reinterpret_cast<f32x4 *>((float *)space_ + OUT) + thread;
         if (group > 0)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
@@ -288,7 +291,7 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
     // instruction's layout a request would touch 32 rows, 16 bytes in each.
     constexpr int COLS = TN * 32, PITCH = COLS + 4;
     const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
-    float *stage = (float *)space + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
+    float *stage = (float *)space_ + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
     const int64_t where = !TRIANGLE && splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -312,6 +315,32 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
             }
         wave_order();
     }
+}
+
+template <typename V, int BM, int BN, int WAVES_M, int WAVES_N, int STEP, int STAGES, int GROUPS, bool AK, bool BK, bool SPLIT, bool TRIANGLE, class Epilogue>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64 * GROUPS)
+gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t mblocks, uint32_t nblocks, uint32_t splits, Epilogue epilogue)
+{
+    __shared__ __align__(16) char space[space16<BM, BN, STEP, STAGES, GROUPS, SPLIT>()];
+    gemm16_block<V, BM, BN, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, AK, BK, SPLIT, TRIANGLE>(M, N, K, A, B, mblocks, nblocks, splits, epilogue, blockIdx.x, gridDim.x, space);
+}
+
+// Two products in one launch, the first with both contraction indices near and the second with both row indices near (a layer's dx and dw): where neither fills
+// the card, its compute units and the latency of a launch are shared.  Workgroups from `both` on do `extra`, which depends on neither.
+template <class Epilogue> struct Product16 { int64_t M, N, K; Planes16 A, B; uint32_t mblocks, nblocks; Epilogue epilogue; };
+template <typename V, int BM, int WAVES_M, int WAVES_N, int STEP, int STAGES, int GROUPS, class Epilogue, class Extra>
+__global__ void __launch_bounds__(WAVES_M * WAVES_N * 64 * GROUPS)
+gemm16_pair_kernel(Product16<Epilogue> p, Product16<Epilogue> q, uint32_t first, uint32_t both, Extra extra)
+{
+    __shared__ __align__(16) char space[space16<BM, BM, STEP, STAGES, GROUPS, false>()];
+    if (blockIdx.x < first)
+        gemm16_block<V, BM, BM, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, true, true, false, false>(p.M, p.N, p.K, p.A, p.B, p.mblocks, p.nblocks, 1, p.epilogue, blockIdx.x,
+                                                                                                 first, space);
+    else if (blockIdx.x < both)
+        gemm16_block<V, BM, BM, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, false, false, false, false>(q.M, q.N, q.K, q.A, q.B, q.mblocks, q.nblocks, 1, q.epilogue,
+                                                                                                   blockIdx.x - first, both - first, space);
+    else
+        extra(blockIdx.x - both, reinterpret_cast<float *>(space));
 }
 
 // C = A B for few rows, at most 32 TM: the weights are what has to be read.  A workgroup has 32 columns; its eight waves take steps of 32 indices in turn,

@@ -47,10 +47,12 @@ template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
     }
 };
 
+template <int BM, int BN, int STEP, int GROUPS> constexpr int space_f32() { return GROUPS * 2 * STEP * (BM + BN + 8); }
+
+// Workgroup `id`; `space`: space_f32() floats of LDS.
 template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
-__global__ void __launch_bounds__(256 * GROUPS)
-gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
-                int64_t sb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
+__device__ __forceinline__ void gemm_f32_block(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
+                                               int64_t sb, uint32_t mblocks, uint32_t nblocks, const Epilogue &epilogue, uint32_t id, float *space)
 {
     typedef StepPieces<T, BM, STEP, AK> PiecesA;
     typedef StepPieces<T, BN, STEP, BK> PiecesB;
@@ -59,8 +61,9 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
     constexpr int STEP_FLOATS = STEP * (PiecesA::PITCH + PiecesB::PITCH);
     static_assert(TILES * 32 * 36 <= 2 * GROUPS * STEP_FLOATS, "results leave by way of the steps' space");
     static_assert((PARTS - 1) * BM * BN <= 2 * GROUPS * STEP_FLOATS, "partial results fit the steps' space");
-    __shared__ __align__(16) float lds[GROUPS][2][STEP_FLOATS];
-    const uint32_t per = mblocks * nblocks, g = blockIdx.x / per, b = blockIdx.x % per;
+    static_assert(GROUPS * 2 * STEP_FLOATS == space_f32<BM, BN, STEP, GROUPS>(), "the caller's space");
+    float (*lds)[2][STEP_FLOATS] = reinterpret_cast<float (*)[2][STEP_FLOATS]>(space);
+    const uint32_t per = mblocks * nblocks, g = id / per, b = id % per;
     const int64_t m0 = (int64_t)(b / nblocks) * BM, n0 = (int64_t)(b % nblocks) * BN;
     A += (int64_t)g * sa;
     B += (int64_t)g * sb;
@@ -104,7 +107,7 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
     if constexpr (PARTS > 1) {
         constexpr int STRIDE = TM * TN * 4 * TILES * 64;            // pieces of four of one part
         const int part = group * SHARES + share;
-        f32x4 *mine = reinterpret_cast<f32x4 *>(&lds[0][0][0]) + tile * 64 + lane;
+        f32x4 *mine = reinterpret_cast<f32x4 *>(space) + tile * 64 + lane;
         __syncthreads();
         if (part > 0)
 #pragma unroll
@@ -132,7 +135,7 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
     // results leave by way of LDS, so that neighbouring lanes have neighbouring columns of a row
     __syncthreads();
     if (group * SHARES + share > 0) return;
-    float *stage = &lds[0][0][0] + __builtin_amdgcn_readfirstlane(tile) * (32 * 36);
+    float *stage = space + __builtin_amdgcn_readfirstlane(tile) * (32 * 36);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -146,6 +149,31 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
                 epilogue(g, m0 + wm + i * 32 + r + lane / 8, n0 + wn + j * 32 + lane % 8 * 4, load4(stage + (r + lane / 8) * 36 + lane % 8 * 4));
             wave_order();
         }
+}
+
+template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
+__global__ void __launch_bounds__(256 * GROUPS)
+gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
+                int64_t sb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
+{
+    __shared__ __align__(16) float space[space_f32<BM, BN, STEP, GROUPS>()];
+    gemm_f32_block<T, BM, BN, STEP, GROUPS, AK, BK>(M, N, K, A, lda, sa, B, ldb, sb, mblocks, nblocks, epilogue, blockIdx.x, space);
+}
+
+// Two products in one launch, the first with both contraction indices near and the second with both row indices near (a layer's dx and dw).  Workgroups from
+// `both` on do `extra`, which depends on neither.
+template <class Epilogue> struct ProductF32 { int64_t M, N, K; const float *A, *B; int64_t lda, sa, ldb, sb; uint32_t mblocks, nblocks; Epilogue epilogue; };
+template <int BM, int STEP, int GROUPS, class Epilogue, class Extra>
+__global__ void __launch_bounds__(256 * GROUPS) gemm_f32_pair_kernel(ProductF32<Epilogue> p, ProductF32<Epilogue> q, uint32_t first, uint32_t both, Extra extra)
+{
+    __shared__ __align__(16) float space[space_f32<BM, BM, STEP, GROUPS>()];
+    if (blockIdx.x < first)
+        gemm_f32_block<float, BM, BM, STEP, GROUPS, true, true>(p.M, p.N, p.K, p.A, p.lda, p.sa, p.B, p.ldb, p.sb, p.mblocks, p.nblocks, p.epilogue, blockIdx.x, space);
+    else if (blockIdx.x < both)
+        gemm_f32_block<float, BM, BM, STEP, GROUPS, false, false>(q.M, q.N, q.K, q.A, q.lda, q.sa, q.B, q.ldb, q.sb, q.mblocks, q.nblocks, q.epilogue, blockIdx.x - first,
+                                                                 space);
+    else
+        extra(blockIdx.x - both, space);
 }
 
 template <typename T, int BM, int BN, int STEP, int GROUPS, class Epilogue>

@@ -312,6 +312,83 @@ static void launch_product32(hipStream_t s, int64_t batch, int64_t M, int64_t N,
     });
 }
 
+// out [rows][cols] alone
+template <typename T> static LinearEpilogue<T> plain_epilogue(int64_t rows, int64_t cols, void *out, int64_t ld, int64_t step)
+{
+    return LinearEpilogue<T>{rows, cols, nullptr, nullptr, (T *)out, nullptr, 0, ld, 0, 0, 0, step, 0, ACT_NONE};
+}
+
+// ---- db --------------------------------------------------------------------------------------------------------------
+
+// Column sums of dz from those of runs of rows: 64 columns per workgroup; four waves take the runs in turn, then their sums are added in order.
+template <typename T> struct BiasSum {
+    int64_t batch, cols, parts; const float *sums; T *db; int64_t sdb;
+    __host__ __device__ uint32_t across() const { return (uint32_t)((cols + 63) / 64); }
+    uint32_t blocks() const { return db ? (uint32_t)batch * across() : 0; }
+    __device__ __forceinline__ void operator()(uint32_t id, float *space) const
+    {
+        const int wave = threadIdx.x >> 6, at = threadIdx.x & 63;
+        const int64_t g = id / across(), n = (int64_t)(id % across()) * 64 + at;
+        if (wave < 4) {
+            float sum = 0.0f;
+            if (n < cols)
+#pragma unroll 8
+                for (int64_t k = wave; k < parts; k += 4) sum += sums[(g * parts + k) * cols + n];
+            space[wave * 64 + at] = sum;
+        }
+        __syncthreads();
+        if (wave == 0 && n < cols) store_value(db + g * sdb + n, (space[at] + space[64 + at]) + (space[128 + at] + space[192 + at]));
+    }
+};
+template <typename T> __global__ void __launch_bounds__(256) bias_sum_kernel(BiasSum<T> b)
+{
+    __shared__ float space[256];
+    b(blockIdx.x, space);
+}
+
+// ---- dx and dw in one launch -----------------------------------------------------------------------------------------
+
+// dx = d w^T, dw = x^T d and db where neither product would fill the card alone, or false.
+static bool launch_pair16(hipStream_t s, const LinearGradArgs &a, const Planes16 &d, const Planes16 &w, const Planes16 &x, const BiasSum<uint16_t> &bias)
+{
+    if (a.rows <= FEW_ROWS && a.dout > 1024) return false;         // dx from few_rows_kernel: a long chain of steps otherwise
+    const Plan16 px = plan16(a.batch, a.rows, a.din, a.dout), pw = plan16(a.batch, a.din, a.dout, a.rows);
+    if (px.block == 256 || pw.block == 256 || px.splits > 1 || pw.splits > 1) return false;
+    const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
+    const auto both = [&](int64_t b) { return blocks(b, a.rows, a.din) + blocks(b, a.din, a.dout); };
+    const auto go = [&](auto f) {
+        const auto product = [&](int64_t M, int64_t N, int64_t K, const Planes16 &l, const Planes16 &r, void *out, int64_t ld, int64_t step) {
+            return Product16<LinearEpilogue<uint16_t>>{M, N, K, l, r, (uint32_t)((M + f.BM - 1) / f.BM), (uint32_t)((N + f.BM - 1) / f.BM), plain_epilogue<uint16_t>(M, N, out, ld, step)};
+        };
+        const uint32_t first = (uint32_t)blocks(f.BM, a.rows, a.din), all = (uint32_t)both(f.BM);
+        gemm16_pair_kernel<bf16x8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS><<<all + bias.blocks(), f.WM * f.WN * 64 * f.GROUPS, 0, s>>>(
+            product(a.rows, a.din, a.dout, d, w, a.dx, a.lddx, a.sdx), product(a.din, a.dout, a.rows, x, d, a.dw, a.lddw, a.sdw), first, all, bias);
+    };
+    if (both(128) >= 512) go(Shape<128, 128, 2, 2, 64, 2>());
+    else if (both(128) >= 128) go(Shape<128, 128, 2, 4, 64, 4>());
+    else if (both(64) > 256 || (a.dout < 512 && a.rows < 512)) go(Shape<64, 64, 2, 2, 64, 4>());
+    else go(Shape<64, 64, 2, 2, 64, 4, 2>());
+    return true;
+}
+
+static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d, int64_t ldd, int64_t sd, const BiasSum<float> &bias)
+{
+    const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
+    if (as_planes(a.batch, a.rows, a.din, a.dout) || as_planes(a.batch, a.din, a.dout, a.rows)) return false;
+    if ((blocks(128, a.rows, a.din) >= 256 && a.dout >= 256) || (blocks(128, a.din, a.dout) >= 256 && a.rows >= 256)) return false;
+    const auto product = [&](int64_t M, int64_t N, int64_t K, const void *l, int64_t ldl, int64_t sl, const void *r, int64_t ldr, int64_t sr, void *out, int64_t ld, int64_t step) {
+        return ProductF32<LinearEpilogue<float>>{M, N, K, (const float *)l, (const float *)r, ldl, sl, ldr, sr, (uint32_t)((M + 63) / 64), (uint32_t)((N + 63) / 64),
+                                                 plain_epilogue<float>(M, N, out, ld, step)};
+    };
+    const auto p = product(a.rows, a.din, a.dout, d, ldd, sd, a.w, a.ldw, a.sw, a.dx, a.lddx, a.sdx);
+    const auto q = product(a.din, a.dout, a.rows, a.x, a.ldx, a.sx, d, ldd, sd, a.dw, a.lddw, a.sdw);
+    const uint32_t first = (uint32_t)blocks(64, a.rows, a.din), all = first + (uint32_t)blocks(64, a.din, a.dout);
+    if (all >= 768) gemm_f32_pair_kernel<64, 32, 1><<<all + bias.blocks(), 256, 0, s>>>(p, q, first, all, bias);
+    else if (all >= 384) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, bias);
+    else gemm_f32_pair_kernel<64, 32, 4><<<all + bias.blocks(), 1024, 0, s>>>(p, q, first, all, bias);
+    return true;
+}
+
 // ---- dz and db -------------------------------------------------------------------------------------------------------
 
 // A workgroup takes `run` rows of SLOPE_COLS columns, a wave every fourth row, a lane 16 bytes: dz, and the column sums of dz (before its rounding) over
@@ -382,34 +459,12 @@ slope_kernel(int64_t rows, int64_t cols, int run, const T *__restrict__ dy, int6
         sums[((int64_t)g * gridDim.y + blockIdx.y) * cols + (int64_t)blockIdx.x * COLS + c] = (part[0][c] + part[1][c]) + (part[2][c] + part[3][c]);
 }
 
-// 64 columns per workgroup; four waves take the parts in turn, then their sums are added in order.
-template <typename T>
-__global__ void __launch_bounds__(256) bias_sum_kernel(int64_t cols, int64_t parts, const float *__restrict__ sums, T *__restrict__ db, int64_t sdb)
-{
-    __shared__ float part[4][64];
-    const int wave = threadIdx.x >> 6, at = threadIdx.x & 63;
-    const int64_t g = blockIdx.y, n = (int64_t)blockIdx.x * 64 + at;
-    float sum = 0.0f;
-    if (n < cols)
-#pragma unroll 8
-        for (int64_t k = wave; k < parts; k += 4) sum += sums[(g * parts + k) * cols + n];
-    part[wave][at] = sum;
-    __syncthreads();
-    if (wave == 0 && n < cols) store_value(db + g * sdb + n, (part[0][at] + part[1][at]) + (part[2][at] + part[3][at]));
-}
-
 // ---- launchers -------------------------------------------------------------------------------------------------------
 
 template <typename T> static LinearEpilogue<T> forward_epilogue(const LinearArgs &a)
 {
     return LinearEpilogue<T>{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz, a.sb, a.sr, a.sy, a.sz, a.act};
 }
-// out [rows][cols] alone
-template <typename T> static LinearEpilogue<T> plain_epilogue(int64_t rows, int64_t cols, void *out, int64_t ld, int64_t step)
-{
-    return LinearEpilogue<T>{rows, cols, nullptr, nullptr, (T *)out, nullptr, 0, ld, 0, 0, 0, step, 0, ACT_NONE};
-}
-
 static FloatSource float_source(const void *p, int64_t ld, int64_t step, int64_t rows, int64_t cols, bool near) { return FloatSource{p, ld, step, rows, cols, near}; }
 
 int64_t linear_workspace(const LinearArgs &a)
@@ -461,14 +516,19 @@ int64_t linear_grad_workspace(const LinearGradArgs &a)
     return n + Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + (dx > dw ? dx : dw);
 }
 
-template <typename T> static void launch_slopes(hipStream_t s, const LinearGradArgs &a, T *dz, float *sums)
+template <typename T> static void launch_bias(hipStream_t s, const BiasSum<T> &b)
+{
+    if (b.blocks()) bias_sum_kernel<T><<<b.blocks(), 256, 0, s>>>(b);
+}
+
+// dz, and what is left to do for db.
+template <typename T> static BiasSum<T> launch_slopes(hipStream_t s, const LinearGradArgs &a, T *dz, float *sums)
 {
     if ((dz || a.db) && a.rows > 0)
         slope_kernel<T><<<dim3((uint32_t)((dz_wide(a) + SLOPE_COLS<T> - 1) / SLOPE_COLS<T>), (uint32_t)sum_parts(a), (uint32_t)a.batch), 256, 0, s>>>(
             a.rows, a.dout, slope_run(a), (const T *)a.dy, a.lddy, a.sdy, (const T *)a.z, a.ldz, a.sz, a.act, dz,
             dz_wide(a), a.db ? sums : nullptr);
-    if (a.db)
-        bias_sum_kernel<T><<<dim3((uint32_t)((a.dout + 63) / 64), (uint32_t)a.batch), 256, 0, s>>>(a.dout, sum_parts(a), sums, (T *)a.db, a.sdb);
+    return BiasSum<T>{a.batch, a.dout, sum_parts(a), sums, (T *)a.db, a.sdb};
 }
 
 void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
@@ -482,9 +542,11 @@ void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
         at += round_up(a.batch * a.rows * dz_wide(a) * (a.bf16 ? 2 : 4), 256);
     }
     if (!a.bf16) {
-        launch_slopes<float>(s, a, (float *)dz, sums);
+        const BiasSum<float> bias = launch_slopes<float>(s, a, (float *)dz, sums);
         const void *d = dz ? dz : a.dy;
         const int64_t ldd = dz ? a.dout : a.lddy, sd = dz ? (a.batch > 1 ? a.rows * a.dout : 0) : a.sdy;
+        if (a.dx && a.dw && a.rows > 0 && launch_pair32(s, a, d, ldd, sd, bias)) return;
+        launch_bias(s, bias);
         if (a.dx && a.rows > 0)
             launch_product32(s, a.batch, a.rows, a.din, a.dout, float_source(d, ldd, sd, a.rows, a.dout, true), float_source(a.w, a.ldw, a.sw, a.din, a.dout, true),
                              plain_epilogue<float>(a.rows, a.din, a.dx, a.lddx, a.sdx), at);
@@ -493,13 +555,15 @@ void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
                              plain_epilogue<float>(a.din, a.dout, a.dw, a.lddw, a.sdw), at);
         return;
     }
-    launch_slopes<uint16_t>(s, a, (uint16_t *)dz, sums);
+    const BiasSum<uint16_t> bias = launch_slopes<uint16_t>(s, a, (uint16_t *)dz, sums);
     Layouts l{};
     const Planes16 d = dz ? Planes16{(const char *)dz, nullptr, dz_wide(a), a.rows * dz_wide(a)} : Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).take(a.batch, at, l);
     Planes16 w{}, x{};
     if (a.dx && a.rows > 0) w = Source(a.w, a.ldw, a.sw, a.din, a.dout).take(a.batch, at, l);
     if (a.dw) x = Source(a.x, a.ldx, a.sx, a.rows, a.din).take(a.batch, at, l);
     lay_out(s, l);
+    if (a.dx && a.dw && a.rows > 0 && launch_pair16(s, a, d, w, x, bias)) return;
+    launch_bias(s, bias);
     if (a.dx && a.rows > 0)
         launch_product16(s, a.batch, a.rows, a.din, a.dout, d, true, w, true, plain_epilogue<uint16_t>(a.rows, a.din, a.dx, a.lddx, a.sdx), at);
     if (a.dw)
