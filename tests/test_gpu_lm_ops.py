@@ -571,6 +571,53 @@ def test_losses_of_nothing():
     assert float(loss[0]) == pytest.approx(math.log(2)) and bool((ratio == 0).all()) and grad.shape == (0, 10)
 
 
+# ---- far apart in memory -----------------------------------------------------------------------------------------------
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes and 2^31 values in one operand: the last rows are as those of a call of their own."""
+    g = gen(13)
+    z = torch.randn(17000, 131072, generator=g, device="cuda", dtype=BF16)
+    labels = torch.randint(0, 131072, (17000,), generator=g, device="cuda", dtype=torch.int32)
+    old, adv, w = torch.full((17000,), -12.0, device="cuda"), torch.ones(17000, device="cuda"), torch.ones(17000, device="cuda")
+    w[:-3] = 0.0
+    last = nm.netmax_policy_loss(z[-3:].clone(), labels[-3:].clone(), old[-3:].clone(), adv[-3:].clone(), w[-3:].clone())
+    loss, logp, grad = nm.netmax_policy_loss(z, labels, old, adv, w, grad=z)
+    assert torch.equal(loss[-3:], last[0]) and torch.equal(logp[-3:], last[1]) and torch.equal(grad[-3:], last[2]) and not bool(grad[0].any())
+    del z, grad
+    x, wt = torch.randn(600_000, 4104, generator=g, device="cuda", dtype=BF16), normal(g, 4104, 72, dtype=BF16)
+    y = nm.netmax_linear(x, wt)
+    within(y[-300:], x[-300:].double() @ wt.double(), 4108 * 2.0 ** -24 * (x[-300:].double().abs() @ wt.double().abs()) + 2.0 ** -8 * y[-300:].double().abs() * 1.01, "y")
+    dy = torch.zeros(600_000, 72, device="cuda", dtype=BF16)
+    dy[-200:] = normal(g, 200, 72, dtype=BF16)
+    dx, dw, db = nm.netmax_linear_grad(dy, x, wt)
+    a, b = x[-200:].double(), dy[-200:].double()
+    within(dw, a.t() @ b, 204 * 2.0 ** -24 * (a.abs().t() @ b.abs()) + 2.0 ** -8 * (a.t() @ b).abs(), "dw")
+    within(dx[-200:], b @ wt.double().t(), 76 * 2.0 ** -24 * (b.abs() @ wt.double().abs().t()) + 2.0 ** -8 * (b @ wt.double().t()).abs(), "dx")
+    assert not bool(dx[:-200].any())
+    del x, y, dx
+    m = torch.randn(520, 2056, 2056, generator=g, device="cuda", dtype=BF16)
+    alone = nm.netmax_orthogonalize(m[-2:].clone())
+    assert off(nm.netmax_orthogonalize(m, out=m)[-2:], alone.double()) < ORTH_TOL[BF16]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_the_same_bits_every_time(dtype):
+    g = gen(14)
+    x, w, b, dy = normal(g, 5000, 300, dtype=dtype), normal(g, 300, 130, dtype=dtype), normal(g, 130, dtype=dtype), normal(g, 5000, 130, dtype=dtype)
+    a = gradient_like(g, 3, 500, 333, dtype)
+    z, labels = logits_and_labels(g, 600, 3001, dtype)
+    offsets, ref = torch.tensor([0, 250, 600], dtype=torch.int32, device="cuda"), torch.full((600,), -8.0, device="cuda")
+
+    def work():
+        y, pre = nm.netmax_linear(x, w, b, act="gelu", keep_preact=True)
+        return [y, *nm.netmax_linear_grad(dy, x, w, pre, act="gelu"), nm.netmax_orthogonalize(a), *nm.netmax_policy_loss(z, labels, ref, ref, ref_logp=ref, kl=0.1),
+                *nm.netmax_preference_loss(z, labels, offsets, None, ref)]
+
+    first = work()
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(first, work()))
+
+
 # ---- streams and refusals --------------------------------------------------------------------------------------------
 
 def test_operators_on_another_stream():
