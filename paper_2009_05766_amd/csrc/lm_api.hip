@@ -47,7 +47,8 @@ static int check_linear(const netmax_linear_shape *s)
     return NETMAX_OK;
 }
 
-static int check_matrix(const char *name, const void *p, bool needed, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t step)
+// `written`: results of a batch need a place each.
+static int check_matrix(const char *name, const void *p, bool needed, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t step, bool written = false)
 {
     char buf[160];
     if (!p) {
@@ -55,8 +56,8 @@ static int check_matrix(const char *name, const void *p, bool needed, int32_t dt
         snprintf(buf, sizeof buf, "%s is NULL", name);
         return netmax_fail(NETMAX_EINVAL, buf);
     }
-    if (aligned(p, dtype) && strides_ok(batch, rows, cols, ld, step)) return NETMAX_OK;
-    snprintf(buf, sizeof buf, "%s: misaligned, or rows closer together than they are long, or a negative stride", name);
+    if (aligned(p, dtype) && strides_ok(batch, rows, cols, ld, step) && !(written && batch > 1 && step == 0)) return NETMAX_OK;
+    snprintf(buf, sizeof buf, "%s: misaligned, or rows closer together than they are long, or a negative stride, or results in the same place", name);
     return netmax_fail(NETMAX_EINVAL, buf);
 }
 
@@ -97,8 +98,8 @@ extern "C" int netmax_linear(const netmax_linear_shape *s, const void *x, const 
     TRY(check_matrix("w", w, true, d, s->batch, s->d_in, s->d_out, s->ldw, s->sw));
     TRY(check_matrix("bias", bias, false, d, s->batch, 1, s->d_out, s->d_out, s->sb));
     TRY(check_matrix("residual", residual, false, d, s->batch, s->rows, s->d_out, s->ldr, s->sr));
-    TRY(check_matrix("y", y, true, d, s->batch, s->rows, s->d_out, s->ldy, s->sy));
-    TRY(check_matrix("z", z, false, d, s->batch, s->rows, s->d_out, s->ldz, s->sz));
+    TRY(check_matrix("y", y, true, d, s->batch, s->rows, s->d_out, s->ldy, s->sy, true));
+    TRY(check_matrix("z", z, false, d, s->batch, s->rows, s->d_out, s->ldz, s->sz, true));
     LinearArgs a = linear_args(s);
     a.x = x; a.w = w; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
     TRY(check_work(work, work_bytes, linear_workspace(a)));
@@ -134,9 +135,9 @@ extern "C" int netmax_linear_grad(const netmax_linear_shape *s, const void *dy, 
     TRY(check_matrix("x", x, any && dw, d, s->batch, s->rows, s->d_in, s->ldx, s->sx));
     TRY(check_matrix("w", w, any && dx, d, s->batch, s->d_in, s->d_out, s->ldw, s->sw));
     TRY(check_matrix("z", z, any && s->act != NETMAX_ACT_NONE, d, s->batch, s->rows, s->d_out, s->ldz, s->sz));
-    TRY(check_matrix("dx", dx, false, d, s->batch, s->rows, s->d_in, s->lddx, s->sdx));
-    TRY(check_matrix("dw", dw, false, d, s->batch, s->d_in, s->d_out, s->lddw, s->sdw));
-    TRY(check_matrix("db", db, false, d, s->batch, 1, s->d_out, s->d_out, s->sdb));
+    TRY(check_matrix("dx", dx, false, d, s->batch, s->rows, s->d_in, s->lddx, s->sdx, true));
+    TRY(check_matrix("dw", dw, false, d, s->batch, s->d_in, s->d_out, s->lddw, s->sdw, true));
+    TRY(check_matrix("db", db, false, d, s->batch, 1, s->d_out, s->d_out, s->sdb, true));
     LinearGradArgs a = linear_grad_args(s);
     a.dy = dy; a.x = x; a.w = w; a.z = z; a.dx = dx; a.dw = dw; a.db = db;
     TRY(check_work(work, work_bytes, linear_grad_workspace(a)));
@@ -179,8 +180,8 @@ extern "C" int netmax_orthogonalize(const netmax_orth_shape *s, const void *g, c
     if (s->batch == 0) return NETMAX_OK;
     TRY(check_matrix("g", g, true, s->dtype, s->batch, s->rows, s->cols, s->ldg, s->sg));
     TRY(check_matrix("m", m, m_out != nullptr, NETMAX_F32, s->batch, s->rows, s->cols, s->ldm, s->sm));
-    TRY(check_matrix("m_out", m_out, m != nullptr, NETMAX_F32, s->batch, s->rows, s->cols, s->ldm, s->sm));
-    TRY(check_matrix("out", out, true, s->dtype, s->batch, s->rows, s->cols, s->ldo, s->so));
+    TRY(check_matrix("m_out", m_out, m != nullptr, NETMAX_F32, s->batch, s->rows, s->cols, s->ldm, s->sm, true));
+    TRY(check_matrix("out", out, true, s->dtype, s->batch, s->rows, s->cols, s->ldo, s->so, true));
     OrthArgs a = orth_args(s);
     a.g = g; a.m = m; a.m_out = m_out; a.out = out;
     TRY(check_work(work, work_bytes, orth_workspace(a)));

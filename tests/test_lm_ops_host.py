@@ -24,7 +24,7 @@ def refused(rc, text):
 @pytest.mark.parametrize("kw,text", [
     (dict(batch=-1), "batch"), (dict(batch=65536), "batch"), (dict(rows=-1), "rows"), (dict(d_in=0), "d_in"), (dict(d_out=0), "d_out"), (dict(d_in=1 << 22), "d_in"),
     (dict(rows=1 << 40), "too large"), (dict(rows=65535 * 64 + 1), "too large"), (dict(dtype=7), "dtype"), (dict(act=9), "activation"), (dict(act=-1), "activation"),
-    (dict(ldx=15), "x:"), (dict(ldw=23), "w:"), (dict(ldy=23), "y:"), (dict(ldr=1), "residual:"), (dict(ldz=0), "z:"), (dict(batch=2, sx=-8), "x:"), (dict(ldx=-16), "x:"),
+    (dict(batch=2, sx=128, sr=192, sz=192), "y:"), (dict(batch=2, sy=192), "z:"), (dict(ldx=15), "x:"), (dict(ldw=23), "w:"), (dict(ldy=23), "y:"), (dict(ldr=1), "residual:"), (dict(ldz=0), "z:"), (dict(batch=2, sx=-8), "x:"), (dict(ldx=-16), "x:"),
 ])
 def test_linear_refuses(kw, text):
     lib, s = nm.load(), linear_shape(**kw)
