@@ -215,11 +215,20 @@ __device__ __forceinline__ double label_logp(float zy, const Partial &r)
     return (double)zy - (double)r.top - log((double)r.sum);
 }
 
+// A workgroup per row (or pair): threads along a dimension of a launch have to be fewer than 2^32, so many rows take two.
+static dim3 grid_of(int64_t rows)
+{
+    constexpr int64_t ACROSS = 1 << 21;
+    return dim3((uint32_t)(rows < ACROSS ? rows : ACROSS), (uint32_t)((rows + ACROSS - 1) / ACROSS));
+}
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // PIECES = 0: the row is read twice.
 template <typename T, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) policy_loss_kernel(TokenRows rows, PolicyArgs a)
 {
-    const int64_t t = blockIdx.x;
+    const int64_t t = workgroup();
+    if (t >= rows.tokens) return;
     const Row<T> z((const T *)rows.logits + t * rows.ld, rows.vocab), out((T *)a.grad + t * a.ldg, rows.vocab);
     float w;
     int label;
@@ -264,7 +273,8 @@ __global__ void __launch_bounds__(THREADS) policy_loss_kernel(TokenRows rows, Po
 template <typename T, int THREADS, int PIECES>
 __global__ void __launch_bounds__(THREADS) preference_rows_kernel(TokenRows rows, PreferenceArgs a)
 {
-    const int64_t t = blockIdx.x;
+    const int64_t t = workgroup();
+    if (t >= rows.tokens) return;
     const Row<T> z((const T *)rows.logits + t * rows.ld, rows.vocab);
     float w;
     int label;
@@ -296,9 +306,11 @@ __device__ __forceinline__ void sequence_rows(const int32_t *offsets, int64_t q,
 __global__ void __launch_bounds__(PAIR_THREADS) preference_pairs_kernel(int64_t tokens, PreferenceArgs a)
 {
     __shared__ double part[2][PAIR_THREADS];
+    const int64_t p = workgroup();
+    if (p >= a.pairs) return;
     for (int side = 0; side < 2; ++side) {
         int64_t first, end;
-        sequence_rows(a.offsets, 2 * (int64_t)blockIdx.x + side, tokens, first, end);
+        sequence_rows(a.offsets, 2 * p + side, tokens, first, end);
         double sum = 0.0;
         for (int64_t t = first + threadIdx.x; t < end; t += PAIR_THREADS) sum += a.terms[t];
         part[side][threadIdx.x] = sum;
@@ -310,7 +322,6 @@ __global__ void __launch_bounds__(PAIR_THREADS) preference_pairs_kernel(int64_t 
         __syncthreads();
     }
     if (threadIdx.x != 0) return;
-    const int64_t p = blockIdx.x;
     const double e = a.smoothing, h = (double)a.beta * (part[0][0] - part[1][0]), tail = log1p(exp(-fabs(h)));
     const double below = tail + (h < 0.0 ? -h : 0.0), above = tail + (h > 0.0 ? h : 0.0);       // -log sigma(h), -log sigma(-h)
     const double dh = h >= 0.0 ? e - exp(-h) / (1.0 + exp(-h)) : exp(h) / (1.0 + exp(h)) - (1.0 - e);
@@ -325,7 +336,8 @@ __global__ void __launch_bounds__(PAIR_THREADS) preference_pairs_kernel(int64_t 
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) preference_gradient_kernel(TokenRows rows, PreferenceArgs a)
 {
-    const int64_t t = rows.tokens - 1 - blockIdx.x;
+    const int64_t t = rows.tokens - 1 - workgroup();
+    if (t < 0) return;
     const Row<T> z((const T *)rows.logits + t * rows.ld, rows.vocab), out((T *)a.grad + t * a.ldg, rows.vocab);
     float w;
     int label;
@@ -360,7 +372,7 @@ template <typename T, class Go> static void with_row(int64_t vocab, const Go &go
 template <typename T> static void policy_of(hipStream_t s, const TokenRows &rows, const PolicyArgs &a)
 {
     with_row<T>(rows.vocab, [&](auto threads, auto pieces) {
-        policy_loss_kernel<T, threads(), pieces()><<<(uint32_t)rows.tokens, threads(), 0, s>>>(rows, a);
+        policy_loss_kernel<T, threads(), pieces()><<<grid_of(rows.tokens), threads(), 0, s>>>(rows, a);
     });
 }
 
@@ -374,9 +386,9 @@ void launch_policy_loss(hipStream_t s, const TokenRows &rows, const PolicyArgs &
 template <typename T> static void preference_of(hipStream_t s, const TokenRows &rows, const PreferenceArgs &a)
 {
     with_row<T>(rows.vocab, [&](auto threads, auto pieces) {
-        if (rows.tokens > 0) preference_rows_kernel<T, threads(), pieces()><<<(uint32_t)rows.tokens, threads(), 0, s>>>(rows, a);
-        preference_pairs_kernel<<<(uint32_t)a.pairs, PAIR_THREADS, 0, s>>>(rows.tokens, a);
-        if (rows.tokens > 0 && a.grad) preference_gradient_kernel<T, threads() < 512 ? 256 : 512><<<(uint32_t)rows.tokens, threads() < 512 ? 256 : 512, 0, s>>>(rows, a);
+        if (rows.tokens > 0) preference_rows_kernel<T, threads(), pieces()><<<grid_of(rows.tokens), threads(), 0, s>>>(rows, a);
+        preference_pairs_kernel<<<grid_of(a.pairs), PAIR_THREADS, 0, s>>>(rows.tokens, a);
+        if (rows.tokens > 0 && a.grad) preference_gradient_kernel<T, threads() < 512 ? 256 : 512><<<grid_of(rows.tokens), threads() < 512 ? 256 : 512, 0, s>>>(rows, a);
     });
 }
 

@@ -601,6 +601,23 @@ def test_offsets_past_32_bits():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_many_tokens(dtype):
+    """More rows than a launch has threads along one dimension for: parts of them give what calls of their own give."""
+    g, n = gen(19), 16_800_002
+    z, labels = normal(g, n, 3, dtype=dtype), torch.randint(0, 3, (n,), generator=g, device="cuda", dtype=torch.int32)
+    old, adv, w = normal(g, n) - 1.0, normal(g, n), torch.ones(n, device="cuda")
+    got = nm.netmax_policy_loss(z, labels, old, adv, w)
+    parts = [slice(0, 1000), slice((1 << 21) - 500, (1 << 21) + 500), slice(n - 1000, n)]
+    for p in parts:
+        for a, b in zip(got, nm.netmax_policy_loss(*(v[p].clone() for v in (z, labels, old, adv, w)))):
+            assert torch.equal(a[p], b)
+    loss, ratio, grad = nm.netmax_preference_loss(z, labels, torch.arange(n + 1, device="cuda", dtype=torch.int32), w, old, scale=1.0)
+    for p in parts:
+        alone = nm.netmax_preference_loss(z[p].clone(), labels[p].clone(), torch.arange(1001, device="cuda", dtype=torch.int32), w[p].clone(), old[p].clone(), scale=1.0)
+        assert torch.equal(loss[p.start // 2:p.stop // 2], alone[0]) and torch.equal(ratio[p], alone[1]) and torch.equal(grad[p], alone[2])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_the_same_bits_every_time(dtype):
     g = gen(14)
     x, w, b, dy = normal(g, 5000, 300, dtype=dtype), normal(g, 300, 130, dtype=dtype), normal(g, 130, dtype=dtype), normal(g, 5000, 130, dtype=dtype)
