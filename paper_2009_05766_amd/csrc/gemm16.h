@@ -330,17 +330,17 @@ gemm16_kernel(int64_t M, int64_t N, int64_t K, Planes16 A, Planes16 B, uint32_t 
 template <class Epilogue> struct Product16 { int64_t M, N, K; Planes16 A, B; uint32_t mblocks, nblocks; Epilogue epilogue; };
 template <typename V, int BM, int WAVES_M, int WAVES_N, int STEP, int STAGES, int GROUPS, class Epilogue, class Extra>
 __global__ void __launch_bounds__(WAVES_M * WAVES_N * 64 * GROUPS)
-gemm16_pair_kernel(Product16<Epilogue> p, Product16<Epilogue> q, uint32_t first, uint32_t both, Extra extra)
+gemm16_pair_kernel(Product16<Epilogue> p, Product16<Epilogue> q, uint32_t first, uint32_t both, int swap, Extra extra)
 {
     __shared__ __align__(16) char space[space16<BM, BM, STEP, STAGES, GROUPS, false>()];
-    if (blockIdx.x < first)
-        gemm16_block<V, BM, BM, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, true, true, false, false>(p.M, p.N, p.K, p.A, p.B, p.mblocks, p.nblocks, 1, p.epilogue, blockIdx.x,
-                                                                                                 first, space);
-    else if (blockIdx.x < both)
+    const uint32_t id = pair_place(blockIdx.x, first, both, swap);
+    if (id < first)
+        gemm16_block<V, BM, BM, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, true, true, false, false>(p.M, p.N, p.K, p.A, p.B, p.mblocks, p.nblocks, 1, p.epilogue, id, first, space);
+    else if (id < both)
         gemm16_block<V, BM, BM, WAVES_M, WAVES_N, STEP, STAGES, GROUPS, false, false, false, false>(q.M, q.N, q.K, q.A, q.B, q.mblocks, q.nblocks, 1, q.epilogue,
-                                                                                                   blockIdx.x - first, both - first, space);
+                                                                                                   id - first, both - first, space);
     else
-        extra(blockIdx.x - both, reinterpret_cast<float *>(space));
+        extra(id - both, reinterpret_cast<float *>(space));
 }
 
 // C = A B for few rows, at most 32 TM: the weights are what has to be read.  A workgroup has 32 columns; its eight waves take steps of 32 indices in turn,

@@ -164,16 +164,17 @@ gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_
 // `both` on do `extra`, which depends on neither.
 template <class Epilogue> struct ProductF32 { int64_t M, N, K; const float *A, *B; int64_t lda, sa, ldb, sb; uint32_t mblocks, nblocks; Epilogue epilogue; };
 template <int BM, int STEP, int GROUPS, class Epilogue, class Extra>
-__global__ void __launch_bounds__(256 * GROUPS) gemm_f32_pair_kernel(ProductF32<Epilogue> p, ProductF32<Epilogue> q, uint32_t first, uint32_t both, Extra extra)
+__global__ void __launch_bounds__(256 * GROUPS) gemm_f32_pair_kernel(ProductF32<Epilogue> p, ProductF32<Epilogue> q, uint32_t first, uint32_t both, int swap,
+                                                                         Extra extra)
 {
     __shared__ __align__(16) float space[space_f32<BM, BM, STEP, GROUPS>()];
-    if (blockIdx.x < first)
-        gemm_f32_block<float, BM, BM, STEP, GROUPS, true, true>(p.M, p.N, p.K, p.A, p.lda, p.sa, p.B, p.ldb, p.sb, p.mblocks, p.nblocks, p.epilogue, blockIdx.x, space);
-    else if (blockIdx.x < both)
-        gemm_f32_block<float, BM, BM, STEP, GROUPS, false, false>(q.M, q.N, q.K, q.A, q.lda, q.sa, q.B, q.ldb, q.sb, q.mblocks, q.nblocks, q.epilogue, blockIdx.x - first,
-                                                                 space);
+    const uint32_t id = pair_place(blockIdx.x, first, both, swap);
+    if (id < first)
+        gemm_f32_block<float, BM, BM, STEP, GROUPS, true, true>(p.M, p.N, p.K, p.A, p.lda, p.sa, p.B, p.ldb, p.sb, p.mblocks, p.nblocks, p.epilogue, id, space);
+    else if (id < both)
+        gemm_f32_block<float, BM, BM, STEP, GROUPS, false, false>(q.M, q.N, q.K, q.A, q.lda, q.sa, q.B, q.ldb, q.sb, q.mblocks, q.nblocks, q.epilogue, id - first, space);
     else
-        extra(blockIdx.x - both, space);
+        extra(id - both, space);
 }
 
 template <typename T, int BM, int BN, int STEP, int GROUPS, class Epilogue>
@@ -197,7 +198,7 @@ void launch_gemm_f32(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t
 {
     const auto blocks = [&](int64_t m, int64_t n) { return batch * ((M + m - 1) / m) * ((N + n - 1) / n); };
     // blocks of 128 where they are many and the contraction pays for their start; the fewer blocks, the more waves on each
-    if (blocks(128, 128) >= 256 && K >= 256) launch_gemm_f32_blocks<T, 128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
+    if (blocks(128, 128) >= 256 && K >= 256 && worth_blocks(128, M, N)) launch_gemm_f32_blocks<T, 128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
     else if (blocks(64, 64) >= 512) launch_gemm_f32_blocks<T, 64, 64, 32, 1>(s, batch, M, N, K, a, b, epilogue);
     else if (blocks(64, 64) > 128) launch_gemm_f32_blocks<T, 64, 64, 32, 4>(s, batch, M, N, K, a, b, epilogue);
     else launch_gemm_f32_blocks<T, 64, 32, 32, 4>(s, batch, M, N, K, a, b, epilogue);

@@ -38,13 +38,14 @@ __device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v
 // One launch for every block shape: `go` gets it as BM, BN, waves, step, stages and groups of gemm16_kernel.
 template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_, int GROUPS_ = 1>
 struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_, GROUPS = GROUPS_; };
-template <bool SPLIT, class Blocks, class Go> static void with_small_shape(int64_t K, const Blocks &blocks, const Go &go)
+template <bool SPLIT, class Blocks, class Go> static void with_small_shape(int64_t M, int64_t N, int64_t K, const Blocks &blocks, const Go &go)
 {
     // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has (1 x 2660 x 512, X^T X:
     // 17.3 us in one group of waves, 15.1 in two; short contractions lose by the join)
-    if (SPLIT && blocks(256) >= 128) go(Shape<256, 128, 4, 2, 32, 3>());
-    else if (blocks(128) >= 512) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
-    else if (blocks(128) >= 128) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
+    const bool far = worth_blocks(128, M, N);
+    if (SPLIT && blocks(256) >= 128 && far && worth_blocks(256, M, N)) go(Shape<256, 128, 4, 2, 32, 3>());
+    else if (blocks(128) >= 512 && far) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    else if (blocks(128) >= 128 && far) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
     else if (blocks(64) > 256 || K < 512) go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
     else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4, 2>());
 }

@@ -96,8 +96,8 @@ static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
 {
     const auto blocks = [&](int64_t b) { return batch * ((M + b - 1) / b) * ((N + b - 1) / b); };
     const int64_t steps = (K + 63) / 64;
-    if (blocks(256) >= 192) return {256, 1};
-    const int block = blocks(128) >= 96 && M > 64 && N > 64 ? 128 : 64;
+    if (blocks(256) >= 192 && worth_blocks(256, M, N)) return {256, 1};
+    const int block = blocks(128) >= 96 && worth_blocks(128, M, N) ? 128 : 64;
     const int64_t here = blocks(block) > 0 ? blocks(block) : 1, want = 256 / here, most = steps / 16;
     const int64_t splits = want < most ? want : most;
     return {block, (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits)};
@@ -170,27 +170,28 @@ __device__ __forceinline__ void store_split(uint16_t *hi, uint16_t *lo, f32x4 v)
     *reinterpret_cast<uint2 *>(lo) = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
 }
 
-// [batch][rows][cols] with a power for each row; planes [batch][rows][wide], zeros behind each row; a wave per row.
+// [batch][rows][cols] with a power for each row; planes [batch][rows][wide], zeros behind each row; a wave per row at a time.
 __global__ void __launch_bounds__(256)
 split_rows_kernel(int64_t all_rows, int64_t rows, int64_t cols, int64_t wide, const float *__restrict__ in, int64_t ld, int64_t step, uint16_t *__restrict__ hi,
                   uint16_t *__restrict__ lo, int *__restrict__ powers)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), g = row / rows;
-    if (row >= all_rows) return;
-    const float *p = in + g * step + (row - g * rows) * ld;
-    float most = 0.0f;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < all_rows; row += (int64_t)gridDim.x * 4) {
+        const int64_t g = row / rows;
+        const float *p = in + g * step + (row - g * rows) * ld;
+        float most = 0.0f;
 #pragma unroll 4
-    for (int64_t c = lane * 4; c < cols; c += 256) {
-        const f32x4 v = load_up_to_four(p, c, cols);
-        most = fmaxf(fmaxf(most, fmaxf(finite_size(v[0]), finite_size(v[1]))), fmaxf(finite_size(v[2]), finite_size(v[3])));
-    }
+        for (int64_t c = lane * 4; c < cols; c += 256) {
+            const f32x4 v = load_up_to_four(p, c, cols);
+            most = fmaxf(fmaxf(most, fmaxf(finite_size(v[0]), finite_size(v[1]))), fmaxf(finite_size(v[2]), finite_size(v[3])));
+        }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    const int power = power_for(most);
-    if (lane == 0) powers[row] = -power;
+        for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+        const int power = power_for(most);
+        if (lane == 0) powers[row] = -power;
 #pragma unroll 4
-    for (int64_t c = lane * 4; c < wide; c += 256) store_split(hi + row * wide + c, lo + row * wide + c, scaled(load_up_to_four(p, c, cols), power));
+        for (int64_t c = lane * 4; c < wide; c += 256) store_split(hi + row * wide + c, lo + row * wide + c, scaled(load_up_to_four(p, c, cols), power));
+    }
 }
 
 // The largest values of the columns in runs of `run` rows: [batch][runs][cols].  A workgroup has 256 columns, a wave every fourth row.
@@ -281,7 +282,7 @@ struct FloatSource {
         powers = to;
         between = step ? (near ? rows : cols) : 0;
         if (near) {
-            split_rows_kernel<<<(uint32_t)((all + 3) / 4), 256, 0, s>>>(all, rows, cols, wide, (const float *)p, ld, step, hi, lo, to);
+            split_rows_kernel<<<(uint32_t)(all < 1 << 20 ? (all + 3) / 4 : 1 << 18), 256, 0, s>>>(all, rows, cols, wide, (const float *)p, ld, step, hi, lo, to);
         } else {
             const int64_t run = round_up((rows + runs() - 1) / runs(), 4), each = rows < 4096 ? 16 : 64;     // rows of a workgroup: few leave compute units without work
             const uint32_t across = (uint32_t)((wide + 255) / 256), n = (uint32_t)((rows + run - 1) / run);
@@ -307,7 +308,7 @@ static void launch_product32(hipStream_t s, int64_t batch, int64_t M, int64_t N,
     }
     PowerEpilogue<Epilogue> powers{e, nullptr, nullptr, M, N, 0, 0};
     const Planes16 pa = a.take(s, batch, work, powers.by_row, powers.sr), pb = b.take(s, batch, work + a.bytes(batch), powers.by_column, powers.sc);
-    with_small_shape<true>(K, [&](int64_t n) { return batch * ((M + n - 1) / n) * ((N + n - 1) / n); }, [&](auto f) {
+    with_small_shape<true>(M, N, K, [&](int64_t n) { return batch * ((M + n - 1) / n) * ((N + n - 1) / n); }, [&](auto f) {
         launch_gemm16_blocks<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, true>(s, batch, M, N, K, pa, a.near, pb, b.near, 1, powers);
     });
 }
@@ -348,24 +349,34 @@ template <typename T> __global__ void __launch_bounds__(256) bias_sum_kernel(Bia
 
 // ---- dx and dw in one launch -----------------------------------------------------------------------------------------
 
+// Whether the workgroups of both products and of db, at most, are less than a launch can have.
+static bool one_launch(const LinearGradArgs &a)
+{
+    const auto up = [](int64_t n) { return (n + 63) / 64; };
+    return a.batch * (up(a.rows) * up(a.din) + up(a.din) * up(a.dout) + up(a.dout)) < 1 << 24;
+}
+
 // dx = d w^T, dw = x^T d and db where neither product would fill the card alone, or false.
 static bool launch_pair16(hipStream_t s, const LinearGradArgs &a, const Planes16 &d, const Planes16 &w, const Planes16 &x, const BiasSum<uint16_t> &bias)
 {
+    if (!one_launch(a)) return false;
     if (a.rows <= FEW_ROWS && a.dout > 1024) return false;         // dx from few_rows_kernel: a long chain of steps otherwise
     const Plan16 px = plan16(a.batch, a.rows, a.din, a.dout), pw = plan16(a.batch, a.din, a.dout, a.rows);
     if (px.block == 256 || pw.block == 256 || px.splits > 1 || pw.splits > 1) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
     const auto both = [&](int64_t b) { return blocks(b, a.rows, a.din) + blocks(b, a.din, a.dout); };
+    const int swap = a.rows > a.dout;                               // the longer chains of steps start first
     const auto go = [&](auto f) {
         const auto product = [&](int64_t M, int64_t N, int64_t K, const Planes16 &l, const Planes16 &r, void *out, int64_t ld, int64_t step) {
             return Product16<LinearEpilogue<uint16_t>>{M, N, K, l, r, (uint32_t)((M + f.BM - 1) / f.BM), (uint32_t)((N + f.BM - 1) / f.BM), plain_epilogue<uint16_t>(M, N, out, ld, step)};
         };
         const uint32_t first = (uint32_t)blocks(f.BM, a.rows, a.din), all = (uint32_t)both(f.BM);
         gemm16_pair_kernel<bf16x8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS><<<all + bias.blocks(), f.WM * f.WN * 64 * f.GROUPS, 0, s>>>(
-            product(a.rows, a.din, a.dout, d, w, a.dx, a.lddx, a.sdx), product(a.din, a.dout, a.rows, x, d, a.dw, a.lddw, a.sdw), first, all, bias);
+            product(a.rows, a.din, a.dout, d, w, a.dx, a.lddx, a.sdx), product(a.din, a.dout, a.rows, x, d, a.dw, a.lddw, a.sdw), first, all, swap, bias);
     };
-    if (both(128) >= 512) go(Shape<128, 128, 2, 2, 64, 2>());
-    else if (both(128) >= 128) go(Shape<128, 128, 2, 4, 64, 4>());
+    const bool far = worth_blocks(128, a.rows, a.din) && worth_blocks(128, a.din, a.dout);
+    if (both(128) >= 512 && far) go(Shape<128, 128, 2, 2, 64, 2>());
+    else if (both(128) >= 128 && far) go(Shape<128, 128, 2, 4, 64, 4>());
     else if (both(64) > 256 || (a.dout < 512 && a.rows < 512)) go(Shape<64, 64, 2, 2, 64, 4>());
     else go(Shape<64, 64, 2, 2, 64, 4, 2>());
     return true;
@@ -373,19 +384,22 @@ static bool launch_pair16(hipStream_t s, const LinearGradArgs &a, const Planes16
 
 static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d, int64_t ldd, int64_t sd, const BiasSum<float> &bias)
 {
+    if (!one_launch(a)) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
     if (as_planes(a.batch, a.rows, a.din, a.dout) || as_planes(a.batch, a.din, a.dout, a.rows)) return false;
-    if ((blocks(128, a.rows, a.din) >= 256 && a.dout >= 256) || (blocks(128, a.din, a.dout) >= 256 && a.rows >= 256)) return false;
+    if ((blocks(128, a.rows, a.din) >= 256 && a.dout >= 256 && worth_blocks(128, a.rows, a.din)) ||
+        (blocks(128, a.din, a.dout) >= 256 && a.rows >= 256 && worth_blocks(128, a.din, a.dout))) return false;
     const auto product = [&](int64_t M, int64_t N, int64_t K, const void *l, int64_t ldl, int64_t sl, const void *r, int64_t ldr, int64_t sr, void *out, int64_t ld, int64_t step) {
         return ProductF32<LinearEpilogue<float>>{M, N, K, (const float *)l, (const float *)r, ldl, sl, ldr, sr, (uint32_t)((M + 63) / 64), (uint32_t)((N + 63) / 64),
                                                  plain_epilogue<float>(M, N, out, ld, step)};
     };
     const auto p = product(a.rows, a.din, a.dout, d, ldd, sd, a.w, a.ldw, a.sw, a.dx, a.lddx, a.sdx);
     const auto q = product(a.din, a.dout, a.rows, a.x, a.ldx, a.sx, d, ldd, sd, a.dw, a.lddw, a.sdw);
+    const int swap = a.rows > a.dout;
     const uint32_t first = (uint32_t)blocks(64, a.rows, a.din), all = first + (uint32_t)blocks(64, a.din, a.dout);
-    if (all >= 768) gemm_f32_pair_kernel<64, 32, 1><<<all + bias.blocks(), 256, 0, s>>>(p, q, first, all, bias);
-    else if (all >= 384) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, bias);
-    else gemm_f32_pair_kernel<64, 32, 4><<<all + bias.blocks(), 1024, 0, s>>>(p, q, first, all, bias);
+    if (all >= 768) gemm_f32_pair_kernel<64, 32, 1><<<all + bias.blocks(), 256, 0, s>>>(p, q, first, all, swap, bias);
+    else if (all >= 384) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, swap, bias);
+    else gemm_f32_pair_kernel<64, 32, 4><<<all + bias.blocks(), 1024, 0, s>>>(p, q, first, all, swap, bias);
     return true;
 }
 

@@ -216,8 +216,8 @@ template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, in
     const auto go = [&](auto f) { launch_gemm16_triangle<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, SPLIT>(s, batch, side, K, x, near, e); };
     const auto blocks = [&](int64_t b) { const int64_t n = (side + b - 1) / b; return batch * n * (n + 1) / 2; };
     if constexpr (!SPLIT)
-        if (blocks(256) >= 192) { go(Paired()); return; }
-    with_small_shape<SPLIT>(K, blocks, go);
+        if (blocks(256) >= 192 && worth_blocks(256, side, side)) { go(Paired()); return; }
+    with_small_shape<SPLIT>(side, side, K, blocks, go);
 }
 
 template <bool SPLIT, class Epilogue>
@@ -229,12 +229,12 @@ static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, con
     const auto go = [&](auto f) { launch_gemm16_step<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e); };
     const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
     if constexpr (!SPLIT)
-        if (blocks(256) >= 192) {
+        if (blocks(256) >= 192 && worth_blocks(256, a.rows, a.cols)) {
             if constexpr (std::is_same<Epilogue, StepEpilogue>::value) go(Paired());
             else go(Shape<256, 256, 2, 4, 64, 2>());
             return;
         }
-    with_small_shape<SPLIT>(k, blocks, go);
+    with_small_shape<SPLIT>(a.rows, a.cols, k, blocks, go);
 }
 
 template <typename T> static void orth_of(hipStream_t s, const OrthArgs &a, char *work)

@@ -26,8 +26,8 @@ static bool product_fits(int64_t a, int64_t b, int64_t c)
 {
     return a >= 0 && b >= 0 && c >= 0 && (double)a * (double)b * (double)c <= (double)MOST && a <= MOST && b <= MOST && c <= MOST;
 }
-// Blocks of 64 x 64 results of a whole batch: one launch's workgroups.
-static bool blocks_fit(int64_t batch, int64_t m, int64_t n) { return (double)batch * (double)((m + 63) / 64) * (double)((n + 63) / 64) < 2147483648.0; }
+// Blocks of 64 x 64 results of a whole batch: one launch's workgroups of 256 threads, and a launch has fewer than 2^32 of them.
+static bool blocks_fit(int64_t batch, int64_t m, int64_t n) { return (double)batch * (double)((m + 63) / 64) * (double)((n + 63) / 64) < 16777216.0; }
 
 static bool strides_ok(int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t step)
 {

@@ -118,6 +118,12 @@ def test_linear_batches(batch, rows, d_in, d_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("batch,rows,d_in,d_out", [(100, 250, 250, 500), (300, 200, 72, 64), (200, 100, 96, 80), (40, 500, 120, 33), (40, 70, 40, 600), (300, 70, 300, 20)])
+def test_linear_large_batches_of_small_layers(batch, rows, d_in, d_out, dtype):
+    check_linear(rows, d_in, d_out, dtype, "gelu", batch=batch, seed=batch + rows)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("pad", [1, 3, 8, 24])
 @pytest.mark.parametrize("batch", [0, 3])
 def test_linear_distances_of_rows(pad, batch, dtype):
@@ -313,6 +319,13 @@ def test_orthogonalize_many_matrices(batch, rows, cols, dtype):
     want, _ = orth64(a, None, 0.0, False)
     got = nm.netmax_orthogonalize(a)
     assert max(off(got[k], want[k]) for k in range(batch)) < ORTH_TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("batch,rows,cols", [(200, 250, 500), (200, 500, 250), (300, 60, 70), (600, 33, 120), (150, 128, 100)])
+def test_orthogonalize_many_matrices_that_fill_their_blocks(batch, rows, cols, dtype):
+    """As above; blocks are chosen by what lies behind the edges, too."""
+    test_orthogonalize_many_matrices(batch, rows, cols, dtype)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])

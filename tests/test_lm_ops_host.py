@@ -31,6 +31,12 @@ def test_linear_refuses(kw, text):
     refused(lib.netmax_linear(C.byref(s), A, A, A, A, A, A, None, 0, None), text)
 
 
+@pytest.mark.parametrize("kw", [dict(batch=1000, rows=1 << 21), dict(batch=65535, rows=8, d_in=1 << 15), dict(batch=65535, rows=1, d_out=1 << 15)])
+def test_more_blocks_than_a_launch_can_have(kw):
+    lib, s = nm.load(), linear_shape(**kw)
+    refused(lib.netmax_linear(C.byref(s), A, A, A, A, A, A, None, 0, None), "too large")
+
+
 def test_linear_refuses_pointers():
     lib, s = nm.load(), linear_shape()
     for k, name in ((1, "x is NULL"), (2, "w is NULL"), (5, "y is NULL")):
