@@ -19,6 +19,8 @@
 #pragma once
 #include "gemm.h"
 
+#include <type_traits>
+
 namespace netmax {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -289,31 +291,54 @@ __device__ __forceinline__ void gemm16_block(int64_t M, int64_t N, int64_t K, co
     }
     // Results leave by way of LDS, 32 rows of a wave at a time, so that neighbouring lanes have neighbouring columns of a row: straight from the
     // instruction's layout a request would touch 32 rows, 16 bytes in each.
-    constexpr int COLS = TN * 32, PITCH = COLS + 4;
-    const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5;
+    constexpr int COLS = TN * 32, PITCH = COLS + 4, ROWS = 256 / COLS, CALLS = 32 / ROWS;
+    const int lane = threadIdx.x & 63, at = lane & 31, half = lane >> 5, row = lane / (COLS / 4), col = lane % (COLS / 4) * 4;
     float *stage = (float *)space_ + __builtin_amdgcn_readfirstlane(wave) * (32 * PITCH);
-    const int64_t where = !TRIANGLE && splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    const int64_t where = !TRIANGLE && splits > 1 ? (int64_t)split * (all / (mblocks * nblocks)) + g : g, n = n0 + wn + col;
+    const auto put = [&](int i) {
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 store4(stage + at * PITCH + j * 32 + e * 8 + half * 4, f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]});
         wave_order();
+    };
+    if constexpr (TRIANGLE) {                                       // read where it is used: seen ahead, 1 x 2660 x 512 took 8 us more per product
 #pragma unroll
-        for (int r = 0; r < 32; r += 256 / COLS) {
-            const int row = r + lane / (COLS / 4), col = lane % (COLS / 4) * 4;
-            epilogue(where, m0 + wm + i * 32 + row, n0 + wn + col, load4(stage + row * PITCH + col));
-        }
-        if constexpr (TRIANGLE)                                     // the mirror image: rows are columns
+        for (int i = 0; i < TM; ++i) {
+            put(i);
 #pragma unroll
-            for (int c = 0; c < COLS; c += 8) {
-                const int row = c + lane / 8, col = lane % 8 * 4;
-                const float *p = stage + col * PITCH + row;
-                epilogue.mirror(where, n0 + wn + row, m0 + wm + i * 32 + col, f32x4{p[0], p[PITCH], p[2 * PITCH], p[3 * PITCH]});
+            for (int r = 0; r < 32; r += ROWS) epilogue(where, m0 + wm + i * 32 + r + row, n, load4(stage + (r + row) * PITCH + col));
+#pragma unroll
+            for (int c = 0; c < COLS; c += 8) {                     // the mirror image: rows are columns
+                const int down = c + lane / 8, across = lane % 8 * 4;
+                const float *p = stage + across * PITCH + down;
+                epilogue.mirror(where, n0 + wn + down, m0 + wm + i * 32 + across, f32x4{p[0], p[PITCH], p[2 * PITCH], p[3 * PITCH]});
             }
-        wave_order();
+            wave_order();
+        }
+    } else {
+        const auto leave = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            const typename Epilogue::Columns columns = epilogue.template columns<FULL>(where, n);
+            typename Epilogue::Seen seen[CALLS];
+#pragma unroll
+            for (int r = 0; r < CALLS; ++r) seen[r] = epilogue.template see<FULL>(where, m0 + wm + r * ROWS + row, n);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                put(i);
+#pragma unroll
+                for (int r = 0; r < CALLS; ++r) {
+                    const int64_t m = m0 + wm + i * 32 + r * ROWS + row;
+                    const typename Epilogue::Seen now = seen[r];
+                    if (i + 1 < TM) seen[r] = epilogue.template see<FULL>(where, m + 32, n);
+                    epilogue.template leave<FULL>(where, m, n, load4(stage + (r * ROWS + row) * PITCH + col), columns, now);
+                }
+                wave_order();
+            }
+        };
+        if (m0 + wm + TM * 32 <= epilogue.rows_here() && n0 + wn + COLS <= epilogue.cols_here()) leave(std::true_type());
+        else leave(std::false_type());
     }
 }
 

@@ -16,7 +16,15 @@ struct TwoHalves {
 };
 __device__ __forceinline__ float joined(uint16_t hi, uint16_t lo) { return (float)__builtin_bit_cast(_Float16, lo) + (float)__builtin_bit_cast(_Float16, hi); }
 
-// Four neighbours of a row of planes; the planes' rows are padded to multiples of 8.
+// Four neighbours of a row of planes, as they lie in memory; the planes' rows are padded to multiples of 8.  Read as global memory by name: where the compiler
+// does not know (behind a choice), its requests are waited for with those to LDS.
+struct RawPlanes { u32x2 hi, lo; };
+__device__ __forceinline__ f32x4 joined(const RawPlanes &p)
+{
+    return f32x4{joined((uint16_t)p.hi[0], (uint16_t)p.lo[0]), joined((uint16_t)(p.hi[0] >> 16), (uint16_t)(p.lo[0] >> 16)), joined((uint16_t)p.hi[1], (uint16_t)p.lo[1]),
+                 joined((uint16_t)(p.hi[1] >> 16), (uint16_t)(p.lo[1] >> 16))};
+}
+__device__ __forceinline__ u32x2 load_half_fours(const uint16_t *p) { return *(const __attribute__((address_space(1))) u32x2 *)p; }
 __device__ __forceinline__ f32x4 load_planes(const uint16_t *hi, const uint16_t *lo)
 {
     const uint2 h = *reinterpret_cast<const uint2 *>(hi), l = *reinterpret_cast<const uint2 *>(lo);

@@ -70,9 +70,15 @@ static void lay_out(hipStream_t s, const Layouts &l)
 // Partial results of one share of the contraction: [splits][batch][M][wide], float.
 struct PartEpilogue {
     int64_t M, N, wide; float *p;
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    __device__ __forceinline__ int64_t rows_here() const { return M; }
+    __device__ __forceinline__ int64_t cols_here() const { return N; }
+    struct Columns { };
+    struct Seen { };
+    template <bool FULL> __device__ __forceinline__ Columns columns(int64_t, int64_t) const { return Columns{}; }
+    template <bool FULL> __device__ __forceinline__ Seen see(int64_t, int64_t, int64_t) const { return Seen{}; }
+    template <bool FULL> __device__ __forceinline__ void leave(int64_t g, int64_t m, int64_t n, f32x4 v, const Columns &, const Seen &) const
     {
-        if (m < M && n < N) store4(p + (g * M + m) * wide + n, v);
+        if (FULL || (m < M && n < N)) store4(p + (g * M + m) * wide + n, v);
     }
 };
 
@@ -248,14 +254,27 @@ split_columns_kernel(int64_t rows, int64_t cols, int64_t wide, int run, int runs
 // The powers taken back, then another epilogue.
 template <class Inner> struct PowerEpilogue {
     Inner inner; const int *by_row, *by_column; int64_t M, N, sr, sc;
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    __device__ __forceinline__ int64_t rows_here() const { return M; }
+    __device__ __forceinline__ int64_t cols_here() const { return N; }
+    struct Columns { int power[4]; typename Inner::Columns inner; };
+    struct Seen { int power; typename Inner::Seen inner; };
+    template <bool FULL> __device__ __forceinline__ Columns columns(int64_t g, int64_t n) const
     {
-        if (m >= M || n >= N) return;
-        const int power = by_row[g * sr + m];
+        Columns c{{0, 0, 0, 0}, inner.template columns<FULL>(g, n)};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (n + e < N) v[e] = ldexpf(v[e], power + by_column[g * sc + n + e]);
-        inner(g, m, n, v);
+            if (FULL || n + e < N) c.power[e] = by_column[g * sc + n + e];
+        return c;
+    }
+    template <bool FULL> __device__ __forceinline__ Seen see(int64_t g, int64_t m, int64_t n) const
+    {
+        return Seen{FULL || m < M ? by_row[g * sr + m] : 0, inner.template see<FULL>(g, m, n)};
+    }
+    template <bool FULL> __device__ __forceinline__ void leave(int64_t g, int64_t m, int64_t n, f32x4 v, const Columns &c, const Seen &s) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], s.power + c.power[e]);
+        inner.template leave<FULL>(g, m, n, v, c.inner, s.inner);
     }
 };
 

@@ -13,8 +13,8 @@
 //   bfloat16     products of hi planes (11 bits), the term a X from both planes.  B's diagonal, its large part near the end, is kept in float and
 //                joins a X: the rounding of B then halves the result's error, to 0.6e-3 where the rounding of the result itself is 1.7e-3
 // A and B are symmetric: their blocks on and below the diagonal are computed and written to both sides.
-// 8 x 2048 x 4096 bfloat16, five steps: 3.94 ms, of it momentum and norm 0.30 (1.34 GB), A and B 1.67, X 2.04 (its planes, in and
-// out, take as long as half of the products).  16 x 784 x 512 float: 0.45 ms, bound by the chain of seventeen launches of 14 to 45 us.
+// 8 x 2048 x 4096 bfloat16, five steps: 3.74 ms, of it momentum and norm 0.30 (1.34 GB), A and B 1.67, X 1.8 (its planes, in and
+// out, take as long as half of the products).  16 x 784 x 512 float: 0.41 ms, bound by the chain of seventeen launches of 14 to 45 us.
 #include "half_planes.h"
 #include "orth.h"
 
@@ -58,40 +58,59 @@ struct SquareEpilogue {
 struct StepEpilogue {
     int64_t rows, cols, wide; float a; bool tall;
     const uint16_t *own_hi, *own_lo; uint16_t *hi, *lo; const float *diagonal;
-    __device__ __forceinline__ f32x4 value(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    __device__ __forceinline__ int64_t rows_here() const { return rows; }
+    __device__ __forceinline__ int64_t cols_here() const { return cols; }
+    struct Columns { f32x4 f; };
+    struct Seen { RawPlanes x; float diagonal; };
+    template <bool FULL> __device__ __forceinline__ Columns columns(int64_t g, int64_t n) const
     {
-        const int64_t at = (g * rows + m) * wide + n;
-        f32x4 f = {a, a, a, a};
-        if (diagonal) {
-            if (tall) {
+        Columns c{f32x4{a, a, a, a}};
+        if (diagonal && tall)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < cols) f[e] += diagonal[g * cols + n + e];
-            } else {
-                f += diagonal[g * rows + m];
-            }
-        }
-        const f32x4 x = load_planes(own_hi + at, own_lo + at);
+            for (int e = 0; e < 4; ++e)
+                if (FULL || n + e < cols) c.f[e] += diagonal[g * cols + n + e];
+        return c;
+    }
+    template <bool FULL> __device__ __forceinline__ Seen see(int64_t g, int64_t m, int64_t n) const
+    {
+        Seen s{};
+        if (!FULL && (m >= rows || n >= wide)) return s;
+        const int64_t at = (g * rows + m) * wide + n;
+        s.x = RawPlanes{load_half_fours(own_hi + at), load_half_fours(own_lo + at)};
+        if (diagonal && !tall) s.diagonal = diagonal[g * rows + m];
+        return s;
+    }
+    template <bool FULL> __device__ __forceinline__ f32x4 value(int64_t n, f32x4 v, const Columns &c, const Seen &s) const
+    {
+        const f32x4 x = joined(s.x);
         v *= 1.0f / SQUARE_SCALE;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = n + e < cols ? fmaf(f[e], x[e], v[e]) : 0.0f;
+        for (int e = 0; e < 4; ++e) v[e] = FULL || n + e < cols ? fmaf(c.f[e] + s.diagonal, x[e], v[e]) : 0.0f;
         return v;
     }
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    template <bool FULL> __device__ __forceinline__ void leave(int64_t g, int64_t m, int64_t n, f32x4 v, const Columns &c, const Seen &s) const
     {
-        if (m >= rows || n >= wide) return;
+        if (!FULL && (m >= rows || n >= wide)) return;
         const int64_t at = (g * rows + m) * wide + n;
-        store_planes(hi + at, lo + at, value(g, m, n, v));
+        store_planes(hi + at, lo + at, value<FULL>(n, v, c, s));
     }
 };
 
 // The last step: scale X to the caller's memory.
 template <typename T> struct LastEpilogue {
     StepEpilogue step; float scale; T *out; int64_t ldo, so;
-    __device__ __forceinline__ void operator()(int64_t g, int64_t m, int64_t n, f32x4 v) const
+    __device__ __forceinline__ int64_t rows_here() const { return step.rows; }
+    __device__ __forceinline__ int64_t cols_here() const { return step.cols; }
+    typedef StepEpilogue::Columns Columns;
+    typedef StepEpilogue::Seen Seen;
+    template <bool FULL> __device__ __forceinline__ Columns columns(int64_t g, int64_t n) const { return step.columns<FULL>(g, n); }
+    template <bool FULL> __device__ __forceinline__ Seen see(int64_t g, int64_t m, int64_t n) const { return step.see<FULL>(g, m, n); }
+    template <bool FULL> __device__ __forceinline__ void leave(int64_t g, int64_t m, int64_t n, f32x4 v, const Columns &c, const Seen &s) const
     {
-        if (m >= step.rows || n >= step.cols) return;
-        store_up_to_four(out + g * so + m * ldo, n, step.cols, scale * step.value(g, m, n, v));
+        if (!FULL && (m >= step.rows || n >= step.cols)) return;
+        v = scale * step.value<FULL>(n, v, c, s);
+        T *row = out + g * so + m * ldo;
+        if (FULL) store_four(row + n, v); else store_up_to_four(row, n, step.cols, v);
     }
 };
 
