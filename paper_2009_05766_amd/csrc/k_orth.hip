@@ -227,7 +227,7 @@ int64_t orth_workspace(const OrthArgs &a)
 }
 
 // Many blocks: 256 x 128, two workgroups on a compute unit, so that the results of one (planes in and out, as long as half of the products) leave under
-// the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us.
+// the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us (388 since the epilogue sees ahead).
 typedef Shape<256, 128, 4, 2, 32, 3> Paired;
 
 template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
