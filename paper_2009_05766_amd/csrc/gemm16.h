@@ -368,6 +368,10 @@ gemm16_pair_kernel(Product16<Epilogue> p, Product16<Epilogue> q, uint32_t first,
         extra(id - both, reinterpret_cast<float *>(space));
 }
 
+// A block's shape as a value: what gemm16_kernel is instantiated with.
+template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_, int GROUPS_ = 1>
+struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_, GROUPS = GROUPS_; };
+
 // C = A B for few rows, at most 32 TM: the weights are what has to be read.  A workgroup has 32 columns; its eight waves take steps of 32 indices in turn,
 // each with its own space in LDS for a few steps under way and without a barrier.  The waves' sums are added in LDS in order.  Neighbouring
 // workgroups share an L2, as they share the lines of 128 bytes that 64 bytes of a row of weights lie in.  Bound by what is under way per compute unit: one
@@ -463,16 +467,16 @@ inline bool fits16(const void *p, int64_t ld, int64_t step, int64_t stored)
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && step % 8 == 0 && stored % 8 == 0 && ld < (1 << 22);
 }
 
-template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, bool SPLIT, class Epilogue>
+template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, class Epilogue>
 void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, uint32_t splits,
                           const Epilogue &e)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64 * GROUPS);
-    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, true, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, false, SPLIT, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, false, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, true, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
+    else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, false, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
 }
 
 // The lower triangle of blocks of a symmetric product, A B with B = A transposed as stored: both operands have the same orientation.

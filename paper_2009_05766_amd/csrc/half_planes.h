@@ -43,9 +43,7 @@ __device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v
     if (lo) *reinterpret_cast<uint2 *>(lo) = make_uint2(half_bits(a.lo) | half_bits(b.lo) << 16, half_bits(c.lo) | half_bits(d.lo) << 16);
 }
 
-// One launch for every block shape: `go` gets it as BM, BN, waves, step, stages and groups of gemm16_kernel.
-template <int BM_, int BN_, int WM_, int WN_, int STEP_, int STAGES_, int GROUPS_ = 1>
-struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP = STEP_, STAGES = STAGES_, GROUPS = GROUPS_; };
+// One launch for every block shape: `go` gets it.
 template <bool SPLIT, class Blocks, class Go> static void with_small_shape(int64_t M, int64_t N, int64_t K, const Blocks &blocks, const Go &go)
 {
     // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has (1 x 2660 x 512, X^T X:

@@ -1,9 +1,10 @@
 // y = act(x w + b) + r for a batch of layers, and its gradients:
 //     dz = dy act'(z),  dx = dz w^T,  dw = x^T dz,  db = sum over the rows of dz.
 // bfloat16 is multiplied as it is (gemm16.h); operands whose rows that cannot take where they lie are laid out anew first.  float is multiplied in
-// float (gemm_f32.h) or, in products large enough to pay for the planes, as planes of halves.
+// float (gemm_f32.h) at every size: a row split into 16-bit planes with one power of two for all of it loses its small values beside a large one, and an
+// infinity there meets low planes of either sign, so that a result would depend on the size of its layer.
+#include "gemm16.h"
 #include "gemm_f32.h"
-#include "half_planes.h"
 #include "linear.h"
 
 namespace netmax {
@@ -122,11 +123,11 @@ static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, 
                             const Epilogue &e)
 {
     const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block) * splits;
-    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (blocks > 256 || K < 512 * splits) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2, false>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else if (blocks > 256 || K < 512 * splits) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2>(s, batch, M, N, K, a, ak, b, bk, splits, e);
 }
 
 // `work`: part_bytes() of it.
@@ -145,191 +146,6 @@ static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N,
     const int64_t wide = round_up(N, 4), quads = batch * M * wide / 4;
     launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, p.splits, PartEpilogue{M, N, wide, (float *)work});
     join_parts_kernel<<<(uint32_t)((quads + 255) / 256 < 2048 ? (quads + 255) / 256 : 2048), 256, 0, s>>>(batch, M, wide, p.splits, (const float *)work, e);
-}
-
-// ---- float operands as planes of halves ------------------------------------------------------------------------------
-//
-// Every row of results (column, for the right operand) has a power of two of its own that brings its largest operand value to 2^14 .. 2^15, so that an
-// operand's error is 2^-39 of the largest value that meets it or 2^-22 of itself, whichever is more, and a row of small values is as exact as
-// any other.  The three products of planes are then as exact as float ones and take a third of the matrix instructions' time of
-// 16-bit products instead of sixteen times that.  Infinities and NaNs stay what they are, reach their own rows and columns only, and do
-// not count for the power.
-
-__device__ __forceinline__ float finite_size(float v) { const float a = fabsf(v); return a < INFINITY ? a : 0.0f; }
-// The power for a largest value: 0 for a row of zeros.
-__device__ __forceinline__ int power_for(float most) { return most > 0.0f ? 15 - (most < 0x1p-126f ? -125 : __builtin_amdgcn_frexp_expf(most)) : 0; }
-__device__ __forceinline__ f32x4 scaled(f32x4 v, int power)
-{
-    return f32x4{ldexpf(v[0], power), ldexpf(v[1], power), ldexpf(v[2], power), ldexpf(v[3], power)};
-}
-// An infinity has no low plane (inf - inf).
-__device__ __forceinline__ void store_split(uint16_t *hi, uint16_t *lo, f32x4 v)
-{
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const TwoHalves t(v[e]);
-        h[e] = half_bits(t.hi);
-        l[e] = fabsf(v[e]) < INFINITY ? half_bits(t.lo) : 0u;
-    }
-    *reinterpret_cast<uint2 *>(hi) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-    *reinterpret_cast<uint2 *>(lo) = make_uint2(l[0] | l[1] << 16, l[2] | l[3] << 16);
-}
-
-// [batch][rows][cols] with a power for each row; planes [batch][rows][wide], zeros behind each row; a wave per row at a time.
-__global__ void __launch_bounds__(256)
-split_rows_kernel(int64_t all_rows, int64_t rows, int64_t cols, int64_t wide, const float *__restrict__ in, int64_t ld, int64_t step, uint16_t *__restrict__ hi,
-                  uint16_t *__restrict__ lo, int *__restrict__ powers)
-{
-    const int lane = threadIdx.x & 63;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < all_rows; row += (int64_t)gridDim.x * 4) {
-        const int64_t g = row / rows;
-        const float *p = in + g * step + (row - g * rows) * ld;
-        float most = 0.0f;
-#pragma unroll 4
-        for (int64_t c = lane * 4; c < cols; c += 256) {
-            const f32x4 v = load_up_to_four(p, c, cols);
-            most = fmaxf(fmaxf(most, fmaxf(finite_size(v[0]), finite_size(v[1]))), fmaxf(finite_size(v[2]), finite_size(v[3])));
-        }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-        const int power = power_for(most);
-        if (lane == 0) powers[row] = -power;
-#pragma unroll 4
-        for (int64_t c = lane * 4; c < wide; c += 256) store_split(hi + row * wide + c, lo + row * wide + c, scaled(load_up_to_four(p, c, cols), power));
-    }
-}
-
-// The largest values of the columns in runs of `run` rows: [batch][runs][cols].  A workgroup has 256 columns, a wave every fourth row.
-__global__ void __launch_bounds__(256)
-column_sizes_kernel(int64_t rows, int64_t cols, int64_t run, const float *__restrict__ in, int64_t ld, int64_t step, float *__restrict__ sizes)
-{
-    __shared__ __align__(16) float part[4][256];
-    const int wave = threadIdx.x >> 6, at = (threadIdx.x & 63) * 4;
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 256 + at, end = (int64_t)(blockIdx.y + 1) * run < rows ? (int64_t)(blockIdx.y + 1) * run : rows;
-    f32x4 most = {0, 0, 0, 0};
-    if (n < cols)
-#pragma unroll 4
-        for (int64_t r = (int64_t)blockIdx.y * run + wave; r < end; r += 4) {
-            const f32x4 v = load_up_to_four(in + g * step + r * ld, n, cols);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], finite_size(v[e]));
-        }
-    store4(&part[wave][at], most);
-    __syncthreads();
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c < cols)
-        sizes[(g * gridDim.y + blockIdx.y) * cols + c] = fmaxf(fmaxf(part[0][threadIdx.x], part[1][threadIdx.x]), fmaxf(part[2][threadIdx.x], part[3][threadIdx.x]));
-}
-
-// [batch][rows][cols] with a power for each column, from the sizes of its runs.
-__global__ void __launch_bounds__(256)
-split_columns_kernel(int64_t rows, int64_t cols, int64_t wide, int run, int runs, const float *__restrict__ in, int64_t ld, int64_t step, const float *__restrict__ sizes,
-                     uint16_t *__restrict__ hi, uint16_t *__restrict__ lo, int *__restrict__ powers)
-{
-    const int wave = threadIdx.x >> 6;
-    const int64_t g = blockIdx.z, n = (int64_t)blockIdx.x * 256 + (threadIdx.x & 63) * 4, r0 = (int64_t)blockIdx.y * run;
-    if (n >= wide) return;
-    f32x4 most = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int k = 0; k < runs; ++k) {
-        const f32x4 v = load_up_to_four(sizes + (g * runs + k) * cols, n, cols);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) most[e] = fmaxf(most[e], v[e]);
-    }
-    int power[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        power[e] = power_for(most[e]);
-        if (blockIdx.y == 0 && wave == 0 && n + e < cols) powers[g * cols + n + e] = -power[e];
-    }
-#pragma unroll 4
-    for (int64_t r = r0 + wave; r < r0 + run && r < rows; r += 4) {
-        const f32x4 v = load_up_to_four(in + g * step + r * ld, n, cols);
-        const int64_t at = (g * rows + r) * wide + n;
-        store_split(hi + at, lo + at, f32x4{ldexpf(v[0], power[0]), ldexpf(v[1], power[1]), ldexpf(v[2], power[2]), ldexpf(v[3], power[3])});
-    }
-}
-
-// The powers taken back, then another epilogue.
-template <class Inner> struct PowerEpilogue {
-    Inner inner; const int *by_row, *by_column; int64_t M, N, sr, sc;
-    __device__ __forceinline__ int64_t rows_here() const { return M; }
-    __device__ __forceinline__ int64_t cols_here() const { return N; }
-    struct Columns { int power[4]; typename Inner::Columns inner; };
-    struct Seen { int power; typename Inner::Seen inner; };
-    template <bool FULL> __device__ __forceinline__ Columns columns(int64_t g, int64_t n) const
-    {
-        Columns c{{0, 0, 0, 0}, inner.template columns<FULL>(g, n)};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (FULL || n + e < N) c.power[e] = by_column[g * sc + n + e];
-        return c;
-    }
-    template <bool FULL> __device__ __forceinline__ Seen see(int64_t g, int64_t m, int64_t n) const
-    {
-        return Seen{FULL || m < M ? by_row[g * sr + m] : 0, inner.template see<FULL>(g, m, n)};
-    }
-    template <bool FULL> __device__ __forceinline__ void leave(int64_t g, int64_t m, int64_t n, f32x4 v, const Columns &c, const Seen &s) const
-    {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], s.power + c.power[e]);
-        inner.template leave<FULL>(g, m, n, v, c.inner, s.inner);
-    }
-};
-
-// Whether a float product is multiplied as planes: where the time that it saves (100 against 300 TFLOP/s) is several times what planes take (reading
-// an operand two or three times and writing it once, and up to five launches).  4096 x 4096 x 4096: 1.37 ms in float, 0.52 ms as planes; 1200 x 1000 x 1100: 45
-// and 57 us.
-static bool as_planes(int64_t batch, int64_t M, int64_t N, int64_t K) { return M * N >= 256 * (M + N) && (double)batch * M * N * K >= 2.5e9; }
-
-// A float matrix [rows][cols] of a batch as planes, with a power for each row (`near`: the contraction runs along the rows) or each column.
-struct FloatSource {
-    const void *p; int64_t ld, step, rows, cols; bool near;
-    int64_t own(int64_t batch) const { return step ? batch : 1; }
-    int64_t runs() const { return rows < 2048 ? (rows + 63) / 64 : 32; }
-    int64_t plane_bytes(int64_t batch) const { return round_up(own(batch) * rows * round_up(cols, 8) * 2, 256); }
-    int64_t power_bytes(int64_t batch) const { return round_up(own(batch) * (near ? rows : cols) * 4, 256); }
-    int64_t size_bytes(int64_t batch) const { return near ? 0 : round_up(own(batch) * runs() * cols * 4, 256); }
-    int64_t bytes(int64_t batch) const { return 2 * plane_bytes(batch) + power_bytes(batch) + size_bytes(batch); }
-    Planes16 take(hipStream_t s, int64_t batch, char *work, const int *&powers, int64_t &between) const
-    {
-        const int64_t wide = round_up(cols, 8), all = own(batch) * rows;
-        uint16_t *hi = (uint16_t *)work, *lo = (uint16_t *)(work + plane_bytes(batch));
-        int *to = (int *)(work + 2 * plane_bytes(batch));
-        float *sizes = (float *)(work + 2 * plane_bytes(batch) + power_bytes(batch));
-        powers = to;
-        between = step ? (near ? rows : cols) : 0;
-        if (near) {
-            split_rows_kernel<<<(uint32_t)(all < 1 << 20 ? (all + 3) / 4 : 1 << 18), 256, 0, s>>>(all, rows, cols, wide, (const float *)p, ld, step, hi, lo, to);
-        } else {
-            const int64_t run = round_up((rows + runs() - 1) / runs(), 4), each = rows < 4096 ? 16 : 64;     // rows of a workgroup: few leave compute units without work
-            const uint32_t across = (uint32_t)((wide + 255) / 256), n = (uint32_t)((rows + run - 1) / run);
-            column_sizes_kernel<<<dim3(across, n, (uint32_t)own(batch)), 256, 0, s>>>(rows, cols, run, (const float *)p, ld, step, sizes);
-            split_columns_kernel<<<dim3(across, (uint32_t)((rows + each - 1) / each), (uint32_t)own(batch)), 256, 0, s>>>(rows, cols, wide, (int)each, (int)n, (const float *)p, ld, step, sizes,
-                                                                                                              hi, lo, to);
-        }
-        return Planes16{(const char *)hi, (const char *)lo, wide, step ? rows * wide : 0};
-    }
-};
-
-// C = A B of float operands; `work`: product32_bytes() of it.
-static int64_t product32_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, const FloatSource &a, const FloatSource &b)
-{
-    return as_planes(batch, M, N, K) ? a.bytes(batch) + b.bytes(batch) : 0;
-}
-template <class Epilogue>
-static void launch_product32(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const FloatSource &a, const FloatSource &b, const Epilogue &e, char *work)
-{
-    if (!as_planes(batch, M, N, K)) {
-        launch_gemm_f32<float>(s, batch, M, N, K, Operand{a.p, a.ld, a.step, a.near}, Operand{b.p, b.ld, b.step, b.near}, e);
-        return;
-    }
-    PowerEpilogue<Epilogue> powers{e, nullptr, nullptr, M, N, 0, 0};
-    const Planes16 pa = a.take(s, batch, work, powers.by_row, powers.sr), pb = b.take(s, batch, work + a.bytes(batch), powers.by_column, powers.sc);
-    with_small_shape<true>(M, N, K, [&](int64_t n) { return batch * ((M + n - 1) / n) * ((N + n - 1) / n); }, [&](auto f) {
-        launch_gemm16_blocks<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, true>(s, batch, M, N, K, pa, a.near, pb, b.near, 1, powers);
-    });
 }
 
 // out [rows][cols] alone
@@ -405,7 +221,6 @@ static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d,
 {
     if (!one_launch(a)) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
-    if (as_planes(a.batch, a.rows, a.din, a.dout) || as_planes(a.batch, a.din, a.dout, a.rows)) return false;
     if ((blocks(128, a.rows, a.din) >= 256 && a.dout >= 256 && worth_blocks(128, a.rows, a.din)) ||
         (blocks(128, a.din, a.dout) >= 256 && a.rows >= 256 && worth_blocks(128, a.din, a.dout))) return false;
     const auto product = [&](int64_t M, int64_t N, int64_t K, const void *l, int64_t ldl, int64_t sl, const void *r, int64_t ldr, int64_t sr, void *out, int64_t ld, int64_t step) {
@@ -498,20 +313,17 @@ template <typename T> static LinearEpilogue<T> forward_epilogue(const LinearArgs
 {
     return LinearEpilogue<T>{a.rows, a.dout, (const T *)a.bias, (const T *)a.residual, (T *)a.y, (T *)a.z, a.ldr, a.ldy, a.ldz, a.sb, a.sr, a.sy, a.sz, a.act};
 }
-static FloatSource float_source(const void *p, int64_t ld, int64_t step, int64_t rows, int64_t cols, bool near) { return FloatSource{p, ld, step, rows, cols, near}; }
 
 int64_t linear_workspace(const LinearArgs &a)
 {
-    if (!a.bf16)
-        return product32_bytes(a.batch, a.rows, a.dout, a.din, float_source(a.x, a.ldx, a.sx, a.rows, a.din, true), float_source(a.w, a.ldw, a.sw, a.din, a.dout, false));
+    if (!a.bf16) return 0;
     return Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + part_bytes(a.batch, a.rows, a.dout, a.din, true);
 }
 
 void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
 {
     if (!a.bf16) {
-        launch_product32(s, a.batch, a.rows, a.dout, a.din, float_source(a.x, a.ldx, a.sx, a.rows, a.din, true), float_source(a.w, a.ldw, a.sw, a.din, a.dout, false),
-                         forward_epilogue<float>(a), (char *)work);
+        launch_gemm_f32<float>(s, a.batch, a.rows, a.dout, a.din, Operand{a.x, a.ldx, a.sx, true}, Operand{a.w, a.ldw, a.sw, false}, forward_epilogue<float>(a));
         return;
     }
     char *at = (char *)work;
@@ -538,13 +350,7 @@ int64_t linear_grad_workspace(const LinearGradArgs &a)
     int64_t n = sum_bytes(a);
     if (a.act != ACT_NONE) n += round_up(a.batch * a.rows * dz_wide(a) * (a.bf16 ? 2 : 4), 256);
     else if (a.bf16) n += Source(a.dy, a.lddy, a.sdy, a.rows, a.dout).bytes(a.batch);
-    if (!a.bf16) {
-        // dz (or dy) lies in rows of dout either way; the two products use the same memory in turn
-        const int64_t sd = a.batch > 1 ? 1 : 0;
-        const int64_t dx = product32_bytes(a.batch, a.rows, a.din, a.dout, float_source(nullptr, 0, sd, a.rows, a.dout, true), float_source(a.w, a.ldw, a.sw, a.din, a.dout, true));
-        const int64_t dw = product32_bytes(a.batch, a.din, a.dout, a.rows, float_source(a.x, a.ldx, a.sx, a.rows, a.din, false), float_source(nullptr, 0, sd, a.rows, a.dout, false));
-        return n + (dx > dw ? dx : dw);
-    }
+    if (!a.bf16) return n;
     const int64_t dx = part_bytes(a.batch, a.rows, a.din, a.dout, true), dw = part_bytes(a.batch, a.din, a.dout, a.rows, false);
     return n + Source(a.x, a.ldx, a.sx, a.rows, a.din).bytes(a.batch) + Source(a.w, a.ldw, a.sw, a.din, a.dout).bytes(a.batch) + (dx > dw ? dx : dw);
 }
@@ -581,11 +387,11 @@ void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
         if (a.dx && a.dw && a.rows > 0 && launch_pair32(s, a, d, ldd, sd, bias)) return;
         launch_bias(s, bias);
         if (a.dx && a.rows > 0)
-            launch_product32(s, a.batch, a.rows, a.din, a.dout, float_source(d, ldd, sd, a.rows, a.dout, true), float_source(a.w, a.ldw, a.sw, a.din, a.dout, true),
-                             plain_epilogue<float>(a.rows, a.din, a.dx, a.lddx, a.sdx), at);
+            launch_gemm_f32<float>(s, a.batch, a.rows, a.din, a.dout, Operand{d, ldd, sd, true}, Operand{a.w, a.ldw, a.sw, true},
+                                   plain_epilogue<float>(a.rows, a.din, a.dx, a.lddx, a.sdx));
         if (a.dw)
-            launch_product32(s, a.batch, a.din, a.dout, a.rows, float_source(a.x, a.ldx, a.sx, a.rows, a.din, false), float_source(d, ldd, sd, a.rows, a.dout, false),
-                             plain_epilogue<float>(a.din, a.dout, a.dw, a.lddw, a.sdw), at);
+            launch_gemm_f32<float>(s, a.batch, a.din, a.dout, a.rows, Operand{a.x, a.ldx, a.sx, false}, Operand{d, ldd, sd, false},
+                                   plain_epilogue<float>(a.din, a.dout, a.dw, a.lddw, a.sdw));
         return;
     }
     const BiasSum<uint16_t> bias = launch_slopes<uint16_t>(s, a, (uint16_t *)dz, sums);

@@ -1,0 +1,90 @@
+"""Values at which the operators for language models can go wrong without any size being unusual: infinities and values of very different size in one row,
+masked logits, one logit far above all others, activations in their tails.
+
+Tolerances.  A float sum of K products is off by at most (K + 4) 2^-24 times the sum of the products' magnitudes, whatever else its row holds; the result's own
+rounding is 2^-24 of it."""
+import math
+
+import pytest
+import torch
+
+import paper_2009_05766_amd as nm
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def within(got, want, tol, what):
+    d = (got.double() - want).abs()
+    bad = ~(d <= tol)
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {float((d / tol.clamp(min=1e-300)).max()):.3g} of the bound"
+
+
+# ---- float layers, from small to large: the same rules ----------------------------------------------------------------
+
+SIDES = [200, 700, 1664]
+
+
+@pytest.mark.parametrize("n", SIDES)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_infinities_in_float_layers(n, sign):
+    """An infinity times a weight that is not 0 is an infinity of the product's sign, in y and in every gradient; other rows and columns do not see it."""
+    g = gen(n)
+    x, w, dy = normal(g, n, n), normal(g, n, n, scale=n ** -0.5), normal(g, n, n)
+    w[7, ::3] = 1.0                                    # few bits, both signs
+    w[7, 1::3] = -0.5
+    x[3, 7] = sign * INF
+    want = sign * INF * torch.sign(w[7])
+    y = nm.netmax_linear(x, w)
+    assert torch.equal(y[3], want) and bool(torch.isfinite(y[:3]).all()) and bool(torch.isfinite(y[4:]).all())
+    assert torch.equal(nm.netmax_linear(x, w, act="relu")[3], want.clamp(min=0.0))
+    x[3, 7] = 1.0
+    x[2, ::3] = -2.0
+    w[::3, 5] = 0.25
+    dy[2, 5] = sign * INF
+    dx, dw, db = nm.netmax_linear_grad(dy, x, w)
+    assert torch.equal(dx[2], sign * INF * torch.sign(w[:, 5])) and torch.equal(dw[:, 5], sign * INF * torch.sign(x[2])) and float(db[5]) == sign * INF
+    for t, rest in ((dx, torch.cat([dx[:2], dx[3:]])), (dw, torch.cat([dw[:, :5], dw[:, 6:]], 1))):
+        assert bool(torch.isfinite(rest).all())
+
+
+@pytest.mark.parametrize("n", SIDES)
+@pytest.mark.parametrize("large", [2.0 ** 25, 2.0 ** 40, 1e12, 3e38])
+def test_large_values_that_meet_zeros_in_float_layers(n, large):
+    """One value of a row far above the others, met by zeros only: the other products keep the accuracy that they have without it."""
+    g = gen(n + 1)
+    x, w, dy = normal(g, n, n), normal(g, n, n, scale=n ** -0.5), normal(g, n, n)
+    x[::2, 0] = large
+    w[0] = 0.0
+    w[:, 9] = 0.0                                      # of dy, column 9 in dx
+    dy[::4, 9] = -large
+    x[n - 3] = 0.0                                     # of dy, row n - 3 in dw
+    dy[n - 3] = large
+    X, W, DY = x.double(), w.double(), dy.double()
+    y = nm.netmax_linear(x, w)
+    tol = (n + 4) * 2.0 ** -24
+    within(y, X @ W, tol * (X.abs() @ W.abs()) + 2.0 ** -24 * (X @ W).abs(), "y")
+    dx, dw, db = nm.netmax_linear_grad(dy, x, w)
+    live = torch.ones(n, dtype=torch.bool, device="cuda")
+    live[n - 3] = False                                # that token's own row of dx, and the column of dw that holds the others, are sums of large terms
+    T = lambda t: t.transpose(0, 1).contiguous()  # noqa: E731
+    if large < 1e30:
+        within(dx, DY @ T(W), tol * (DY.abs() @ T(W).abs()) + 2.0 ** -24 * (DY @ T(W)).abs(), "dx")
+        within(dw, T(X) @ DY, tol * (T(X).abs() @ DY.abs()) + 2.0 ** -24 * (T(X) @ DY).abs(), "dw")
+    else:                                              # sums of them leave the type's range
+        within(dx[live], (DY @ T(W))[live], (tol * (DY.abs() @ T(W).abs()) + 2.0 ** -24 * (DY @ T(W)).abs())[live], "dx")
+        cols = torch.ones(n, dtype=torch.bool, device="cuda")
+        cols[9] = False
+        rows = torch.ones(n, dtype=torch.bool, device="cuda")
+        rows[0] = False
+        within(dw[rows][:, cols], (T(X) @ DY)[rows][:, cols], (tol * (T(X).abs() @ DY.abs()) + 2.0 ** -24 * (T(X) @ DY).abs())[rows][:, cols], "dw")
