@@ -346,7 +346,8 @@ int netmax_policy_loss(int64_t tokens, int64_t vocab, int32_t dtype, const void 
  * sequence 2 p is the chosen one of pair p and 2 p + 1 the rejected one.  With R_q = sum over its tokens of weight (log p - ref_logp) and
  * h = beta (R_2p - R_2p+1):   loss[p] = scale (-(1 - smoothing) log sigma(h) - smoothing log sigma(-h)),   ratio[q] = R_q.
  * Logits, labels, weight and grad as for netmax_policy_loss (the gradient of the sum of loss[p]); tokens outside of all sequences have gradient 0;
- * an empty sequence has R_q = 0.  The sums over a sequence are taken in double, in a fixed order. */
+ * an empty sequence has R_q = 0.  The sums over a sequence are taken in double, in a fixed order.  A label whose logit is -inf makes its sequence's R_q -inf:
+ * the loss is then its limit, 0 or inf (a term whose factor, smoothing or 1 - smoothing, is 0 does not count), and NaN only if both sequences have one. */
 int64_t netmax_preference_workspace(int64_t tokens, int64_t pairs);
 int netmax_preference_loss(int64_t tokens, int64_t vocab, int32_t dtype, const void *logits, int64_t ld, const int32_t *labels, int64_t pairs,
                            const int32_t *offsets, const float *ref_logp, const float *weight, float beta, float smoothing, float scale, float *loss,

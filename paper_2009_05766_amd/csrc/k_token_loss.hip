@@ -325,7 +325,8 @@ __global__ void __launch_bounds__(PAIR_THREADS) preference_pairs_kernel(int64_t 
     const double e = a.smoothing, h = (double)a.beta * (part[0][0] - part[1][0]), tail = log1p(exp(-fabs(h)));
     const double below = tail + (h < 0.0 ? -h : 0.0), above = tail + (h > 0.0 ? h : 0.0);       // -log sigma(h), -log sigma(-h)
     const double dh = h >= 0.0 ? e - exp(-h) / (1.0 + exp(-h)) : exp(h) / (1.0 + exp(h)) - (1.0 - e);
-    a.loss[p] = (float)((double)a.scale * ((1.0 - e) * below + e * above));
+    // a sequence with a masked label has the ratio -inf and h may be infinite: a term without weight is left out, 0 inf would be no number
+    a.loss[p] = (float)((double)a.scale * ((e < 1.0 ? (1.0 - e) * below : 0.0) + (e > 0.0 ? e * above : 0.0)));
     for (int side = 0; side < 2; ++side) {
         a.ratio[2 * p + side] = (float)part[side][0];
         a.slope[2 * p + side] = (float)((double)a.scale * (double)a.beta * (side ? -dh : dh));

@@ -88,3 +88,46 @@ def test_large_values_that_meet_zeros_in_float_layers(n, large):
         rows = torch.ones(n, dtype=torch.bool, device="cuda")
         rows[0] = False
         within(dw[rows][:, cols], (T(X) @ DY)[rows][:, cols], (tol * (T(X).abs() @ DY.abs()) + 2.0 ** -24 * (T(X) @ DY).abs())[rows][:, cols], "dw")
+
+
+# ---- losses: masked logits and peaks ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+@pytest.mark.parametrize("side", [0, 1], ids=["chosen", "rejected"])
+@pytest.mark.parametrize("what", ["label", "row"])
+def test_preference_loss_of_masked_logits(what, side, smoothing, dtype):
+    """A sampled token without probability makes its sequence's ratio -inf: the pair's loss is 0 or inf, never no number; other pairs do not see it."""
+    g = gen(31)
+    t, v, beta, scale = 14, 1003, 0.25, 0.5
+    z, labels = normal(g, t, v, dtype=dtype, scale=2.0), torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    offsets = torch.tensor([0, 4, 7, 9, 14], dtype=torch.int32, device="cuda")
+    w, ref = torch.rand(t, generator=g, device="cuda") + 0.5, torch.full((t,), -7.0, device="cuda")
+    q = torch.log_softmax(z.double(), 1)
+    bad = 2 if side == 0 else 5                        # a token of the first pair's chosen or rejected sequence
+    hidden = z[bad, int(labels[bad])].clone()
+    if what == "label":
+        z[bad, int(labels[bad])] = -INF
+    else:
+        z[bad] = -INF
+    q[bad] = torch.log_softmax(z[bad].double(), 0) if what == "label" else -INF
+    lp = q.gather(1, labels.long()[:, None])[:, 0]
+    loss, ratio, grad = nm.netmax_preference_loss(z, labels, offsets, w, ref, beta=beta, smoothing=smoothing, scale=scale)
+    e = float(torch.tensor(smoothing, dtype=F32))
+    down = (1 - e) if side == 0 else e                 # the factor of the term that is infinite
+    assert float(loss[0]) == (INF if down > 0 else 0.0)
+    R = [float((w[a:b].double() * (lp[a:b] - ref[a:b].double())).sum()) for a, b in zip(offsets[:-1].tolist(), offsets[1:].tolist())]
+    assert float(ratio[side]) == -INF and R[side] == -INF
+    for k in range(4):
+        if k != side:
+            assert float(ratio[k]) == pytest.approx(R[k], rel=1e-5, abs=1e-5)
+    h = beta * (R[2] - R[3])
+    assert float(loss[1]) == pytest.approx(scale * ((1 - e) * math.log1p(math.exp(-h)) + e * math.log1p(math.exp(h))), rel=1e-5)
+    # sigma(h) - (1 - e) at its limits
+    dh = [-(1 - e) if side == 0 else e, 1 / (1 + math.exp(-h)) - (1 - e)]
+    slope = torch.zeros(t, dtype=torch.float64, device="cuda")
+    for k, (a, b) in enumerate(zip(offsets[:-1].tolist(), offsets[1:].tolist())):
+        slope[a:b] = w[a:b].double() * beta * scale * (dh[k // 2] if k % 2 == 0 else -dh[k // 2])
+    want = torch.zeros_like(q).scatter_(1, labels.long()[:, None], slope[:, None]) - slope[:, None] * q.exp()
+    assert bool(torch.isfinite(grad).all()) and torch.allclose(grad.double(), want, rtol=2.0 ** -7 if dtype == BF16 else 1e-5, atol=1e-9)
+    assert math.isfinite(float(hidden))
