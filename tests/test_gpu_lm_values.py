@@ -131,3 +131,28 @@ def test_preference_loss_of_masked_logits(what, side, smoothing, dtype):
     want = torch.zeros_like(q).scatter_(1, labels.long()[:, None], slope[:, None]) - slope[:, None] * q.exp()
     assert bool(torch.isfinite(grad).all()) and torch.allclose(grad.double(), want, rtol=2.0 ** -7 if dtype == BF16 else 1e-5, atol=1e-9)
     assert math.isfinite(float(hidden))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [7, 1003, 5003, 30011, 49999, 65536, 131072])
+@pytest.mark.parametrize("above", [4.0, 8.0, 16.0, 25.75, 30.0, 41.0])
+def test_log_probability_of_a_peak(above, vocab, dtype):
+    """One logit far above all others, as of a trained model, in the first, a middle and the last piece of a row.  An added term a errs by at most 2^-24 of a sum below 2
+    and by at most a itself; a thread adds up to 32 times, workgroups ten; the terms' exponentials are exact to 2^-21 plus 2^-22 for each unit of their argument."""
+    g = gen(vocab)
+    places = sorted({0, 5 % vocab, vocab // 3, vocab // 2, (2 * vocab) // 3 + 1, vocab - 1})
+    t = len(places)
+    z = normal(g, t, vocab, dtype=dtype, scale=0.25)
+    labels = torch.tensor(places, dtype=torch.int32, device="cuda")
+    z.scatter_(1, labels.long()[:, None], torch.full((t, 1), above, device="cuda", dtype=dtype))
+    q = torch.log_softmax(z.double(), 1)
+    lp = q.gather(1, labels.long()[:, None])[:, 0]
+    old, zero = torch.zeros(t, device="cuda"), torch.zeros(t, device="cuda")
+    others = -torch.expm1(lp)
+    tol = torch.clamp(2 * others, max=42 * 2.0 ** -24) + others * (2.0 ** -21 + 2.0 ** -22 * above) + 2.0 ** -23 * lp.abs()
+    _, logp, _ = nm.netmax_policy_loss(z, labels, old, zero, need_grad=False)
+    assert bool((logp <= 0).all()), (logp, lp)
+    within(logp, lp, tol, "log probability")
+    offsets = torch.tensor([0, t, t], dtype=torch.int32, device="cuda")
+    _, ratio, _ = nm.netmax_preference_loss(z, labels, offsets, None, old, need_grad=False)
+    assert float(ratio[0]) <= 0.0 and abs(float(ratio[0]) - float(lp.sum())) <= float(tol.sum())
