@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(THREADS) policy_loss_kernel(TokenRows rows, Po
     else r = streamed_sum<T, THREADS>(z);
     const double logp = label_logp(zy, r);
     const float adv = a.advantage[t], ratio = expf((float)(logp - (double)a.old_logp[t]));
-    const float kept = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high), free = ratio * adv, clipped = kept * adv;
+    // a ratio past the type's range is inf, and no advantage is none of it
+    const float kept = fminf(fmaxf(ratio, 1.0f - a.low), 1.0f + a.high), free = adv == 0.0f && ratio == INFINITY ? 0.0f : ratio * adv, clipped = kept * adv;
     float loss = free <= clipped ? -free : clipped < free ? -clipped : free + clipped, slope = free <= clipped ? -free : clipped < free ? 0.0f : free + clipped;
     if (a.ref_logp && a.kl != 0.0f) {
         const float d = (float)((double)a.ref_logp[t] - logp), more = expm1f(d);

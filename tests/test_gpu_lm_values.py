@@ -156,3 +156,13 @@ def test_log_probability_of_a_peak(above, vocab, dtype):
     offsets = torch.tensor([0, t, t], dtype=torch.int32, device="cuda")
     _, ratio, _ = nm.netmax_preference_loss(z, labels, offsets, None, old, need_grad=False)
     assert float(ratio[0]) <= 0.0 and abs(float(ratio[0]) - float(lp.sum())) <= float(tol.sum())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_policy_loss_without_advantage(dtype):
+    """Ratios past the type's range: an advantage of 0 leaves nothing of them; a positive one is clipped, a negative one is not."""
+    z = torch.zeros(3, 4, device="cuda", dtype=dtype)
+    labels, old = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.full((3,), -100.0, device="cuda")
+    loss, _, grad = nm.netmax_policy_loss(z, labels, old, torch.tensor([0.0, 2.0, -2.0], device="cuda"))
+    assert loss[:2].tolist() == [0.0, pytest.approx(-2.4)] and float(loss[2]) == INF
+    assert bool((grad[:2] == 0).all())
