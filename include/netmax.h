@@ -284,7 +284,8 @@ int netmax_consensus_dist_static(int32_t M, int64_t D, int64_t ld, const float *
  * the next call on the same stream.  Every call enqueues its kernels and returns without waiting.  Texts of errors:
  * netmax_last_error(NULL).  Matrices are row-major with rows `ld` elements apart and, in a batch, `s` elements from one matrix to the
  * next (0: the same one for all, for inputs); vectors of a batch lie `s` apart.  Sums are held in float or more and the results rounded once. */
-typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NETMAX_ACT_SILU = 3 } netmax_act; /* GELU: the error function's */
+typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NETMAX_ACT_SILU = 3 } netmax_act; /* GELU: the error
+ * function's, to (8 + z^2) 2^-23 of itself; SiLU to (8 + |z|) 2^-23 */
 
 typedef struct {
     int64_t batch;          /* layers, e.g. one per worker: 0 .. 65535 */

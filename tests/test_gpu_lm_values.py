@@ -166,3 +166,31 @@ def test_policy_loss_without_advantage(dtype):
     loss, _, grad = nm.netmax_policy_loss(z, labels, old, torch.tensor([0.0, 2.0, -2.0], device="cuda"))
     assert loss[:2].tolist() == [0.0, pytest.approx(-2.4)] and float(loss[2]) == INF
     assert bool((grad[:2] == 0).all())
+
+
+# ---- activations in their tails -----------------------------------------------------------------------------------------
+
+def test_gelu_in_its_tails():
+    """Relative to the value, where 1 + erf has cancelled: exponential, reciprocal and polynomial to 8 2^-23 together; the exponent -z^2 / 2 is rounded three times."""
+    z = torch.linspace(-11.0, 6.0, 64 * 512, device="cuda").view(-1, 64)
+    eye, one = torch.eye(64, device="cuda"), torch.ones(512, 64, device="cuda")
+    Z = z.double()
+    below = 0.5 * torch.special.erfc(-Z / math.sqrt(2))
+    bell = torch.exp(-0.5 * Z * Z) / math.sqrt(2 * math.pi)
+    tol = (8 + Z * Z) * 2.0 ** -23
+    y = nm.netmax_linear(z, eye, act="gelu")
+    within(y, Z * below, tol * (Z * below).abs(), "GELU")
+    dx, _, _ = nm.netmax_linear_grad(one, z, eye, z, act="gelu")
+    within(dx, below + Z * bell, tol * (below + Z.abs() * bell), "its slope")
+
+
+def test_silu_in_its_tails():
+    z = torch.linspace(-60.0, 20.0, 64 * 512, device="cuda").view(-1, 64)
+    eye, one = torch.eye(64, device="cuda"), torch.ones(512, 64, device="cuda")
+    Z = z.double()
+    s, rest = torch.sigmoid(Z), torch.sigmoid(-Z)
+    tol = (8 + Z.abs()) * 2.0 ** -23
+    within(nm.netmax_linear(z, eye, act="silu"), Z * s, tol * (Z * s).abs(), "SiLU")
+    dx, _, _ = nm.netmax_linear_grad(one, z, eye, z, act="silu")
+    # 1 - s is rounded to 2^-24 of 1, and meets |z| s
+    within(dx, s * (1 + Z * rest), tol * s * (1 + Z.abs() * rest) + 2.0 ** -23 * Z.abs() * s, "its slope")
