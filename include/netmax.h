@@ -283,7 +283,9 @@ int netmax_consensus_dist_static(int32_t M, int64_t D, int64_t ld, const float *
  * function; -1 if the arguments are refused; 0: work may be NULL).  A workspace holds nothing between calls and may be used again by
  * the next call on the same stream.  Every call enqueues its kernels and returns without waiting.  Texts of errors:
  * netmax_last_error(NULL).  Matrices are row-major with rows `ld` elements apart and, in a batch, `s` elements from one matrix to the
- * next (0: the same one for all, for inputs); vectors of a batch lie `s` apart.  Sums are held in float or more and the results rounded once. */
+ * next (0: the same one for all, for inputs); vectors of a batch lie `s` apart.  Sums are held in float or more and the results rounded once.
+ * Memory that a call writes may not be shared with another result, the workspace or an operand that the call may still read: such calls are refused, except
+ * where a call's comment allows it.  Operands that only interleave (columns of one wide matrix) share nothing. */
 typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NETMAX_ACT_SILU = 3 } netmax_act; /* GELU: the error
  * function's, to (8 + z^2) 2^-23 of itself; SiLU to (8 + |z|) 2^-23 */
 
@@ -300,7 +302,7 @@ typedef struct {
 
 /* y = act(z) + residual, z = x w + bias, for every layer of the batch: x [rows][d_in], w [d_in][d_out] (the layout of a perceptron's W),
  * bias [d_out], residual and y [rows][d_out].  bias and residual may be NULL; z may be NULL or receives z, which netmax_linear_grad needs.
- * y may be the residual's memory with the residual's strides.  The workspace depends on the alignment of x and w (bfloat16 rows that do not start at multiples of
+ * y may be the residual's memory with the residual's strides (and be nothing else's).  The workspace depends on the alignment of x and w (bfloat16 rows that do not start at multiples of
  * 16 bytes are laid out anew): pass the pointers of the call. */
 int64_t netmax_linear_workspace(const netmax_linear_shape *shape, const void *x, const void *w);
 int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w, const void *bias, const void *residual, void *y, void *z,
@@ -309,7 +311,8 @@ int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w
 /* The gradients of that layer from dy = dl/dy (which is the residual's gradient, too): with dz = dy act'(z) (ReLU's derivative at 0 is 0),
  * dx = dz w^T, dw = x^T dz, db = the sum of dz over the rows; each may be NULL.  z as netmax_linear left it, NULL for NETMAX_ACT_NONE.
  * bfloat16: dz is rounded to bfloat16 for the products, as the errors of a perceptron are; db sums it before that.  rows = 0 gives dw = 0 and db = 0.
- * Results of the same call are the same bits every time. */
+ * Results of the same call are the same bits every time.  With an activation, results may lie in the memory of dy and z, which have been read before the first of them is
+ * written; x may be shared if dw, w if dx is NULL. */
 int64_t netmax_linear_grad_workspace(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w);
 int netmax_linear_grad(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w, const void *z, void *dx, void *dw, void *db,
                        void *work, int64_t work_bytes, void *stream);
@@ -327,7 +330,8 @@ typedef struct {
 /* An orthogonalised momentum step for every matrix of the batch: m_out = mu m + g, u = g + mu m_out (nesterov) or m_out,
  * X = u / max(||u||_F, eps), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X, out = scale X.  With (3.4445, -4.7750, 2.0315) and five
  * steps the singular values end near 1.  X is held in halves with 22 bits: coefficients that let a singular value of X grow past 32, or one of
- * b (X X^T) + c (X X^T)^2 past 255, give results that are not finite.  bfloat16: products of 11 bits.  m and m_out may be the same memory; both NULL: u = g.  out may be g's memory with g's strides.
+ * b (X X^T) + c (X X^T)^2 past 255, give results that are not finite.  bfloat16: products of 11 bits.  m and m_out may be the same memory; both NULL: u = g.  out may lie in
+ * the memory of g, and in m's if m_out is another.
  * To mix such updates: write them to g (tile layout, netmax_pack) of a context with momentum 0 and call netmax_mix. */
 int64_t netmax_orthogonalize_workspace(const netmax_orth_shape *shape);
 int netmax_orthogonalize(const netmax_orth_shape *shape, const void *g, const float *m, float *m_out, void *out, void *work, int64_t work_bytes, void *stream);

@@ -2,6 +2,7 @@
 #include "errors.h"
 #include "linear.h"
 #include "orth.h"
+#include "places.h"
 #include "token_loss.h"
 
 #include <cstdio>
@@ -80,6 +81,26 @@ static int check_work(const void *work, int64_t have, int64_t need)
     return netmax_fail(NETMAX_EINVAL, buf);
 }
 
+// ---- memory that a call writes: nothing that it still reads, and nothing twice ---------------------------------------
+
+struct Named { const char *name; Place at; };
+static int64_t size_of(int32_t dtype) { return dtype == NETMAX_BF16 ? 2 : 4; }
+
+static int check_apart(const Named &a, const Named &b)
+{
+    if (!share_memory(a.at, b.at)) return NETMAX_OK;
+    char buf[160];
+    snprintf(buf, sizeof buf, "%s and %s share memory", a.name, b.name);
+    return netmax_fail(NETMAX_EINVAL, buf);
+}
+template <int N> static int check_apart(const Named &a, const Named (&others)[N])
+{
+    for (const Named &o : others) TRY(check_apart(a, o));
+    return NETMAX_OK;
+}
+// The workspace, if the call needs one, lies apart from everything else.
+static Named workspace_at(const void *work, int64_t bytes) { return Named{"the workspace", Place(bytes ? work : nullptr, 1, 1, 1, bytes, 0, 0)}; }
+
 extern "C" int64_t netmax_linear_workspace(const netmax_linear_shape *s, const void *x, const void *w)
 {
     if (check_linear(s) != NETMAX_OK) return -1;
@@ -102,7 +123,15 @@ extern "C" int netmax_linear(const netmax_linear_shape *s, const void *x, const 
     TRY(check_matrix("z", z, false, d, s->batch, s->rows, s->d_out, s->ldz, s->sz, true));
     LinearArgs a = linear_args(s);
     a.x = x; a.w = w; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
-    TRY(check_work(work, work_bytes, linear_workspace(a)));
+    const int64_t need = linear_workspace(a), es = size_of(d);
+    TRY(check_work(work, work_bytes, need));
+    const Named in_x{"x", Place(x, es, s->batch, s->rows, s->d_in, s->ldx, s->sx)}, in_w{"w", Place(w, es, s->batch, s->d_in, s->d_out, s->ldw, s->sw)},
+        in_b{"bias", Place(bias, es, s->batch, 1, s->d_out, 0, s->sb)}, in_r{"residual", Place(residual, es, s->batch, s->rows, s->d_out, s->ldr, s->sr)},
+        out_y{"y", Place(y, es, s->batch, s->rows, s->d_out, s->ldy, s->sy)}, out_z{"z", Place(z, es, s->batch, s->rows, s->d_out, s->ldz, s->sz)};
+    TRY(check_apart(out_y, {in_x, in_w, in_b, out_z}));
+    if (!(out_y.at == in_r.at)) TRY(check_apart(out_y, in_r));       // value by value in place
+    TRY(check_apart(out_z, {in_x, in_w, in_b, in_r}));
+    TRY(check_apart(workspace_at(work, need), {in_x, in_w, in_b, in_r, out_y, out_z}));
     launch_linear((hipStream_t)stream, a, work);
     return launched("linear");
 }
@@ -140,7 +169,21 @@ extern "C" int netmax_linear_grad(const netmax_linear_shape *s, const void *dy, 
     TRY(check_matrix("db", db, false, d, s->batch, 1, s->d_out, s->d_out, s->sdb, true));
     LinearGradArgs a = linear_grad_args(s);
     a.dy = dy; a.x = x; a.w = w; a.z = z; a.dx = dx; a.dw = dw; a.db = db;
-    TRY(check_work(work, work_bytes, linear_grad_workspace(a)));
+    const int64_t need = linear_grad_workspace(a), es = size_of(d);
+    TRY(check_work(work, work_bytes, need));
+    const auto place = [&](const char *name, const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t step) { return Named{name, Place(p, es, s->batch, rows, cols, ld, step)}; };
+    // what the products read while results are written; with an activation dy and z are read before anything is
+    const bool late = s->act == NETMAX_ACT_NONE && (dx || dw);
+    const Named in_dy = place("dy", dy, s->rows, s->d_out, s->ldy, s->sy), in_z = place("z", s->act == NETMAX_ACT_NONE ? nullptr : z, s->rows, s->d_out, s->ldz, s->sz),
+        in_x = place("x", dw ? x : nullptr, s->rows, s->d_in, s->ldx, s->sx), in_w = place("w", dx ? w : nullptr, s->d_in, s->d_out, s->ldw, s->sw),
+        out_x = place("dx", dx, s->rows, s->d_in, s->lddx, s->sdx), out_w = place("dw", dw, s->d_in, s->d_out, s->lddw, s->sdw), out_b = place("db", db, 1, s->d_out, 0, s->sdb);
+    for (const Named *o : {&out_x, &out_w, &out_b}) {
+        if (late) TRY(check_apart(*o, in_dy));
+        TRY(check_apart(*o, {in_x, in_w}));
+    }
+    TRY(check_apart(out_x, {out_w, out_b}));
+    TRY(check_apart(out_w, out_b));
+    TRY(check_apart(workspace_at(work, need), {in_dy, in_z, in_x, in_w, out_x, out_w, out_b}));
     launch_linear_grad((hipStream_t)stream, a, work);
     return launched("linear gradient");
 }
@@ -184,7 +227,14 @@ extern "C" int netmax_orthogonalize(const netmax_orth_shape *s, const void *g, c
     TRY(check_matrix("out", out, true, s->dtype, s->batch, s->rows, s->cols, s->ldo, s->so, true));
     OrthArgs a = orth_args(s);
     a.g = g; a.m = m; a.m_out = m_out; a.out = out;
-    TRY(check_work(work, work_bytes, orth_workspace(a)));
+    const int64_t need = orth_workspace(a), es = size_of(s->dtype);
+    TRY(check_work(work, work_bytes, need));
+    // out is written when g and m have been read, m_out while they are
+    const Named in_g{"g", Place(g, es, s->batch, s->rows, s->cols, s->ldg, s->sg)}, in_m{"m", Place(m, 4, s->batch, s->rows, s->cols, s->ldm, s->sm)},
+        out_m{"m_out", Place(m_out, 4, s->batch, s->rows, s->cols, s->ldm, s->sm)}, out_u{"out", Place(out, es, s->batch, s->rows, s->cols, s->ldo, s->so)};
+    TRY(check_apart(out_m, {in_g, out_u}));
+    if (!(out_m.at == in_m.at)) TRY(check_apart(out_m, in_m));       // value by value in place
+    TRY(check_apart(workspace_at(work, need), {in_g, in_m, out_m, out_u}));
     launch_orth((hipStream_t)stream, a, work);
     return launched("orthogonalize");
 }
@@ -211,6 +261,14 @@ extern "C" int netmax_policy_loss(int64_t tokens, int64_t vocab, int32_t dtype, 
     if (tokens == 0) return NETMAX_OK;
     if (!old_logp || !advantage || !loss) return netmax_fail(NETMAX_EINVAL, "old_logp, advantage or loss is NULL");
     if (kl != 0.0f && !ref_logp) return netmax_fail(NETMAX_EINVAL, "a KL term needs ref_logp");
+    const auto each = [&](const char *name, const void *p) { return Named{name, Place(p, 4, 1, 1, tokens, 0, 0)}; };
+    const Named in_z{"logits", Place(logits, size_of(dtype), 1, tokens, vocab, ld, 0)}, out_g{"grad", Place(grad, size_of(dtype), 1, tokens, vocab, ldg, 0)},
+        out_l = each("loss", loss), out_p = each("logp", logp);
+    const Named in[] = {each("labels", labels), each("old_logp", old_logp), each("ref_logp", ref_logp), each("advantage", advantage), each("weight", weight)};
+    for (const Named *o : {&out_l, &out_p, &out_g}) TRY(check_apart(*o, in));
+    TRY(check_apart(out_l, {in_z, out_p, out_g}));
+    TRY(check_apart(out_p, {in_z, out_g}));
+    if (!(out_g.at == in_z.at)) TRY(check_apart(out_g, in_z));       // row by row in place
     const TokenRows rows{tokens, vocab, ld, logits, labels, weight, dtype == NETMAX_BF16};
     launch_policy_loss((hipStream_t)stream, rows, PolicyArgs{old_logp, ref_logp, advantage, clip_low, clip_high, kl, loss, logp, grad, ldg});
     return launched("policy loss");
@@ -232,7 +290,19 @@ extern "C" int netmax_preference_loss(int64_t tokens, int64_t vocab, int32_t dty
     if (pairs < 1 || pairs > 0x3FFFFFFF) return netmax_fail(NETMAX_EINVAL, "need 1 <= pairs < 2^30");
     if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return netmax_fail(NETMAX_EINVAL, "need 0 <= smoothing <= 1");
     if (!offsets || !loss || !ratio || (tokens > 0 && !ref_logp)) return netmax_fail(NETMAX_EINVAL, "offsets, ref_logp, loss or ratio is NULL");
-    TRY(check_work(work, work_bytes, netmax_preference_workspace(tokens, pairs)));
+    const int64_t need = netmax_preference_workspace(tokens, pairs);
+    TRY(check_work(work, work_bytes, need));
+    const auto each = [&](const char *name, const void *p, int64_t n) { return Named{name, Place(p, 4, 1, 1, n, 0, 0)}; };
+    const Named in_z{"logits", Place(logits, size_of(dtype), 1, tokens, vocab, ld, 0)}, out_g{"grad", Place(grad, size_of(dtype), 1, tokens, vocab, ldg, 0)},
+        out_l = each("loss", loss, pairs), out_r = each("ratio", ratio, 2 * pairs);
+    const Named in[] = {each("labels", labels, tokens), each("offsets", offsets, 2 * pairs + 1), each("weight", weight, tokens), each("ref_logp", ref_logp, tokens)};
+    for (const Named *o : {&out_l, &out_r, &out_g}) TRY(check_apart(*o, in));
+    TRY(check_apart(out_l, {in_z, out_r, out_g}));
+    TRY(check_apart(out_r, {in_z, out_g}));
+    if (!(out_g.at == in_z.at)) TRY(check_apart(out_g, in_z));       // row by row in place
+    const Named space = workspace_at(work, need);
+    TRY(check_apart(space, in));
+    TRY(check_apart(space, {in_z, out_l, out_r, out_g}));
     char *w = (char *)work;
     const TokenRows rows{tokens, vocab, ld, logits, labels, weight, dtype == NETMAX_BF16};
     launch_preference_loss((hipStream_t)stream, rows,

@@ -1,0 +1,53 @@
+"""Tensors that share memory in the operators for language models: refused where the call would race, the same results where it does not."""
+import pytest
+import torch
+
+import paper_2009_05766_amd as nm
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def normal(g, *shape, dtype=F32, scale=1.0):
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_shared_memory_is_refused(dtype):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy, z = (normal(g, 128, 128, dtype=dtype) for _ in range(4))
+    kept = [t.clone() for t in (x, w, dy, z)]
+    f, labels = torch.zeros(128, device="cuda"), torch.zeros(128, dtype=torch.int32, device="cuda")
+    for call in (lambda: nm.netmax_linear(x, w, y=x), lambda: nm.netmax_linear(x, w, y=w), lambda: nm.netmax_linear(x, w, y=dy, z=dy), lambda: nm.netmax_linear(x[:64], w, y=x[63:127]),
+                 lambda: nm.netmax_linear(x, w, None, dy, z=dy), lambda: nm.netmax_linear(x[:127], w, None, dy[1:], y=dy[:127]),
+                 lambda: nm.netmax_linear_grad(dy, x, w, dx=dy), lambda: nm.netmax_linear_grad(dy, x, w, dw=dy), lambda: nm.netmax_linear_grad(dy, x, w, z, act="gelu", dx=x),
+                 lambda: nm.netmax_linear_grad(dy, x, w, z, act="gelu", dw=w), lambda: nm.netmax_linear_grad(dy, x, w, dx=z, dw=z),
+                 lambda: nm.netmax_policy_loss(x[:64], labels[:64], f[:64], f[:64], grad=x[1:65])):
+        with pytest.raises(nm.NetmaxError) as e:
+            call()
+        assert e.value.code == nm.NETMAX_EINVAL and "share memory" in str(e.value)
+    assert all(torch.equal(a, b) for a, b in zip((x, w, dy, z), kept))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_memory_that_may_be_shared(dtype):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n = 200
+    x, w, dy = normal(g, n, n, dtype=dtype), normal(g, n, n, dtype=dtype, scale=n ** -0.5), normal(g, n, n, dtype=dtype)
+    y, z = nm.netmax_linear(x, w, act="gelu", keep_preact=True)
+    want = nm.netmax_linear_grad(dy, x, w, z, act="gelu")
+    a, b = dy.clone(), z.clone()
+    got = nm.netmax_linear_grad(a, x, w, b, act="gelu", dx=a, dw=b)             # over dy and z, which have been read
+    assert got[0] is a and all(torch.equal(p, q) for p, q in zip(got, want))
+    a, alone = x.clone(), nm.netmax_linear_grad(dy, x, w, z, act="gelu", need_weight=False)[0]
+    assert torch.equal(nm.netmax_linear_grad(dy, a, w, z, act="gelu", need_weight=False, dx=a)[0], alone)
+    # columns of one wide matrix
+    wide = torch.full((n, 3 * n + 8), 5.0, device="cuda", dtype=dtype)
+    wide[:, :n] = x
+    assert torch.equal(nm.netmax_linear(wide[:, :n], w, act="gelu", y=wide[:, n:2 * n], z=wide[:, 2 * n:3 * n])[0], y)
+    assert torch.equal(wide[:, :n], x) and torch.equal(wide[:, 2 * n:3 * n], z) and bool((wide[:, 3 * n:] == 5.0).all())
+    # an update over the gradient, a few rows further on
+    u = normal(g, n + 3, n, dtype=dtype)
+    want = nm.netmax_orthogonalize(u[:n].clone())
+    assert torch.equal(nm.netmax_orthogonalize(u[:n], out=u[3:]), want)
