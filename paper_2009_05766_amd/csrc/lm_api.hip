@@ -19,7 +19,8 @@ static int launched(const char *what)
 }
 
 static bool dtype_known(int32_t d) { return d == NETMAX_F32 || d == NETMAX_BF16; }
-static bool aligned(const void *p, int32_t dtype) { return (uintptr_t)p % (dtype == NETMAX_BF16 ? 2 : 4) == 0; }
+static int64_t size_of(int32_t dtype) { return dtype == NETMAX_BF16 ? 2 : 4; }
+static bool aligned(const void *p, int32_t dtype) { return (uintptr_t)p % size_of(dtype) == 0; }
 
 // Sizes that keep every product of them, in bytes, far inside 64 bits.
 constexpr int64_t MOST = (int64_t)1 << 40;
@@ -48,7 +49,7 @@ static int check_linear(const netmax_linear_shape *s)
     return NETMAX_OK;
 }
 
-// `written`: results of a batch need a place each.
+// `written`: results of a batch need memory of their own each.
 static int check_matrix(const char *name, const void *p, bool needed, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t step, bool written = false)
 {
     char buf[160];
@@ -57,7 +58,8 @@ static int check_matrix(const char *name, const void *p, bool needed, int32_t dt
         snprintf(buf, sizeof buf, "%s is NULL", name);
         return netmax_fail(NETMAX_EINVAL, buf);
     }
-    if (aligned(p, dtype) && strides_ok(batch, rows, cols, ld, step) && !(written && batch > 1 && step == 0)) return NETMAX_OK;
+    if (aligned(p, dtype) && strides_ok(batch, rows, cols, ld, step) &&
+        !(written && batch > 1 && (step == 0 || batch_overlaps(Place(p, size_of(dtype), batch, rows, cols, ld, step))))) return NETMAX_OK;
     snprintf(buf, sizeof buf, "%s: misaligned, or rows closer together than they are long, or a negative stride, or results in the same place", name);
     return netmax_fail(NETMAX_EINVAL, buf);
 }
@@ -84,7 +86,6 @@ static int check_work(const void *work, int64_t have, int64_t need)
 // ---- memory that a call writes: nothing that it still reads, and nothing twice ---------------------------------------
 
 struct Named { const char *name; Place at; };
-static int64_t size_of(int32_t dtype) { return dtype == NETMAX_BF16 ? 2 : 4; }
 
 static int check_apart(const Named &a, const Named &b)
 {

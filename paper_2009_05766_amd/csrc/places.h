@@ -87,4 +87,13 @@ inline bool share_memory(const Place &a, const Place &b)
     return false;
 }
 
+// Whether matrices of one batch have a byte in common (their rows do not).
+inline bool batch_overlaps(const Place &a)
+{
+    int64_t left = MOST_COMPARISONS;
+    for (int64_t n = 1; n < a.batch && n * a.step < a.span(); ++n)
+        if (matrices_share(a, a, n * a.step, left)) return true;
+    return false;
+}
+
 }  // namespace netmax

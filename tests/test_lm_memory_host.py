@@ -77,3 +77,25 @@ APART = [
 def test_what_lies_apart_is_launched(call, k):
     (status, error, launches), = call(APART[k])
     assert status == nm.NETMAX_OK and error == "" and len(launches) >= 1
+
+
+OVERLAPPING = [
+    (linear(64, 128, 128, batch=3, sy=1), "y"), (linear(64, 128, 128, batch=3, sy=64 * 128 - 1), "y"), (linear(64, 128, 128, batch=3, z=at(3), sz=100), "z"),
+    (linear(64, 32, 32, batch=4, ldy=128, sy=31), "y"), (linear(64, 32, 32, batch=5, ldy=128, sy=32), "y"),
+    (grad(64, 128, 128, batch=3, sdx=128), "dx"), (grad(64, 128, 128, batch=3, sdw=4), "dw"), (grad(64, 128, 128, batch=3, sdb=127), "db"),
+    (orth(96, 64, batch=2, so=64), "out"), (orth(96, 64, batch=2, sm=64, m_out=at(5)), "m_out"),
+]
+
+
+@pytest.mark.parametrize("k", range(len(OVERLAPPING)), ids=[f"{c[0]}-{name}-{k}" for k, (c, name) in enumerate(OVERLAPPING)])
+def test_results_of_a_batch_that_overlap_are_refused(call, k):
+    c, name = OVERLAPPING[k]
+    (status, error, launches), = call(c)
+    assert status == nm.NETMAX_EINVAL and error.startswith(name + ":") and error.endswith("results in the same place") and launches == []
+
+
+@pytest.mark.parametrize("c", [linear(64, 32, 32, batch=4, ldy=128, sy=32), linear(1, 32, 32, batch=4, ldy=1, sy=32), linear(64, 32, 32, batch=4, ldy=32, sy=64 * 32, ldx=128, sx=0),
+                               grad(64, 32, 32, batch=3, lddw=96, sdw=32, sdb=32), orth(8, 4, batch=3, ldo=12, so=4)], ids=lambda c: c[0])
+def test_results_of_a_batch_that_interleave_are_written(call, c):
+    (status, error, launches), = call(c)
+    assert status == nm.NETMAX_OK and len(launches) >= 1
