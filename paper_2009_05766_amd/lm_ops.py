@@ -44,16 +44,6 @@ def _first(name: str, t, dims: Tuple[int, ...]):
         _refuse(f"{name} is {t.dtype}: float32 or bfloat16 is needed")
 
 
-def _written(name: str, t: torch.Tensor):
-    """Refuses outputs some of whose elements share memory (a broadcast one): their writes would race."""
-    for n, s in zip(t.shape[:-1], t.stride()[:-1]):
-        if n > 1 and s < t.shape[-1]:
-            _refuse(f"rows of the output {name} overlap")
-    if t.dim() == 3 and t.shape[0] > 1 and t.shape[1] > 1 and t.shape[2] > 0 and t.stride(0) < (t.shape[1] - 1) * t.stride(1) + t.shape[2] \
-            and t.stride(1) < (t.shape[0] - 1) * t.stride(0) + t.shape[2]:
-        _refuse(f"matrices of the output {name} overlap")
-
-
 def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -114,9 +104,9 @@ def netmax_linear(x, w, bias=None, residual=None, *, act: str = "none", keep_pre
     if y is None:
         y = torch.empty((*lead, rows, d_out), dtype=dt, device=x.device)
     else:
-        _written("y", _check_tensor("y", y, x, (*lead, rows, d_out), dt))
+        _check_tensor("y", y, x, (*lead, rows, d_out), dt)
     if z is not None:
-        _written("z", _check_tensor("z", z, x, (*lead, rows, d_out), dt))
+        _check_tensor("z", z, x, (*lead, rows, d_out), dt)
     elif keep_preact:
         z = torch.empty((*lead, rows, d_out), dtype=dt, device=x.device)
     ldx, sx = _strides(x)
@@ -150,7 +140,7 @@ def netmax_linear_grad(dy, x, w, z=None, *, act: str = "none", need_input: bool 
 
     def output(name, t, needed, shape):
         if t is not None:
-            _written(name, _check_tensor(name, t, x, shape, dt))
+            _check_tensor(name, t, x, shape, dt)
             return t
         return torch.empty(shape, dtype=dt, device=dev) if needed else None
 
@@ -181,7 +171,6 @@ def netmax_orthogonalize(g, m=None, *, m_out=None, out=None, mu: float = 0.95, n
     if m is not None:
         _check_tensor("m", m, g, g.shape, torch.float32)
         m_out = m if m_out is None else _check_tensor("m_out", m_out, g, g.shape, torch.float32)
-        _written("m_out", m_out)
         if m_out.stride() != m.stride():
             _refuse("m_out must have the strides of m")
     elif m_out is not None:
@@ -189,7 +178,7 @@ def netmax_orthogonalize(g, m=None, *, m_out=None, out=None, mu: float = 0.95, n
     if out is None:
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
     else:
-        _written("out", _check_tensor("out", out, g, g.shape, g.dtype))
+        _check_tensor("out", out, g, g.shape, g.dtype)
     ldg, sg = _strides(g)
     ldm, sm = _strides(m)
     ldo, so = _strides(out)
@@ -212,7 +201,7 @@ def _token_rows(logits, labels, weight, grad, need_grad):
     if weight is not None:
         _check_tensor("weight", weight, logits, (tokens,), torch.float32)
     if grad is not None:
-        _written("grad", _check_tensor("grad", grad, logits, logits.shape, logits.dtype))
+        _check_tensor("grad", grad, logits, logits.shape, logits.dtype)
     elif need_grad:
         grad = torch.empty_like(logits) if dense else torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
     return tokens, vocab, grad

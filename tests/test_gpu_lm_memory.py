@@ -51,3 +51,21 @@ def test_memory_that_may_be_shared(dtype):
     u = normal(g, n + 3, n, dtype=dtype)
     want = nm.netmax_orthogonalize(u[:n].clone())
     assert torch.equal(nm.netmax_orthogonalize(u[:n], out=u[3:]), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_results_that_interleave(dtype):
+    """Rows of one matrix of a batch between those of another, in no order: each where it belongs, nothing beside them touched."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w = normal(g, 3, 2, 8, dtype=dtype), normal(g, 3, 8, 4, dtype=dtype)
+    room = torch.full((80,), 5.0, device="cuda", dtype=dtype)
+    y = room.as_strided((3, 2, 4), (20, 30, 1))                                 # rows at 0 30, 20 50, 40 70
+    want = nm.netmax_linear(x, w)
+    assert nm.netmax_linear(x, w, y=y) is y and torch.equal(y, want)
+    left = torch.ones(80, dtype=torch.bool, device="cuda")
+    left.as_strided((3, 2, 4), (20, 30, 1)).fill_(False)
+    assert bool((room[left] == 5.0).all()) and int(left.sum()) == 56
+    for bad in (room.as_strided((3, 2, 4), (0, 4, 1)), room.as_strided((3, 2, 4), (8, 3, 1)), room.as_strided((3, 2, 4), (6, 4, 1))):
+        with pytest.raises(nm.NetmaxError) as e:
+            nm.netmax_linear(x, w, y=bad)
+        assert e.value.code == nm.NETMAX_EINVAL
