@@ -1,7 +1,10 @@
 """The operators for language models on PyTorch tensors: one function for each C entry point of include/netmax.h, with the same name.
 
 Tensors live on one GPU, with the values of a row next to each other (any distance between rows and matrices); outputs that are not given
-are allocated.  The work is enqueued on the tensors' device, on its current stream; workspaces come from torch's allocator on that stream."""
+are allocated.  The work is enqueued on the tensors' device, on its current stream; workspaces come from torch's allocator on that stream.
+
+Gradients are calls of their own (`netmax_linear_grad`; the losses return theirs), and nothing is recorded for torch's automatic differentiation: tensors
+that require a gradient are refused while it records, rather than left without one.  Memory that a call writes counts as changed in place."""
 from __future__ import annotations
 
 import ctypes as C
@@ -20,9 +23,16 @@ def _refuse(text: str):
     raise NetmaxError(NETMAX_EINVAL, text)
 
 
+def _no_graph(name: str):
+    if torch.is_grad_enabled():
+        _refuse(f"{name} requires a gradient, which this call does not record: call it under torch.no_grad() or with a detached tensor")
+
+
 def _check_tensor(name: str, t, like: torch.Tensor, shape: Tuple[int, ...], dtype: torch.dtype) -> torch.Tensor:
     # what is right takes one look; what is wrong is looked at closely
     if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == like.get_device() and t.shape == shape and (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] <= 1):
+        if t.requires_grad:
+            _no_graph(name)
         return t
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} must be a tensor")
@@ -42,6 +52,15 @@ def _first(name: str, t, dims: Tuple[int, ...]):
         _refuse(f"{name} has {t.dim()} dimensions")
     if t.dtype not in _DTYPES:
         _refuse(f"{name} is {t.dtype}: float32 or bfloat16 is needed")
+    if t.requires_grad:
+        _no_graph(name)
+
+
+def _changed(*outputs):
+    """The caller's tensors that a call has written, for whoever saved them before."""
+    for t in outputs:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
 
 
 def _p(t: Optional[torch.Tensor]):
@@ -101,6 +120,7 @@ def netmax_linear(x, w, bias=None, residual=None, *, act: str = "none", keep_pre
         _check_tensor("bias", bias, x, (*lead, d_out), dt)
     if residual is not None:
         _check_tensor("residual", residual, x, (*lead, rows, d_out), dt)
+    given = (y, z)
     if y is None:
         y = torch.empty((*lead, rows, d_out), dtype=dt, device=x.device)
     else:
@@ -119,6 +139,7 @@ def netmax_linear(x, w, bias=None, residual=None, *, act: str = "none", keep_pre
     lib, ref = load(), C.byref(shape)
     work = _workspace(lib.netmax_linear_workspace(ref, _p(x), _p(w)), x.device)
     _call(lib.netmax_linear, x.device, ref, _p(x), _p(w), _p(bias), _p(residual), _p(y), _p(z), _p(work), 0 if work is None else work.numel())
+    _changed(*given)
     return (y, z) if keep_preact or z is not None else y
 
 
@@ -144,6 +165,7 @@ def netmax_linear_grad(dy, x, w, z=None, *, act: str = "none", need_input: bool 
             return t
         return torch.empty(shape, dtype=dt, device=dev) if needed else None
 
+    given = (dx, dw, db)
     dx = output("dx", dx, need_input, (*lead, rows, d_in))
     dw = output("dw", dw, need_weight, (*lead, d_in, d_out))
     db = output("db", db, need_bias, (*lead, d_out))
@@ -159,6 +181,7 @@ def netmax_linear_grad(dy, x, w, z=None, *, act: str = "none", need_input: bool 
     lib, ref = load(), C.byref(shape)
     work = _workspace(lib.netmax_linear_grad_workspace(ref, _p(dy), _p(x), _p(w)), dev)
     _call(lib.netmax_linear_grad, dev, ref, _p(dy), _p(x), _p(w), _p(z), _p(dx), _p(dw), _p(db), _p(work), 0 if work is None else work.numel())
+    _changed(*given)
     return dx, dw, db
 
 
@@ -175,6 +198,7 @@ def netmax_orthogonalize(g, m=None, *, m_out=None, out=None, mu: float = 0.95, n
             _refuse("m_out must have the strides of m")
     elif m_out is not None:
         _refuse("m_out without m")
+    given = (out, m_out)
     if out is None:
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
     else:
@@ -188,10 +212,12 @@ def netmax_orthogonalize(g, m=None, *, m_out=None, out=None, mu: float = 0.95, n
     lib, ref = load(), C.byref(shape)
     work = _workspace(lib.netmax_orthogonalize_workspace(ref), g.device)
     _call(lib.netmax_orthogonalize, g.device, ref, _p(g), _p(m), _p(m_out), _p(out), _p(work), 0 if work is None else work.numel())
+    _changed(*given)
     return out
 
 
 def _token_rows(logits, labels, weight, grad, need_grad):
+    given = grad
     _first("logits", logits, (2,))
     tokens, vocab = logits.shape
     dense = logits.is_contiguous()
@@ -204,13 +230,13 @@ def _token_rows(logits, labels, weight, grad, need_grad):
         _check_tensor("grad", grad, logits, logits.shape, logits.dtype)
     elif need_grad:
         grad = torch.empty_like(logits) if dense else torch.empty((tokens, vocab), dtype=logits.dtype, device=logits.device)
-    return tokens, vocab, grad
+    return tokens, vocab, grad, given
 
 
 def netmax_policy_loss(logits, labels, old_logp, advantage, weight=None, *, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0,
                        need_grad: bool = True, grad=None):
     """The clipped policy loss of sampled tokens: (loss [tokens], log probabilities [tokens], gradient of the sum of all losses by the logits or None)."""
-    tokens, vocab, grad = _token_rows(logits, labels, weight, grad, need_grad)
+    tokens, vocab, grad, given = _token_rows(logits, labels, weight, grad, need_grad)
     dev = logits.device
     for name, t in (("old_logp", old_logp), ("advantage", advantage), ("ref_logp", ref_logp)):
         if t is not None or name != "ref_logp":
@@ -218,6 +244,7 @@ def netmax_policy_loss(logits, labels, old_logp, advantage, weight=None, *, ref_
     loss, logp = torch.empty_like(old_logp), torch.empty_like(old_logp)
     _call(load().netmax_policy_loss, dev, tokens, vocab, _DTYPES[logits.dtype], _p(logits), logits.stride(0), _p(labels), _p(old_logp), _p(ref_logp),
           _p(advantage), _p(weight), clip_low, clip_high, kl, _p(loss), _p(logp), _p(grad), 0 if grad is None else grad.stride(0))
+    _changed(given)
     return loss, logp, grad
 
 
@@ -225,7 +252,7 @@ def netmax_preference_loss(logits, labels, offsets, weight=None, ref_logp=None, 
                            scale: Optional[float] = None, need_grad: bool = True, grad=None):
     """The loss of paired log ratios: (loss [pairs], log ratios [2 pairs], gradient of the sum of all losses by the logits or None).
     offsets: int32 [2 pairs + 1], chosen and rejected sequences in turn; scale defaults to 1 / pairs."""
-    tokens, vocab, grad = _token_rows(logits, labels, weight, grad, need_grad)
+    tokens, vocab, grad, given = _token_rows(logits, labels, weight, grad, need_grad)
     dev = logits.device
     if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 3 or offsets.shape[0] % 2 == 0:
         _refuse("offsets must hold 2 pairs + 1 numbers, for at least one pair")
@@ -239,4 +266,5 @@ def netmax_preference_loss(logits, labels, offsets, weight=None, ref_logp=None, 
     _call(lib.netmax_preference_loss, dev, tokens, vocab, _DTYPES[logits.dtype], _p(logits), logits.stride(0), _p(labels), pairs, _p(offsets), _p(ref_logp),
           _p(weight), beta, smoothing, 1.0 / pairs if scale is None else scale, _p(loss), _p(ratio), _p(grad), 0 if grad is None else grad.stride(0),
           _p(work), 0 if work is None else work.numel())
+    _changed(given)
     return loss, ratio, grad
