@@ -467,6 +467,7 @@ inline bool fits16(const void *p, int64_t ld, int64_t step, int64_t stored)
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && step % 8 == 0 && stored % 8 == 0 && ld < (1 << 22);
 }
 
+// Three pairs of orientations: where A's contraction index is not near, neither is B's.
 template <typename V, int BM, int BN, int WM, int WN, int STEP, int STAGES, int GROUPS, class Epilogue>
 void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, uint32_t splits,
                           const Epilogue &e)
@@ -475,7 +476,6 @@ void launch_gemm16_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, in
     const dim3 grid((uint32_t)(batch * mb * nb * splits)), block(WM * WN * 64 * GROUPS);
     if (ak && bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, true, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
     else if (ak) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, true, false, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
-    else if (bk) gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, true, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
     else gemm16_kernel<V, BM, BN, WM, WN, STEP, STAGES, GROUPS, false, false, false, false><<<grid, block, 0, s>>>(M, N, K, a, b, mb, nb, splits, e);
 }
 

@@ -1,4 +1,4 @@
-// C = A B for operands of any type, shape, stride and orientation, multiplied in float on v_mfma_f32_32x32x2_f32.
+// C = A B for float operands of any shape and stride on v_mfma_f32_32x32x2_f32.
 //
 // Four waves have a block of BM x BN results; a step of STEP contraction indices lies in LDS as [k][m] and [k][n], the instruction's own layout (lane
 // l: row l % 32, index l / 32), while the next step is on its way in registers.  Where blocks are few, GROUPS groups of four waves share a block's
@@ -12,11 +12,11 @@
 namespace netmax {
 
 // The values of one step that a thread brings: pieces of four neighbours in memory.
-template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
+template <int ROWS, int STEP, bool K_NEAR> struct StepPieces {
     static constexpr int PIECES = ROWS * STEP / 4 / 256;
     static constexpr int PITCH = ROWS + 4;
     f32x4 v[PIECES];
-    __device__ __forceinline__ void request(const T *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K)
+    __device__ __forceinline__ void request(const float *p, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t K)
     {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
@@ -50,12 +50,12 @@ template <typename T, int ROWS, int STEP, bool K_NEAR> struct StepPieces {
 template <int BM, int BN, int STEP, int GROUPS> constexpr int space_f32() { return GROUPS * 2 * STEP * (BM + BN + 8); }
 
 // Workgroup `id`; `space`: space_f32() floats of LDS.
-template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
-__device__ __forceinline__ void gemm_f32_block(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
+template <int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
+__device__ __forceinline__ void gemm_f32_block(int64_t M, int64_t N, int64_t K, const float *__restrict__ A, int64_t lda, int64_t sa, const float *__restrict__ B, int64_t ldb,
                                                int64_t sb, uint32_t mblocks, uint32_t nblocks, const Epilogue &epilogue, uint32_t id, float *space)
 {
-    typedef StepPieces<T, BM, STEP, AK> PiecesA;
-    typedef StepPieces<T, BN, STEP, BK> PiecesB;
+    typedef StepPieces<BM, STEP, AK> PiecesA;
+    typedef StepPieces<BN, STEP, BK> PiecesB;
     // a wave has TM x TN squares of 32 x 32 results; SHARES waves of a group share a square and the indices of a step
     constexpr int TM = BM >= 128 ? 2 : 1, TN = BN >= 128 ? 2 : 1, ACROSS = BN / 32 / TN, TILES = BM / 32 / TM * ACROSS, SHARES = 4 / TILES, PARTS = GROUPS * SHARES;
     constexpr int STEP_FLOATS = STEP * (PiecesA::PITCH + PiecesB::PITCH);
@@ -151,13 +151,13 @@ __device__ __forceinline__ void gemm_f32_block(int64_t M, int64_t N, int64_t K, 
         }
 }
 
-template <typename T, int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
+template <int BM, int BN, int STEP, int GROUPS, bool AK, bool BK, class Epilogue>
 __global__ void __launch_bounds__(256 * GROUPS)
-gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const T *__restrict__ A, int64_t lda, int64_t sa, const T *__restrict__ B, int64_t ldb,
+gemm_f32_kernel(int64_t M, int64_t N, int64_t K, const float *__restrict__ A, int64_t lda, int64_t sa, const float *__restrict__ B, int64_t ldb,
                 int64_t sb, uint32_t mblocks, uint32_t nblocks, Epilogue epilogue)
 {
     __shared__ __align__(16) float space[space_f32<BM, BN, STEP, GROUPS>()];
-    gemm_f32_block<T, BM, BN, STEP, GROUPS, AK, BK>(M, N, K, A, lda, sa, B, ldb, sb, mblocks, nblocks, epilogue, blockIdx.x, space);
+    gemm_f32_block<BM, BN, STEP, GROUPS, AK, BK>(M, N, K, A, lda, sa, B, ldb, sb, mblocks, nblocks, epilogue, blockIdx.x, space);
 }
 
 // Two products in one launch, the first with both contraction indices near and the second with both row indices near (a layer's dx and dw).  Workgroups from
@@ -170,38 +170,37 @@ __global__ void __launch_bounds__(256 * GROUPS) gemm_f32_pair_kernel(ProductF32<
     __shared__ __align__(16) float space[space_f32<BM, BM, STEP, GROUPS>()];
     const uint32_t id = pair_place(blockIdx.x, first, both, swap);
     if (id < first)
-        gemm_f32_block<float, BM, BM, STEP, GROUPS, true, true>(p.M, p.N, p.K, p.A, p.lda, p.sa, p.B, p.ldb, p.sb, p.mblocks, p.nblocks, p.epilogue, id, space);
+        gemm_f32_block<BM, BM, STEP, GROUPS, true, true>(p.M, p.N, p.K, p.A, p.lda, p.sa, p.B, p.ldb, p.sb, p.mblocks, p.nblocks, p.epilogue, id, space);
     else if (id < both)
-        gemm_f32_block<float, BM, BM, STEP, GROUPS, false, false>(q.M, q.N, q.K, q.A, q.lda, q.sa, q.B, q.ldb, q.sb, q.mblocks, q.nblocks, q.epilogue, id - first, space);
+        gemm_f32_block<BM, BM, STEP, GROUPS, false, false>(q.M, q.N, q.K, q.A, q.lda, q.sa, q.B, q.ldb, q.sb, q.mblocks, q.nblocks, q.epilogue, id - first, space);
     else
         extra(id - both, space);
 }
 
-template <typename T, int BM, int BN, int STEP, int GROUPS, class Epilogue>
+// An operator's products have one of three pairs of orientations: A's contraction index is near in the first two, and where it is not, neither is B's.
+template <int BM, int BN, int STEP, int GROUPS, class Epilogue>
 void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {
     const uint32_t mb = (uint32_t)((M + BM - 1) / BM), nb = (uint32_t)((N + BN - 1) / BN);
     const dim3 grid((uint32_t)(batch * mb * nb));
-    const T *pa = (const T *)a.p, *pb = (const T *)b.p;
+    const float *pa = (const float *)a.p, *pb = (const float *)b.p;
     if (a.k_near && b.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
+        gemm_f32_kernel<BM, BN, STEP, GROUPS, true, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
     else if (a.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, true, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
-    else if (b.k_near)
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, true><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
+        gemm_f32_kernel<BM, BN, STEP, GROUPS, true, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
     else
-        gemm_f32_kernel<T, BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
+        gemm_f32_kernel<BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
 }
 
-template <typename T, class Epilogue>
+template <class Epilogue>
 void launch_gemm_f32(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {
     const auto blocks = [&](int64_t m, int64_t n) { return batch * ((M + m - 1) / m) * ((N + n - 1) / n); };
     // blocks of 128 where they are many and the contraction pays for their start; the fewer blocks, the more waves on each
-    if (blocks(128, 128) >= 256 && K >= 256 && worth_blocks(128, M, N)) launch_gemm_f32_blocks<T, 128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
-    else if (blocks(64, 64) >= 512) launch_gemm_f32_blocks<T, 64, 64, 32, 1>(s, batch, M, N, K, a, b, epilogue);
-    else if (blocks(64, 64) > 128) launch_gemm_f32_blocks<T, 64, 64, 32, 4>(s, batch, M, N, K, a, b, epilogue);
-    else launch_gemm_f32_blocks<T, 64, 32, 32, 4>(s, batch, M, N, K, a, b, epilogue);
+    if (blocks(128, 128) >= 256 && K >= 256 && worth_blocks(128, M, N)) launch_gemm_f32_blocks<128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
+    else if (blocks(64, 64) >= 512) launch_gemm_f32_blocks<64, 64, 32, 1>(s, batch, M, N, K, a, b, epilogue);
+    else if (blocks(64, 64) > 128) launch_gemm_f32_blocks<64, 64, 32, 4>(s, batch, M, N, K, a, b, epilogue);
+    else launch_gemm_f32_blocks<64, 32, 32, 4>(s, batch, M, N, K, a, b, epilogue);
 }
 
 }  // namespace netmax

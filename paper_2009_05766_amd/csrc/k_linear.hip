@@ -119,15 +119,20 @@ static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, bool a
 }
 
 template <class Epilogue>
-static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, int splits,
-                            const Epilogue &e)
+static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, const Epilogue &e)
 {
-    const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block) * splits;
-    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else if (blocks > 256 || K < 512 * splits) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, splits, e);
-    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2>(s, batch, M, N, K, a, ak, b, bk, splits, e);
+    const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block);
+    if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+    else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+    else if (blocks > 256 || K < 512) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+}
+// Shares of a contraction: at most 256 workgroups in all, each with 16 steps or more.
+static void launch_parts16(hipStream_t s, const Plan16 &p, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, const PartEpilogue &e)
+{
+    if (p.block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, (uint32_t)p.splits, e);
+    else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2>(s, batch, M, N, K, a, ak, b, bk, (uint32_t)p.splits, e);
 }
 
 // `work`: part_bytes() of it.
@@ -140,11 +145,11 @@ static void launch_product16(hipStream_t s, int64_t batch, int64_t M, int64_t N,
     }
     const Plan16 p = plan16(batch, M, N, K);
     if (p.splits == 1) {
-        launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, 1, e);
+        launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, e);
         return;
     }
     const int64_t wide = round_up(N, 4), quads = batch * M * wide / 4;
-    launch_blocks16(s, p.block, batch, M, N, K, a, ak, b, bk, p.splits, PartEpilogue{M, N, wide, (float *)work});
+    launch_parts16(s, p, batch, M, N, K, a, ak, b, bk, PartEpilogue{M, N, wide, (float *)work});
     join_parts_kernel<<<(uint32_t)((quads + 255) / 256 < 2048 ? (quads + 255) / 256 : 2048), 256, 0, s>>>(batch, M, wide, p.splits, (const float *)work, e);
 }
 
@@ -323,7 +328,7 @@ int64_t linear_workspace(const LinearArgs &a)
 void launch_linear(hipStream_t s, const LinearArgs &a, void *work)
 {
     if (!a.bf16) {
-        launch_gemm_f32<float>(s, a.batch, a.rows, a.dout, a.din, Operand{a.x, a.ldx, a.sx, true}, Operand{a.w, a.ldw, a.sw, false}, forward_epilogue<float>(a));
+        launch_gemm_f32(s, a.batch, a.rows, a.dout, a.din, Operand{a.x, a.ldx, a.sx, true}, Operand{a.w, a.ldw, a.sw, false}, forward_epilogue<float>(a));
         return;
     }
     char *at = (char *)work;
@@ -387,10 +392,10 @@ void launch_linear_grad(hipStream_t s, const LinearGradArgs &a, void *work)
         if (a.dx && a.dw && a.rows > 0 && launch_pair32(s, a, d, ldd, sd, bias)) return;
         launch_bias(s, bias);
         if (a.dx && a.rows > 0)
-            launch_gemm_f32<float>(s, a.batch, a.rows, a.din, a.dout, Operand{d, ldd, sd, true}, Operand{a.w, a.ldw, a.sw, true},
+            launch_gemm_f32(s, a.batch, a.rows, a.din, a.dout, Operand{d, ldd, sd, true}, Operand{a.w, a.ldw, a.sw, true},
                                    plain_epilogue<float>(a.rows, a.din, a.dx, a.lddx, a.sdx));
         if (a.dw)
-            launch_gemm_f32<float>(s, a.batch, a.din, a.dout, a.rows, Operand{a.x, a.ldx, a.sx, false}, Operand{d, ldd, sd, false},
+            launch_gemm_f32(s, a.batch, a.din, a.dout, a.rows, Operand{a.x, a.ldx, a.sx, false}, Operand{d, ldd, sd, false},
                                    plain_epilogue<float>(a.din, a.dout, a.dw, a.lddw, a.sdw));
         return;
     }

@@ -2,6 +2,7 @@
 // library), so that the C entry points run their host code and launches are printed.  Addresses are numbers that nothing follows.
 //   lm_calls_driver libnetmax.so < calls
 // A call is a line: linear, grad, orth, policy or preference, then name=number for members of its shape struct and its arguments; what is not named is 0.
+// The line "kernels" is answered by all kernels of the library.
 // work=ADDRESS comes with the size that the call's workspace function gives.  A line of output: status, '|', text of the error, '|', launches as
 // name<template arguments>@workgroups, without spaces.
 #include <hip/hip_runtime_api.h>
@@ -23,11 +24,13 @@ static size_t g_shared;
 static hipStream_t g_stream;
 static std::ostringstream g_out;
 
-// "void netmax::name<...>(...)" as name<...>
-static std::string plain_name(const char *mangled)
+// "void netmax::name<...>(...)" as name<...>; 16-bit types that the demangler may not know by names that it does
+static std::string plain_name(std::string mangled)
 {
+    for (const auto &[from, to] : {std::pair<std::string, std::string>("DF16b", "u6__bf16"), {"DF16_", "Dh"}})
+        for (size_t at; (at = mangled.find(from)) != std::string::npos;) mangled.replace(at, from.size(), to);
     int status = 0;
-    char *whole = abi::__cxa_demangle(mangled, nullptr, nullptr, &status);
+    char *whole = abi::__cxa_demangle(mangled.c_str(), nullptr, nullptr, &status);
     const std::string s(whole ? whole : mangled);
     free(whole);
     const size_t from = s.find("netmax::");
@@ -87,6 +90,8 @@ int main(int argc, char **argv)
         const auto i = [&](const char *name) { return reinterpret_cast<int32_t *>((uintptr_t)v[name]); };
         g_out.str("");
         int rc = -100;
+        if (op == "kernels")
+            for (const auto &k : g_names) g_out << ' ' << k.second << "@0";
         if (op == "linear" || op == "grad") {
             const netmax_linear_shape s{n("batch"), n("rows"), n("d_in"), n("d_out"), (int32_t)n("dtype"), (int32_t)n("act"), n("ldx"), n("ldw"), n("ldr"), n("ldy"), n("ldz"), n("sx"), n("sw"),
                                         n("sb"), n("sr"), n("sy"), n("sz"), n("lddx"), n("lddw"), n("sdx"), n("sdw"), n("sdb")};
