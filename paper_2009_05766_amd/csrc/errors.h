@@ -1,8 +1,5 @@
-// What the files of the C ABI share: the text of the last error that has no context, and the check behind a launch.
+// What the files of the C ABI share: the text of the last error that has no context.
 #pragma once
-#include <hip/hip_runtime.h>
-#include <string>
-
 #include "../../include/netmax.h"
 
 // Records `msg` for netmax_last_error(NULL) on this thread and returns `code`.
