@@ -49,8 +49,7 @@ template <bool SPLIT, class Blocks, class Go> static void with_small_shape(int64
     // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has (1 x 2660 x 512, X^T X:
     // 17.3 us in one group of waves, 15.1 in two; short contractions lose by the join)
     const bool far = worth_blocks(128, M, N);
-    if (SPLIT && blocks(256) >= 128 && far && worth_blocks(256, M, N)) go(Shape<256, 128, 4, 2, 32, 3>());
-    else if (blocks(128) >= 512 && far) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    if (blocks(128) >= 512 && far) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
     else if (blocks(128) >= 128 && far) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
     else if (blocks(64) > 256 || K < 512) go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
     else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4, 2>());

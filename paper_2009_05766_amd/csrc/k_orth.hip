@@ -227,7 +227,9 @@ int64_t orth_workspace(const OrthArgs &a)
 }
 
 // Many blocks: 256 x 128, two workgroups on a compute unit, so that the results of one (planes in and out, as long as half of the products) leave under
-// the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us (388 since the epilogue sees ahead).
+// the products of the other.  8 x 2048 x 4096, step: 404 us, in blocks of 256 x 256 446 us (388 since the epilogue sees ahead).  Whole updates on two planes (float), steps in
+// these blocks and in 128 x 128: 16 x 784 x 512 423 and 436 us, 4 x 2048 x 2048 2.69 and 2.71 ms, 20 x 784 x 512 545 and 515 us; their squares are better off in
+// 128 x 128 (24 x 768 x 768 1.12 ms, 1.38 with the squares in 256 x 128; 43 x 512 x 520 0.85 and 1.10).
 typedef Shape<256, 128, 4, 2, 32, 3> Paired;
 
 template <bool SPLIT> static void launch_square(hipStream_t s, int64_t batch, int64_t side, int64_t K, const Planes16 &x, bool near, const SquareEpilogue &e)
@@ -247,7 +249,9 @@ static void launch_step(hipStream_t s, const OrthArgs &a, const Planes16 &x, con
     const Planes16 &l = tall ? x : b, &r = tall ? b : x;            // B is symmetric: its rows are its columns
     const auto go = [&](auto f) { launch_gemm16_step<half8, f.BM, f.BN, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS, SPLIT>(s, a.batch, a.rows, a.cols, k, l, r, tall, e); };
     const auto blocks = [&](int64_t n) { return a.batch * ((a.rows + n - 1) / n) * ((a.cols + n - 1) / n); };
-    if constexpr (!SPLIT)
+    if constexpr (SPLIT) {
+        if (blocks(256) >= 128 && worth_blocks(128, a.rows, a.cols) && worth_blocks(256, a.rows, a.cols)) { go(Paired()); return; }
+    } else
         if (blocks(256) >= 192 && worth_blocks(256, a.rows, a.cols)) {
             if constexpr (std::is_same<Epilogue, StepEpilogue>::value) go(Paired());
             else go(Shape<256, 256, 2, 4, 64, 2>());
