@@ -192,12 +192,17 @@ void launch_gemm_f32_blocks(hipStream_t s, int64_t batch, int64_t M, int64_t N, 
         gemm_f32_kernel<BM, BN, STEP, GROUPS, false, false><<<grid, 256 * GROUPS, 0, s>>>(M, N, K, pa, a.ld, a.step, pb, b.ld, b.step, mb, nb, epilogue);
 }
 
+// Blocks of 128 x 128 where they are many and the contraction pays for their start: 2944 x 1024 x 2944 (529 blocks) 225 us and 192 in blocks of 64, 3328 (676) 226 and 232,
+// 4096 cubed (1024) 1137 and 1301.
+constexpr int64_t F32_LARGE = 640;
+
 template <class Epilogue>
 void launch_gemm_f32(hipStream_t s, int64_t batch, int64_t M, int64_t N, int64_t K, const Operand &a, const Operand &b, const Epilogue &epilogue)
 {
     const auto blocks = [&](int64_t m, int64_t n) { return batch * ((M + m - 1) / m) * ((N + n - 1) / n); };
-    // blocks of 128 where they are many and the contraction pays for their start; the fewer blocks, the more waves on each
-    if (blocks(128, 128) >= 256 && K >= 256 && worth_blocks(128, M, N)) launch_gemm_f32_blocks<128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
+    // the fewer blocks, the more waves on each.  One group of waves or four: 1408 x 1024 x 1408 (484 blocks) 56 and 53, 1472 (529) 72 and 78; blocks of 64 x 64 or 64 x 32:
+    // 704 x 1024 x 704 (121) 27 and 18, 768 (144) 27 and 34
+    if (blocks(128, 128) >= F32_LARGE && K >= 256 && worth_blocks(128, M, N)) launch_gemm_f32_blocks<128, 128, 16, 1>(s, batch, M, N, K, a, b, epilogue);
     else if (blocks(64, 64) >= 512) launch_gemm_f32_blocks<64, 64, 32, 1>(s, batch, M, N, K, a, b, epilogue);
     else if (blocks(64, 64) > 128) launch_gemm_f32_blocks<64, 64, 32, 4>(s, batch, M, N, K, a, b, epilogue);
     else launch_gemm_f32_blocks<64, 32, 32, 4>(s, batch, M, N, K, a, b, epilogue);

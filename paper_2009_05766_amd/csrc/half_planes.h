@@ -46,11 +46,14 @@ __device__ __forceinline__ void store_planes(uint16_t *hi, uint16_t *lo, f32x4 v
 // One launch for every block shape: `go` gets it.
 template <bool SPLIT, class Blocks, class Go> static void with_small_shape(int64_t M, int64_t N, int64_t K, const Blocks &blocks, const Go &go)
 {
-    // the largest blocks that still give most compute units one; the fewer there are, the more waves and steps under way each has (1 x 2660 x 512, X^T X:
-    // 17.3 us in one group of waves, 15.1 in two; short contractions lose by the join)
+    // the fewer blocks, the more waves and steps under way each has (1 x 2660 x 512, X^T X: 17.3 us in one group of waves, 15.1 in two; short contractions lose by the
+    // join).  Whole updates of five steps with these on both sides of each line, bfloat16: steps of 60 x 256 x 256 (240 blocks of 128) in four waves and two stages 198 and
+    // in eight and four 194, 68 (272) 216 and 230, squares of 24 x 512 x 512 (240) 312 and 264, 88 x 256 x 256 (264) 286 and 322; in blocks of 128 and of 64, steps of 8 x 512 x 512 (128)
+    // 158 and 148, 36 x 256 x 256 (144) 145 and 152, squares of 13 x 512 x 784 (130) 276 and 238, 2048 x 2048 (136) 410 and 451; blocks of 64 in one group and
+    // two, 3 x 576 x 576 (243) 142 and 137, 4 (324) 144 and 167; on two planes (float) the same lines
     const bool far = worth_blocks(128, M, N);
-    if (blocks(128) >= 512 && far) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
-    else if (blocks(128) >= 128 && far) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
+    if (blocks(128) > 256 && far) go(Shape<128, 128, 2, 2, SPLIT ? 32 : 64, 2>());
+    else if (blocks(128) > 128 && far) go(Shape<128, 128, 2, 4, SPLIT ? 32 : 64, 4>());
     else if (blocks(64) > 256 || K < 512) go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4>());
     else go(Shape<64, 64, 2, 2, SPLIT ? 32 : 64, 4, 2>());
 }

@@ -98,18 +98,22 @@ __global__ void __launch_bounds__(256) join_parts_kernel(int64_t batch, int64_t 
 
 // Blocks and shares of a product: large blocks where they fill the card, smaller ones otherwise, and the contraction shared out where even those are few
 // and long: a share is at least 16 steps (about 8 us, what the join costs; 1111 x 777 x 2049 in two shares of 64 x 64 blocks took 16 + 8 us, in one 17).
+//   256 or 128   2816 x 4096 x 2816 (121 large blocks) 89 and 83, 2816 x 4096 x 3328 (143) 86 and 108, 4096 cubed 118 and 143
+//   128 or 64    1024 x 1024 x 2048 (128 blocks) 12.3 and 10.7, 1536 x 1024 x 1536 (144) 12.7 and 16.2; with shares 1152 x 4096 x 1152 (81) 24 and 27, 1280 x 8192 x 1280
+//                (100) 41 and 55, but 896 x 4096 x 896 (49) 20 and 18
 struct Plan16 { int block; int splits; };
 static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
 {
     const auto blocks = [&](int64_t b) { return batch * ((M + b - 1) / b) * ((N + b - 1) / b); };
     const int64_t steps = (K + 63) / 64;
-    if (blocks(256) >= 192 && worth_blocks(256, M, N)) return {256, 1};
-    const int block = blocks(128) >= 96 && worth_blocks(128, M, N) ? 128 : 64;
+    if (blocks(256) > 128 && worth_blocks(256, M, N)) return {256, 1};
+    const int block = (blocks(128) > 128 || (blocks(128) >= 80 && K >= 4096)) && worth_blocks(128, M, N) ? 128 : 64;
     const int64_t here = blocks(block) > 0 ? blocks(block) : 1, want = 256 / here, most = steps / 16;
     const int64_t splits = want < most ? want : most;
     return {block, (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits)};
 }
-// Few rows that lie along the contraction have a kernel of their own (few_rows_kernel).
+// Few rows that lie along the contraction have a kernel of their own (few_rows_kernel).  32 x 4096 x 4096: 13.9, in blocks 12.6 and a second launch; 64 x 2048 x 2048: 6.8
+// and 9.5; long contractions of 64 rows, 64 x 4096 x 4096, are better off in blocks (17.6 and 13.4), which as a call are bound by the host at 14.
 constexpr int64_t FEW_ROWS = 64;
 static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, bool ak)
 {
@@ -118,12 +122,15 @@ static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, bool a
     return p.splits > 1 ? round_up(p.splits * batch * M * round_up(N, 4) * 4, 256) : 0;
 }
 
+// Blocks of 128 in four waves and two stages, two of them on a compute unit, or in eight waves and four stages, alone there: 2048 cubed (256 blocks) 29.4 and 24.3, 2176 x 2048 x
+// 2176 (289) 34.5 and 38.8.  Blocks of 64 in one group or two: 960 x 1024 x 960 (225 blocks) 8.5 and 7.8, 1088 x 1024 x 1088 (289) 10.4 and 13.9; 640 x 512 x 640 6.2 and 6.3, with
+// 128 indices 4.5 and 4.9.
 template <class Epilogue>
 static void launch_blocks16(hipStream_t s, int block, int64_t batch, int64_t M, int64_t N, int64_t K, const Planes16 &a, bool ak, const Planes16 &b, bool bk, const Epilogue &e)
 {
     const int64_t blocks = batch * ((M + block - 1) / block) * ((N + block - 1) / block);
     if (block == 256) launch_gemm16_blocks<bf16x8, 256, 256, 2, 4, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
-    else if (block == 128 && blocks >= 512) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
+    else if (block == 128 && blocks > 256) launch_gemm16_blocks<bf16x8, 128, 128, 2, 2, 64, 2, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
     else if (block == 128) launch_gemm16_blocks<bf16x8, 128, 128, 2, 4, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
     else if (blocks > 256 || K < 512) launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 1>(s, batch, M, N, K, a, ak, b, bk, 1, e);
     else launch_gemm16_blocks<bf16x8, 64, 64, 2, 2, 64, 4, 2>(s, batch, M, N, K, a, ak, b, bk, 1, e);
@@ -202,8 +209,10 @@ static bool launch_pair16(hipStream_t s, const LinearGradArgs &a, const Planes16
     if (!one_launch(a)) return false;
     if (a.rows <= FEW_ROWS && a.dout > 1024) return false;         // dx from few_rows_kernel: a long chain of steps otherwise
     const Plan16 px = plan16(a.batch, a.rows, a.din, a.dout), pw = plan16(a.batch, a.din, a.dout, a.rows);
-    if (px.block == 256 || pw.block == 256 || px.splits > 1 || pw.splits > 1) return false;
+    if (px.splits > 1 || pw.splits > 1) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
+    // 3328 cubed (169 blocks of 256 in each) in one launch 164, in large blocks one after the other 170; 4096 cubed (256) so 248
+    if ((px.block == 256 && blocks(256, a.rows, a.din) >= 192) || (pw.block == 256 && blocks(256, a.din, a.dout) >= 192)) return false;
     const auto both = [&](int64_t b) { return blocks(b, a.rows, a.din) + blocks(b, a.din, a.dout); };
     const int swap = a.rows > a.dout;                               // the longer chains of steps start first
     const auto go = [&](auto f) {
@@ -214,9 +223,11 @@ static bool launch_pair16(hipStream_t s, const LinearGradArgs &a, const Planes16
         gemm16_pair_kernel<bf16x8, f.BM, f.WM, f.WN, f.STEP, f.STAGES, f.GROUPS><<<all + bias.blocks(), f.WM * f.WN * 64 * f.GROUPS, 0, s>>>(
             product(a.rows, a.din, a.dout, d, w, a.dx, a.lddx, a.sdx), product(a.din, a.dout, a.rows, x, d, a.dw, a.lddw, a.sdw), first, all, swap, bias);
     };
+    // as launch_blocks16, by the blocks of both: 1408 cubed (242) 22.4 and 17.9, 1536 cubed (288) 27.4 and 31.2; 128 or 64, 1024 cubed (128) 13.6 and 10.1, 1152 cubed
+    // (162) 14.5 and 16.7; blocks of 64 in one group or two, 512 cubed (128) 5.9 and 6.3, 704 cubed (242) 6.9 and 7.4, 768 cubed (288) 8.4 and 12.3
     const bool far = worth_blocks(128, a.rows, a.din) && worth_blocks(128, a.din, a.dout);
-    if (both(128) >= 512 && far) go(Shape<128, 128, 2, 2, 64, 2>());
-    else if (both(128) >= 128 && far) go(Shape<128, 128, 2, 4, 64, 4>());
+    if (both(128) > 256 && far) go(Shape<128, 128, 2, 2, 64, 2>());
+    else if (both(128) > 128 && far) go(Shape<128, 128, 2, 4, 64, 4>());
     else if (both(64) > 256 || (a.dout < 512 && a.rows < 512)) go(Shape<64, 64, 2, 2, 64, 4>());
     else go(Shape<64, 64, 2, 2, 64, 4, 2>());
     return true;
@@ -226,8 +237,8 @@ static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d,
 {
     if (!one_launch(a)) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
-    if ((blocks(128, a.rows, a.din) >= 256 && a.dout >= 256 && worth_blocks(128, a.rows, a.din)) ||
-        (blocks(128, a.din, a.dout) >= 256 && a.rows >= 256 && worth_blocks(128, a.din, a.dout))) return false;
+    if ((blocks(128, a.rows, a.din) >= F32_LARGE && a.dout >= 256 && worth_blocks(128, a.rows, a.din)) ||
+        (blocks(128, a.din, a.dout) >= F32_LARGE && a.rows >= 256 && worth_blocks(128, a.din, a.dout))) return false;
     const auto product = [&](int64_t M, int64_t N, int64_t K, const void *l, int64_t ldl, int64_t sl, const void *r, int64_t ldr, int64_t sr, void *out, int64_t ld, int64_t step) {
         return ProductF32<LinearEpilogue<float>>{M, N, K, (const float *)l, (const float *)r, ldl, sl, ldr, sr, (uint32_t)((M + 63) / 64), (uint32_t)((N + 63) / 64),
                                                  plain_epilogue<float>(M, N, out, ld, step)};
@@ -236,8 +247,10 @@ static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d,
     const auto q = product(a.din, a.dout, a.rows, a.x, a.ldx, a.sx, d, ldd, sd, a.dw, a.lddw, a.sdw);
     const int swap = a.rows > a.dout;
     const uint32_t first = (uint32_t)blocks(64, a.rows, a.din), all = first + (uint32_t)blocks(64, a.din, a.dout);
+    // one group of waves, two or four: 960 cubed (450 blocks) 53 us and 45 in two, 1216 cubed (722) 86 and 85, 1280 cubed (800) 109 in both; 640 cubed (200) 21.2 in two and 20.6 in
+    // four, 832 cubed (338) 39 and 48
     if (all >= 768) gemm_f32_pair_kernel<64, 32, 1><<<all + bias.blocks(), 256, 0, s>>>(p, q, first, all, swap, bias);
-    else if (all >= 384) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, swap, bias);
+    else if (all > 256) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, swap, bias);
     else gemm_f32_pair_kernel<64, 32, 4><<<all + bias.blocks(), 1024, 0, s>>>(p, q, first, all, swap, bias);
     return true;
 }

@@ -11,7 +11,8 @@ F32, BF16 = ops.F32, ops.BF16
 
 @pytest.mark.parametrize("rows,d_in,d_out,batch,dtype", [
     (42, 533, 2501, 0, BF16), (1, 408, 1560, 12, BF16), (1009, 9, 2057, 4, BF16), (2445, 336, 8, 9, BF16), (232, 2032, 351, 16, BF16), (2126, 653, 2057, 0, BF16), (1300, 2100, 1200, 0, BF16),
-    (2100, 1200, 1300, 0, BF16), (70, 1000, 1100, 0, BF16), (520, 130, 140, 40, BF16), (384, 390, 400, 60, BF16), (280, 1944, 1976, 0, F32), (3535, 1165, 359, 0, F32), (130, 200, 190, 30, F32)])
+    (2100, 1200, 1300, 0, BF16), (70, 1000, 1100, 0, BF16), (520, 130, 140, 40, BF16), (384, 390, 400, 60, BF16), (4096, 72, 1168, 9, BF16), (1152, 4104, 1200, 0, BF16), (1152, 1200, 4104, 0, BF16), (4104, 1150, 1200, 0, BF16),
+    (280, 1944, 1976, 0, F32), (3535, 1165, 359, 0, F32), (130, 200, 190, 30, F32), (2370, 443, 259, 12, F32)])
 def test_layers(rows, d_in, d_out, batch, dtype):
     ops.check_linear(rows, d_in, d_out, dtype, "gelu", batch=batch, seed=rows)
 
@@ -30,7 +31,7 @@ def test_one_gradient_alone(which, rows, d_in, d_out, dtype):
 
 
 @pytest.mark.parametrize("batch,rows,cols,dtype", [
-    (1, 538, 526, F32), (1, 530, 537, F32), (1, 512, 642, BF16), (1, 723, 531, BF16), (132, 72, 434, F32), (242, 69, 273, BF16), (44, 1821, 65, BF16), (260, 313, 67, F32),
+    (1, 538, 526, F32), (1, 530, 537, F32), (1, 512, 642, BF16), (1, 723, 531, BF16), (132, 72, 434, F32), (242, 69, 273, BF16), (44, 1821, 65, BF16), (260, 313, 67, F32), (46, 65, 293, BF16), (48, 293, 65, F32), (142, 69, 78, F32), (140, 78, 69, BF16),
     (86, 384, 400, F32), (86, 400, 384, F32), (86, 384, 400, BF16), (86, 400, 384, BF16)])
 def test_updates(batch, rows, cols, dtype):
     ops.test_orthogonalize_many_matrices(batch, rows, cols, dtype)
