@@ -291,8 +291,8 @@ typedef enum { NETMAX_ACT_NONE = 0, NETMAX_ACT_RELU = 1, NETMAX_ACT_GELU = 2, NE
 
 typedef struct {
     int64_t batch;          /* layers, e.g. one per worker: 0 .. 65535 */
-    int64_t rows;           /* tokens per layer, >= 0 */
-    int64_t d_in, d_out;    /* 1 .. 2^22 - 1 */
+    int64_t rows;           /* tokens per layer: 0 .. 64 * 65535 */
+    int64_t d_in, d_out;    /* 1 .. 2^22 - 1; batch times the 64 x 64 blocks of x, of w and of y: fewer than 2^24 each, as many as one launch can have */
     int32_t dtype;          /* netmax_dtype of all matrices and vectors */
     int32_t act;            /* netmax_act */
     int64_t ldx, ldw, ldr, ldy, ldz;            /* rows of x, w, residual, y (and dy), z */
@@ -302,6 +302,7 @@ typedef struct {
 
 /* y = act(z) + residual, z = x w + bias, for every layer of the batch: x [rows][d_in], w [d_in][d_out] (the layout of a perceptron's W),
  * bias [d_out], residual and y [rows][d_out].  bias and residual may be NULL; z may be NULL or receives z, which netmax_linear_grad needs.
+ * bfloat16: y is computed from z in float and rounded once; z as it is left is rounded too.
  * y may be the residual's memory with the residual's strides (and be nothing else's).  The workspace depends on the alignment of x and w (bfloat16 rows that do not start at multiples of
  * 16 bytes are laid out anew): pass the pointers of the call. */
 int64_t netmax_linear_workspace(const netmax_linear_shape *shape, const void *x, const void *w);
@@ -310,7 +311,8 @@ int netmax_linear(const netmax_linear_shape *shape, const void *x, const void *w
 
 /* The gradients of that layer from dy = dl/dy (which is the residual's gradient, too): with dz = dy act'(z) (ReLU's derivative at 0 is 0),
  * dx = dz w^T, dw = x^T dz, db = the sum of dz over the rows; each may be NULL.  z as netmax_linear left it, NULL for NETMAX_ACT_NONE.
- * bfloat16: dz is rounded to bfloat16 for the products, as the errors of a perceptron are; db sums it before that.  rows = 0 gives dw = 0 and db = 0.
+ * bfloat16: act' is taken at z as it was left, rounded, and dz is rounded for the products, as the errors of a perceptron are (2.4e-3 of a
+ * gradient's norm in all, 1.7e-3 without); db sums dz before that.  rows = 0 gives dw = 0 and db = 0.
  * Results of the same call are the same bits every time.  With an activation, results may lie in the memory of dy and z, which have been read before the first of them is
  * written; x may be shared if dw, w if dx is NULL. */
 int64_t netmax_linear_grad_workspace(const netmax_linear_shape *shape, const void *dy, const void *x, const void *w);
@@ -319,7 +321,7 @@ int netmax_linear_grad(const netmax_linear_shape *shape, const void *dy, const v
 
 typedef struct {
     int64_t batch;          /* matrices, e.g. one per worker: 0 .. 65535 */
-    int64_t rows, cols;     /* 1 .. 2^22 - 1 */
+    int64_t rows, cols;     /* 1 .. 2^22 - 1; batch times the 64 x 64 blocks of a matrix: fewer than 2^24 */
     int32_t dtype;          /* netmax_dtype of g and out; the momentum is float */
     int32_t steps;          /* Newton-Schulz products, 1 .. 64 */
     int32_t nesterov;
@@ -329,14 +331,14 @@ typedef struct {
 
 /* An orthogonalised momentum step for every matrix of the batch: m_out = mu m + g, u = g + mu m_out (nesterov) or m_out,
  * X = u / max(||u||_F, eps), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X, out = scale X.  With (3.4445, -4.7750, 2.0315) and five
- * steps the singular values end near 1.  X is held in halves with 22 bits: coefficients that let a singular value of X grow past 32, or one of
+ * steps the singular values end near 1 (the coefficients of K. Jordan et al., Muon, 2024).  X is held in halves with 22 bits: coefficients that let a singular value of X grow past 32, or one of
  * b (X X^T) + c (X X^T)^2 past 255, give results that are not finite.  bfloat16: products of 11 bits.  m and m_out may be the same memory; both NULL: u = g.  out may lie in
  * the memory of g, and in m's if m_out is another.
  * To mix such updates: write them to g (tile layout, netmax_pack) of a context with momentum 0 and call netmax_mix. */
 int64_t netmax_orthogonalize_workspace(const netmax_orth_shape *shape);
 int netmax_orthogonalize(const netmax_orth_shape *shape, const void *g, const float *m, float *m_out, void *out, void *work, int64_t work_bytes, void *stream);
 
-/* The clipped policy loss with a KL term on the logits of sampled tokens, and the gradient of the sum of all losses by the logits.
+/* The clipped policy loss (J. Schulman et al., Proximal Policy Optimization Algorithms, 2017) with a KL term on the logits of sampled tokens, and the gradient of the sum of all losses by the logits.
  * For a token with logits z, label y, log p = z_y - log sum exp z and r = exp(log p - old_logp):
  *     loss = weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(d) - d - 1)),   d = ref_logp - log p
  * (where both terms of the minimum are equal, the gradient is the unclipped one's).  logits [tokens][vocab], dtype, rows ld apart; labels int32,
@@ -347,7 +349,7 @@ int netmax_policy_loss(int64_t tokens, int64_t vocab, int32_t dtype, const void 
                        const float *ref_logp, const float *advantage, const float *weight, float clip_low, float clip_high, float kl, float *loss,
                        float *logp, void *grad, int64_t ldg, void *stream);
 
-/* The loss of paired log ratios: sequence q holds tokens offsets[q] .. offsets[q + 1] - 1 (offsets: device int32 [2 pairs + 1], not decreasing),
+/* The loss of paired log ratios (R. Rafailov et al., Direct Preference Optimization, 2023): sequence q holds tokens offsets[q] .. offsets[q + 1] - 1 (offsets: device int32 [2 pairs + 1], not decreasing),
  * sequence 2 p is the chosen one of pair p and 2 p + 1 the rejected one.  With R_q = sum over its tokens of weight (log p - ref_logp) and
  * h = beta (R_2p - R_2p+1):   loss[p] = scale (-(1 - smoothing) log sigma(h) - smoothing log sigma(-h)),   ratio[q] = R_q.
  * Logits, labels, weight and grad as for netmax_policy_loss (the gradient of the sum of loss[p]); tokens outside of all sequences have gradient 0;
