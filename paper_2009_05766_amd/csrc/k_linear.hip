@@ -112,7 +112,7 @@ static Plan16 plan16(int64_t batch, int64_t M, int64_t N, int64_t K)
     const int64_t splits = want < most ? want : most;
     return {block, (int)(splits < 1 ? 1 : splits > 32 ? 32 : splits)};
 }
-// Few rows that lie along the contraction have a kernel of their own (few_rows_kernel).  32 x 4096 x 4096: 13.9, in blocks 12.6 and a second launch; 64 x 2048 x 2048: 6.8
+// Few rows that lie along the contraction have a kernel of their own (few_rows_kernel).  In a graph, 1 x 2048 x 8192: 6.8 us, in blocks with shares 10.2; 32 x 4096 x 4096: 13.9, in blocks 12.6 and a second launch; 64 x 2048 x 2048: 6.8
 // and 9.5; long contractions of 64 rows, 64 x 4096 x 4096, are better off in blocks (17.6 and 13.4), which as a call are bound by the host at 14.
 constexpr int64_t FEW_ROWS = 64;
 static int64_t part_bytes(int64_t batch, int64_t M, int64_t N, int64_t K, bool ak)
@@ -237,8 +237,11 @@ static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d,
 {
     if (!one_launch(a)) return false;
     const auto blocks = [&](int64_t b, int64_t m, int64_t n) { return a.batch * ((m + b - 1) / b) * ((n + b - 1) / b); };
-    if ((blocks(128, a.rows, a.din) >= F32_LARGE && a.dout >= 256 && worth_blocks(128, a.rows, a.din)) ||
-        (blocks(128, a.din, a.dout) >= F32_LARGE && a.rows >= 256 && worth_blocks(128, a.din, a.dout))) return false;
+    // one after the other where one of them is worth blocks of 128 (4096 cubed 2.24 ms, 2.55 in blocks of 64), or fills the card and the other has few and long chains, which then
+    // have more waves each: 16384 x 256 x 256 223 us, in one launch 478; 2048 cubed 352 and 339, 8192 x 512 x 4096 766 and 683
+    const auto large = [&](int64_t m, int64_t n, int64_t k, int64_t from) { return blocks(128, m, n) >= from && k >= 256 && worth_blocks(128, m, n); };
+    const int64_t dx_from = blocks(64, a.din, a.dout) < 128 ? 256 : F32_LARGE, dw_from = blocks(64, a.rows, a.din) < 128 ? 256 : F32_LARGE;
+    if (large(a.rows, a.din, a.dout, dx_from) || large(a.din, a.dout, a.rows, dw_from)) return false;
     const auto product = [&](int64_t M, int64_t N, int64_t K, const void *l, int64_t ldl, int64_t sl, const void *r, int64_t ldr, int64_t sr, void *out, int64_t ld, int64_t step) {
         return ProductF32<LinearEpilogue<float>>{M, N, K, (const float *)l, (const float *)r, ldl, sl, ldr, sr, (uint32_t)((M + 63) / 64), (uint32_t)((N + 63) / 64),
                                                  plain_epilogue<float>(M, N, out, ld, step)};
@@ -247,10 +250,10 @@ static bool launch_pair32(hipStream_t s, const LinearGradArgs &a, const void *d,
     const auto q = product(a.din, a.dout, a.rows, a.x, a.ldx, a.sx, d, ldd, sd, a.dw, a.lddw, a.sdw);
     const int swap = a.rows > a.dout;
     const uint32_t first = (uint32_t)blocks(64, a.rows, a.din), all = first + (uint32_t)blocks(64, a.din, a.dout);
-    // one group of waves, two or four: 960 cubed (450 blocks) 53 us and 45 in two, 1216 cubed (722) 86 and 85, 1280 cubed (800) 109 in both; 640 cubed (200) 21.2 in two and 20.6 in
-    // four, 832 cubed (338) 39 and 48
+    // one group of waves or two: 960 cubed (450 blocks) 53 and 45 us, 1216 cubed (722) 86 and 85, 1280 cubed (800) 109 in both; two or four: 1400 x 640 x 640 (320) 46 and 39, 832
+    // cubed (338) 39 and 48, 600 x 2048 x 64 (352) 20 and 18, 896 cubed (392) 42 and 48
     if (all >= 768) gemm_f32_pair_kernel<64, 32, 1><<<all + bias.blocks(), 256, 0, s>>>(p, q, first, all, swap, bias);
-    else if (all > 256) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, swap, bias);
+    else if (all >= 384) gemm_f32_pair_kernel<64, 32, 2><<<all + bias.blocks(), 512, 0, s>>>(p, q, first, all, swap, bias);
     else gemm_f32_pair_kernel<64, 32, 4><<<all + bias.blocks(), 1024, 0, s>>>(p, q, first, all, swap, bias);
     return true;
 }
