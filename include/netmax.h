@@ -331,7 +331,8 @@ typedef struct {
 
 /* An orthogonalised momentum step for every matrix of the batch: m_out = mu m + g, u = g + mu m_out (nesterov) or m_out,
  * X = u / max(||u||_F, eps), then `steps` times X <- a X + b (X X^T) X + c (X X^T)^2 X, out = scale X.  With (3.4445, -4.7750, 2.0315) and five
- * steps the singular values end near 1 (the coefficients of K. Jordan et al., Muon, 2024).  X is held in halves with 22 bits: coefficients that let a singular value of X grow past 32, or one of
+ * steps the singular values end near 1 (the coefficients of K. Jordan et al., Muon, 2024).  X is held in halves with 22 bits, down to 2^-35: results are exact
+ * relative to their norm (float 2e-6), and entries of u below 2^-13 of its norm keep fewer bits.  Coefficients that let a singular value of X grow past 32, or one of
  * b (X X^T) + c (X X^T)^2 past 255, give results that are not finite.  bfloat16: products of 11 bits.  m and m_out may be the same memory; both NULL: u = g.  out may lie in
  * the memory of g, and in m's if m_out is another.
  * To mix such updates: write them to g (tile layout, netmax_pack) of a context with momentum 0 and call netmax_mix. */

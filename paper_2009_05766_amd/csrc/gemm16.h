@@ -1,8 +1,8 @@
 // C = A B for operands of 16 bits (bfloat16 or half) on v_mfma_f32_32x32x16, accumulated in float.
 //
 // A workgroup has a block of BM x BN results.  Steps of STEP contraction indices of both operands go from memory straight into LDS (16 bytes per lane and
-// request), STAGES of them under way or in use; one barrier per step.  Large products are bound by the card's power: 8192 x 4096 x 8192 runs at 1.15
-// to 1.25 PFLOP/s with the matrix instructions busy 63 % of 1.8 GHz (without its loads 2.0 GHz, on zeros 2.3 GHz).  Blocks of 256 x 256 in eight
+// request), STAGES of them under way or in use; one barrier per step.  Large products are bound by the card's power: 8192 x 4096 x 8192 with a plain epilogue runs at 1.25
+// PFLOP/s in all three pairs of orientations, with the matrix instructions busy 63 % of 1.8 GHz (without its loads 2.0 GHz, on zeros 2.3 GHz); with GELU and z 515 us.  Blocks of 256 x 256 in eight
 // waves read the least per product: 440 us, 256 x 128 510 us, 128 x 128 540 us.  Small ones are bound by the latency of steps: 16 products 512 x 512 x 784
 // take 14.2 us with eight waves and four stages on a 128 x 128 block, 16.0 us with four waves and two.
 // Each operand lies in LDS as it lies in memory:
@@ -375,8 +375,7 @@ struct Shape { static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STEP
 // C = A B for few rows, at most 32 TM: the weights are what has to be read.  A workgroup has 32 columns; its eight waves take steps of 32 indices in turn,
 // each with its own space in LDS for a few steps under way and without a barrier.  The waves' sums are added in LDS in order.  Neighbouring
 // workgroups share an L2, as they share the lines of 128 bytes that 64 bytes of a row of weights lie in.  Bound by what is under way per compute unit: one
-// row, 2048 x 8192 7.8 us (4.3 TB/s), 32 rows, 4096 x 4096 14.7 us (2.3 TB/s: 128 workgroups, and A is as much again); by blocks of 64 x 64 with the
-// contraction shared out and a second launch 12.3 and 15.6 us.
+// row, 2048 x 8192 7.5 us (4.5 TB/s), 32 rows, 4096 x 4096 14.8 us (2.3 TB/s: 128 workgroups, and A is as much again).
 constexpr int FEW_WAVES = 8;
 
 template <typename V, int TM, bool BK, class Epilogue>

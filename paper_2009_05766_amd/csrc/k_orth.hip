@@ -13,8 +13,8 @@
 //   bfloat16     products of hi planes (11 bits), the term a X from both planes.  B's diagonal, its large part near the end, is kept in float and
 //                joins a X: the rounding of B then halves the result's error, to 0.6e-3 where the rounding of the result itself is 1.7e-3
 // A and B are symmetric: their blocks on and below the diagonal are computed and written to both sides.
-// 8 x 2048 x 4096 bfloat16, five steps: 3.74 ms, of it momentum and norm 0.30 (1.34 GB), A and B 1.67, X 1.8 (its planes, in and
-// out, take as long as half of the products).  16 x 784 x 512 float: 0.41 ms, bound by the chain of seventeen launches of 14 to 45 us.
+// 8 x 2048 x 4096 bfloat16, five steps: 3.77 ms, of it momentum and norm 0.30 (1.34 GB), A and B 1.66, X 1.81 (its planes, in and
+// out, take as long as half of the products).  16 x 784 x 512 float: 0.42 ms, bound by the chain of seventeen launches of 14 to 32 us.
 #include "half_planes.h"
 #include "orth.h"
 

@@ -12,8 +12,8 @@
 // has a larger one: the exponential of a value that decides the row is then 1, and its log probability is not spoilt by the rounding of a large argument
 // (2^-24 of it).  Pieces are counted from the row's first value, wherever that lies in memory, so that a row's results do not depend on its place.
 //
-// policy, 8192 x 131072 bfloat16 (a row in ten without weight): 780 to 840 us for 4.08 GB, the rate of a large copy (5.2 TB/s); read twice, without
-// registers, 2.7 ms.  preference, 16384 x 50000 (a quarter without weight): rows 330 us, gradient 510 us for 1.23 and 2.87 GB: the slopes of a
+// policy, 8192 x 131072 bfloat16 (a row in ten without weight): 795 us for 4.08 GB, the rate of a large copy (5.1 TB/s); read twice, without
+// registers, 2.7 ms.  preference, 16384 x 50000 (a quarter without weight): rows 233 us, gradient 518 us for 1.23 and 2.87 GB: the slopes of a
 // sequence's rows depend on all of them, so rows that count are read twice.
 #include "gemm.h"
 #include "token_loss.h"
