@@ -361,6 +361,77 @@ int netmax_preference_loss(int64_t tokens, int64_t vocab, int32_t dtype, const v
                            const int32_t *offsets, const float *ref_logp, const float *weight, float beta, float smoothing, float scale, float *loss,
                            float *ratio, void *grad, int64_t ldg, void *work, int64_t work_bytes, void *stream);
 
+/* ---- Operators around the layers of a language model: embedding, norms of a block, clipping ------------------------- */
+
+typedef struct {
+    int64_t batch;          /* tables, e.g. one per worker: 0 .. 65535 */
+    int64_t tokens;         /* per table: 0 .. 2^31 - 1 */
+    int64_t vocab, width;   /* 1 .. 2^22 - 1 */
+    int32_t dtype;          /* netmax_dtype of table, y and their gradients */
+    int32_t accumulate;     /* gradient: added to what dtable holds */
+    float scale;
+    int64_t s_ids;          /* token ids of a batch */
+    int64_t ldt, st, ldy, sy;                   /* rows of the table (and its gradient) and of y (and dy), and of a batch */
+} netmax_embed_shape;
+
+/* y[t] = scale table[ids[t]] for every table of the batch: ids int32 [tokens], table [vocab][width], y [tokens][width].  An id outside of 0 .. vocab - 1 is padding: its row of
+ * y is 0. */
+int netmax_embed(const netmax_embed_shape *shape, const int32_t *ids, const void *table, void *y, void *stream);
+
+/* The gradient of the table: dtable[v] = scale times the sum of dy[t] over the tokens t with ids[t] = v, summed in float in a fixed order; rows of tokens that do not occur are 0,
+ * with `accumulate` they are left as they are and the others added to (in float, rounded once).  Rows of dy whose id is padding are not looked at.  Results are the same bits every time. */
+int64_t netmax_embed_grad_workspace(const netmax_embed_shape *shape);
+int netmax_embed_grad(const netmax_embed_shape *shape, const int32_t *ids, const void *dy, void *dtable, void *work, int64_t work_bytes, void *stream);
+
+typedef enum { NETMAX_NORM_RMS = 0, NETMAX_NORM_LAYER = 1 } netmax_norm;
+typedef enum { NETMAX_GATE_NONE = 0, NETMAX_GATE_SIGMOID = 1, NETMAX_GATE_TANH = 2 } netmax_gate;
+
+typedef struct { void *p; int64_t ld, s; } netmax_span;         /* first value, rows, matrices of a batch (a vector has no ld); p may be NULL where it says so */
+
+typedef struct {
+    int64_t batch;          /* 0 .. 65535 */
+    int64_t rows;           /* tokens of each: 0 .. 2^31 - 1 */
+    int64_t width;          /* values of a row: 1 .. 2^22 - 1 */
+    int32_t dtype;          /* netmax_dtype of all rows and vectors */
+    int32_t norm;           /* netmax_norm */
+    int32_t gate_act;       /* netmax_gate: what the gate's values go through */
+    int32_t gate_rows;      /* 0: the gate is a vector, the same for all rows; 1: rows of its own */
+    int32_t post, pre;      /* whether the block's output is normed; whether there is a y */
+    float x_scale, f_scale, eps;                                /* eps > 0 */
+} netmax_block_norm_shape;
+
+typedef struct { netmax_span x, f, gate, post_gain, post_bias, pre_gain, pre_bias, h, y; } netmax_block_norm_data;
+typedef struct { netmax_span dy, dh, dx, df, dgate, dpost_gain, dpost_bias, dpre_gain, dpre_bias; } netmax_block_norm_grads;
+
+/* What lies between two blocks of a model.  For a block's output f and the residual stream x, both [rows][width]:
+ *     u = N(f) post_gain + post_bias (f itself without `post`),   h = x_scale x + f_scale act(gate) u,   y = N(h) pre_gain + pre_bias
+ * with N(v) = v / sqrt(mean v^2 + eps) over a row, for a layer norm of v less its mean.  h is the new residual stream, y the next block's input.  f may be NULL (y = N(x_scale x), as
+ * before the first block, or of heads; then there is no gate and no post_gain); gate, gains and biases may be NULL (1, 1 and 0); h and y may be NULL, but not both, and y has to be
+ * without `pre`.  Squares and means are summed in double; y comes from h in float, not from the rounded one.  h and y may each lie in the place of x, f or a gate of rows, with its strides. */
+int netmax_block_norm(const netmax_block_norm_shape *shape, const netmax_block_norm_data *data, void *stream);
+
+/* Its gradients from dy and dh, what reaches y and, beside y, h (dh may be NULL with `pre`; dy is NULL without): dx, df and dgate of what it was given, and those of gains and biases (of a
+ * gate that is the same for all rows, too) summed over the rows, in float, their partial sums in double and in a fixed order.  Every one may be NULL; data's h and y are not looked at: h is computed anew from x
+ * and f.  dx, df and a dgate of rows may each lie in the place of dy, dh, x, f or a gate of rows, with its strides.  rows = 0 gives sums of 0.  Results are the same bits every time. */
+int64_t netmax_block_norm_grad_workspace(const netmax_block_norm_shape *shape, const netmax_block_norm_grads *grads);
+int netmax_block_norm_grad(const netmax_block_norm_shape *shape, const netmax_block_norm_data *data, const netmax_block_norm_grads *grads, void *work, int64_t work_bytes, void *stream);
+
+typedef struct {
+    const void *g; void *out;                   /* a gradient, and where it goes scaled (may be g, with g's strides; not looked at for the norm alone) */
+    int64_t rows, cols;                         /* of each of the batch */
+    int64_t ldg, sg, ldo, so;
+    int32_t dtype;                              /* netmax_dtype of both */
+} netmax_gradient;
+
+/* The norm of all n gradients of a model together, norm = sqrt(sum of squares), for each of `batch` models (0 .. 65535, e.g. workers; gradients are `sg` apart), and the gradients scaled down
+ * to max_norm: out = g if norm <= max_norm, else g max_norm / norm.  Squares are summed in double and in a fixed order: the norm is that of the values over their whole range, rounded once, and inf only where it
+ * is past float's range or one of them is inf.  A norm that is inf or NaN is not hidden: the factor is then 0 (0 times inf is NaN) or NaN.  norm: device float [batch], may be NULL for
+ * netmax_clip_grads.  max_norm may be inf.  `gradients` is host memory that is not needed after the call; up to 65535 of them, each of up to
+ * 2^36 pieces of 16 bytes, counted from every row's start. */
+int64_t netmax_grad_norm_workspace(int64_t batch, int64_t n, const netmax_gradient *gradients);
+int netmax_grad_norm(int64_t batch, int64_t n, const netmax_gradient *gradients, float *norm, void *work, int64_t work_bytes, void *stream);
+int netmax_clip_grads(int64_t batch, int64_t n, const netmax_gradient *gradients, float max_norm, float *norm, void *work, int64_t work_bytes, void *stream);
+
 /* Device pointer of the current parameters x^t (one of x_a, x_b; tile layout), NULL if nothing is bound. */
 const float *netmax_params(const netmax_ctx *ctx);
 

@@ -22,6 +22,8 @@ NETMAX_FLAT, NETMAX_MLP = 0, 1
 NETMAX_F32, NETMAX_BF16 = 0, 1
 NETMAX_MIX_POLICY, NETMAX_MIX_FIXED = 0, 1
 NETMAX_ACT_NONE, NETMAX_ACT_RELU, NETMAX_ACT_GELU, NETMAX_ACT_SILU = range(4)
+NETMAX_NORM_RMS, NETMAX_NORM_LAYER = range(2)
+NETMAX_GATE_NONE, NETMAX_GATE_SIGMOID, NETMAX_GATE_TANH = range(3)
 
 EXPORTS = (
     "netmax_init", "netmax_build_tables", "netmax_generate_policy", "netmax_set_policy", "netmax_set_lr", "netmax_bind_state",
@@ -30,6 +32,8 @@ EXPORTS = (
     "netmax_last_error", "netmax_destroy",
     "netmax_linear_workspace", "netmax_linear", "netmax_linear_grad_workspace", "netmax_linear_grad", "netmax_orthogonalize_workspace",
     "netmax_orthogonalize", "netmax_policy_loss", "netmax_preference_workspace", "netmax_preference_loss",
+    "netmax_embed", "netmax_embed_grad_workspace", "netmax_embed_grad", "netmax_block_norm", "netmax_block_norm_grad_workspace", "netmax_block_norm_grad",
+    "netmax_grad_norm_workspace", "netmax_grad_norm", "netmax_clip_grads",
 )
 
 
@@ -62,6 +66,23 @@ class netmax_orth_shape(C.Structure):
     _fields_ = ([(n, C.c_int64) for n in ("batch", "rows", "cols")] + [(n, C.c_int32) for n in ("dtype", "steps", "nesterov")] +
                 [(n, C.c_float) for n in ("mu", "a", "b", "c", "eps", "scale")] +
                 [(n, C.c_int64) for n in ("ldg", "sg", "ldm", "sm", "ldo", "so")])
+
+
+class netmax_embed_shape(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("batch", "tokens", "vocab", "width")] + [("dtype", C.c_int32), ("accumulate", C.c_int32), ("scale", C.c_float)] +
+                [(n, C.c_int64) for n in ("s_ids", "ldt", "st", "ldy", "sy")])
+
+
+class netmax_block_norm_shape(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("batch", "rows", "width")] + [(n, C.c_int32) for n in ("dtype", "norm", "gate_act", "gate_rows", "post", "pre")] +
+                [(n, C.c_float) for n in ("x_scale", "f_scale", "eps")])
+
+
+netmax_block_norm_data = netmax_block_norm_grads = C.c_int64 * 27      # nine spans of an address and two distances each
+
+
+class netmax_gradient(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p)] + [(n, C.c_int64) for n in ("rows", "cols", "ldg", "sg", "ldo", "so")] + [("dtype", C.c_int32)]
 
 
 _lib = None
@@ -123,6 +144,15 @@ def load():
         "netmax_policy_loss": (C.c_int, [i64, i64, i32, vp, i64, vp, vp, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp]),
         "netmax_preference_workspace": (i64, [i64, i64]),
         "netmax_preference_loss": (C.c_int, [i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, i64, vp]),
+        "netmax_embed": (C.c_int, [C.POINTER(netmax_embed_shape)] + [vp] * 4),
+        "netmax_embed_grad_workspace": (i64, [C.POINTER(netmax_embed_shape)]),
+        "netmax_embed_grad": (C.c_int, [C.POINTER(netmax_embed_shape)] + [vp] * 4 + [i64, vp]),
+        "netmax_block_norm": (C.c_int, [C.POINTER(netmax_block_norm_shape), vp, vp]),
+        "netmax_block_norm_grad_workspace": (i64, [C.POINTER(netmax_block_norm_shape), vp]),
+        "netmax_block_norm_grad": (C.c_int, [C.POINTER(netmax_block_norm_shape)] + [vp] * 3 + [i64, vp]),
+        "netmax_grad_norm_workspace": (i64, [i64, i64, vp]),
+        "netmax_grad_norm": (C.c_int, [i64, i64] + [vp] * 3 + [i64, vp]),
+        "netmax_clip_grads": (C.c_int, [i64, i64, vp, f32, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)

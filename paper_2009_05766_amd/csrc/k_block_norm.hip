@@ -1,0 +1,353 @@
+// The norms before and after a block with its gate and the residual stream, and their gradients.
+//
+//   N(v) = v r, r = 1 / sqrt(mean v^2 + eps)                               or, as a layer norm, with v - mean v in the place of v
+//   u = N(f) g1 + b1,  h = a x + b act(q) u,  y = N(h) g2 + b2             f: the block's output, x: the residual stream, q: the gate
+// Gradients from dy and dh (what reaches h by other ways), with fn = N(f), hn = N(h) and means over a row (those of the mean itself for a layer norm only):
+//   e = dy g2,      D = dh + r2 (e - mean e - hn mean(e hn)),              dx = a D,  dq = b act'(q) u D
+//   c = b act(q) D g1,                                                     df = r1 (c - mean c - fn mean(c fn))
+//   dg2 = sum dy hn,  db2 = sum dy,  dg1 = sum b act(q) D fn,  db1 = sum b act(q) D over the rows; dq too, if q is the same for all rows
+// h is computed anew from x and f, in float, so that nothing has to be kept and the gradients do not depend on h's rounding.
+// Bound by memory: x, f and q are read, h and y written; the gradients read dy and dh as well and write dx, df and dq.
+//
+// Squares are summed in double (a float's is exact there): rows of any size have their mean square, over the whole range of the type.  A layer norm's mean is
+// subtracted as two floats, so that rows far from 0 keep their bits.
+#include "block_norm.h"
+#include "piece.h"
+
+namespace netmax {
+
+constexpr int THREADS = 256;
+
+// ---- a row -----------------------------------------------------------------------------------------------------------
+
+struct Unit { float mean, rest, r; };              // N(v) = ((v - mean) - rest) r
+__device__ __forceinline__ float unit_of(const Unit &n, float v) { return ((v - n.mean) - n.rest) * n.r; }
+
+__device__ __forceinline__ void gate_of(int act, float q, float &value, float &slope)
+{
+    if (act == GATE_SIGMOID) {
+        value = sigmoid_of(q);
+        slope = value * sigmoid_of(-q);
+    } else if (act == GATE_TANH) {
+        value = tanhf(q);
+        slope = fabsf(q) < 1.0f ? 1.0f - value * value : 4.0f * sigmoid_of(2.0f * q) * sigmoid_of(-2.0f * q);      // far out 1 - tanh^2 cancels
+    } else {
+        value = q;
+        slope = 1.0f;
+    }
+}
+
+// Where a row's operands lie.
+template <typename T> struct RowAt {
+    const T *x, *f, *q, *g1, *b1, *g2, *b2;
+    __device__ __forceinline__ RowAt(const NormArgs &a, int64_t b, int64_t t)
+        : x(at(a.x, b, t)), f(at(a.f, b, t)), q(at(a.gate, b, a.gate_rows ? t : 0)), g1(at(a.post_gain, b, 0)), b1(at(a.post_bias, b, 0)), g2(at(a.pre_gain, b, 0)), b2(at(a.pre_bias, b, 0)) { }
+    static __device__ __forceinline__ T *at(const Span &s, int64_t b, int64_t t) { return s.p ? (T *)s.p + b * s.s + t * s.ld : nullptr; }
+};
+
+// Values of one piece of a row, with those of operands that are not there by what leaves them out.
+template <typename T> struct Values {
+    static constexpr int VALUES = Piece<T>::VALUES;
+    float fn[VALUES], u[VALUES], q[VALUES], slope[VALUES], h[VALUES];
+    __device__ __forceinline__ Values(const NormArgs &a, const RowAt<T> &row, int64_t col, const Unit &post)
+    {
+        const int64_t left = a.width - col;
+        const Piece<T> x = load_piece(row.x + col, left);
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) { fn[e] = 0.0f; u[e] = 0.0f; q[e] = 1.0f; slope[e] = 0.0f; h[e] = a.x_scale * x.get(e); }
+        if (!row.f) return;
+        const Piece<T> f = load_piece(row.f + col, left);
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) fn[e] = u[e] = a.post ? unit_of(post, f.get(e)) : f.get(e);
+        if (row.g1) {
+            const Piece<T> g = load_piece(row.g1 + col, left);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) u[e] *= g.get(e);
+        }
+        if (row.b1) {
+            const Piece<T> g = load_piece(row.b1 + col, left);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) u[e] += g.get(e);
+        }
+        if (row.q) {
+            const Piece<T> g = load_piece(row.q + col, left);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) gate_of(a.act, g.get(e), q[e], slope[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) h[e] = fmaf(a.f_scale * q[e], u[e], h[e]);
+    }
+};
+
+// ---- rows of any length, read anew for each of their sums ------------------------------------------------------------
+
+template <int N, typename S> __device__ __forceinline__ void sum_over(S (&v)[N], S (*room)[N])
+{
+    __syncthreads();                               // the sums before have been read
+    workgroup_sum<THREADS>(v, room);
+}
+
+// value(col, v): the values at a column.
+template <typename T, class Get> __device__ __forceinline__ Unit unit_over(const NormArgs &a, const Get &get, double (*room)[1])
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    double mean = 0.0;
+    if (a.layer) {
+        double sum[1] = {0.0};
+        for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+            float v[VALUES];
+            get(col, v);
+            for (int e = 0; e < VALUES && col + e < a.width; ++e) sum[0] += v[e];
+        }
+        sum_over(sum, room);
+        mean = sum[0] / (double)a.width;
+    }
+    double sum[1] = {0.0};
+    for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+        float v[VALUES];
+        get(col, v);
+        for (int e = 0; e < VALUES && col + e < a.width; ++e) sum[0] = fma((double)v[e] - mean, (double)v[e] - mean, sum[0]);
+    }
+    sum_over(sum, room);
+    Unit n;
+    n.mean = (float)mean;
+    n.rest = (float)(mean - (double)n.mean);
+    n.r = (float)rsqrt(sum[0] / (double)a.width + (double)a.eps);
+    return n;
+}
+
+template <typename T> __device__ __forceinline__ void units_of(const NormArgs &a, const RowAt<T> &row, Unit &post, Unit &pre, double (*room)[1])
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    if (a.post && row.f)
+        post = unit_over<T>(a, [&](int64_t col, float (&v)[VALUES]) {
+            const Piece<T> f = load_piece(row.f + col, a.width - col);
+            for (int e = 0; e < VALUES; ++e) v[e] = f.get(e);
+        }, room);
+    if (a.pre)
+        pre = unit_over<T>(a, [&](int64_t col, float (&v)[VALUES]) {
+            const Values<T> at(a, row, col, post);
+            for (int e = 0; e < VALUES; ++e) v[e] = at.h[e];
+        }, room);
+}
+
+template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_kernel(NormArgs a)
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    __shared__ double room[THREADS / 64][1];
+    for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
+        const RowAt<T> row(a, blockIdx.y, t);
+        Unit post{}, pre{};
+        units_of(a, row, post, pre, room);
+        T *h = RowAt<T>::at(a.h, blockIdx.y, t), *y = RowAt<T>::at(a.y, blockIdx.y, t);
+        for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+            const int64_t left = a.width - col;
+            const Values<T> at(a, row, col, post);
+            Piece<T> out;
+            float v[VALUES];
+            if (a.pre) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) v[e] = unit_of(pre, at.h[e]);
+                if (row.g2) {
+                    const Piece<T> g = load_piece(row.g2 + col, left);
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) v[e] *= g.get(e);
+                }
+                if (row.b2) {
+                    const Piece<T> g = load_piece(row.b2 + col, left);
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) v[e] += g.get(e);
+                }
+                out.set(v);
+                if (y) store_piece(y + col, left, out);
+            }
+            if (h) {
+                out.set(at.h);
+                store_piece(h + col, left, out);
+            }
+        }
+    }
+}
+
+// Sums over the rows, in order: dg1, db1, dg2, db2, dq.  A workgroup's rows leave their sums in its own row of partial sums [SUMS][padded].
+constexpr int SUMS = 5;
+struct Partials { float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS]; };  // place: which of the rows that are there, -1: none
+
+template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_kernel(NormArgs a, Partials to)
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    __shared__ double room[THREADS / 64][1];
+    __shared__ float pair[THREADS / 64][2];
+    float *mine = to.p + (blockIdx.y * to.workgroups + blockIdx.x) * to.sums * to.padded;
+    const float share = 1.0f / (float)a.width;
+    for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
+        const RowAt<T> row(a, blockIdx.y, t);
+        Unit post{}, pre{};
+        units_of(a, row, post, pre, room);
+        const T *dy = RowAt<T>::at(a.dy, blockIdx.y, t), *dh = RowAt<T>::at(a.dh, blockIdx.y, t);
+        float along[2] = {0.0f, 0.0f}, back[2] = {0.0f, 0.0f};
+        // e and hn
+        const auto before = [&](const Values<T> &at, int64_t col, float (&d)[VALUES], float (&e)[VALUES], float (&hn)[VALUES]) {
+            const int64_t left = a.width - col;
+            const Piece<T> v = load_piece(dy + col, left);
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) { d[k] = e[k] = v.get(k); hn[k] = unit_of(pre, at.h[k]); }
+            if (!row.g2) return;
+            const Piece<T> g = load_piece(row.g2 + col, left);
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) e[k] *= g.get(k);
+        };
+        if (a.pre) {
+            for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+                const Values<T> at(a, row, col, post);
+                float d[VALUES], e[VALUES], hn[VALUES];
+                before(at, col, d, e, hn);
+                for (int k = 0; k < VALUES && col + k < a.width; ++k) { along[0] += e[k]; along[1] = fmaf(e[k], hn[k], along[1]); }
+            }
+            sum_over(along, pair);
+        }
+        const float mean_e = a.layer ? along[0] * share : 0.0f, mean_eh = along[1] * share;
+        // D
+        const auto reaches = [&](const Values<T> &at, int64_t col, float (&D)[VALUES], float (&d)[VALUES], float (&hn)[VALUES]) {
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) D[k] = d[k] = hn[k] = 0.0f;
+            if (dh) {
+                const Piece<T> v = load_piece(dh + col, a.width - col);
+#pragma unroll
+                for (int k = 0; k < VALUES; ++k) D[k] = v.get(k);
+            }
+            if (!a.pre) return;
+            float e[VALUES];
+            before(at, col, d, e, hn);
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) D[k] = fmaf(pre.r, (e[k] - mean_e) - hn[k] * mean_eh, D[k]);
+        };
+        const auto gain_post = [&](int64_t col, float (&g)[VALUES]) {
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) g[k] = 1.0f;
+            if (!row.g1) return;
+            const Piece<T> v = load_piece(row.g1 + col, a.width - col);
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) g[k] = v.get(k);
+        };
+        if (row.f && a.post) {
+            for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+                const Values<T> at(a, row, col, post);
+                float D[VALUES], d[VALUES], hn[VALUES], g[VALUES];
+                reaches(at, col, D, d, hn);
+                gain_post(col, g);
+                for (int k = 0; k < VALUES && col + k < a.width; ++k) {
+                    const float c = a.f_scale * at.q[k] * D[k] * g[k];
+                    back[0] += c;
+                    back[1] = fmaf(c, at.fn[k], back[1]);
+                }
+            }
+            sum_over(back, pair);
+        }
+        const float mean_c = a.layer ? back[0] * share : 0.0f, mean_cf = back[1] * share;
+        T *dx = RowAt<T>::at(a.dx, blockIdx.y, t), *df = RowAt<T>::at(a.df, blockIdx.y, t), *dq = a.gate_rows ? RowAt<T>::at(a.dgate, blockIdx.y, t) : nullptr;
+        for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
+            const int64_t left = a.width - col;
+            const Values<T> at(a, row, col, post);
+            float D[VALUES], d[VALUES], hn[VALUES], g[VALUES], v[VALUES], add[SUMS][VALUES];
+            reaches(at, col, D, d, hn);
+            Piece<T> out;
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) v[k] = a.x_scale * D[k];
+            out.set(v);
+            if (dx) store_piece(dx + col, left, out);
+            gain_post(col, g);
+#pragma unroll
+            for (int k = 0; k < VALUES; ++k) {
+                const float du = a.f_scale * at.q[k] * D[k];
+                add[0][k] = du * at.fn[k];
+                add[1][k] = du;
+                add[2][k] = d[k] * hn[k];
+                add[3][k] = d[k];
+                add[4][k] = a.f_scale * at.slope[k] * at.u[k] * D[k];
+                v[k] = a.post ? post.r * ((du * g[k] - mean_c) - at.fn[k] * mean_cf) : du;
+            }
+            if (df) {
+                out.set(v);
+                store_piece(df + col, left, out);
+            }
+            if (dq) {
+                out.set(add[4]);
+                store_piece(dq + col, left, out);
+            }
+#pragma unroll
+            for (int s = 0; s < SUMS; ++s)
+                if (to.place[s] >= 0)
+#pragma unroll
+                    for (int k = 0; k < VALUES; ++k) {
+                        float *p = mine + to.place[s] * to.padded + col + k;
+                        *p = t == blockIdx.x ? add[s][k] : *p + add[s][k];
+                    }
+        }
+    }
+}
+
+// Column sums: 64 columns for a workgroup, a quarter of the partial sums for each of its waves.
+template <typename T> __global__ void __launch_bounds__(THREADS) join_sums_kernel(NormArgs a, Partials from)
+{
+    __shared__ double part[THREADS / 64][64];
+    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    double sum = 0.0;
+    if (col < a.width)
+        for (int64_t w = threadIdx.x >> 6; w < from.workgroups; w += THREADS / 64)
+            sum += from.p[((blockIdx.z * from.workgroups + w) * from.sums + blockIdx.y) * from.padded + col];
+    part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64 || col >= a.width) return;
+    for (int w = 1; w < THREADS / 64; ++w) sum += part[w][threadIdx.x];
+    store_value(RowAt<T>::at(from.out[blockIdx.y], blockIdx.z, 0) + col, (float)sum);
+}
+
+// ---- launches --------------------------------------------------------------------------------------------------------
+
+void launch_block_norm(hipStream_t s, const NormArgs &a)
+{
+    if (a.batch == 0 || a.rows == 0) return;
+    const dim3 grid((uint32_t)(a.rows < (1 << 20) ? a.rows : 1 << 20), (uint32_t)a.batch);
+    if (a.bf16) long_norm_kernel<uint16_t><<<grid, THREADS, 0, s>>>(a);
+    else long_norm_kernel<float><<<grid, THREADS, 0, s>>>(a);
+}
+
+static Partials partials_of(const NormArgs &a, void *work)
+{
+    Partials to{};
+    const Span *const outs[SUMS] = {&a.dpost_gain, &a.dpost_bias, &a.dpre_gain, &a.dpre_bias, &a.dgate};
+    for (int s = 0; s < SUMS; ++s) {
+        const bool there = outs[s]->p && !(s == 4 && a.gate_rows);
+        to.place[s] = there ? to.sums : -1;
+        if (there) to.out[to.sums++] = *outs[s];
+    }
+    to.p = (float *)work;
+    to.padded = up_to(a.width, 8);
+    const int64_t most = a.batch * 8 < 512 ? 512 / a.batch : 8;
+    to.workgroups = a.rows < most ? a.rows : most;
+    return to;
+}
+
+int64_t block_norm_grad_workspace(const NormArgs &a)
+{
+    if (a.batch == 0) return 0;
+    const Partials to = partials_of(a, nullptr);
+    return 4 * a.batch * to.workgroups * to.sums * to.padded;
+}
+
+template <typename T> static void block_norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
+{
+    if (to.workgroups > 0) long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+    if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + 63) / 64), to.sums, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+}
+
+void launch_block_norm_grad(hipStream_t s, const NormArgs &a, void *work)
+{
+    if (a.batch == 0) return;
+    const Partials to = partials_of(a, work);
+    if (a.bf16) block_norm_grad_of<uint16_t>(s, a, to);
+    else block_norm_grad_of<float>(s, a, to);
+}
+
+}  // namespace netmax

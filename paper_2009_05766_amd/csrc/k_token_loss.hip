@@ -15,7 +15,7 @@
 // policy, 8192 x 131072 bfloat16 (a row in ten without weight): 795 us for 4.08 GB, the rate of a large copy (5.1 TB/s); read twice, without
 // registers, 2.7 ms.  preference, 16384 x 50000 (a quarter without weight): rows 233 us, gradient 518 us for 1.23 and 2.87 GB: the slopes of a
 // sequence's rows depend on all of them, so rows that count are read twice.
-#include "gemm.h"
+#include "piece.h"
 #include "token_loss.h"
 
 #include <type_traits>
@@ -24,26 +24,6 @@ namespace netmax {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LOWEST = -0x1.fffffep127f;         // less than any value but -inf, and differences to it are no NaN
-
-// 16 bytes of a row, at any address of a value.
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-    static constexpr int VALUES = 4;
-    typedef f32x4_any Memory;
-    f32x4 v;
-    __device__ __forceinline__ float get(int k) const { return v[k]; }
-    __device__ __forceinline__ void set(const float (&x)[4]) { v = f32x4{x[0], x[1], x[2], x[3]}; }
-};
-template <> struct Piece<uint16_t> {
-    static constexpr int VALUES = 8;
-    typedef u32x4_any Memory;
-    u32x4 v;
-    __device__ __forceinline__ float get(int k) const { return __uint_as_float(k & 1 ? v[k >> 1] & 0xFFFF0000u : v[k >> 1] << 16); }
-    __device__ __forceinline__ void set(const float (&x)[8])
-    {
-        v = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-    }
-};
 
 template <typename T> struct Row {
     T *p; int64_t vocab;
