@@ -84,7 +84,7 @@ template <typename T> struct Values {
 template <int N, typename S> __device__ __forceinline__ void sum_over(S (&v)[N], S (*room)[N])
 {
     __syncthreads();                               // the sums before have been read
-    workgroup_sum<THREADS>(v, room);
+    row_sum<THREADS>(v, room);
 }
 
 // value(col, v): the values at a column.
@@ -303,14 +303,364 @@ template <typename T> __global__ void __launch_bounds__(THREADS) join_sums_kerne
     store_value(RowAt<T>::at(from.out[blockIdx.y], blockIdx.z, 0) + col, (float)sum);
 }
 
+// ---- rows that a group of lanes keeps in registers -------------------------------------------------------------------
+//
+// LANES lanes hold a row's operands, PIECES pieces each, between its sums: everything is read once.  Narrow rows share a workgroup.
+
+constexpr int threads_of(int lanes) { return lanes < THREADS ? THREADS : lanes; }
+
+// What of a row the lane's piece k holds: `left` values from its column on, none if that is not positive.
+template <typename T, int LANES> struct Lane {
+    static constexpr int VALUES = Piece<T>::VALUES;
+    int64_t width, first;
+    __device__ __forceinline__ Lane(int64_t width_) : width(width_), first((int64_t)(threadIdx.x % LANES) * VALUES) { }
+    __device__ __forceinline__ int64_t col(int k) const { return first + (int64_t)k * LANES * VALUES; }
+    __device__ __forceinline__ int64_t left(int k) const { return width - col(k); }
+    template <int PIECES> __device__ __forceinline__ void load(const T *row, Piece<T> (&to)[PIECES], bool there = true) const
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            if (row && there && left(k) > 0) to[k] = load_piece(row + col(k), left(k));
+            else to[k].v = decltype(to[k].v){};
+        }
+    }
+    template <int PIECES> __device__ __forceinline__ void store(T *row, int k, const float (&v)[PIECES][VALUES]) const
+    {
+        Piece<T> out;
+        out.set(v[k]);
+        if (left(k) > 0) store_piece(row + col(k), left(k), out);
+    }
+    // values behind the row become 0
+    __device__ __forceinline__ void clear(int k, float (&v)[VALUES]) const
+    {
+        if (left(k) < VALUES)
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = e < left(k) ? v[e] : 0.0f;
+    }
+};
+
+// get(k, v): the values of the lane's piece k, 0 behind the row.
+template <typename T, int LANES, int PIECES, bool LAYER, class Get>
+__device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get &get, double share, double eps, double (*room)[1], double (*second)[1])
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    double mean = 0.0;
+    if constexpr (LAYER) {
+        double sum[1] = {0.0};
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            float v[VALUES];
+            get(k, v);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) sum[0] += v[e];
+        }
+        row_sum<LANES>(sum, room);
+        mean = sum[0] * share;
+    }
+    double sum[1] = {0.0};
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        float v[VALUES];
+        get(k, v);
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) {
+            const double d = LAYER && e >= lane.left(k) ? 0.0 : (double)v[e] - mean;
+            sum[0] = fma(d, d, sum[0]);
+        }
+    }
+    row_sum<LANES>(sum, second);
+    Unit n;
+    n.mean = (float)mean;
+    n.rest = (float)(mean - (double)n.mean);
+    n.r = (float)rsqrt(sum[0] * share + eps);
+    return n;
+}
+template <bool LAYER> __device__ __forceinline__ float unit_held_of(const Unit &n, float v) { return LAYER ? unit_of(n, v) : v * n.r; }
+
+template <typename T, int LANES, int PIECES, bool LAYER>
+__global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
+{
+    constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES;
+    __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
+    const int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    if (GROUPS > 1 && t >= a.rows) return;                          // whole groups, and no barriers
+    const RowAt<T> row(a, blockIdx.y, t);
+    const Lane<T, LANES> lane(a.width);
+    const double share = 1.0 / (double)a.width;
+    Piece<T> x[PIECES], f[PIECES], q[PIECES], g1[PIECES], b1[PIECES], g2[PIECES], b2[PIECES];
+    lane.load(row.x, x);
+    lane.load(row.f, f);
+    lane.load(row.q, q);
+    lane.load(row.g1, g1);
+    lane.load(row.b1, b1);
+    lane.load(row.g2, g2);
+    lane.load(row.b2, b2);
+    float h[PIECES][VALUES];
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) h[k][e] = a.x_scale * x[k].get(e);
+    if (row.f) {
+        Unit post{0.0f, 0.0f, 1.0f};
+        if (a.post) post = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = f[k].get(e);
+        }, share, a.eps, room[0], room[1]);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            float u[VALUES];
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) u[e] = unit_held_of<LAYER>(post, f[k].get(e));
+            if (row.g1)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) u[e] *= g1[k].get(e);
+            if (row.b1)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) u[e] += b1[k].get(e);
+            if (row.q) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    float value, slope;
+                    gate_of(a.act, q[k].get(e), value, slope);
+                    h[k][e] = fmaf(a.f_scale * value, u[e], h[k][e]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) h[k][e] = fmaf(a.f_scale, u[e], h[k][e]);
+            }
+            lane.clear(k, h[k]);
+        }
+    }
+    T *to_h = RowAt<T>::at(a.h, blockIdx.y, t), *to_y = RowAt<T>::at(a.y, blockIdx.y, t);
+    if (to_h)
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) lane.store(to_h, k, h);
+    if (!to_y) return;
+    const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) v[e] = h[k][e];
+    }, share, a.eps, room[2], room[3]);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) h[k][e] = unit_held_of<LAYER>(pre, h[k][e]);
+        if (row.g2)
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) h[k][e] *= g2[k].get(e);
+        if (row.b2)
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) h[k][e] += b2[k].get(e);
+        lane.store(to_y, k, h);
+    }
+}
+
+// Which sums over the rows a kernel holds in registers: those of a norm alone, those of a block's gains and gate, or all.
+enum Form : int { NORM_ALONE = 0, BLOCK_GAINS = 1, BLOCK_ALL = 2 };
+
+template <typename T, int LANES, int PIECES, bool LAYER, int FORM>
+__global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a, Partials to)
+{
+    constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES;
+    constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS;
+    __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
+    __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][2];
+    __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
+    const Lane<T, LANES> lane(a.width);
+    const double share = 1.0 / (double)a.width;
+    const float share_f = (float)share;
+    Piece<T> g1[PIECES], b1[PIECES], g2[PIECES], q[PIECES];
+    const RowAt<T> vectors(a, blockIdx.y, 0);
+    if constexpr (BLOCK) { lane.load(vectors.g1, g1); lane.load(vectors.b1, b1); lane.load(vectors.q, q, !a.gate_rows); }
+    lane.load(vectors.g2, g2);
+    float sums[SUMS][PIECES][VALUES] = {};
+    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES; t < a.rows; t += (int64_t)gridDim.x * GROUPS) {
+        const RowAt<T> row(a, blockIdx.y, t);
+        Piece<T> x[PIECES], f[PIECES], dy[PIECES], dh[PIECES];
+        lane.load(row.x, x);
+        if constexpr (BLOCK) {
+            lane.load(row.f, f);
+            if (a.gate_rows) lane.load(row.q, q);
+        }
+        lane.load(RowAt<T>::at(a.dy, blockIdx.y, t), dy);
+        lane.load(RowAt<T>::at(a.dh, blockIdx.y, t), dh);
+        Unit post{0.0f, 0.0f, 1.0f};
+        if (BLOCK && a.post) post = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = f[k].get(e);
+        }, share, a.eps, room[0], room[1]);
+        // u of a piece
+        const auto branch = [&](int k, float (&fn)[VALUES], float (&u)[VALUES]) {
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) fn[e] = u[e] = unit_held_of<LAYER>(post, f[k].get(e));
+            if (row.g1)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) u[e] *= g1[k].get(e);
+            if (row.b1)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) u[e] += b1[k].get(e);
+        };
+        float d[PIECES][VALUES];                   // D
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) d[k][e] = dh[k].get(e);
+        if (a.pre) {
+            float h[PIECES][VALUES];
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) h[k][e] = a.x_scale * x[k].get(e);
+                if constexpr (BLOCK) {
+                    float fn[VALUES], u[VALUES];
+                    branch(k, fn, u);
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) {
+                        float value = 1.0f, slope;
+                        if (row.q) gate_of(a.act, q[k].get(e), value, slope);
+                        h[k][e] = fmaf(a.f_scale * value, u[e], h[k][e]);
+                    }
+                    lane.clear(k, h[k]);
+                }
+            }
+            const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) v[e] = h[k][e];
+            }, share, a.eps, room[2], room[3]);
+            float along[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    const float v = dy[k].get(e), w = row.g2 ? v * g2[k].get(e) : v;
+                    h[k][e] = unit_held_of<LAYER>(pre, h[k][e]);
+                    along[0] += w;
+                    along[1] = fmaf(w, h[k][e], along[1]);
+                    sums[2][k][e] = fmaf(v, h[k][e], sums[2][k][e]);
+                    if (BIASES) sums[3][k][e] += v;
+                }
+            row_sum<LANES>(along, pairs[0]);
+            const float mean_e = LAYER ? along[0] * share_f : 0.0f, mean_eh = along[1] * share_f;
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    const float v = dy[k].get(e), w = row.g2 ? v * g2[k].get(e) : v;
+                    d[k][e] = fmaf(pre.r, (w - mean_e) - h[k][e] * mean_eh, d[k][e]);
+                }
+        }
+        T *dx = RowAt<T>::at(a.dx, blockIdx.y, t);
+        float out[PIECES][VALUES];
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            lane.clear(k, d[k]);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) out[k][e] = a.x_scale * d[k][e];
+            if (dx) lane.store(dx, k, out);
+        }
+        if constexpr (BLOCK) {
+            T *df = RowAt<T>::at(a.df, blockIdx.y, t), *dq = a.gate_rows ? RowAt<T>::at(a.dgate, blockIdx.y, t) : nullptr;
+            float back[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                float fn[VALUES], u[VALUES], gate[VALUES];
+                branch(k, fn, u);
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    float value = 1.0f, slope = 0.0f;
+                    if (row.q) gate_of(a.act, q[k].get(e), value, slope);
+                    gate[e] = a.f_scale * slope * u[e] * d[k][e];
+                    if (!a.gate_rows) sums[4][k][e] += gate[e];
+                    d[k][e] *= a.f_scale * value;                   // b act(q) D
+                    if (BIASES) sums[1][k][e] += d[k][e];
+                    sums[0][k][e] = fmaf(d[k][e], fn[e], sums[0][k][e]);
+                    if (row.g1) d[k][e] *= g1[k].get(e);            // c
+                    back[0] += d[k][e];
+                    back[1] = fmaf(d[k][e], fn[e], back[1]);
+                }
+                if (dq) {
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) out[k][e] = gate[e];
+                    lane.store(dq, k, out);
+                }
+            }
+            if (a.post) row_sum<LANES>(back, pairs[1]);
+            const float mean_c = LAYER && a.post ? back[0] * share_f : 0.0f, mean_cf = a.post ? back[1] * share_f : 0.0f;
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    const float fn = unit_held_of<LAYER>(post, f[k].get(e));
+                    out[k][e] = a.post ? post.r * ((d[k][e] - mean_c) - fn * mean_cf) : d[k][e];
+                }
+                if (df) lane.store(df, k, out);
+            }
+        }
+    }
+    float *mine = to.p + (blockIdx.y * to.workgroups + blockIdx.x) * to.sums * to.padded;
+#pragma unroll
+    for (int s = 0; s < SUMS; ++s) {
+        if ((!BLOCK && s != 2 && s != 3) || (!BIASES && (s == 1 || s == 3))) continue;
+        if (to.place[s] < 0) continue;
+        if constexpr (GROUPS > 1) {                // rows of the same workgroup, in order
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) shared_sums[threadIdx.x / LANES][(k * LANES + threadIdx.x % LANES) * VALUES + e] = sums[s][k][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < LANES * PIECES * VALUES && c < to.padded; c += THREADS) {
+                float sum = 0.0f;
+                for (int g = 0; g < GROUPS; ++g) sum += shared_sums[g][c];
+                mine[to.place[s] * to.padded + c] = sum;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                if (lane.left(k) > 0)
+#pragma unroll
+                    for (int e = 0; e < VALUES; e += 4)
+                        *reinterpret_cast<f32x4 *>(mine + to.place[s] * to.padded + lane.col(k) + e) = f32x4{sums[s][k][e], sums[s][k][e + 1], sums[s][k][e + 2], sums[s][k][e + 3]};
+        }
+    }
+}
+
 // ---- launches --------------------------------------------------------------------------------------------------------
+
+template <typename T> static int64_t pieces_of(int64_t width) { return (width + Piece<T>::VALUES - 1) / Piece<T>::VALUES; }
+
+// Lanes and pieces for a row of n pieces; longer ones than any of them hold are streamed.
+template <int LANES_, int PIECES_> struct Held { static constexpr int LANES = LANES_, PIECES = PIECES_; };
+template <class Go, class Long> static void with_row(int64_t n, const Go &go, const Long &stream)
+{
+    if (n <= 8) go(Held<8, 1>());
+    else if (n <= 16) go(Held<16, 1>());
+    else if (n <= 32) go(Held<32, 1>());
+    else if (n <= 64) go(Held<64, 1>());
+    else if (n <= 128) go(Held<64, 2>());
+    else if (n <= 256) go(Held<256, 1>());
+    else if (n <= 512) go(Held<256, 2>());
+    else if (n <= 1024) go(Held<512, 2>());
+    else if (n <= 2048) go(Held<1024, 2>());
+    else stream();
+}
+
+template <typename T> static void block_norm_of(hipStream_t s, const NormArgs &a)
+{
+    with_row(pieces_of<T>(a.width), [&](auto held) {
+        constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES, GROUPS = threads_of(LANES) / LANES;
+        const dim3 grid((uint32_t)((a.rows + GROUPS - 1) / GROUPS), (uint32_t)a.batch);
+        if (a.layer) norm_kernel<T, LANES, PIECES, true><<<grid, threads_of(LANES), 0, s>>>(a);
+        else norm_kernel<T, LANES, PIECES, false><<<grid, threads_of(LANES), 0, s>>>(a);
+    }, [&]() {
+        long_norm_kernel<T><<<dim3((uint32_t)(a.rows < (1 << 20) ? a.rows : 1 << 20), (uint32_t)a.batch), THREADS, 0, s>>>(a);
+    });
+}
 
 void launch_block_norm(hipStream_t s, const NormArgs &a)
 {
     if (a.batch == 0 || a.rows == 0) return;
-    const dim3 grid((uint32_t)(a.rows < (1 << 20) ? a.rows : 1 << 20), (uint32_t)a.batch);
-    if (a.bf16) long_norm_kernel<uint16_t><<<grid, THREADS, 0, s>>>(a);
-    else long_norm_kernel<float><<<grid, THREADS, 0, s>>>(a);
+    if (a.bf16) block_norm_of<uint16_t>(s, a);
+    else block_norm_of<float>(s, a);
 }
 
 static Partials partials_of(const NormArgs &a, void *work)
@@ -324,8 +674,10 @@ static Partials partials_of(const NormArgs &a, void *work)
     }
     to.p = (float *)work;
     to.padded = up_to(a.width, 8);
-    const int64_t most = a.batch * 8 < 512 ? 512 / a.batch : 8;
-    to.workgroups = a.rows < most ? a.rows : most;
+    int64_t rows = 1;                              // of a workgroup at once
+    with_row(a.bf16 ? pieces_of<uint16_t>(a.width) : pieces_of<float>(a.width), [&](auto held) { rows = threads_of(decltype(held)::LANES) / decltype(held)::LANES; }, []() { });
+    const int64_t most = a.batch * 8 < 512 ? 512 / a.batch : 8, all = (a.rows + rows - 1) / rows;
+    to.workgroups = all < most ? all : most;
     return to;
 }
 
@@ -336,9 +688,24 @@ int64_t block_norm_grad_workspace(const NormArgs &a)
     return 4 * a.batch * to.workgroups * to.sums * to.padded;
 }
 
+template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to, int64_t rows_there)
+{
+    const dim3 grid((uint32_t)to.workgroups, (uint32_t)a.batch);
+    const bool block = rows_there, biases = to.place[1] >= 0 || to.place[3] >= 0;
+    if (!block) norm_grad_kernel<T, LANES, PIECES, LAYER, NORM_ALONE><<<grid, threads_of(LANES), 0, s>>>(a, to);
+    else if (!biases) norm_grad_kernel<T, LANES, PIECES, LAYER, BLOCK_GAINS><<<grid, threads_of(LANES), 0, s>>>(a, to);
+    else norm_grad_kernel<T, LANES, PIECES, LAYER, BLOCK_ALL><<<grid, threads_of(LANES), 0, s>>>(a, to);
+}
+
 template <typename T> static void block_norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
 {
-    if (to.workgroups > 0) long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+    if (to.workgroups > 0) with_row(pieces_of<T>(a.width), [&](auto held) {
+        constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
+        if (a.layer) norm_grad_of<T, LANES, PIECES, true>(s, a, to, a.f.p != nullptr);
+        else norm_grad_of<T, LANES, PIECES, false>(s, a, to, a.f.p != nullptr);
+    }, [&]() {
+        long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+    });
     if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + 63) / 64), to.sums, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
 }
 

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(THREADS) squares_kernel(Items items, double *p
         const Item &t = items.at[find.tensor(u)];
         sum[0] += t.bf16 ? squares_of<uint16_t>(t, u, blockIdx.y) : squares_of<float>(t, u, blockIdx.y);
     }
-    workgroup_sum<THREADS>(sum, room);
+    row_sum<THREADS>(sum, room);
     if (threadIdx.x == 0) partials[blockIdx.y * row_of_partials + blockIdx.x] = sum[0];
 }
 
@@ -78,7 +78,7 @@ __device__ __forceinline__ double total_of(const double *partials, int64_t n)
     __shared__ double room[THREADS / 64][1];
     double sum[1] = {0.0};
     for (int64_t k = threadIdx.x; k < n; k += THREADS) sum[0] += partials[k];
-    workgroup_sum<THREADS>(sum, room);
+    row_sum<THREADS>(sum, room);
     return sum[0];
 }
 

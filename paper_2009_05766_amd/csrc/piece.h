@@ -51,14 +51,44 @@ template <typename T> __device__ __forceinline__ void store_piece(T *p, int64_t 
     }
 }
 
-// Sums of a whole workgroup, in a fixed order; every thread gets them.  One barrier: the caller separates two sums through the same LDS by another.
-template <int THREADS, int N, typename S> __device__ __forceinline__ void workgroup_sum(S (&v)[N], S (*room)[N])
+// Sums over LANES neighbouring lanes (a power of two, 64 at most), each of which gets them: the lanes of a row of 16 exchange values on their way into the addition.
+template <int CONTROL> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xF, 0xF, true); }
+template <int CONTROL> __device__ __forceinline__ float moved(float v) { return __uint_as_float(moved<CONTROL>(__float_as_uint(v))); }
+template <int CONTROL> __device__ __forceinline__ double moved(double v)
+{
+    return __hiloint2double((int)moved<CONTROL>((uint32_t)__double2hiint(v)), (int)moved<CONTROL>((uint32_t)__double2loint(v)));
+}
+template <bool HALVES> __device__ __forceinline__ float both(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto w = HALVES ? __builtin_amdgcn_permlane32_swap(u, u, false, false) : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+template <bool HALVES> __device__ __forceinline__ double both(double v)
+{
+    const uint32_t lo = (uint32_t)__double2loint(v), hi = (uint32_t)__double2hiint(v);
+    const auto l = HALVES ? __builtin_amdgcn_permlane32_swap(lo, lo, false, false) : __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+    const auto h = HALVES ? __builtin_amdgcn_permlane32_swap(hi, hi, false, false) : __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    return __hiloint2double((int)h[0], (int)l[0]) + __hiloint2double((int)h[1], (int)l[1]);
+}
+template <int LANES, typename S> __device__ __forceinline__ S lanes_sum(S v)
+{
+    if constexpr (LANES >= 2) v += moved<0xB1>(v);                  // lanes 1 0 3 2
+    if constexpr (LANES >= 4) v += moved<0x4E>(v);                  // lanes 2 3 0 1
+    if constexpr (LANES >= 8) v += moved<0x141>(v);                 // eight in reverse
+    if constexpr (LANES >= 16) v += moved<0x140>(v);                // sixteen in reverse
+    if constexpr (LANES >= 32) v = both<false>(v);
+    if constexpr (LANES >= 64) v = both<true>(v);
+    return v;
+}
+
+// Sums over the LANES lanes that work on one row: part of a wave, or a workgroup of so many threads, through `room`, with one barrier; before a `room` is used again there is
+// another one (of another sum, or the caller's).
+template <int LANES, int N, typename S> __device__ __forceinline__ void row_sum(S (&v)[N], S (*room)[N])
 {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], d);
-    if constexpr (THREADS > 64) {
+    for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[k]);
+    if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int k = 0; k < N; ++k) room[threadIdx.x >> 6][k] = v[k];
@@ -66,7 +96,7 @@ template <int THREADS, int N, typename S> __device__ __forceinline__ void workgr
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = 0;
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w)
+        for (int w = 0; w < LANES / 64; ++w)
 #pragma unroll
             for (int k = 0; k < N; ++k) v[k] += room[w][k];
     }
