@@ -11,7 +11,8 @@ enum Gate : int { GATE_NONE = 0, GATE_SIGMOID = 1, GATE_TANH = 2 };
 
 struct NormArgs {
     int64_t batch, rows, width;
-    int bf16, layer, act, gate_rows, post, pre; float x_scale, f_scale, eps;
+    int bf16, layer, act, gate_rows, post, pre; float x_scale, f_scale;
+    double eps, share;                                 // share: 1 / width
     Span x, f, gate, post_gain, post_bias, pre_gain, pre_bias, h, y;
     Span dy, dh, dx, df, dgate, dpost_gain, dpost_bias, dpre_gain, dpre_bias;
 };

@@ -9,10 +9,12 @@
 // h is computed anew from x and f, in float, so that nothing has to be kept and the gradients do not depend on h's rounding.
 // Bound by memory: x, f and q are read, h and y written; the gradients read dy and dh as well and write dx, df and dq.
 //
-// Squares are summed in double (a float's is exact there): rows of any size have their mean square, over the whole range of the type.  A layer norm's mean is
-// subtracted as two floats, so that rows far from 0 keep their bits.
+// Means and squares are summed in double (a float's square is exact there): rows of any size have their mean square, over the whole range of the type.  Where a lane holds few values of a
+// row it sums their squares in float, as long as that is far from both ends of float's range.  A layer norm's mean is subtracted as two floats, so that rows far from 0 keep their bits.
 #include "block_norm.h"
 #include "piece.h"
+
+#include <type_traits>
 
 namespace netmax {
 
@@ -34,6 +36,31 @@ __device__ __forceinline__ void gate_of(int act, float q, float &value, float &s
     } else {
         value = q;
         slope = 1.0f;
+    }
+}
+
+// scale times values or slopes of a piece of a gate.
+template <typename T> __device__ __forceinline__ void gates_of(int act, float scale, const Piece<T> &q, float (&gate)[Piece<T>::VALUES])
+{
+    if (act == GATE_NONE) {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::VALUES; ++e) gate[e] = scale * q.get(e);
+    } else {
+#pragma unroll
+        for (int e = 0; e < Piece<T>::VALUES; ++e) {
+            float value, slope;
+            gate_of(act, q.get(e), value, slope);
+            gate[e] = scale * value;
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ void slopes_of(int act, float scale, const Piece<T> &q, float (&slopes)[Piece<T>::VALUES])
+{
+#pragma unroll
+    for (int e = 0; e < Piece<T>::VALUES; ++e) {
+        float value, slope;
+        gate_of(act, q.get(e), value, slope);
+        slopes[e] = scale * slope;
     }
 }
 
@@ -100,7 +127,7 @@ template <typename T, class Get> __device__ __forceinline__ Unit unit_over(const
             for (int e = 0; e < VALUES && col + e < a.width; ++e) sum[0] += v[e];
         }
         sum_over(sum, room);
-        mean = sum[0] / (double)a.width;
+        mean = sum[0] * a.share;
     }
     double sum[1] = {0.0};
     for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
@@ -112,7 +139,7 @@ template <typename T, class Get> __device__ __forceinline__ Unit unit_over(const
     Unit n;
     n.mean = (float)mean;
     n.rest = (float)(mean - (double)n.mean);
-    n.r = (float)rsqrt(sum[0] / (double)a.width + (double)a.eps);
+    n.r = (float)rsqrt(sum[0] * a.share + a.eps);
     return n;
 }
 
@@ -179,7 +206,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
     __shared__ double room[THREADS / 64][1];
     __shared__ float pair[THREADS / 64][2];
     float *mine = to.p + (blockIdx.y * to.workgroups + blockIdx.x) * to.sums * to.padded;
-    const float share = 1.0f / (float)a.width;
+    const float share = (float)a.share;
     for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
         const RowAt<T> row(a, blockIdx.y, t);
         Unit post{}, pre{};
@@ -287,19 +314,22 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
     }
 }
 
-// Column sums: 64 columns for a workgroup, a quarter of the partial sums for each of its waves.
-template <typename T> __global__ void __launch_bounds__(THREADS) join_sums_kernel(NormArgs a, Partials from)
+// Column sums: 64 columns for a workgroup, whose waves take turns at the partial sums.
+constexpr int JOIN_WAVES = 16;
+template <typename T> __global__ void __launch_bounds__(JOIN_WAVES * 64) join_sums_kernel(NormArgs a, Partials from)
 {
-    __shared__ double part[THREADS / 64][64];
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    __shared__ double part[JOIN_WAVES][64];
+    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), row = from.sums * from.padded;
+    const float *p = from.p + (blockIdx.z * from.workgroups * from.sums + blockIdx.y) * from.padded + col;
     double sum = 0.0;
     if (col < a.width)
-        for (int64_t w = threadIdx.x >> 6; w < from.workgroups; w += THREADS / 64)
-            sum += from.p[((blockIdx.z * from.workgroups + w) * from.sums + blockIdx.y) * from.padded + col];
+#pragma unroll 8
+        for (int64_t w = threadIdx.x >> 6; w < from.workgroups; w += JOIN_WAVES) sum += p[w * row];
     part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
     __syncthreads();
     if (threadIdx.x >= 64 || col >= a.width) return;
-    for (int w = 1; w < THREADS / 64; ++w) sum += part[w][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < JOIN_WAVES; ++w) sum += part[w][threadIdx.x];
     store_value(RowAt<T>::at(from.out[blockIdx.y], blockIdx.z, 0) + col, (float)sum);
 }
 
@@ -307,28 +337,59 @@ template <typename T> __global__ void __launch_bounds__(THREADS) join_sums_kerne
 //
 // LANES lanes hold a row's operands, PIECES pieces each, between its sums: everything is read once.  Narrow rows share a workgroup.
 
-constexpr int threads_of(int lanes) { return lanes < THREADS ? THREADS : lanes; }
+constexpr int threads_of(int lanes) { return lanes <= 64 ? THREADS : lanes; }
 
-// What of a row the lane's piece k holds: `left` values from its column on, none if that is not positive.
+// What of a row the lane's piece k holds: `left` values from its column on, none if that is not positive.  Rows are short here: 32 bits count their bytes.
+//
+// Rows are fetched without a branch around any load, whose result would have to be waited for where the branches meet: a lane whose piece ends behind the row reads the row's last full piece, and
+// moves its values once they have come (settle); what is not there is fetched from another operand's row and cleared.
 template <typename T, int LANES> struct Lane {
     static constexpr int VALUES = Piece<T>::VALUES;
-    int64_t width, first;
-    __device__ __forceinline__ Lane(int64_t width_) : width(width_), first((int64_t)(threadIdx.x % LANES) * VALUES) { }
-    __device__ __forceinline__ int64_t col(int k) const { return first + (int64_t)k * LANES * VALUES; }
-    __device__ __forceinline__ int64_t left(int k) const { return width - col(k); }
-    template <int PIECES> __device__ __forceinline__ void load(const T *row, Piece<T> (&to)[PIECES], bool there = true) const
+    int32_t width; uint32_t first;
+    __device__ __forceinline__ Lane(int64_t width_) : width((int32_t)width_), first(threadIdx.x % LANES * VALUES) { }
+    __device__ __forceinline__ uint32_t col(int k) const { return first + k * LANES * VALUES; }
+    __device__ __forceinline__ int32_t left(int k) const { return width - (int32_t)col(k); }
+    __device__ __forceinline__ T *at(const T *row, uint32_t column) const { return (T *)((char *)row + (uint32_t)(column * sizeof(T))); }
+    template <int PIECES> __device__ __forceinline__ void fetch(const T *row, Piece<T> (&to)[PIECES]) const
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) to[k].v = *reinterpret_cast<const typename Piece<T>::Memory *>(at(row, left(k) >= VALUES ? col(k) : (uint32_t)(width - VALUES)));
+    }
+    template <int PIECES> __device__ __forceinline__ void settle(Piece<T> (&v)[PIECES], bool there = true) const
     {
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            if (row && there && left(k) > 0) to[k] = load_piece(row + col(k), left(k));
-            else to[k].v = decltype(to[k].v){};
+            if (left(k) >= VALUES && there) continue;
+            if (left(k) <= 0 || !there) v[k].v = decltype(v[k].v){};
+            else shift_down(v[k], VALUES - left(k));
         }
     }
-    template <int PIECES> __device__ __forceinline__ void store(T *row, int k, const float (&v)[PIECES][VALUES]) const
+    template <int PIECES> __device__ __forceinline__ void load(const T *row, Piece<T> (&to)[PIECES]) const
+    {
+        fetch(row, to);
+        settle(to);
+    }
+    // values that are not there are `other`; behind the row 0
+    template <int PIECES> __device__ __forceinline__ void load_or(const T *row, Piece<T> (&to)[PIECES], float other) const
+    {
+        if (row) { load(row, to); return; }
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            float v[VALUES];
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = e < left(k) ? other : 0.0f;
+            to[k].set(v);
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int k, const Piece<T> &v) const
+    {
+        if (row && left(k) > 0) store_piece(at(row, col(k)), left(k), v);
+    }
+    __device__ __forceinline__ void store(T *row, int k, const float (&v)[VALUES]) const
     {
         Piece<T> out;
-        out.set(v[k]);
-        if (left(k) > 0) store_piece(row + col(k), left(k), out);
+        out.set(v);
+        store(row, k, out);
     }
     // values behind the row become 0
     __device__ __forceinline__ void clear(int k, float (&v)[VALUES]) const
@@ -339,12 +400,20 @@ template <typename T, int LANES> struct Lane {
     }
 };
 
+// 1 / sqrt(v), v > 0: the hardware's in float on a mantissa, one step of Newton's iteration, to 1.5 units in the last place.
+__device__ __forceinline__ float inverse_root(double v)
+{
+    const int twice = __builtin_amdgcn_frexp_exp(v) & ~1;
+    const float m = (float)__builtin_amdgcn_ldexp(v, -twice), r = __builtin_amdgcn_rsqf(m);
+    return __builtin_amdgcn_ldexpf(fmaf(r * 0.5f, fmaf(-m * r, r, 1.0f), r), -twice / 2);
+}
+
 // get(k, v): the values of the lane's piece k, 0 behind the row.
 template <typename T, int LANES, int PIECES, bool LAYER, class Get>
 __device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get &get, double share, double eps, double (*room)[1], double (*second)[1])
 {
     constexpr int VALUES = Piece<T>::VALUES;
-    double mean = 0.0;
+    Unit n{};
     if constexpr (LAYER) {
         double sum[1] = {0.0};
 #pragma unroll
@@ -355,24 +424,40 @@ __device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get 
             for (int e = 0; e < VALUES; ++e) sum[0] += v[e];
         }
         row_sum<LANES>(sum, room);
-        mean = sum[0] * share;
+        const double mean = sum[0] * share;
+        n.mean = (float)mean;
+        n.rest = (float)(mean - (double)n.mean);
     }
-    double sum[1] = {0.0};
+    const auto centred = [&](int k, float (&v)[VALUES]) {
+        get(k, v);
+        if constexpr (LAYER) {
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = (v[e] - n.mean) - n.rest;
+            lane.clear(k, v);
+        }
+    };
+    float square[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < PIECES; ++k) {
         float v[VALUES];
-        get(k, v);
+        centred(k, v);
 #pragma unroll
-        for (int e = 0; e < VALUES; ++e) {
-            const double d = LAYER && e >= lane.left(k) ? 0.0 : (double)v[e] - mean;
-            sum[0] = fma(d, d, sum[0]);
+        for (int e = 0; e < VALUES; ++e) square[e & 3] = fmaf(v[e], v[e], square[e & 3]);
+    }
+    const float all = (square[0] + square[1]) + (square[2] + square[3]);
+    double sum[1] = {(double)all};
+    if (!(all > 0x1p-90f && all < 0x1p120f)) {     // squares that left float's range, or may have
+        sum[0] = 0.0;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            float v[VALUES];
+            centred(k, v);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) sum[0] = fma((double)v[e], (double)v[e], sum[0]);
         }
     }
     row_sum<LANES>(sum, second);
-    Unit n;
-    n.mean = (float)mean;
-    n.rest = (float)(mean - (double)n.mean);
-    n.r = (float)rsqrt(sum[0] * share + eps);
+    n.r = inverse_root(sum[0] * share + eps);
     return n;
 }
 template <bool LAYER> __device__ __forceinline__ float unit_held_of(const Unit &n, float v) { return LAYER ? unit_of(n, v) : v * n.r; }
@@ -386,15 +471,17 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
     if (GROUPS > 1 && t >= a.rows) return;                          // whole groups, and no barriers
     const RowAt<T> row(a, blockIdx.y, t);
     const Lane<T, LANES> lane(a.width);
-    const double share = 1.0 / (double)a.width;
+    const double share = a.share;
     Piece<T> x[PIECES], f[PIECES], q[PIECES], g1[PIECES], b1[PIECES], g2[PIECES], b2[PIECES];
-    lane.load(row.x, x);
-    lane.load(row.f, f);
-    lane.load(row.q, q);
-    lane.load(row.g1, g1);
-    lane.load(row.b1, b1);
-    lane.load(row.g2, g2);
-    lane.load(row.b2, b2);
+    lane.fetch(row.x, x);
+    if (row.f) lane.fetch(row.f, f);
+    if (row.q) lane.fetch(row.q, q);
+    if (row.g1) lane.fetch(row.g1, g1);
+    if (row.b1) lane.fetch(row.b1, b1);
+    if (row.g2) lane.fetch(row.g2, g2);
+    if (row.b2) lane.fetch(row.b2, b2);
+    lane.settle(x);
+    lane.settle(f);
     float h[PIECES][VALUES];
 #pragma unroll
     for (int k = 0; k < PIECES; ++k)
@@ -406,9 +493,12 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) v[e] = f[k].get(e);
         }, share, a.eps, room[0], room[1]);
+        lane.settle(q);
+        lane.settle(g1);
+        lane.settle(b1);
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            float u[VALUES];
+            float u[VALUES], gate[VALUES];
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) u[e] = unit_held_of<LAYER>(post, f[k].get(e));
             if (row.g1)
@@ -417,29 +507,26 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
             if (row.b1)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) u[e] += b1[k].get(e);
-            if (row.q) {
+            if (row.q) gates_of<T>(a.act, a.f_scale, q[k], gate);
+            else
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) {
-                    float value, slope;
-                    gate_of(a.act, q[k].get(e), value, slope);
-                    h[k][e] = fmaf(a.f_scale * value, u[e], h[k][e]);
-                }
-            } else {
+                for (int e = 0; e < VALUES; ++e) gate[e] = a.f_scale;
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) h[k][e] = fmaf(a.f_scale, u[e], h[k][e]);
-            }
-            lane.clear(k, h[k]);
+            for (int e = 0; e < VALUES; ++e) h[k][e] = fmaf(gate[e], u[e], h[k][e]);
+            if (LAYER) lane.clear(k, h[k]);
         }
     }
     T *to_h = RowAt<T>::at(a.h, blockIdx.y, t), *to_y = RowAt<T>::at(a.y, blockIdx.y, t);
     if (to_h)
 #pragma unroll
-        for (int k = 0; k < PIECES; ++k) lane.store(to_h, k, h);
+        for (int k = 0; k < PIECES; ++k) lane.store(to_h, k, h[k]);
     if (!to_y) return;
     const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
 #pragma unroll
         for (int e = 0; e < VALUES; ++e) v[e] = h[k][e];
     }, share, a.eps, room[2], room[3]);
+    lane.settle(g2);
+    lane.settle(b2);
 #pragma unroll
     for (int k = 0; k < PIECES; ++k) {
 #pragma unroll
@@ -450,156 +537,219 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
         if (row.b2)
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) h[k][e] += b2[k].get(e);
-        lane.store(to_y, k, h);
+        lane.store(to_y, k, h[k]);
     }
 }
 
-// Which sums over the rows a kernel holds in registers: those of a norm alone, those of a block's gains and gate, or all.
-enum Form : int { NORM_ALONE = 0, BLOCK_GAINS = 1, BLOCK_ALL = 2 };
+// The compiler does not know any more what these hold: they have come by now, and what was unpacked from them is not kept, but unpacked anew.
+template <typename T, int PIECES> __device__ __forceinline__ void let_go(Piece<T> (&p)[PIECES])
+{
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) asm volatile("" : "+v"(p[k].v));
+}
+
+// What a kernel holds in registers: operands and sums over the rows of a norm alone, of a block without biases, or of any block; of a block whose gate has rows of its own, or of others.
+enum Form : int { NORM_ALONE = 0, BLOCK_GAINS = 1, BLOCK_ALL = 2, GATED_GAINS = 3, GATED_ALL = 4 };
 
 template <typename T, int LANES, int PIECES, bool LAYER, int FORM>
 __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a, Partials to)
 {
-    constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES;
-    constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS;
+    constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES, MEANS = LAYER ? 2 : 1;
+    constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS && FORM != GATED_GAINS, GATED = FORM == GATED_GAINS || FORM == GATED_ALL;
+    constexpr bool AHEAD = LANES < 1024 || !BLOCK || FORM == BLOCK_GAINS;                     // as far as registers go
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
-    __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][2];
+    __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][MEANS];
     __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
     const Lane<T, LANES> lane(a.width);
-    const double share = 1.0 / (double)a.width;
-    const float share_f = (float)share;
-    Piece<T> g1[PIECES], b1[PIECES], g2[PIECES], q[PIECES];
+    const double share = a.share;
+    const float share_f = (float)a.share;
     const RowAt<T> vectors(a, blockIdx.y, 0);
-    if constexpr (BLOCK) { lane.load(vectors.g1, g1); lane.load(vectors.b1, b1); lane.load(vectors.q, q, !a.gate_rows); }
-    lane.load(vectors.g2, g2);
-    float sums[SUMS][PIECES][VALUES] = {};
-    for (int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES; t < a.rows; t += (int64_t)gridDim.x * GROUPS) {
-        const RowAt<T> row(a, blockIdx.y, t);
-        Piece<T> x[PIECES], f[PIECES], dy[PIECES], dh[PIECES];
-        lane.load(row.x, x);
-        if constexpr (BLOCK) {
-            lane.load(row.f, f);
-            if (a.gate_rows) lane.load(row.q, q);
-        }
-        lane.load(RowAt<T>::at(a.dy, blockIdx.y, t), dy);
-        lane.load(RowAt<T>::at(a.dh, blockIdx.y, t), dh);
-        Unit post{0.0f, 0.0f, 1.0f};
-        if (BLOCK && a.post) post = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+    Piece<T> g1[PIECES], b1[PIECES], g2[PIECES];
+    float gate[BLOCK ? PIECES : 1][VALUES];        // b act(q)
+    lane.load_or(vectors.g2, g2, 1.0f);
+    if constexpr (BLOCK) {
+        Piece<T> q[PIECES];
+        lane.load_or(vectors.g1, g1, 1.0f);
+        if constexpr (BIASES) lane.load_or(vectors.b1, b1, 0.0f);
+        lane.load_or(GATED ? nullptr : vectors.q, q, 1.0f);
 #pragma unroll
-            for (int e = 0; e < VALUES; ++e) v[e] = f[k].get(e);
-        }, share, a.eps, room[0], room[1]);
-        // u of a piece
+        for (int k = 0; k < PIECES; ++k) gates_of<T>(GATED || !vectors.q ? GATE_NONE : a.act, a.f_scale, q[k], gate[k]);
+    }
+    float sums[SUMS][PIECES][VALUES] = {};
+    // the next row is under way while one is worked on
+    struct Operands { Piece<T> x[PIECES], f[PIECES], q[PIECES], dy[PIECES], dh[PIECES]; };
+    const auto fetch = [&](int64_t t, Operands &o) {
+        const RowAt<T> row(a, blockIdx.y, t);
+        const T *dy = RowAt<T>::at(a.dy, blockIdx.y, t), *dh = RowAt<T>::at(a.dh, blockIdx.y, t);
+        lane.fetch(row.x, o.x);
+        if constexpr (BLOCK) lane.fetch(row.f, o.f);
+        if constexpr (GATED) lane.fetch(row.q, o.q);
+        lane.fetch(a.dy.p ? dy : row.x, o.dy);
+        lane.fetch(a.dh.p ? dh : row.x, o.dh);
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    Operands next;
+    if (AHEAD) fetch(t < a.rows ? t : a.rows - 1, next);
+    for (; t < a.rows; t += step) {
+        Operands row = next;
+        if (AHEAD) fetch(t + step < a.rows ? t + step : t, next);
+        else fetch(t, row);
+        lane.settle(row.x);
+        lane.settle(row.dy, a.dy.p);
+        lane.settle(row.dh, a.dh.p);
+        if constexpr (BLOCK) {
+            lane.settle(row.f);
+            if constexpr (GATED) lane.settle(row.q);
+            let_go(g1);
+            if constexpr (BIASES) let_go(b1);
+        }
+        let_go(g2);
+        Unit post{0.0f, 0.0f, 1.0f};
+        if constexpr (BLOCK) {
+            if (a.post) post = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) v[e] = row.f[k].get(e);
+            }, share, a.eps, room[0], room[1]);
+            if constexpr (GATED)
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) gates_of<T>(a.act, a.f_scale, row.q[k], gate[k]);
+        }
+        // fn and u
         const auto branch = [&](int k, float (&fn)[VALUES], float (&u)[VALUES]) {
 #pragma unroll
-            for (int e = 0; e < VALUES; ++e) fn[e] = u[e] = unit_held_of<LAYER>(post, f[k].get(e));
-            if (row.g1)
-#pragma unroll
-                for (int e = 0; e < VALUES; ++e) u[e] *= g1[k].get(e);
-            if (row.b1)
-#pragma unroll
-                for (int e = 0; e < VALUES; ++e) u[e] += b1[k].get(e);
+            for (int e = 0; e < VALUES; ++e) {
+                fn[e] = unit_held_of<LAYER>(post, row.f[k].get(e));
+                u[e] = BIASES ? fmaf(fn[e], g1[k].get(e), b1[k].get(e)) : fn[e] * g1[k].get(e);
+            }
         };
-        float d[PIECES][VALUES];                   // D
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k)
-#pragma unroll
-            for (int e = 0; e < VALUES; ++e) d[k][e] = dh[k].get(e);
+        float d[PIECES][VALUES];                   // h, hn, then D
         if (a.pre) {
-            float h[PIECES][VALUES];
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) h[k][e] = a.x_scale * x[k].get(e);
+                for (int e = 0; e < VALUES; ++e) d[k][e] = a.x_scale * row.x[k].get(e);
                 if constexpr (BLOCK) {
                     float fn[VALUES], u[VALUES];
                     branch(k, fn, u);
 #pragma unroll
-                    for (int e = 0; e < VALUES; ++e) {
-                        float value = 1.0f, slope;
-                        if (row.q) gate_of(a.act, q[k].get(e), value, slope);
-                        h[k][e] = fmaf(a.f_scale * value, u[e], h[k][e]);
-                    }
-                    lane.clear(k, h[k]);
+                    for (int e = 0; e < VALUES; ++e) d[k][e] = fmaf(gate[k][e], u[e], d[k][e]);
+                    if (LAYER) lane.clear(k, d[k]);
                 }
             }
             const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) v[e] = h[k][e];
+                for (int e = 0; e < VALUES; ++e) v[e] = d[k][e];
             }, share, a.eps, room[2], room[3]);
-            float along[2] = {0.0f, 0.0f};
+            float along[MEANS] = {};
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    const float v = dy[k].get(e), w = row.g2 ? v * g2[k].get(e) : v;
-                    h[k][e] = unit_held_of<LAYER>(pre, h[k][e]);
-                    along[0] += w;
-                    along[1] = fmaf(w, h[k][e], along[1]);
-                    sums[2][k][e] = fmaf(v, h[k][e], sums[2][k][e]);
+                    const float v = row.dy[k].get(e), w = v * g2[k].get(e);
+                    d[k][e] = unit_held_of<LAYER>(pre, d[k][e]);
+                    along[0] = fmaf(w, d[k][e], along[0]);
+                    if (LAYER) along[MEANS - 1] += w;
+                    sums[2][k][e] = fmaf(v, d[k][e], sums[2][k][e]);
                     if (BIASES) sums[3][k][e] += v;
                 }
             row_sum<LANES>(along, pairs[0]);
-            const float mean_e = LAYER ? along[0] * share_f : 0.0f, mean_eh = along[1] * share_f;
+            let_go(row.dy);
+            let_go(g2);
+            const float mean_eh = along[0] * share_f, mean_e = LAYER ? along[MEANS - 1] * share_f : 0.0f;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    const float v = dy[k].get(e), w = row.g2 ? v * g2[k].get(e) : v;
-                    d[k][e] = fmaf(pre.r, (w - mean_e) - h[k][e] * mean_eh, d[k][e]);
+                    const float w = row.dy[k].get(e) * g2[k].get(e);
+                    d[k][e] = fmaf(pre.r, fmaf(-d[k][e], mean_eh, LAYER ? w - mean_e : w), row.dh[k].get(e));
                 }
+        } else {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) d[k][e] = row.dh[k].get(e);
         }
-        T *dx = RowAt<T>::at(a.dx, blockIdx.y, t);
-        float out[PIECES][VALUES];
+        Piece<T> dx[PIECES], df[PIECES], dq[PIECES];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            lane.clear(k, d[k]);
+            if (LAYER) lane.clear(k, d[k]);
+            float out[VALUES];
 #pragma unroll
-            for (int e = 0; e < VALUES; ++e) out[k][e] = a.x_scale * d[k][e];
-            if (dx) lane.store(dx, k, out);
+            for (int e = 0; e < VALUES; ++e) out[e] = a.x_scale * d[k][e];
+            dx[k].set(out);
         }
         if constexpr (BLOCK) {
-            T *df = RowAt<T>::at(a.df, blockIdx.y, t), *dq = a.gate_rows ? RowAt<T>::at(a.dgate, blockIdx.y, t) : nullptr;
-            float back[2] = {0.0f, 0.0f};
+            float back[MEANS] = {};
+            let_go(row.f);
+            let_go(g1);
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
-                float fn[VALUES], u[VALUES], gate[VALUES];
+                float fn[VALUES], u[VALUES];
                 branch(k, fn, u);
+                if constexpr (GATED) {
+                    float out[VALUES];
+                    slopes_of<T>(a.act, a.f_scale, row.q[k], out);
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) out[e] *= u[e] * d[k][e];
+                    dq[k].set(out);
+                }
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    float value = 1.0f, slope = 0.0f;
-                    if (row.q) gate_of(a.act, q[k].get(e), value, slope);
-                    gate[e] = a.f_scale * slope * u[e] * d[k][e];
-                    if (!a.gate_rows) sums[4][k][e] += gate[e];
-                    d[k][e] *= a.f_scale * value;                   // b act(q) D
-                    if (BIASES) sums[1][k][e] += d[k][e];
-                    sums[0][k][e] = fmaf(d[k][e], fn[e], sums[0][k][e]);
-                    if (row.g1) d[k][e] *= g1[k].get(e);            // c
-                    back[0] += d[k][e];
-                    back[1] = fmaf(d[k][e], fn[e], back[1]);
-                }
-                if (dq) {
-#pragma unroll
-                    for (int e = 0; e < VALUES; ++e) out[k][e] = gate[e];
-                    lane.store(dq, k, out);
+                    if (!GATED) sums[4][k][e] = fmaf(u[e], d[k][e], sums[4][k][e]);
+                    const float du = gate[k][e] * d[k][e];
+                    if (BIASES) sums[1][k][e] += du;
+                    sums[0][k][e] = fmaf(du, fn[e], sums[0][k][e]);
+                    d[k][e] = du * g1[k].get(e);                    // c
+                    back[0] = fmaf(d[k][e], fn[e], back[0]);
+                    if (LAYER) back[MEANS - 1] += d[k][e];
                 }
             }
             if (a.post) row_sum<LANES>(back, pairs[1]);
-            const float mean_c = LAYER && a.post ? back[0] * share_f : 0.0f, mean_cf = a.post ? back[1] * share_f : 0.0f;
+            const float mean_cf = a.post ? back[0] * share_f : 0.0f, mean_c = LAYER && a.post ? back[MEANS - 1] * share_f : 0.0f;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
+                float out[VALUES];
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    const float fn = unit_held_of<LAYER>(post, f[k].get(e));
-                    out[k][e] = a.post ? post.r * ((d[k][e] - mean_c) - fn * mean_cf) : d[k][e];
+                    const float fn = unit_held_of<LAYER>(post, row.f[k].get(e));
+                    out[e] = post.r * fmaf(-fn, mean_cf, LAYER ? d[k][e] - mean_c : d[k][e]);
                 }
-                if (df) lane.store(df, k, out);
+                df[k].set(out);
+            }
+        }
+        // the next row has come by now: waited for behind the writes, it would be waited for with them
+        if constexpr (AHEAD) { let_go(next.x); let_go(next.dy); let_go(next.dh); }
+        if constexpr (AHEAD && BLOCK) let_go(next.f);
+        if constexpr (AHEAD && GATED) let_go(next.q);
+        T *to_x = RowAt<T>::at(a.dx, blockIdx.y, t);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) lane.store(to_x, k, dx[k]);
+        if constexpr (BLOCK) {
+            T *to_f = RowAt<T>::at(a.df, blockIdx.y, t), *to_q = RowAt<T>::at(a.dgate, blockIdx.y, t);
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                lane.store(to_f, k, df[k]);
+                if constexpr (GATED) lane.store(to_q, k, dq[k]);
             }
         }
     }
+    if constexpr (BLOCK && !GATED)                 // a gate that is the same for all rows has one slope, too
+        if (to.place[4] >= 0) {
+            Piece<T> q[PIECES];
+            lane.load_or(vectors.q, q, 1.0f);
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                float slope[VALUES];
+                slopes_of<T>(a.act, a.f_scale, q[k], slope);
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) sums[4][k][e] *= slope[e];
+            }
+        }
     float *mine = to.p + (blockIdx.y * to.workgroups + blockIdx.x) * to.sums * to.padded;
 #pragma unroll
     for (int s = 0; s < SUMS; ++s) {
-        if ((!BLOCK && s != 2 && s != 3) || (!BIASES && (s == 1 || s == 3))) continue;
+        if ((!BLOCK && s != 2 && s != 3) || (!BIASES && (s == 1 || s == 3)) || (GATED && s == 4)) continue;
         if (to.place[s] < 0) continue;
         if constexpr (GROUPS > 1) {                // rows of the same workgroup, in order
             __syncthreads();
@@ -632,7 +782,8 @@ template <typename T> static int64_t pieces_of(int64_t width) { return (width + 
 template <int LANES_, int PIECES_> struct Held { static constexpr int LANES = LANES_, PIECES = PIECES_; };
 template <class Go, class Long> static void with_row(int64_t n, const Go &go, const Long &stream)
 {
-    if (n <= 8) go(Held<8, 1>());
+    if (n <= 1) stream();                          // rows of no more than a piece
+    else if (n <= 8) go(Held<8, 1>());
     else if (n <= 16) go(Held<16, 1>());
     else if (n <= 32) go(Held<32, 1>());
     else if (n <= 64) go(Held<64, 1>());
@@ -640,6 +791,22 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
     else if (n <= 256) go(Held<256, 1>());
     else if (n <= 512) go(Held<256, 2>());
     else if (n <= 1024) go(Held<512, 2>());
+    else if (n <= 2048) go(Held<1024, 2>());
+    else stream();
+}
+
+// Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes.
+template <class Go, class Long> static void with_row_grad(int64_t n, const Go &go, const Long &stream)
+{
+    if (n <= 1) stream();                          // rows of no more than a piece
+    else if (n <= 8) go(Held<8, 1>());
+    else if (n <= 16) go(Held<16, 1>());
+    else if (n <= 32) go(Held<32, 1>());
+    else if (n <= 64) go(Held<64, 1>());
+    else if (n <= 128) go(Held<128, 1>());
+    else if (n <= 256) go(Held<256, 1>());
+    else if (n <= 512) go(Held<512, 1>());
+    else if (n <= 1024) go(Held<1024, 1>());
     else if (n <= 2048) go(Held<1024, 2>());
     else stream();
 }
@@ -674,9 +841,13 @@ static Partials partials_of(const NormArgs &a, void *work)
     }
     to.p = (float *)work;
     to.padded = up_to(a.width, 8);
-    int64_t rows = 1;                              // of a workgroup at once
-    with_row(a.bf16 ? pieces_of<uint16_t>(a.width) : pieces_of<float>(a.width), [&](auto held) { rows = threads_of(decltype(held)::LANES) / decltype(held)::LANES; }, []() { });
-    const int64_t most = a.batch * 8 < 512 ? 512 / a.batch : 8, all = (a.rows + rows - 1) / rows;
+    int64_t rows = 1, threads = THREADS;           // rows of a workgroup at once
+    with_row_grad(a.bf16 ? pieces_of<uint16_t>(a.width) : pieces_of<float>(a.width), [&](auto held) {
+        threads = threads_of(decltype(held)::LANES);
+        rows = threads / decltype(held)::LANES;
+    }, []() { });
+    // as many as the card holds at once, if each has two turns
+    const int64_t places = 256 * (1024 / threads), most = a.batch * 8 < places ? places / a.batch : 8, turns = (a.rows + rows - 1) / rows, all = (turns + 1) / 2;
     to.workgroups = all < most ? all : most;
     return to;
 }
@@ -688,25 +859,28 @@ int64_t block_norm_grad_workspace(const NormArgs &a)
     return 4 * a.batch * to.workgroups * to.sums * to.padded;
 }
 
-template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to, int64_t rows_there)
+template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
 {
     const dim3 grid((uint32_t)to.workgroups, (uint32_t)a.batch);
-    const bool block = rows_there, biases = to.place[1] >= 0 || to.place[3] >= 0;
-    if (!block) norm_grad_kernel<T, LANES, PIECES, LAYER, NORM_ALONE><<<grid, threads_of(LANES), 0, s>>>(a, to);
-    else if (!biases) norm_grad_kernel<T, LANES, PIECES, LAYER, BLOCK_GAINS><<<grid, threads_of(LANES), 0, s>>>(a, to);
-    else norm_grad_kernel<T, LANES, PIECES, LAYER, BLOCK_ALL><<<grid, threads_of(LANES), 0, s>>>(a, to);
+    const bool gated = a.gate_rows && a.gate.p, biases = a.post_bias.p || to.place[1] >= 0 || to.place[3] >= 0;
+    const auto go = [&](auto form) { norm_grad_kernel<T, LANES, PIECES, LAYER, form()><<<grid, threads_of(LANES), 0, s>>>(a, to); };
+    if (!a.f.p) go(std::integral_constant<int, NORM_ALONE>());
+    else if (gated && biases) go(std::integral_constant<int, GATED_ALL>());
+    else if (gated) go(std::integral_constant<int, GATED_GAINS>());
+    else if (biases) go(std::integral_constant<int, BLOCK_ALL>());
+    else go(std::integral_constant<int, BLOCK_GAINS>());
 }
 
 template <typename T> static void block_norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
 {
-    if (to.workgroups > 0) with_row(pieces_of<T>(a.width), [&](auto held) {
+    if (to.workgroups > 0) with_row_grad(pieces_of<T>(a.width), [&](auto held) {
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
-        if (a.layer) norm_grad_of<T, LANES, PIECES, true>(s, a, to, a.f.p != nullptr);
-        else norm_grad_of<T, LANES, PIECES, false>(s, a, to, a.f.p != nullptr);
+        if (a.layer) norm_grad_of<T, LANES, PIECES, true>(s, a, to);
+        else norm_grad_of<T, LANES, PIECES, false>(s, a, to);
     }, [&]() {
         long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
     });
-    if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + 63) / 64), to.sums, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+    if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + 63) / 64), to.sums, (uint32_t)a.batch), JOIN_WAVES * 64, 0, s>>>(a, to);
 }
 
 void launch_block_norm_grad(hipStream_t s, const NormArgs &a, void *work)

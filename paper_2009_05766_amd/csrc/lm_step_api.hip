@@ -95,6 +95,7 @@ static NormArgs norm_args(const netmax_block_norm_shape *s, const netmax_block_n
     NormArgs a{};
     a.batch = s->batch; a.rows = s->rows; a.width = s->width; a.bf16 = s->dtype == NETMAX_BF16; a.layer = s->norm == NETMAX_NORM_LAYER; a.act = s->gate_act;
     a.gate_rows = s->gate_rows != 0; a.post = s->post != 0; a.pre = s->pre != 0; a.x_scale = s->x_scale; a.f_scale = s->f_scale; a.eps = s->eps;
+    a.share = 1.0 / (double)s->width;
     if (d) {
         a.x = span(d->x); a.f = span(d->f); a.gate = span(d->gate); a.post_gain = span(d->post_gain); a.post_bias = span(d->post_bias); a.pre_gain = span(d->pre_gain);
         a.pre_bias = span(d->pre_bias); a.h = span(d->h); a.y = span(d->y);

@@ -24,6 +24,23 @@ template <> struct Piece<uint16_t> {
     }
 };
 
+// Moves values of a piece down by `by` places (1 .. VALUES - 1); zeros come in at the end.
+__device__ __forceinline__ void shift_down(Piece<float> &x, int by)
+{
+    f32x4 v = x.v;
+    if (by & 1) v = f32x4{v[1], v[2], v[3], 0.0f};
+    if (by & 2) v = f32x4{v[2], v[3], 0.0f, 0.0f};
+    x.v = v;
+}
+__device__ __forceinline__ void shift_down(Piece<uint16_t> &x, int by)
+{
+    u32x4 v = x.v;
+    if (by & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    if (by & 2) v = u32x4{v[1], v[2], v[3], 0u};
+    if (by & 4) v = u32x4{v[2], v[3], 0u, 0u};
+    x.v = v;
+}
+
 // A piece of a row from p on, where `left` values of the row lie (1 or more); those behind the row are 0.
 template <typename T> __device__ __forceinline__ Piece<T> load_piece(const T *p, int64_t left)
 {
@@ -94,11 +111,7 @@ template <int LANES, int N, typename S> __device__ __forceinline__ void row_sum(
             for (int k = 0; k < N; ++k) room[threadIdx.x >> 6][k] = v[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = 0;
-#pragma unroll
-        for (int w = 0; w < LANES / 64; ++w)
-#pragma unroll
-            for (int k = 0; k < N; ++k) v[k] += room[w][k];
+        for (int k = 0; k < N; ++k) v[k] = lanes_sum<LANES / 64>(room[threadIdx.x & (LANES / 64 - 1)][k]);
     }
 }
 

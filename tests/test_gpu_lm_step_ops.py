@@ -2,8 +2,9 @@
 
 Tolerances, with e = 2^-24, half a unit in the last of a float's bits, and u the same for the type of a result (2^-24 or 2^-8), all relative to the value that is rounded.
 Embedding: scale v is one product, e + u.  Its gradient sums n rows in float: at most n e times the sum of their magnitudes, then scale (e) and u; added to what is there: e of both more.
-Norms: means and mean squares are double, so that 1 / sqrt comes with e; N(v) takes two subtractions and a product, 4 e of itself (and 2^-47 of a layer norm's mean in its unit: a mean in
-two floats).  What lies behind is propagated element by element (`norm_bounds`): products and sums bring e each; a sum over a row of `width` values e times (width / 64 + 24) of its magnitudes (values of a thread, then
+Norms: means are double; squares are summed in float by a lane (chains of at most four and two more additions: 6 e) and in double from there on, those of a layer norm are of values
+that come with 2 e (4 e of their squares), the root halves that, and 1 / sqrt adds 3.5 e: 8.5 e in all.  N(v) takes two subtractions and a product more, 12 e of itself (and 2^-47 of a
+layer norm's mean in its unit: a mean in two floats).  What lies behind is propagated element by element (`norm_bounds`): products and sums bring e each; a sum over a row of `width` values e times (width / 64 + 24) of its magnitudes (values of a thread, then
 a tree); sums over rows e times (rows + 8).  The sigmoid is good to (8 + |q|) 2^-23 of itself, its slope to twice that, tanh to 2^-21, its slope to 2^-18 near 0 and four times (8 + 2 |q|) 2^-23 / 2 far out:
 below all of them is (8 + 2 |q|) 2^-21.
 Clipping: the norm is a sum in double, rounded once; g factor is a product in double, rounded once."""
@@ -187,7 +188,7 @@ def norm_bounds(d, o, want):
         fn, dfn = d["f"], zero
         if o["post"]:
             fn, r1, m = unit(d["f"])
-            dfn = 4 * E * fn.abs() + 2.0 ** -47 * m.abs() * r1
+            dfn = 12 * E * fn.abs() + 2.0 ** -47 * m.abs() * r1
         u = fn * d["g1"] + d["b1"]
         du_ = d["g1"].abs() * dfn + 2 * E * ((fn * d["g1"]).abs() + d["b1"].abs())
         if d["gate"] is not None:
@@ -204,8 +205,8 @@ def norm_bounds(d, o, want):
     rel = zero
     if o["pre"]:
         hn, r2, m = unit(h)
-        rel = r2 * mean(hn.abs() * dh_) + 2 * E                                         # of 1 / sqrt
-        dhn = r2 * dh_ + hn.abs() * rel + (r2 * mean(dh_) if layer else 0) + 4 * E * hn.abs() + 2.0 ** -47 * m.abs() * r2
+        rel = r2 * mean(hn.abs() * dh_) + 9 * E                                         # of 1 / sqrt
+        dhn = r2 * dh_ + hn.abs() * rel + (r2 * mean(dh_) if layer else 0) + 12 * E * hn.abs() + 2.0 ** -47 * m.abs() * r2
         tol["y"] = d["g2"].abs() * dhn + 2 * E * ((hn * d["g2"]).abs() + d["b2"].abs())
     if "dx" in want:
         K = W / 64 + 24
@@ -228,7 +229,7 @@ def norm_bounds(d, o, want):
             if o["post"]:
                 c, dc = du * d["g1"], d["g1"].abs() * ddu + E * (du * d["g1"]).abs()
                 size = c.abs() + (mean(c.abs()) if layer else 0) + fn.abs() * mean((c * fn).abs())
-                tol["df"] = r1 * (dc + (mean(dc) if layer else 0) + fn.abs() * mean(fn.abs() * dc) + dfn * mean((c * fn).abs()) + fn.abs() * mean(c.abs() * dfn) + (K + 10) * E * size)
+                tol["df"] = r1 * (dc + (mean(dc) if layer else 0) + fn.abs() * mean(fn.abs() * dc) + dfn * mean((c * fn).abs()) + fn.abs() * mean(c.abs() * dfn) + (K + 20) * E * size)
                 tol["dpost_gain"] = (fn.abs() * ddu + du.abs() * dfn).sum(-2) + (N + 8) * E * (du * fn).abs().sum(-2)
                 tol["dpost_bias"] = ddu.sum(-2) + (N + 8) * E * du.abs().sum(-2)
             else:
