@@ -412,8 +412,9 @@ int netmax_block_norm(const netmax_block_norm_shape *shape, const netmax_block_n
 
 /* Its gradients from dy and dh, what reaches y and, beside y, h (dh may be NULL with `pre`; dy is NULL without): dx, df and dgate of what it was given, and those of gains and biases (of a
  * gate that is the same for all rows, too) summed over the rows, in float, their partial sums in double and in a fixed order.  Every one may be NULL; data's h and y are not looked at: h is computed anew from x
- * and f.  dx, df and a dgate of rows may each lie in the place of dy, dh, x, f or a gate of rows, with its strides.  rows = 0 gives sums of 0.  Results are the same bits every time. */
-int64_t netmax_block_norm_grad_workspace(const netmax_block_norm_shape *shape, const netmax_block_norm_grads *grads);
+ * and f.  dx, df and a dgate of rows may each lie in the place of dy, dh, x, f or a gate of rows, with its strides.  rows = 0 gives sums of 0.  Results are the same bits every time.  The workspace depends on
+ * what is there: pass the pointers of the call. */
+int64_t netmax_block_norm_grad_workspace(const netmax_block_norm_shape *shape, const netmax_block_norm_data *data, const netmax_block_norm_grads *grads);
 int netmax_block_norm_grad(const netmax_block_norm_shape *shape, const netmax_block_norm_data *data, const netmax_block_norm_grads *grads, void *work, int64_t work_bytes, void *stream);
 
 typedef struct {

@@ -148,7 +148,7 @@ def load():
         "netmax_embed_grad_workspace": (i64, [C.POINTER(netmax_embed_shape)]),
         "netmax_embed_grad": (C.c_int, [C.POINTER(netmax_embed_shape)] + [vp] * 4 + [i64, vp]),
         "netmax_block_norm": (C.c_int, [C.POINTER(netmax_block_norm_shape), vp, vp]),
-        "netmax_block_norm_grad_workspace": (i64, [C.POINTER(netmax_block_norm_shape), vp]),
+        "netmax_block_norm_grad_workspace": (i64, [C.POINTER(netmax_block_norm_shape), vp, vp]),
         "netmax_block_norm_grad": (C.c_int, [C.POINTER(netmax_block_norm_shape)] + [vp] * 3 + [i64, vp]),
         "netmax_grad_norm_workspace": (i64, [i64, i64, vp]),
         "netmax_grad_norm": (C.c_int, [i64, i64] + [vp] * 3 + [i64, vp]),

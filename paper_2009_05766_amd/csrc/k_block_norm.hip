@@ -198,7 +198,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_kerne
 
 // Sums over the rows, in order: dg1, db1, dg2, db2, dq.  A workgroup's rows leave their sums in its own row of partial sums [SUMS][padded].
 constexpr int SUMS = 5;
-struct Partials { float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS]; };  // place: which of the rows that are there, -1: none
+struct Partials { float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS]; void *unwanted; int64_t bytes; };  // place: which of the rows that are there, -1: none
 
 template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_kernel(NormArgs a, Partials to)
 {
@@ -392,7 +392,7 @@ template <typename T, int LANES> struct Lane {
         store(row, k, out);
     }
     // values behind the row become 0
-    __device__ __forceinline__ void clear(int k, float (&v)[VALUES]) const
+    __device__ __forceinline__ void once(int k, float (&v)[VALUES]) const
     {
         if (left(k) < VALUES)
 #pragma unroll
@@ -408,9 +408,9 @@ __device__ __forceinline__ float inverse_root(double v)
     return __builtin_amdgcn_ldexpf(fmaf(r * 0.5f, fmaf(-m * r, r, 1.0f), r), -twice / 2);
 }
 
-// get(k, v): the values of the lane's piece k, 0 behind the row.
-template <typename T, int LANES, int PIECES, bool LAYER, class Get>
-__device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get &get, double share, double eps, double (*room)[1], double (*second)[1])
+// get(k, v): the values of the lane's piece k, of which lane.once() leaves those that count.
+template <typename T, int LANES, int PIECES, bool LAYER, class Columns, class Get>
+__device__ __forceinline__ Unit unit_held(const Columns &lane, const Get &get, double share, double eps, double (*room)[1], double (*second)[1])
 {
     constexpr int VALUES = Piece<T>::VALUES;
     Unit n{};
@@ -420,6 +420,7 @@ __device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get 
         for (int k = 0; k < PIECES; ++k) {
             float v[VALUES];
             get(k, v);
+            lane.once(k, v);
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) sum[0] += v[e];
         }
@@ -433,8 +434,8 @@ __device__ __forceinline__ Unit unit_held(const Lane<T, LANES> &lane, const Get 
         if constexpr (LAYER) {
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) v[e] = (v[e] - n.mean) - n.rest;
-            lane.clear(k, v);
         }
+        lane.once(k, v);
     };
     float square[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -513,7 +514,6 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
                 for (int e = 0; e < VALUES; ++e) gate[e] = a.f_scale;
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) h[k][e] = fmaf(gate[e], u[e], h[k][e]);
-            if (LAYER) lane.clear(k, h[k]);
         }
     }
     T *to_h = RowAt<T>::at(a.h, blockIdx.y, t), *to_y = RowAt<T>::at(a.y, blockIdx.y, t);
@@ -541,6 +541,50 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
     }
 }
 
+// Gradients: workgroups go through the rows, the next of which is under way while one is worked on.  Reads and writes are waited for in their order, and behind a branch the compiler counts on the
+// fewest of them, so that there is no branch around any: a lane whose piece ends behind the row works on the row's last full piece instead and leaves what its neighbour leaves there, too, in the same bits; it takes part in
+// no sum twice.  Operands that are not there are read from x, results that nobody wants are written to a row of the workspace.  (With branches 16384 x 8192 bfloat16 took 354 us.)
+template <typename T, int LANES, int PIECES> struct Window {
+    static constexpr int VALUES = Piece<T>::VALUES;
+    uint32_t column[PIECES]; int32_t twice[PIECES];                 // first column of a piece; its values that are a neighbour's
+    __device__ __forceinline__ Window(int64_t width)
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            const int32_t col = (int32_t)(threadIdx.x % LANES + k * LANES) * VALUES, last = (int32_t)width - VALUES;
+            column[k] = col < last ? col : last;
+            twice[k] = col <= last ? 0 : col - last < VALUES ? col - last : VALUES;
+        }
+    }
+    __device__ __forceinline__ T *at(const T *row, int k) const { return (T *)((char *)row + (uint32_t)(column[k] * sizeof(T))); }
+    __device__ __forceinline__ void fetch(const T *row, Piece<T> (&to)[PIECES]) const
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) to[k].v = *reinterpret_cast<const typename Piece<T>::Memory *>(at(row, k));
+    }
+    __device__ __forceinline__ void fetch_or(const T *row, Piece<T> (&to)[PIECES], float other) const
+    {
+        if (row) { fetch(row, to); return; }
+        float v[VALUES];
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) v[e] = other;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) to[k].set(v);
+    }
+    __device__ __forceinline__ void leave(T *row, const Piece<T> (&from)[PIECES]) const
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) *reinterpret_cast<typename Piece<T>::Memory *>(at(row, k)) = from[k].v;
+    }
+    // for a sum: values that a neighbour counts become 0
+    __device__ __forceinline__ void once(int k, float (&v)[VALUES]) const
+    {
+        if (twice[k] > 0)
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) v[e] = e < twice[k] ? 0.0f : v[e];
+    }
+};
+
 // The compiler does not know any more what these hold: they have come by now, and what was unpacked from them is not kept, but unpacked anew.
 template <typename T, int PIECES> __device__ __forceinline__ void let_go(Piece<T> (&p)[PIECES])
 {
@@ -560,23 +604,22 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
     __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][MEANS];
     __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
-    const Lane<T, LANES> lane(a.width);
-    const double share = a.share;
-    const float share_f = (float)a.share;
+    const Window<T, LANES, PIECES> lane(a.width);
+    const float share = (float)a.share;
     const RowAt<T> vectors(a, blockIdx.y, 0);
+    T *const unwanted = (T *)to.unwanted + (blockIdx.y * to.workgroups + blockIdx.x) * GROUPS * to.padded + (threadIdx.x / LANES) * to.padded;
     Piece<T> g1[PIECES], b1[PIECES], g2[PIECES];
     float gate[BLOCK ? PIECES : 1][VALUES];        // b act(q)
-    lane.load_or(vectors.g2, g2, 1.0f);
+    lane.fetch_or(vectors.g2, g2, 1.0f);
     if constexpr (BLOCK) {
         Piece<T> q[PIECES];
-        lane.load_or(vectors.g1, g1, 1.0f);
-        if constexpr (BIASES) lane.load_or(vectors.b1, b1, 0.0f);
-        lane.load_or(GATED ? nullptr : vectors.q, q, 1.0f);
+        lane.fetch_or(vectors.g1, g1, 1.0f);
+        if constexpr (BIASES) lane.fetch_or(vectors.b1, b1, 0.0f);
+        lane.fetch_or(GATED ? nullptr : vectors.q, q, 1.0f);
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) gates_of<T>(GATED || !vectors.q ? GATE_NONE : a.act, a.f_scale, q[k], gate[k]);
     }
     float sums[SUMS][PIECES][VALUES] = {};
-    // the next row is under way while one is worked on
     struct Operands { Piece<T> x[PIECES], f[PIECES], q[PIECES], dy[PIECES], dh[PIECES]; };
     const auto fetch = [&](int64_t t, Operands &o) {
         const RowAt<T> row(a, blockIdx.y, t);
@@ -590,27 +633,28 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
     const int64_t step = (int64_t)gridDim.x * GROUPS;
     int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
     Operands next;
-    if (AHEAD) fetch(t < a.rows ? t : a.rows - 1, next);
+    if constexpr (AHEAD) {
+        fetch(t < a.rows ? t : a.rows - 1, next);
+        let_go(next.x); let_go(next.dy); let_go(next.dh);           // come before the loop, as in its turns: what is waited for at its top holds for all of them
+        if constexpr (BLOCK) let_go(next.f);
+        if constexpr (GATED) let_go(next.q);
+    }
     for (; t < a.rows; t += step) {
         Operands row = next;
         if (AHEAD) fetch(t + step < a.rows ? t + step : t, next);
         else fetch(t, row);
-        lane.settle(row.x);
-        lane.settle(row.dy, a.dy.p);
-        lane.settle(row.dh, a.dh.p);
-        if constexpr (BLOCK) {
-            lane.settle(row.f);
-            if constexpr (GATED) lane.settle(row.q);
-            let_go(g1);
-            if constexpr (BIASES) let_go(b1);
-        }
-        let_go(g2);
+        // all of the row has come before the first barrier, behind which other waves may write over it
+        let_go(row.x); let_go(row.dy); let_go(row.dh); let_go(g2);
+        if constexpr (BLOCK) { let_go(row.f); let_go(g1); }
+        if constexpr (BLOCK && BIASES) let_go(b1);
+        if constexpr (GATED) let_go(row.q);
+        if (LANES > 64 && !a.pre && !(BLOCK && a.post)) __syncthreads();
         Unit post{0.0f, 0.0f, 1.0f};
         if constexpr (BLOCK) {
             if (a.post) post = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) v[e] = row.f[k].get(e);
-            }, share, a.eps, room[0], room[1]);
+            }, a.share, a.eps, room[0], room[1]);
             if constexpr (GATED)
 #pragma unroll
                 for (int k = 0; k < PIECES; ++k) gates_of<T>(a.act, a.f_scale, row.q[k], gate[k]);
@@ -634,51 +678,62 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                     branch(k, fn, u);
 #pragma unroll
                     for (int e = 0; e < VALUES; ++e) d[k][e] = fmaf(gate[k][e], u[e], d[k][e]);
-                    if (LAYER) lane.clear(k, d[k]);
                 }
             }
             const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) v[e] = d[k][e];
-            }, share, a.eps, room[2], room[3]);
+            }, a.share, a.eps, room[2], room[3]);
             float along[MEANS] = {};
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k)
+            for (int k = 0; k < PIECES; ++k) {
+                float w[VALUES];
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    const float v = row.dy[k].get(e), w = v * g2[k].get(e);
+                    const float v = row.dy[k].get(e);
+                    w[e] = v * g2[k].get(e);
                     d[k][e] = unit_held_of<LAYER>(pre, d[k][e]);
-                    along[0] = fmaf(w, d[k][e], along[0]);
-                    if (LAYER) along[MEANS - 1] += w;
                     sums[2][k][e] = fmaf(v, d[k][e], sums[2][k][e]);
                     if (BIASES) sums[3][k][e] += v;
                 }
+                lane.once(k, w);
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    along[0] = fmaf(w[e], d[k][e], along[0]);
+                    if (LAYER) along[MEANS - 1] += w[e];
+                }
+            }
             row_sum<LANES>(along, pairs[0]);
             let_go(row.dy);
             let_go(g2);
-            const float mean_eh = along[0] * share_f, mean_e = LAYER ? along[MEANS - 1] * share_f : 0.0f;
+            const float mean_eh = along[0] * share, mean_e = LAYER ? along[MEANS - 1] * share : 0.0f;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
                     const float w = row.dy[k].get(e) * g2[k].get(e);
-                    d[k][e] = fmaf(pre.r, fmaf(-d[k][e], mean_eh, LAYER ? w - mean_e : w), row.dh[k].get(e));
+                    d[k][e] = pre.r * fmaf(-d[k][e], mean_eh, LAYER ? w - mean_e : w);
                 }
+            if (a.dh.p)
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) d[k][e] += row.dh[k].get(e);
         } else {
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) d[k][e] = row.dh[k].get(e);
         }
-        Piece<T> dx[PIECES], df[PIECES], dq[PIECES];
+        Piece<T> out[PIECES];
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) {
-            if (LAYER) lane.clear(k, d[k]);
-            float out[VALUES];
+            float v[VALUES];
 #pragma unroll
-            for (int e = 0; e < VALUES; ++e) out[e] = a.x_scale * d[k][e];
-            dx[k].set(out);
+            for (int e = 0; e < VALUES; ++e) v[e] = a.x_scale * d[k][e];
+            out[k].set(v);
         }
+        lane.leave(a.dx.p ? RowAt<T>::at(a.dx, blockIdx.y, t) : unwanted, out);
         if constexpr (BLOCK) {
             float back[MEANS] = {};
             let_go(row.f);
@@ -688,11 +743,11 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                 float fn[VALUES], u[VALUES];
                 branch(k, fn, u);
                 if constexpr (GATED) {
-                    float out[VALUES];
-                    slopes_of<T>(a.act, a.f_scale, row.q[k], out);
+                    float v[VALUES];
+                    slopes_of<T>(a.act, a.f_scale, row.q[k], v);
 #pragma unroll
-                    for (int e = 0; e < VALUES; ++e) out[e] *= u[e] * d[k][e];
-                    dq[k].set(out);
+                    for (int e = 0; e < VALUES; ++e) v[e] *= u[e] * d[k][e];
+                    out[k].set(v);
                 }
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
@@ -700,44 +755,35 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                     const float du = gate[k][e] * d[k][e];
                     if (BIASES) sums[1][k][e] += du;
                     sums[0][k][e] = fmaf(du, fn[e], sums[0][k][e]);
-                    d[k][e] = du * g1[k].get(e);                    // c
-                    back[0] = fmaf(d[k][e], fn[e], back[0]);
-                    if (LAYER) back[MEANS - 1] += d[k][e];
+                    d[k][e] = u[e] = du * g1[k].get(e);             // c
+                }
+                lane.once(k, u);
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) {
+                    back[0] = fmaf(u[e], fn[e], back[0]);
+                    if (LAYER) back[MEANS - 1] += u[e];
                 }
             }
+            if constexpr (GATED) lane.leave(a.dgate.p ? RowAt<T>::at(a.dgate, blockIdx.y, t) : unwanted, out);
             if (a.post) row_sum<LANES>(back, pairs[1]);
-            const float mean_cf = a.post ? back[0] * share_f : 0.0f, mean_c = LAYER && a.post ? back[MEANS - 1] * share_f : 0.0f;
+            const float mean_cf = a.post ? back[0] * share : 0.0f, mean_c = LAYER && a.post ? back[MEANS - 1] * share : 0.0f;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
-                float out[VALUES];
+                float v[VALUES];
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
                     const float fn = unit_held_of<LAYER>(post, row.f[k].get(e));
-                    out[e] = post.r * fmaf(-fn, mean_cf, LAYER ? d[k][e] - mean_c : d[k][e]);
+                    v[e] = post.r * fmaf(-fn, mean_cf, LAYER ? d[k][e] - mean_c : d[k][e]);
                 }
-                df[k].set(out);
+                out[k].set(v);
             }
-        }
-        // the next row has come by now: waited for behind the writes, it would be waited for with them
-        if constexpr (AHEAD) { let_go(next.x); let_go(next.dy); let_go(next.dh); }
-        if constexpr (AHEAD && BLOCK) let_go(next.f);
-        if constexpr (AHEAD && GATED) let_go(next.q);
-        T *to_x = RowAt<T>::at(a.dx, blockIdx.y, t);
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) lane.store(to_x, k, dx[k]);
-        if constexpr (BLOCK) {
-            T *to_f = RowAt<T>::at(a.df, blockIdx.y, t), *to_q = RowAt<T>::at(a.dgate, blockIdx.y, t);
-#pragma unroll
-            for (int k = 0; k < PIECES; ++k) {
-                lane.store(to_f, k, df[k]);
-                if constexpr (GATED) lane.store(to_q, k, dq[k]);
-            }
+            lane.leave(a.df.p ? RowAt<T>::at(a.df, blockIdx.y, t) : unwanted, out);
         }
     }
     if constexpr (BLOCK && !GATED)                 // a gate that is the same for all rows has one slope, too
         if (to.place[4] >= 0) {
             Piece<T> q[PIECES];
-            lane.load_or(vectors.q, q, 1.0f);
+            lane.fetch_or(vectors.q, q, 1.0f);
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
                 float slope[VALUES];
@@ -751,25 +797,33 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
     for (int s = 0; s < SUMS; ++s) {
         if ((!BLOCK && s != 2 && s != 3) || (!BIASES && (s == 1 || s == 3)) || (GATED && s == 4)) continue;
         if (to.place[s] < 0) continue;
+        float *row = mine + to.place[s] * to.padded;
         if constexpr (GROUPS > 1) {                // rows of the same workgroup, in order
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) shared_sums[threadIdx.x / LANES][(k * LANES + threadIdx.x % LANES) * VALUES + e] = sums[s][k][e];
+                for (int e = 0; e < VALUES; ++e)
+                    if (e >= lane.twice[k]) shared_sums[threadIdx.x / LANES][lane.column[k] + e] = sums[s][k][e];
             __syncthreads();
-            for (int c = threadIdx.x; c < LANES * PIECES * VALUES && c < to.padded; c += THREADS) {
+            for (int c = threadIdx.x; c < a.width; c += THREADS) {
                 float sum = 0.0f;
                 for (int g = 0; g < GROUPS; ++g) sum += shared_sums[g][c];
-                mine[to.place[s] * to.padded + c] = sum;
+                row[c] = sum;
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k)
-                if (lane.left(k) > 0)
+            for (int k = 0; k < PIECES; ++k) {
+                if (lane.twice[k] == 0) {
 #pragma unroll
                     for (int e = 0; e < VALUES; e += 4)
-                        *reinterpret_cast<f32x4 *>(mine + to.place[s] * to.padded + lane.col(k) + e) = f32x4{sums[s][k][e], sums[s][k][e + 1], sums[s][k][e + 2], sums[s][k][e + 3]};
+                        *reinterpret_cast<f32x4 *>(row + lane.column[k] + e) = f32x4{sums[s][k][e], sums[s][k][e + 1], sums[s][k][e + 2], sums[s][k][e + 3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e)
+                        if (e >= lane.twice[k]) row[lane.column[k] + e] = sums[s][k][e];
+                }
+            }
         }
     }
 }
@@ -849,14 +903,18 @@ static Partials partials_of(const NormArgs &a, void *work)
     // as many as the card holds at once, if each has two turns
     const int64_t places = 256 * (1024 / threads), most = a.batch * 8 < places ? places / a.batch : 8, turns = (a.rows + rows - 1) / rows, all = (turns + 1) / 2;
     to.workgroups = all < most ? all : most;
+    // behind the sums, for results that nobody wants: a row for each of a workgroup's groups of lanes
+    const bool all_wanted = a.dx.p && (!a.f.p || a.df.p) && (!a.f.p || !a.gate_rows || !a.gate.p || a.dgate.p);
+    to.bytes = up_to(4 * a.batch * to.workgroups * to.sums * to.padded, 256);
+    to.unwanted = (char *)work + to.bytes;
+    if (!all_wanted) to.bytes += (a.bf16 ? 2 : 4) * a.batch * to.workgroups * rows * to.padded;
     return to;
 }
 
 int64_t block_norm_grad_workspace(const NormArgs &a)
 {
     if (a.batch == 0) return 0;
-    const Partials to = partials_of(a, nullptr);
-    return 4 * a.batch * to.workgroups * to.sums * to.padded;
+    return partials_of(a, nullptr).bytes;
 }
 
 template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)

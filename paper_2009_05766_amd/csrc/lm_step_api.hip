@@ -156,14 +156,14 @@ extern "C" int netmax_block_norm(const netmax_block_norm_shape *s, const netmax_
     return launched("block norm");
 }
 
-extern "C" int64_t netmax_block_norm_grad_workspace(const netmax_block_norm_shape *s, const netmax_block_norm_grads *g)
+extern "C" int64_t netmax_block_norm_grad_workspace(const netmax_block_norm_shape *s, const netmax_block_norm_data *d, const netmax_block_norm_grads *g)
 {
     if (check_block_norm(s) != NETMAX_OK) return -1;
-    if (!g) {
-        netmax_fail(NETMAX_EINVAL, "grads is NULL");
+    if (!d || !g) {
+        netmax_fail(NETMAX_EINVAL, "data or grads is NULL");
         return -1;
     }
-    return block_norm_grad_workspace(norm_args(s, nullptr, g));
+    return block_norm_grad_workspace(norm_args(s, d, g));
 }
 
 extern "C" int netmax_block_norm_grad(const netmax_block_norm_shape *s, const netmax_block_norm_data *d, const netmax_block_norm_grads *g, void *work, int64_t work_bytes, void *stream)

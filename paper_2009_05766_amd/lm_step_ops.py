@@ -172,7 +172,7 @@ def netmax_block_norm_grad(dy, dh, x, f=None, gate=None, post_gain=None, post_bi
                                     *(_rows if gate_rows else _vector)("dgate", dgate, x, rows if gate_rows else vector, dt), *_vector("dpost_gain", dpost_gain, x, vector, dt),
                                     *_vector("dpost_bias", dpost_bias, x, vector, dt), *_vector("dpre_gain", dpre_gain, x, vector, dt), *_vector("dpre_bias", dpre_bias, x, vector, dt))
     lib, ref = load(), C.byref(shape)
-    work = _workspace(lib.netmax_block_norm_grad_workspace(ref, grads), dev)
+    work = _workspace(lib.netmax_block_norm_grad_workspace(ref, data, grads), dev)
     _call(lib.netmax_block_norm_grad, dev, ref, data, grads, _p(work), 0 if work is None else work.numel())
     _changed(*given)
     return BlockNormGrads(dx, df, dgate, dpost_gain, dpost_bias, dpre_gain, dpre_bias)

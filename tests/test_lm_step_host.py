@@ -117,11 +117,11 @@ def test_norm_grad_refuses_operands(g, d, text):
 
 def test_norm_workspaces_and_nothing():
     lib, s = nm.load(), norm_shape()
-    need = lib.netmax_block_norm_grad_workspace(C.byref(s), grads())
-    assert need >= 5 * 16 * 4 and lib.netmax_block_norm_grad_workspace(C.byref(s), grads(("dy", "dx"))) == 0
-    assert lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(batch=0)), grads()) == 0 and lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(rows=0)), grads()) == 0
+    need = lib.netmax_block_norm_grad_workspace(C.byref(s), data(), grads())
+    assert need >= 5 * 16 * 4 and lib.netmax_block_norm_grad_workspace(C.byref(s), data(("x",)), grads(("dy", "dx"))) == 0
+    assert lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(batch=0)), data(), grads()) == 0 and lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(rows=0)), data(), grads()) == 0
     assert lib.netmax_embed_grad_workspace(C.byref(embed_shape(batch=0, tokens=9999))) == 0 and lib.netmax_embed_grad_workspace(C.byref(embed_shape(tokens=0))) == 0
-    assert lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(width=0)), grads()) == -1 and lib.netmax_block_norm_grad_workspace(C.byref(s), None) == -1
+    assert lib.netmax_block_norm_grad_workspace(C.byref(norm_shape(width=0)), data(), grads()) == -1 and lib.netmax_block_norm_grad_workspace(C.byref(s), data(), None) == -1 and lib.netmax_block_norm_grad_workspace(C.byref(s), None, grads()) == -1
     refused(lib.netmax_block_norm_grad(C.byref(s), data(), grads(), None, 0, None), "workspace")
     refused(lib.netmax_block_norm_grad(C.byref(s), data(), grads(), at(30), need - 1, None), "workspace")
     refused(lib.netmax_block_norm_grad(C.byref(s), data(), grads(), at(30) + 4, need, None), "workspace")
