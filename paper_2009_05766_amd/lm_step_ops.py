@@ -5,16 +5,36 @@ tensors' device and its current stream, nothing recorded for automatic different
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
+import os
+import struct
 from typing import NamedTuple, Optional, Sequence
 
 import torch
 
-from .binding import (NETMAX_GATE_NONE, NETMAX_GATE_SIGMOID, NETMAX_GATE_TANH, NETMAX_NORM_LAYER, NETMAX_NORM_RMS, load, netmax_block_norm_data, netmax_block_norm_grads,
-                      netmax_block_norm_shape, netmax_embed_shape, netmax_gradient)
-from .lm_ops import _DTYPES, _call, _changed, _check_tensor, _first, _no_graph, _p, _refuse, _strides, _workspace
+from .binding import (NETMAX_GATE_NONE, NETMAX_GATE_SIGMOID, NETMAX_GATE_TANH, NETMAX_NORM_LAYER, NETMAX_NORM_RMS, NetmaxError, load, netmax_gradient)
+from .lm_ops import _DTYPES, _refuse, _stream
 
 NORMS = {"rms": NETMAX_NORM_RMS, "layer": NETMAX_NORM_LAYER}
 GATES = {"none": NETMAX_GATE_NONE, "sigmoid": NETMAX_GATE_SIGMOID, "tanh": NETMAX_GATE_TANH}
+_ENTRIES = ("netmax_last_error", "netmax_embed", "netmax_embed_grad_workspace", "netmax_embed_grad", "netmax_block_norm", "netmax_block_norm_grad_workspace", "netmax_block_norm_grad",
+            "netmax_grad_norm_workspace", "netmax_grad_norm", "netmax_clip_grads")
+_calls = None
+
+
+def _load_calls():
+    """The extension module that checks tensors, allocates outputs and calls the C entry points (csrc/lm_calls.cpp); built first only if it is absent."""
+    global _calls
+    from .build import CALLS, build_calls
+    lib = load()
+    if not os.path.exists(CALLS):
+        build_calls()
+    spec = importlib.util.spec_from_file_location("_lm_calls", CALLS)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.setup(NetmaxError, _stream, tuple(C.cast(getattr(lib, n), C.c_void_p).value for n in _ENTRIES))
+    _calls = module
+    return module
 
 
 def _one_of(name: str, value: str, known: dict) -> int:
@@ -23,72 +43,17 @@ def _one_of(name: str, value: str, known: dict) -> int:
     return known[value]
 
 
-# ---- embedding ---------------------------------------------------------------------------------------------------------
-
-def _ids(tokens, like: torch.Tensor):
-    """(tokens of each table, distance of the batch's)."""
-    lead = like.dim() - 2
-    if not isinstance(tokens, torch.Tensor) or tokens.dim() != 1 + lead:
-        _refuse("tokens must have one dimension for one table, two for a batch of them")
-    shape = (*like.shape[:lead], tokens.shape[-1])
-    _check_tensor("tokens", tokens, like, shape, torch.int32)
-    return shape[-1], tokens.stride(0) if lead else 0
-
-
 def netmax_embed(tokens, table, *, scale: float = 1.0, y=None):
     """y = scale table[tokens].  table [vocab, width] and tokens int32 [n], or [batch, vocab, width] and [batch, n] with a table each; tokens outside of the
     vocabulary are padding, with rows of zeros."""
-    _first("table", table, (2, 3))
-    n, s_ids = _ids(tokens, table)
-    lead, (vocab, width) = tuple(table.shape[:-2]), table.shape[-2:]
-    if not table.is_contiguous():
-        _check_tensor("table", table, table, table.shape, table.dtype)
-    given = y
-    if y is None:
-        y = torch.empty((*lead, n, width), dtype=table.dtype, device=table.device)
-    else:
-        _check_tensor("y", y, table, (*lead, n, width), table.dtype)
-    ldt, st = _strides(table)
-    ldy, sy = _strides(y)
-    shape = netmax_embed_shape(lead[0] if lead else 1, n, vocab, width, _DTYPES[table.dtype], 0, scale, s_ids, ldt, st, ldy, sy)
-    _call(load().netmax_embed, table.device, C.byref(shape), _p(tokens), _p(table), _p(y))
-    _changed(given)
-    return y
+    return (_calls or _load_calls()).embed(tokens, table, scale, y)
 
 
 def netmax_embed_grad(dy, tokens, vocab: Optional[int] = None, *, scale: float = 1.0, accumulate: bool = False, dtable=None):
     """The gradient of `netmax_embed`'s table from dy [n, width] or [batch, n, width]; vocab, or the memory dtable, says how many rows it has.  accumulate: added to
     what dtable holds, whose other rows are not touched."""
-    _first("dy", dy, (2, 3))
-    n, s_ids = _ids(tokens, dy)
-    lead, width, given = tuple(dy.shape[:-2]), dy.shape[-1], dtable
-    if dy.shape[-2] != n:
-        _refuse(f"dy has {dy.shape[-2]} rows for {n} tokens")
-    if not dy.is_contiguous():
-        _check_tensor("dy", dy, dy, dy.shape, dy.dtype)
-    if dtable is not None:
-        if not isinstance(dtable, torch.Tensor) or dtable.dim() != dy.dim():
-            _refuse("dtable must have as many dimensions as dy")
-        if vocab is None:
-            vocab = dtable.shape[-2]
-        _check_tensor("dtable", dtable, dy, (*lead, vocab, width), dy.dtype)
-    elif accumulate:
-        _refuse("accumulate needs dtable")
-    elif vocab is None:
-        _refuse("vocab or dtable is needed")
-    else:
-        dtable = torch.empty((*lead, vocab, width), dtype=dy.dtype, device=dy.device)
-    ldt, st = _strides(dtable)
-    ldy, sy = _strides(dy)
-    shape = netmax_embed_shape(lead[0] if lead else 1, n, vocab, width, _DTYPES[dy.dtype], int(bool(accumulate)), scale, s_ids, ldt, st, ldy, sy)
-    lib, ref = load(), C.byref(shape)
-    work = _workspace(lib.netmax_embed_grad_workspace(ref), dy.device)
-    _call(lib.netmax_embed_grad, dy.device, ref, _p(tokens), _p(dy), _p(dtable), _p(work), 0 if work is None else work.numel())
-    _changed(given)
-    return dtable
+    return (_calls or _load_calls()).embed_grad(dy, tokens, vocab, scale, accumulate, dtable)
 
-
-# ---- norms of a block ----------------------------------------------------------------------------------------------------
 
 class BlockNormGrads(NamedTuple):
     """The gradients that `netmax_block_norm_grad` returns, None for what is not there or not needed."""
@@ -101,55 +66,13 @@ class BlockNormGrads(NamedTuple):
     dpre_bias: Optional[torch.Tensor]
 
 
-_NOTHING = (0, 0, 0)
-
-
-def _rows(name, t, x, shape, dtype):
-    if t is None:
-        return _NOTHING
-    _check_tensor(name, t, x, shape, dtype)
-    s = t.stride()
-    return (t.data_ptr(), s[0], 0) if len(s) == 2 else (t.data_ptr(), s[1], s[0])
-
-
-def _vector(name, t, x, shape, dtype):
-    if t is None:
-        return _NOTHING
-    _check_tensor(name, t, x, shape, dtype)
-    return t.data_ptr(), 0, t.stride(0) if len(shape) == 2 else 0
-
-
-def _operands(x, f, gate, post_gain, post_bias, pre_gain, pre_bias):
-    """Their spans, whether the gate has rows of its own, and the shapes of rows and vectors."""
-    _first("x", x, (2, 3))
-    rows, dt = x.shape, x.dtype
-    vector = (*rows[:-2], rows[-1])
-    gate_rows = isinstance(gate, torch.Tensor) and gate.dim() == x.dim()
-    return ((*_rows("x", x, x, rows, dt), *_rows("f", f, x, rows, dt), *(_rows if gate_rows else _vector)("gate", gate, x, rows if gate_rows else vector, dt),
-             *_vector("post_gain", post_gain, x, vector, dt), *_vector("post_bias", post_bias, x, vector, dt), *_vector("pre_gain", pre_gain, x, vector, dt),
-             *_vector("pre_bias", pre_bias, x, vector, dt)), gate_rows, rows, vector)
-
-
-def _norm_shape(x, norm, gate_act, gate_rows, post, pre, x_scale, f_scale, eps):
-    return netmax_block_norm_shape(x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1], _DTYPES[x.dtype], _one_of("norm", norm, NORMS), _one_of("gate_act", gate_act, GATES),
-                                   gate_rows, bool(post), bool(pre), x_scale, f_scale, eps)
-
-
 def netmax_block_norm(x, f=None, gate=None, post_gain=None, post_bias=None, pre_gain=None, pre_bias=None, *, norm: str = "rms", post: bool = True, pre: bool = True,
                       gate_act: str = "none", x_scale: float = 1.0, f_scale: float = 1.0, eps: float = 1e-6, need_h: bool = True, h=None, y=None):
     """(h, y) with h = x_scale x + f_scale act(gate) (N(f) post_gain + post_bias), y = N(h) pre_gain + pre_bias; N: "rms" or "layer".
     x and f [rows, width], or [batch, rows, width] with vectors of their own each; gate [rows, width] or, the same for all rows, [width]; gains and biases [width].
     Without f, y = N(x_scale x) pre_gain + pre_bias, and h is None unless memory for it is given.  post=False: f is not normed; pre=False: y is None."""
-    spans, gate_rows, rows, _ = _operands(x, f, gate, post_gain, post_bias, pre_gain, pre_bias)
-    shape, given = _norm_shape(x, norm, gate_act, gate_rows, post, pre, x_scale, f_scale, eps), (h, y)
-    if h is None and f is not None and need_h:
-        h = torch.empty(rows, dtype=x.dtype, device=x.device)
-    if y is None and pre:
-        y = torch.empty(rows, dtype=x.dtype, device=x.device)
-    data = netmax_block_norm_data(*spans, *_rows("h", h, x, rows, x.dtype), *_rows("y", y, x, rows, x.dtype))
-    _call(load().netmax_block_norm, x.device, C.byref(shape), data)
-    _changed(*given)
-    return h, y
+    return (_calls or _load_calls()).block_norm(x, f, gate, post_gain, post_bias, pre_gain, pre_bias, _one_of("norm", norm, NORMS), post, pre, _one_of("gate_act", gate_act, GATES), x_scale,
+                                                f_scale, eps, need_h, h, y)
 
 
 def netmax_block_norm_grad(dy, dh, x, f=None, gate=None, post_gain=None, post_bias=None, pre_gain=None, pre_bias=None, *, norm: str = "rms", post: bool = True,
@@ -157,25 +80,9 @@ def netmax_block_norm_grad(dy, dh, x, f=None, gate=None, post_gain=None, post_bi
                            need_params: bool = True, dx=None, df=None, dgate=None, dpost_gain=None, dpost_bias=None, dpre_gain=None, dpre_bias=None) -> BlockNormGrads:
     """The gradients of `netmax_block_norm`, called with the same operands and options, from dy and dh (None: nothing reaches h but through y).  need_input: dx, df and the
     gradient of a gate of rows; need_params: those of gains, biases and a gate that is the same for all rows, summed over the rows."""
-    spans, gate_rows, rows, vector = _operands(x, f, gate, post_gain, post_bias, pre_gain, pre_bias)
-    shape, dt, dev = _norm_shape(x, norm, gate_act, gate_rows, post, pre, x_scale, f_scale, eps), x.dtype, x.device
-    given = (dx, df, dgate, dpost_gain, dpost_bias, dpre_gain, dpre_bias)
-
-    def output(t, of, needed, like):
-        return torch.empty(like, dtype=dt, device=dev) if t is None and of is not None and needed else t
-
-    dx, df = output(dx, x, need_input, rows), output(df, f, need_input, rows)
-    dgate = output(dgate, gate, need_input, rows) if gate_rows else output(dgate, gate, need_params, vector)
-    dpost_gain, dpost_bias, dpre_gain, dpre_bias = (output(t, of, need_params, vector) for t, of in ((dpost_gain, post_gain), (dpost_bias, post_bias), (dpre_gain, pre_gain), (dpre_bias, pre_bias)))
-    data = netmax_block_norm_data(*spans, *_NOTHING, *_NOTHING)
-    grads = netmax_block_norm_grads(*_rows("dy", dy, x, rows, dt), *_rows("dh", dh, x, rows, dt), *_rows("dx", dx, x, rows, dt), *_rows("df", df, x, rows, dt),
-                                    *(_rows if gate_rows else _vector)("dgate", dgate, x, rows if gate_rows else vector, dt), *_vector("dpost_gain", dpost_gain, x, vector, dt),
-                                    *_vector("dpost_bias", dpost_bias, x, vector, dt), *_vector("dpre_gain", dpre_gain, x, vector, dt), *_vector("dpre_bias", dpre_bias, x, vector, dt))
-    lib, ref = load(), C.byref(shape)
-    work = _workspace(lib.netmax_block_norm_grad_workspace(ref, data, grads), dev)
-    _call(lib.netmax_block_norm_grad, dev, ref, data, grads, _p(work), 0 if work is None else work.numel())
-    _changed(*given)
-    return BlockNormGrads(dx, df, dgate, dpost_gain, dpost_bias, dpre_gain, dpre_bias)
+    return BlockNormGrads._make((_calls or _load_calls()).block_norm_grad(dy, dh, x, f, gate, post_gain, post_bias, pre_gain, pre_bias, _one_of("norm", norm, NORMS), post, pre,
+                                                                          _one_of("gate_act", gate_act, GATES), x_scale, f_scale, eps, need_input, need_params, dx, df, dgate, dpost_gain,
+                                                                          dpost_bias, dpre_gain, dpre_bias))
 
 
 # ---- clipping ------------------------------------------------------------------------------------------------------------
@@ -184,11 +91,12 @@ class Gradients:
     """Where a model's gradients lie, for `netmax_grad_norm` and `netmax_clip_grads`: a program whose gradients stay in the same memory lays the list out once.
 
     tensors: float32 or bfloat16, of any shapes, rows at one distance, on one GPU; batch: their first dimension counts models (workers), which have a norm each.  out: where the scaled
-    gradients go, of the same shapes and types; None: in place.  The tensors are kept alive; one that is moved to other memory is noticed and refused."""
+    gradients go, of the same shapes and types; None: in place.  The tensors are kept alive; one that is moved to other memory is noticed
+    and refused."""
 
     def __init__(self, tensors: Sequence[torch.Tensor], *, out: Optional[Sequence[torch.Tensor]] = None, batch: bool = False):
-        self.tensors = list(tensors)
-        self.out = self.tensors if out is None else list(out)
+        self.tensors = tuple(tensors)
+        self.out = self.tensors if out is None else tuple(out)
         if not self.tensors:
             _refuse("there are no gradients")
         if len(self.out) != len(self.tensors):
@@ -208,8 +116,8 @@ class Gradients:
                     _refuse("an output must be a tensor of its gradient's shape and type")
             e.ldo, e.so = self._place(o, "an output")[2:]
             e.g, e.out, e.rows, e.cols, e.dtype = g.data_ptr(), o.data_ptr(), rows, cols, _DTYPES[g.dtype]
-        self._all = self.tensors if out is None else self.tensors + self.out
-        self._at = [t.data_ptr() for t in self._all]
+        self._at = struct.pack(f"{2 * len(self.tensors)}P", *(t.data_ptr() for t in self.tensors), *(t.data_ptr() for t in self.out))
+        self._entries_at = C.addressof(self.entries)
 
     def _place(self, t, name):
         """(rows, columns, distance of rows, distance of models)."""
@@ -240,24 +148,8 @@ class Gradients:
             rows *= n
         return rows, shape[-1], ld, step
 
-    def _ready(self):
-        if [t.data_ptr() for t in self._all] != self._at:
-            _refuse("a gradient has moved since the list was laid out")
-        if torch.is_grad_enabled() and any(t.requires_grad for t in self._all):
-            _no_graph("a gradient")
-
     def _run(self, max_norm: Optional[float]):
-        self._ready()
-        lib, dev, n = load(), self.device, len(self.tensors)
-        norm = torch.empty(self.models if self.batch else (), dtype=torch.float32, device=dev)
-        work = _workspace(lib.netmax_grad_norm_workspace(self.models, n, self.entries), dev)
-        size = 0 if work is None else work.numel()
-        if max_norm is None:
-            _call(lib.netmax_grad_norm, dev, self.models, n, self.entries, _p(norm), _p(work), size)
-        else:
-            _call(lib.netmax_clip_grads, dev, self.models, n, self.entries, max_norm, _p(norm), _p(work), size)
-            torch.autograd.graph.increment_version(self.out)
-        return norm
+        return (_calls or _load_calls()).clip(self.tensors, self.out, self._at, self._entries_at, self.models, self.batch, max_norm)
 
 
 def _gradients(gradients, out, batch) -> Gradients:
