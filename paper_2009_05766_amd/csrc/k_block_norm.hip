@@ -314,23 +314,27 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
     }
 }
 
-// Column sums: 64 columns for a workgroup, whose waves take turns at the partial sums.
-constexpr int JOIN_WAVES = 16;
-template <typename T> __global__ void __launch_bounds__(JOIN_WAVES * 64) join_sums_kernel(NormArgs a, Partials from)
+// Column sums: 16 columns for a workgroup, whose 64 groups of lanes take turns at the partial sums.
+constexpr int JOIN_COLUMNS = 16, JOIN_TURNS = 64;
+template <typename T> __global__ void __launch_bounds__(JOIN_COLUMNS * JOIN_TURNS) join_sums_kernel(NormArgs a, Partials from)
 {
-    __shared__ double part[JOIN_WAVES][64];
-    const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), row = from.sums * from.padded;
+    __shared__ double part[JOIN_TURNS][JOIN_COLUMNS];
+    const int32_t turn = threadIdx.x / JOIN_COLUMNS;
+    const int64_t col = (int64_t)blockIdx.x * JOIN_COLUMNS + threadIdx.x % JOIN_COLUMNS, row = from.sums * from.padded;
     const float *p = from.p + (blockIdx.z * from.workgroups * from.sums + blockIdx.y) * from.padded + col;
     double sum = 0.0;
     if (col < a.width)
 #pragma unroll 8
-        for (int64_t w = threadIdx.x >> 6; w < from.workgroups; w += JOIN_WAVES) sum += p[w * row];
-    part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+        for (int64_t w = turn; w < from.workgroups; w += JOIN_TURNS) sum += p[w * row];
+    part[turn][threadIdx.x % JOIN_COLUMNS] = sum;
     __syncthreads();
-    if (threadIdx.x >= 64 || col >= a.width) return;
+    if (threadIdx.x >= 4 * JOIN_COLUMNS) return;
+    sum = 0.0;
 #pragma unroll
-    for (int w = 1; w < JOIN_WAVES; ++w) sum += part[w][threadIdx.x];
-    store_value(RowAt<T>::at(from.out[blockIdx.y], blockIdx.z, 0) + col, (float)sum);
+    for (int k = 0; k < JOIN_TURNS / 4; ++k) sum += part[k * 4 + turn][threadIdx.x % JOIN_COLUMNS];
+    sum += __shfl_xor(sum, JOIN_COLUMNS);
+    sum += __shfl_xor(sum, 2 * JOIN_COLUMNS);
+    if (turn == 0 && col < a.width) store_value(RowAt<T>::at(from.out[blockIdx.y], blockIdx.z, 0) + col, (float)sum);
 }
 
 // ---- rows that a group of lanes keeps in registers -------------------------------------------------------------------
@@ -938,7 +942,7 @@ template <typename T> static void block_norm_grad_of(hipStream_t s, const NormAr
     }, [&]() {
         long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
     });
-    if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + 63) / 64), to.sums, (uint32_t)a.batch), JOIN_WAVES * 64, 0, s>>>(a, to);
+    if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + JOIN_COLUMNS - 1) / JOIN_COLUMNS), to.sums, (uint32_t)a.batch), JOIN_COLUMNS * JOIN_TURNS, 0, s>>>(a, to);
 }
 
 void launch_block_norm_grad(hipStream_t s, const NormArgs &a, void *work)

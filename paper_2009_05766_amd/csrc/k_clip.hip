@@ -13,7 +13,7 @@ namespace netmax {
 
 constexpr int THREADS = 256, DEEP = 4;             // pieces that a thread has under way at once
 constexpr int UNIT = THREADS * DEEP;
-constexpr int MOST_WORKGROUPS = 1024;              // of a launch for all models: four on every compute unit
+constexpr int MOST_WORKGROUPS = 2048;              // of a launch for all models: eight on every compute unit, and as many sums for every workgroup of the second pass to add up
 
 struct Item { const void *g; void *out; int64_t ldg, sg, ldo, so, rows, cols; uint32_t first, bf16; };
 constexpr int LAUNCH = 54;                         // arguments of a launch stay below 4096 bytes, and a wave has a lane for each tensor
@@ -45,18 +45,20 @@ template <typename T> __device__ __forceinline__ double squares_of(const Item &t
     const T *g = (const T *)t.g + model * t.sg;
     const int64_t all = row_pieces(t) * t.rows, p0 = (int64_t)(u - t.first) * UNIT + threadIdx.x;
     Piece<T> x[DEEP];
+    int64_t row[DEEP], col[DEEP];
 #pragma unroll
     for (int k = 0; k < DEEP; ++k) {
-        int64_t row, col;
-        place_of<VALUES>(t, p0 + k * THREADS, row, col);
-        if (p0 + k * THREADS < all) x[k] = load_piece(g + row * t.ldg + col, t.cols - col);
-        else x[k].v = decltype(x[k].v){};
+        place_of<VALUES>(t, p0 + k * THREADS, row[k], col[k]);
+        if (p0 + k * THREADS < all) x[k] = fetch_piece(g + row[k] * t.ldg, col[k], t.cols);
     }
     double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
+        if (p0 + k * THREADS < all) {
+            settle_piece(x[k], col[k], t.cols);
 #pragma unroll
-        for (int e = 0; e < VALUES; ++e) sum = fma((double)x[k].get(e), (double)x[k].get(e), sum);
+            for (int e = 0; e < VALUES; ++e) sum = fma((double)x[k].get(e), (double)x[k].get(e), sum);
+        }
     return sum;
 }
 
@@ -77,6 +79,7 @@ __device__ __forceinline__ double total_of(const double *partials, int64_t n)
 {
     __shared__ double room[THREADS / 64][1];
     double sum[1] = {0.0};
+#pragma unroll 8
     for (int64_t k = threadIdx.x; k < n; k += THREADS) sum[0] += partials[k];
     row_sum<THREADS>(sum, room);
     return sum[0];
@@ -103,11 +106,12 @@ template <typename T> __device__ __forceinline__ void scale_unit(const Item &t, 
 #pragma unroll
     for (int k = 0; k < DEEP; ++k) {
         place_of<VALUES>(t, p0 + k * THREADS, row[k], col[k]);
-        if (p0 + k * THREADS < all) x[k] = load_piece(g + row[k] * t.ldg + col[k], t.cols - col[k]);
+        if (p0 + k * THREADS < all) x[k] = fetch_piece(g + row[k] * t.ldg, col[k], t.cols);
     }
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
         if (p0 + k * THREADS < all) {
+            settle_piece(x[k], col[k], t.cols);
             float v[VALUES];
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) v[e] = (float)((double)x[k].get(e) * factor);

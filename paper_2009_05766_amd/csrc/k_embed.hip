@@ -48,13 +48,13 @@ __global__ void __launch_bounds__(THREADS) embed_kernel(EmbedArgs a, uint32_t sl
 #pragma unroll
     for (int k = 0; k < DEEP; ++k) {
         const int64_t col = at + k * LANES * VALUES;
-        if (known && col < a.width) x[k] = load_piece(from + col, a.width - col);
-        else x[k].v = decltype(x[k].v){};
+        if (known && col < a.width) x[k] = fetch_piece(from, col, a.width);
     }
 #pragma unroll
     for (int k = 0; k < DEEP; ++k) {
         const int64_t col = at + k * LANES * VALUES;
         if (col >= a.width) continue;
+        settle_piece(x[k], col, a.width);
         float v[VALUES];
 #pragma unroll
         for (int e = 0; e < VALUES; ++e) v[e] = known ? a.scale * x[k].get(e) : 0.0f;
@@ -93,7 +93,8 @@ template <typename T> __device__ __forceinline__ void leave_row(const EmbedArgs 
     for (int e = 0; e < VALUES; ++e) v[e] = a.scale * sum[e];
     Piece<T> out;
     if (a.accumulate) {
-        const Piece<T> old = load_piece(row + col, a.width - col);
+        Piece<T> old = fetch_piece(row, col, a.width);
+        settle_piece(old, col, a.width);
 #pragma unroll
         for (int e = 0; e < VALUES; ++e) v[e] += old.get(e);
     }
@@ -123,7 +124,8 @@ template <typename T> __device__ __forceinline__ void zero_rows(const EmbedArgs 
 
 // ---- gradient for few tokens -------------------------------------------------------------------------------------------
 
-constexpr int FEW = 2048, FEW_ROWS = 16;           // tokens; rows of the table that a workgroup looks whether to clear
+constexpr int FEW = 2048, FEW_ROWS = 16;           // tokens (64 words of 64 bits hold their places twice over); rows of the table that a workgroup looks whether to clear
+constexpr uint32_t AHEAD = 8;                      // rows that a lane has under way at once
 
 // LANES lanes for LANES pieces of a row; the other lanes of the workgroup take turns with them at the token's rows.
 template <typename T, int LANES>
@@ -131,18 +133,24 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
 {
     constexpr int VALUES = Piece<T>::VALUES, SHARES = THREADS / LANES;
     __shared__ uint64_t place[FEW / 64];
+    __shared__ uint16_t rows[FEW];
+    __shared__ uint32_t count;
     __shared__ float part[SHARES > 1 ? SHARES : 1][SHARES > 1 ? LANES * VALUES : 1];
     const int32_t *ids = a.ids + blockIdx.z * a.s_ids;
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens;
+    int32_t seen[FEW / THREADS];                   // a share of the ids, all under way at once
+#pragma unroll
+    for (int i = 0; i < FEW / THREADS; ++i) seen[i] = i * THREADS + threadIdx.x < tokens ? ids[i * THREADS + threadIdx.x] : -1;
     if (id >= sums) {
         const int64_t first = (int64_t)(id - sums) * FEW_ROWS;
         if (first >= a.vocab) return;
         if (threadIdx.x == 0) place[0] = 0;
         __syncthreads();
         uint32_t hit = 0;
-        for (uint32_t t = threadIdx.x; t < tokens; t += THREADS) {
-            const int64_t r = (int64_t)ids[t] - first;
+#pragma unroll
+        for (int i = 0; i < FEW / THREADS; ++i) {
+            const int64_t r = (int64_t)seen[i] - first;
             if (r >= 0 && r < FEW_ROWS) hit |= 1u << r;
         }
         if (hit) atomicOr((unsigned long long *)&place[0], (unsigned long long)hit);
@@ -153,28 +161,47 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
     const uint32_t t = id / slabs;
     const int32_t token = ids[t];
     if (token < 0 || token >= a.vocab) return;
-    // where the token stands: a bit for each place from t on; nothing to do if it has been before
+    // where the token stands: a bit for each place; nothing to do if it has been before
     bool before = false;
-    for (uint32_t u = threadIdx.x; u < (tokens + 63 & ~63u); u += THREADS) {
-        const bool same = u < tokens && ids[u] == token;
+#pragma unroll
+    for (int i = 0; i < FEW / THREADS; ++i) {
+        const uint32_t u = i * THREADS + threadIdx.x;
+        const bool same = seen[i] == token;
         const uint64_t mask = __ballot(same);
         if ((threadIdx.x & 63) == 0) place[u / 64] = mask;
         before |= same && u < t;
     }
     if (__syncthreads_or(before)) return;
-    const int share = threadIdx.x / LANES;
-    const int64_t col = ((int64_t)(id % slabs) * LANES + threadIdx.x % LANES) * VALUES;
-    const T *dy = (const T *)a.y + blockIdx.z * a.sy + col;
-    float sum[VALUES] = {};
-    int turn = 0;
-    for (uint32_t w = t / 64; w < (tokens + 63) / 64; ++w)
-        for (uint64_t m = place[w]; m; m &= m - 1) {
-            if (turn == share && col < a.width) {
-                const Piece<T> x = load_piece(dy + (int64_t)(w * 64 + (uint32_t)__builtin_ctzll(m)) * a.ldy, a.width - col);
+    // its places in order: a lane of the first wave for each 64 of them
+    if (threadIdx.x < 64) {
+        uint64_t m = threadIdx.x < FEW / 64 ? place[threadIdx.x] : 0;
+        uint32_t upto = (uint32_t)__popcll(m);
 #pragma unroll
-                for (int e = 0; e < VALUES; ++e) sum[e] += x.get(e);
-            }
-            turn = turn + 1 == SHARES ? 0 : turn + 1;
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t v = __shfl_up(upto, d);
+            upto += (int)threadIdx.x >= d ? v : 0u;
+        }
+        if (threadIdx.x == 63) count = upto;
+        for (uint32_t at = upto - (uint32_t)__popcll(m); m; m &= m - 1) rows[at++] = (uint16_t)(threadIdx.x * 64 + (uint32_t)__builtin_ctzll(m));
+    }
+    __syncthreads();
+    const uint32_t share = threadIdx.x / LANES, all = count;
+    const int64_t col = ((int64_t)(id % slabs) * LANES + threadIdx.x % LANES) * VALUES;
+    const T *dy = (const T *)a.y + blockIdx.z * a.sy;
+    float sum[VALUES] = {};
+    if (col < a.width)
+        for (uint32_t k0 = share; k0 < all; k0 += SHARES * AHEAD) {
+            Piece<T> x[AHEAD];
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k)
+                if (k0 + k * SHARES < all) x[k] = fetch_piece(dy + (int64_t)rows[k0 + k * SHARES] * a.ldy, col, a.width);
+#pragma unroll
+            for (uint32_t k = 0; k < AHEAD; ++k)
+                if (k0 + k * SHARES < all) {
+                    settle_piece(x[k], col, a.width);
+#pragma unroll
+                    for (int e = 0; e < VALUES; ++e) sum[e] += x[k].get(e);
+                }
         }
     if constexpr (SHARES > 1) {
 #pragma unroll
@@ -193,7 +220,7 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
 // Tokens outside of the vocabulary count as token `vocab`, which comes last.  Two stable passes by the lower and the upper half of a token's bits (one where 11 bits
 // hold them all).  A pass is cut into tiles: a tile's workgroup counts its digits, and its first places come from the counts of all tiles.
 
-constexpr int MOST_TILES = 64, MOST_BINS = 2048, WAVES = THREADS / 64;
+constexpr int MOST_TILES = 64, MOST_BINS = 2048, WAVES = THREADS / 64, STEPS = 4;          // STEPS times 64 tokens of a wave are read at once
 
 struct Sorting {
     int64_t tokens, vocab, tile; int32_t tiles, bits, passes;                               // bits of a digit
@@ -235,6 +262,7 @@ template <bool SECOND> __global__ void __launch_bounds__(THREADS) embed_sort_ker
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) next[w][k] = 0;
     __syncthreads();
+#pragma unroll 4
     for (int64_t t = first + lane; t < end; t += 64) atomicAdd(&next[wave][key(t) >> shift & (bins - 1)], 1u);
     __syncthreads();
     // THREADS neighbours at a time: all tokens of smaller digits, and those of the same digit in tiles before
@@ -244,7 +272,7 @@ template <bool SECOND> __global__ void __launch_bounds__(THREADS) embed_sort_ker
         const int k = k0 + threadIdx.x;
         uint32_t all = 0, before = 0;
         if (k < bins)
-#pragma unroll 8
+#pragma unroll 32
             for (int i = 0; i < s.tiles; ++i) {
                 const uint32_t c = counts[(int64_t)i * bins + k];
                 all += c;
@@ -274,25 +302,48 @@ template <bool SECOND> __global__ void __launch_bounds__(THREADS) embed_sort_ker
             }
     }
     __syncthreads();
-    for (int64_t t0 = first; t0 < end; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const bool here = t < end;
-        const uint32_t token = here ? key(t) : 0u, from = SECOND ? (here ? s.place[0][row + t] : 0u) : (uint32_t)t, digit = token >> shift & (bins - 1);
-        uint64_t same = __ballot(here);
-        for (int i = 0; i < s.bits; ++i) {
-            const uint64_t ones = __ballot(digit >> i & 1);
-            same &= digit >> i & 1 ? ones : ~ones;
+    for (int64_t t0 = first; t0 < end; t0 += 64 * STEPS) {
+        uint32_t tokens[STEPS], places[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int64_t t = t0 + i * 64 + lane;
+            tokens[i] = t < end ? key(t) : 0u;
+            places[i] = SECOND ? (t < end ? s.place[0][row + t] : 0u) : (uint32_t)t;
         }
-        const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-        if (here) {
-            const uint32_t at = next[wave][digit] + rank;
-            s.token[SECOND][row + at] = token;
-            s.place[SECOND][row + at] = from;
-            if (!SECOND && s.passes == 2) atomicAdd(&s.counts[1][(b * s.tiles + at / (uint32_t)s.tile) * bins + (token >> s.bits)], 1u);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            if (t0 + i * 64 >= end) break;
+            const bool here = t0 + i * 64 + lane < end;
+            const uint32_t token = tokens[i], digit = token >> shift & (bins - 1);
+            uint64_t same = __ballot(here);
+            for (int j = 0; j < s.bits; ++j) {
+                const uint64_t ones = __ballot(digit >> j & 1);
+                same &= digit >> j & 1 ? ones : ~ones;
+            }
+            const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+            const uint32_t equal = (uint32_t)__popcll(same);
+            const uint32_t at = here ? next[wave][digit] + rank : 0u;
+            if (here) {
+                s.token[SECOND][row + at] = token;
+                s.place[SECOND][row + at] = places[i];
+            }
+            if (!SECOND && s.passes == 2) {        // the second pass's counts: one addition for all of a wave that have a token and a tile in common
+                const uint32_t tile = at / (uint32_t)s.tile, upper = token >> s.bits;
+                for (int j = 0; j < s.bits; ++j) {
+                    const uint64_t ones = __ballot(upper >> j & 1);
+                    same &= upper >> j & 1 ? ones : ~ones;
+                }
+                if (here) {
+                    const int first = __builtin_ctzll(same), last = 63 - __builtin_clzll(same);
+                    const bool together = __shfl(tile, first) == __shfl(tile, last);
+                    if (!together) atomicAdd(&s.counts[1][(b * s.tiles + tile) * bins + upper], 1u);
+                    else if (lane == first) atomicAdd(&s.counts[1][(b * s.tiles + tile) * bins + upper], (uint32_t)__popcll(same));
+                }
+            }
+            wave_order();
+            if (here && rank == 0) next[wave][digit] += equal;
+            wave_order();
         }
-        wave_order();
-        if (here && rank == 0) next[wave][digit] += (uint32_t)__popcll(same);
-        wave_order();
     }
 }
 
@@ -337,7 +388,7 @@ __global__ void __launch_bounds__(THREADS) embed_sum_kernel(EmbedArgs a, Sorted 
     const int g = threadIdx.x / LANES;
     const int64_t c = c0 + g, piece = (int64_t)(id % slabs) * LANES + threadIdx.x % LANES, col = piece * VALUES;
     if (c >= s.chunks || col >= a.width) return;
-    const T *dy = (const T *)a.y + blockIdx.z * a.sy + col;
+    const T *dy = (const T *)a.y + blockIdx.z * a.sy;
     const uint32_t vocab = (uint32_t)a.vocab;
     float sum[VALUES] = {};
     bool begun = token[g][0] != token[g][1];       // the token at hand began in this chunk
@@ -345,11 +396,12 @@ __global__ void __launch_bounds__(THREADS) embed_sum_kernel(EmbedArgs a, Sorted 
         Piece<T> x[DEEP];
 #pragma unroll
         for (int k = 0; k < DEEP; ++k)
-            if (token[g][1 + i0 + k] < vocab) x[k] = load_piece(dy + (int64_t)place[g][i0 + k] * a.ldy, a.width - col);
+            if (token[g][1 + i0 + k] < vocab) x[k] = fetch_piece(dy + (int64_t)place[g][i0 + k] * a.ldy, col, a.width);
 #pragma unroll
         for (int k = 0; k < DEEP; ++k) {
             const uint32_t here = token[g][1 + i0 + k], after = token[g][2 + i0 + k];
             if (here >= vocab) return;             // the last ones
+            settle_piece(x[k], col, a.width);
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) sum[e] += x[k].get(e);
             const bool last = here != after;
@@ -370,22 +422,17 @@ __global__ void __launch_bounds__(THREADS) embed_sum_kernel(EmbedArgs a, Sorted 
 
 // Tokens that begin in a chunk and go on behind it: their tail and the heads of the chunks that follow.
 constexpr int JOIN_LANES = 64, JOIN_SHARES = THREADS / JOIN_LANES;
-template <typename T> __global__ void __launch_bounds__(THREADS) embed_join_kernel(EmbedArgs a, Sorted s, uint32_t slabs)
+template <typename T> __device__ __forceinline__ void join_token(const EmbedArgs &a, const Sorted &s, int64_t c, uint32_t slab, float (*part)[JOIN_LANES * Piece<T>::VALUES])
 {
     constexpr int VALUES = Piece<T>::VALUES;
-    __shared__ float part[JOIN_SHARES][JOIN_LANES * VALUES];
-    const uint32_t id = workgroup();
-    const int64_t c = id / slabs, tokens = a.tokens, behind = (c + 1) * CHUNK;
-    if (behind >= tokens) return;
-    const uint32_t *token = s.token + blockIdx.z * tokens;
-    const uint32_t v = token[behind];
-    if (v >= (uint64_t)a.vocab || token[behind - 1] != v || (c > 0 && token[c * CHUNK - 1] == v)) return;
-    int64_t lo = behind, hi = tokens;              // the first token that is more than v
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (token[mid] <= v) lo = mid + 1; else hi = mid;
+    const uint32_t *token = s.token + blockIdx.z * a.tokens;
+    const uint32_t v = token[(c + 1) * CHUNK];
+    int64_t more = 0;                              // chunks behind this one that begin with it: a lane looks at each
+    for (uint64_t m = ~(uint64_t)0; m == ~(uint64_t)0; more += __popcll(m)) {
+        const int64_t k = c + 1 + more + (threadIdx.x & 63);
+        m = __ballot(k < s.chunks && token[k * CHUNK] == v);
     }
-    const int64_t last = (lo - 1) / CHUNK, piece = (int64_t)(id % slabs) * JOIN_LANES + threadIdx.x % JOIN_LANES, col = piece * VALUES;
+    const int64_t last = c + more, col = ((int64_t)slab * JOIN_LANES + threadIdx.x % JOIN_LANES) * VALUES;
     const int share = threadIdx.x / JOIN_LANES;
     const int64_t at = ((int64_t)blockIdx.z * s.chunks + c) * s.padded + col;
     float sum[VALUES] = {};
@@ -398,6 +445,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) embed_join_kern
 #pragma unroll
             for (int e = 0; e < VALUES; ++e) sum[e] += s.head[at + k * s.padded + e];
     }
+    __syncthreads();                               // the token before has been added up
 #pragma unroll
     for (int e = 0; e < VALUES; ++e) part[share][threadIdx.x % JOIN_LANES * VALUES + e] = sum[e];
     __syncthreads();
@@ -406,6 +454,22 @@ template <typename T> __global__ void __launch_bounds__(THREADS) embed_join_kern
 #pragma unroll
         for (int e = 0; e < VALUES; ++e) sum[e] += part[k][threadIdx.x * VALUES + e];
     leave_row(a, (T *)a.table + blockIdx.z * a.st + v * a.ldt, col, sum);
+}
+
+// A workgroup looks through JOIN_CHUNKS chunks, a lane for each.
+constexpr int JOIN_CHUNKS = 4;
+template <typename T> __global__ void __launch_bounds__(THREADS) embed_join_kernel(EmbedArgs a, Sorted s, uint32_t slabs)
+{
+    __shared__ float part[JOIN_SHARES][JOIN_LANES * Piece<T>::VALUES];
+    const uint32_t id = workgroup();
+    const int64_t first = (int64_t)(id / slabs) * JOIN_CHUNKS, c = first + (threadIdx.x & 63), behind = (c + 1) * CHUNK;
+    const uint32_t *token = s.token + blockIdx.z * a.tokens;
+    bool begins = false;
+    if ((threadIdx.x & 63) < JOIN_CHUNKS && behind < a.tokens) {
+        const uint32_t v = token[behind];
+        begins = v < (uint64_t)a.vocab && token[behind - 1] == v && (c == 0 || token[c * CHUNK - 1] != v);
+    }
+    for (uint64_t m = __ballot(begins); m; m &= m - 1) join_token<T>(a, s, first + __builtin_ctzll(m), id % slabs, part);
 }
 
 // ---- launches --------------------------------------------------------------------------------------------------------
@@ -474,7 +538,7 @@ template <typename T> static void embed_grad_of(hipStream_t s, const EmbedArgs &
         const int64_t sums = (plan.sorted.chunks + GROUPS - 1) / GROUPS * slabs, zeros = a.accumulate ? 0 : (a.vocab + MANY_ROWS - 1) / MANY_ROWS;
         embed_sum_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)slabs, (uint32_t)sums);
         const int64_t join = (pieces_of<T>(a.width) + JOIN_LANES - 1) / JOIN_LANES;
-        embed_join_kernel<T><<<grid_of(plan.sorted.chunks * join, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)join);
+        embed_join_kernel<T><<<grid_of((plan.sorted.chunks + JOIN_CHUNKS - 1) / JOIN_CHUNKS * join, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)join);
     });
 }
 

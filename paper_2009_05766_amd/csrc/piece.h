@@ -56,6 +56,21 @@ template <typename T> __device__ __forceinline__ Piece<T> load_piece(const T *p,
     }
     return x;
 }
+// The piece of a row of `cols` values from column col on (0 .. cols - 1).  One that ends behind the row is read as the row's last full piece and moved when it has come (settled), so that no
+// value is read by itself and no read waits for another.  Rows shorter than a piece are read by their values.
+template <typename T> __device__ __forceinline__ Piece<T> fetch_piece(const T *row, int64_t col, int64_t cols)
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    if (cols < VALUES) return load_piece(row + col, cols - col);
+    Piece<T> x;
+    x.v = *reinterpret_cast<const typename Piece<T>::Memory *>(row + (col <= cols - VALUES ? col : cols - VALUES));
+    return x;
+}
+template <typename T> __device__ __forceinline__ void settle_piece(Piece<T> &x, int64_t col, int64_t cols)
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    if (cols >= VALUES && col > cols - VALUES) shift_down(x, (int)(col - (cols - VALUES)));
+}
 template <typename T> __device__ __forceinline__ void store_piece(T *p, int64_t left, const Piece<T> &x)
 {
     constexpr int VALUES = Piece<T>::VALUES;
