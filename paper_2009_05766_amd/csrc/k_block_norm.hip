@@ -25,18 +25,27 @@ constexpr int THREADS = 256;
 struct Unit { float mean, rest, r; };              // N(v) = ((v - mean) - rest) r
 __device__ __forceinline__ float unit_of(const Unit &n, float v) { return ((v - n.mean) - n.rest) * n.r; }
 
+// act(q) and act'(q).  With w = exp(-|z|), 1 / (1 + exp(-z)) is d = 1 / (1 + w) or w d and its slope w d^2: nothing cancels far out.  tanh q is the same with z = 2 q: (1 - w) d, which cancels near 0,
+// where its series takes over (below 1/4 its next term is less than 2^-26 of it), and 4 w d^2.
 __device__ __forceinline__ void gate_of(int act, float q, float &value, float &slope)
 {
-    if (act == GATE_SIGMOID) {
-        value = sigmoid_of(q);
-        slope = value * sigmoid_of(-q);
-    } else if (act == GATE_TANH) {
-        value = tanhf(q);
-        slope = fabsf(q) < 1.0f ? 1.0f - value * value : 4.0f * sigmoid_of(2.0f * q) * sigmoid_of(-2.0f * q);      // far out 1 - tanh^2 cancels
-    } else {
+    if (act == GATE_NONE) {
         value = q;
         slope = 1.0f;
+        return;
     }
+    const float w = __builtin_amdgcn_exp2f(fabsf(q) * (act == GATE_TANH ? -2.88539008f : -1.44269504f)), d = __builtin_amdgcn_rcpf(1.0f + w);
+    slope = w * d * d;
+    if (act == GATE_SIGMOID) {
+        value = q < 0.0f ? w * d : d;
+        return;
+    }
+    slope *= 4.0f;
+    const float square = q * q;
+    float series = fmaf(square, 62.0f / 2835.0f, -17.0f / 315.0f);
+    series = fmaf(square, series, 2.0f / 15.0f);
+    series = fmaf(square, series, -1.0f / 3.0f);
+    value = fabsf(q) < 0.25f ? fmaf(q * square, series, q) : copysignf((1.0f - w) * d, q);
 }
 
 // scale times values or slopes of a piece of a gate.

@@ -5,7 +5,7 @@
 // Bound by memory: a row read and one written per token; dy read and the whole table written.  No atomics on values: every row of the table is summed by one place in
 // a fixed order, so that a gradient's bits do not change from run to run.
 //
-// Few tokens: a workgroup for each token looks through all of them and, if its token is the first of its kind, sums the rows of the others; one launch.
+// Few tokens: a wave or a workgroup for each token looks through all of them and, if its token is the first of its kind, sums the rows of the others; one launch.
 // Many tokens: they are sorted (stable, by two digits), the sorted ones are cut into chunks of equal length, so that a frequent token is no longer a chain than a rare
 // one, and tokens whose rows end in another chunk than they begin leave partial sums, which are joined in order.
 #include "embed.h"
@@ -127,7 +127,91 @@ template <typename T> __device__ __forceinline__ void zero_rows(const EmbedArgs 
 constexpr int FEW = 2048, FEW_ROWS = 16;           // tokens (64 words of 64 bits hold their places twice over); rows of the table that a workgroup looks whether to clear
 constexpr uint32_t AHEAD = 8;                      // rows that a lane has under way at once
 
-// LANES lanes for LANES pieces of a row; the other lanes of the workgroup take turns with them at the token's rows.
+// Clears rows of the table that no token has.
+template <typename T> __device__ __forceinline__ void clear_few(const EmbedArgs &a, const int32_t *ids, T *table, int64_t first)
+{
+    __shared__ uint32_t hits;
+    if (first >= a.vocab) return;
+    if (threadIdx.x == 0) hits = 0;
+    int32_t seen[FEW / THREADS];
+#pragma unroll
+    for (int i = 0; i < FEW / THREADS; ++i) seen[i] = i * THREADS + threadIdx.x < a.tokens ? ids[i * THREADS + threadIdx.x] : -1;
+    __syncthreads();
+    uint32_t hit = 0;
+#pragma unroll
+    for (int i = 0; i < FEW / THREADS; ++i) {
+        const int64_t r = (int64_t)seen[i] - first;
+        if (r >= 0 && r < FEW_ROWS) hit |= 1u << r;
+    }
+    if (hit) atomicOr(&hits, hit);
+    __syncthreads();
+    zero_rows(a, table, first, a.vocab - first < FEW_ROWS ? (int)(a.vocab - first) : FEW_ROWS, hits);
+}
+
+// The sum over `all` rows of dy of a piece from column col on: those of turn share, share + SHARES, ...
+template <typename T, int SHARES> __device__ __forceinline__ void sum_rows(const EmbedArgs &a, const T *dy, const uint16_t *rows, uint32_t all, uint32_t share, int64_t col, float (&sum)[Piece<T>::VALUES])
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    for (uint32_t k0 = share; k0 < all; k0 += SHARES * AHEAD) {
+        Piece<T> x[AHEAD];
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k)
+            if (k0 + k * SHARES < all) x[k] = fetch_piece(dy + (int64_t)rows[k0 + k * SHARES] * a.ldy, col, a.width);
+#pragma unroll
+        for (uint32_t k = 0; k < AHEAD; ++k)
+            if (k0 + k * SHARES < all) {
+                settle_piece(x[k], col, a.width);
+#pragma unroll
+                for (int e = 0; e < VALUES; ++e) sum[e] += x[k].get(e);
+            }
+    }
+}
+
+// Narrow rows: a wave for each token, LANES lanes for a row, the others take turns with them.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a, uint32_t sums)
+{
+    constexpr int VALUES = Piece<T>::VALUES, SHARES = 64 / LANES, ROUNDS = 8;
+    __shared__ uint16_t places[THREADS / 64][FEW];
+    const int32_t *ids = a.ids + blockIdx.z * a.s_ids;
+    T *table = (T *)a.table + blockIdx.z * a.st;
+    const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens, lane = threadIdx.x & 63;
+    if (id >= sums) {
+        clear_few(a, ids, table, (int64_t)(id - sums) * FEW_ROWS);
+        return;
+    }
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = id * (THREADS / 64) + wave;
+    if (t >= tokens) return;
+    const int32_t token = ids[t];
+    if (token < 0 || token >= a.vocab) return;
+    uint16_t *rows = places[wave];
+    uint32_t all = 0;
+    for (uint32_t u0 = 0; u0 < tokens; u0 += 64 * ROUNDS) {
+        int32_t seen[ROUNDS];
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) seen[i] = u0 + i * 64 + lane < tokens ? ids[u0 + i * 64 + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < ROUNDS; ++i) {
+            const uint32_t u = u0 + i * 64;
+            const bool same = seen[i] == token;
+            const uint64_t mask = __ballot(same);
+            if (mask != 0 && u + (uint32_t)__builtin_ctzll(mask) < t) return;              // it has been before
+            if (same) rows[all + __popcll(mask & (((uint64_t)1 << lane) - 1))] = (uint16_t)(u + lane);
+            all += (uint32_t)__popcll(mask);
+        }
+    }
+    wave_order();
+    const int64_t col = (int64_t)(lane % LANES) * VALUES;
+    float sum[VALUES] = {};
+    if (col < a.width) sum_rows<T, SHARES>(a, (const T *)a.y + blockIdx.z * a.sy, rows, all, lane / LANES, col, sum);
+#pragma unroll
+    for (int d = LANES; d < 64; d <<= 1)
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) sum[e] += __shfl_xor(sum[e], d);
+    if (lane < LANES && col < a.width) leave_row(a, table + token * a.ldt, col, sum);
+}
+
+// Others: a workgroup for each token and slab of LANES pieces, whose lanes take turns at the token's rows.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, uint32_t slabs, uint32_t sums)
 {
@@ -139,25 +223,13 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
     const int32_t *ids = a.ids + blockIdx.z * a.s_ids;
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens;
+    if (id >= sums) {
+        clear_few(a, ids, table, (int64_t)(id - sums) * FEW_ROWS);
+        return;
+    }
     int32_t seen[FEW / THREADS];                   // a share of the ids, all under way at once
 #pragma unroll
     for (int i = 0; i < FEW / THREADS; ++i) seen[i] = i * THREADS + threadIdx.x < tokens ? ids[i * THREADS + threadIdx.x] : -1;
-    if (id >= sums) {
-        const int64_t first = (int64_t)(id - sums) * FEW_ROWS;
-        if (first >= a.vocab) return;
-        if (threadIdx.x == 0) place[0] = 0;
-        __syncthreads();
-        uint32_t hit = 0;
-#pragma unroll
-        for (int i = 0; i < FEW / THREADS; ++i) {
-            const int64_t r = (int64_t)seen[i] - first;
-            if (r >= 0 && r < FEW_ROWS) hit |= 1u << r;
-        }
-        if (hit) atomicOr((unsigned long long *)&place[0], (unsigned long long)hit);
-        __syncthreads();
-        zero_rows(a, table, first, a.vocab - first < FEW_ROWS ? (int)(a.vocab - first) : FEW_ROWS, place[0]);
-        return;
-    }
     const uint32_t t = id / slabs;
     const int32_t token = ids[t];
     if (token < 0 || token >= a.vocab) return;
@@ -185,24 +257,10 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
         for (uint32_t at = upto - (uint32_t)__popcll(m); m; m &= m - 1) rows[at++] = (uint16_t)(threadIdx.x * 64 + (uint32_t)__builtin_ctzll(m));
     }
     __syncthreads();
-    const uint32_t share = threadIdx.x / LANES, all = count;
+    const uint32_t share = threadIdx.x / LANES;
     const int64_t col = ((int64_t)(id % slabs) * LANES + threadIdx.x % LANES) * VALUES;
-    const T *dy = (const T *)a.y + blockIdx.z * a.sy;
     float sum[VALUES] = {};
-    if (col < a.width)
-        for (uint32_t k0 = share; k0 < all; k0 += SHARES * AHEAD) {
-            Piece<T> x[AHEAD];
-#pragma unroll
-            for (uint32_t k = 0; k < AHEAD; ++k)
-                if (k0 + k * SHARES < all) x[k] = fetch_piece(dy + (int64_t)rows[k0 + k * SHARES] * a.ldy, col, a.width);
-#pragma unroll
-            for (uint32_t k = 0; k < AHEAD; ++k)
-                if (k0 + k * SHARES < all) {
-                    settle_piece(x[k], col, a.width);
-#pragma unroll
-                    for (int e = 0; e < VALUES; ++e) sum[e] += x[k].get(e);
-                }
-        }
+    if (col < a.width) sum_rows<T, SHARES>(a, (const T *)a.y + blockIdx.z * a.sy, rows, count, share, col, sum);
     if constexpr (SHARES > 1) {
 #pragma unroll
         for (int e = 0; e < VALUES; ++e) part[share][threadIdx.x % LANES * VALUES + e] = sum[e];
@@ -457,7 +515,7 @@ template <typename T> __device__ __forceinline__ void join_token(const EmbedArgs
 }
 
 // A workgroup looks through JOIN_CHUNKS chunks, a lane for each.
-constexpr int JOIN_CHUNKS = 4;
+constexpr int JOIN_CHUNKS = 2;
 template <typename T> __global__ void __launch_bounds__(THREADS) embed_join_kernel(EmbedArgs a, Sorted s, uint32_t slabs)
 {
     __shared__ float part[JOIN_SHARES][JOIN_LANES * Piece<T>::VALUES];
@@ -515,7 +573,9 @@ template <typename T, class Go> static void with_lanes(int64_t width, const Go &
 {
     const int64_t n = pieces_of<T>(width);
     if (n <= 8) go(std::integral_constant<int, 8>());
+    else if (n <= 16) go(std::integral_constant<int, 16>());
     else if (n <= 32) go(std::integral_constant<int, 32>());
+    else if (n <= 64) go(std::integral_constant<int, 64>());
     else if (n <= 128) go(std::integral_constant<int, 128>());
     else go(std::integral_constant<int, 256>());
 }
@@ -526,8 +586,14 @@ template <typename T> static void embed_grad_of(hipStream_t s, const EmbedArgs &
         constexpr int LANES = lanes(), GROUPS = THREADS / LANES;
         const int64_t slabs = (pieces_of<T>(a.width) + LANES - 1) / LANES;
         if (a.tokens <= FEW) {
-            const int64_t sums = a.tokens * slabs, zeros = a.accumulate ? 0 : (a.vocab + FEW_ROWS - 1) / FEW_ROWS;
-            if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, (uint32_t)sums);
+            const int64_t zeros = a.accumulate ? 0 : (a.vocab + FEW_ROWS - 1) / FEW_ROWS;
+            if constexpr (LANES <= 64) {
+                const int64_t sums = (a.tokens + THREADS / 64 - 1) / (THREADS / 64);
+                if (sums + zeros > 0) embed_grad_narrow_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)sums);
+            } else {
+                const int64_t sums = a.tokens * slabs;
+                if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, (uint32_t)sums);
+            }
             return;
         }
         const Plan plan(a, work);
