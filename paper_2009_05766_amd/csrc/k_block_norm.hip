@@ -207,14 +207,19 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_kerne
 
 // Sums over the rows, in order: dg1, db1, dg2, db2, dq.  A workgroup's rows leave their sums in its own row of partial sums [SUMS][padded].
 constexpr int SUMS = 5;
-struct Partials { float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS]; void *unwanted; int64_t bytes; };  // place: which of the rows that are there, -1: none
+struct Partials {
+    float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS];  // place: which of the rows that are there, -1: none
+    struct RowSums *rows;                          // [batch][rows], where the sums are taken by a kernel of their own
+    void *unwanted; int64_t bytes;                 // room for results that nobody wants; of the whole workspace
+};
+// What a row's gradients at one column need to know of all others.
+struct RowSums { Unit post, pre; float mean_e, mean_eh; };
 
 template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_kernel(NormArgs a, Partials to)
 {
     constexpr int VALUES = Piece<T>::VALUES;
     __shared__ double room[THREADS / 64][1];
     __shared__ float pair[THREADS / 64][2];
-    float *mine = to.p + (blockIdx.y * to.workgroups + blockIdx.x) * to.sums * to.padded;
     const float share = (float)a.share;
     for (int64_t t = blockIdx.x; t < a.rows; t += gridDim.x) {
         const RowAt<T> row(a, blockIdx.y, t);
@@ -243,6 +248,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
             sum_over(along, pair);
         }
         const float mean_e = a.layer ? along[0] * share : 0.0f, mean_eh = along[1] * share;
+        if (to.rows && threadIdx.x == 0) to.rows[blockIdx.y * a.rows + t] = RowSums{post, pre, mean_e, mean_eh};
         // D
         const auto reaches = [&](const Values<T> &at, int64_t col, float (&D)[VALUES], float (&d)[VALUES], float (&hn)[VALUES]) {
 #pragma unroll
@@ -285,7 +291,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
         for (int64_t col = (int64_t)threadIdx.x * VALUES; col < a.width; col += THREADS * VALUES) {
             const int64_t left = a.width - col;
             const Values<T> at(a, row, col, post);
-            float D[VALUES], d[VALUES], hn[VALUES], g[VALUES], v[VALUES], add[SUMS][VALUES];
+            float D[VALUES], d[VALUES], hn[VALUES], g[VALUES], v[VALUES], slopes[VALUES];
             reaches(at, col, D, d, hn);
             Piece<T> out;
 #pragma unroll
@@ -296,11 +302,7 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
 #pragma unroll
             for (int k = 0; k < VALUES; ++k) {
                 const float du = a.f_scale * at.q[k] * D[k];
-                add[0][k] = du * at.fn[k];
-                add[1][k] = du;
-                add[2][k] = d[k] * hn[k];
-                add[3][k] = d[k];
-                add[4][k] = a.f_scale * at.slope[k] * at.u[k] * D[k];
+                slopes[k] = a.f_scale * at.slope[k] * at.u[k] * D[k];
                 v[k] = a.post ? post.r * ((du * g[k] - mean_c) - at.fn[k] * mean_cf) : du;
             }
             if (df) {
@@ -308,17 +310,9 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_
                 store_piece(df + col, left, out);
             }
             if (dq) {
-                out.set(add[4]);
+                out.set(slopes);
                 store_piece(dq + col, left, out);
             }
-#pragma unroll
-            for (int s = 0; s < SUMS; ++s)
-                if (to.place[s] >= 0)
-#pragma unroll
-                    for (int k = 0; k < VALUES; ++k) {
-                        float *p = mine + to.place[s] * to.padded + col + k;
-                        *p = t == blockIdx.x ? add[s][k] : *p + add[s][k];
-                    }
         }
     }
 }
@@ -608,12 +602,12 @@ template <typename T, int PIECES> __device__ __forceinline__ void let_go(Piece<T
 // What a kernel holds in registers: operands and sums over the rows of a norm alone, of a block without biases, or of any block; of a block whose gate has rows of its own, or of others.
 enum Form : int { NORM_ALONE = 0, BLOCK_GAINS = 1, BLOCK_ALL = 2, GATED_GAINS = 3, GATED_ALL = 4 };
 
-template <typename T, int LANES, int PIECES, bool LAYER, int FORM>
+template <typename T, int LANES, int PIECES, bool LAYER, int FORM, bool HELD>
 __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a, Partials to)
 {
     constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES, MEANS = LAYER ? 2 : 1;
     constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS && FORM != GATED_GAINS, GATED = FORM == GATED_GAINS || FORM == GATED_ALL;
-    constexpr bool AHEAD = LANES < 1024 || !BLOCK || FORM == BLOCK_GAINS;                     // as far as registers go
+    constexpr bool AHEAD = LANES < 1024 || (PIECES == 1 && (!BLOCK || FORM == BLOCK_GAINS)) || (PIECES == 2 && !BLOCK);       // as far as registers go
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
     __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][MEANS];
     __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
@@ -681,6 +675,8 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
             }
         };
         float d[PIECES][VALUES];                   // h, hn, then D
+        Unit pre{};
+        float mean_e = 0.0f, mean_eh = 0.0f;
         if (a.pre) {
 #pragma unroll
             for (int k = 0; k < PIECES; ++k) {
@@ -693,7 +689,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                     for (int e = 0; e < VALUES; ++e) d[k][e] = fmaf(gate[k][e], u[e], d[k][e]);
                 }
             }
-            const Unit pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
+            pre = unit_held<T, LANES, PIECES, LAYER>(lane, [&](int k, float (&v)[VALUES]) {
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) v[e] = d[k][e];
             }, a.share, a.eps, room[2], room[3]);
@@ -706,8 +702,8 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                     const float v = row.dy[k].get(e);
                     w[e] = v * g2[k].get(e);
                     d[k][e] = unit_held_of<LAYER>(pre, d[k][e]);
-                    sums[2][k][e] = fmaf(v, d[k][e], sums[2][k][e]);
-                    if (BIASES) sums[3][k][e] += v;
+                    if (HELD) sums[2][k][e] = fmaf(v, d[k][e], sums[2][k][e]);
+                    if (HELD && BIASES) sums[3][k][e] += v;
                 }
                 lane.once(k, w);
 #pragma unroll
@@ -719,7 +715,8 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
             row_sum<LANES>(along, pairs[0]);
             let_go(row.dy);
             let_go(g2);
-            const float mean_eh = along[0] * share, mean_e = LAYER ? along[MEANS - 1] * share : 0.0f;
+            mean_eh = along[0] * share;
+            if (LAYER) mean_e = along[MEANS - 1] * share;
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
@@ -737,6 +734,13 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) d[k][e] = row.dh[k].get(e);
+        }
+        if (!HELD && to.rows && threadIdx.x % LANES == 0) {
+            RowSums &left = to.rows[blockIdx.y * a.rows + t];
+            left.post = post;
+            left.pre = pre;
+            left.mean_e = mean_e;
+            left.mean_eh = mean_eh;
         }
         Piece<T> out[PIECES];
 #pragma unroll
@@ -764,10 +768,10 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
                 }
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
-                    if (!GATED) sums[4][k][e] = fmaf(u[e], d[k][e], sums[4][k][e]);
+                    if (HELD && !GATED) sums[4][k][e] = fmaf(u[e], d[k][e], sums[4][k][e]);
                     const float du = gate[k][e] * d[k][e];
-                    if (BIASES) sums[1][k][e] += du;
-                    sums[0][k][e] = fmaf(du, fn[e], sums[0][k][e]);
+                    if (HELD && BIASES) sums[1][k][e] += du;
+                    if (HELD) sums[0][k][e] = fmaf(du, fn[e], sums[0][k][e]);
                     d[k][e] = u[e] = du * g1[k].get(e);             // c
                 }
                 lane.once(k, u);
@@ -793,6 +797,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
             lane.leave(a.df.p ? RowAt<T>::at(a.df, blockIdx.y, t) : unwanted, out);
         }
     }
+    if constexpr (!HELD) return;
     if constexpr (BLOCK && !GATED)                 // a gate that is the same for all rows has one slope, too
         if (to.place[4] >= 0) {
             Piece<T> q[PIECES];
@@ -841,6 +846,90 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
     }
 }
 
+// ---- sums over the rows by themselves ----------------------------------------------------------------------------------
+//
+// Rows that are too long for their lanes to hold sums as well: with the means of every row known, a thread goes down the rows with one piece of them.  The operands are read a second
+// time (3333 x 9000 bfloat16 725 us with sums that spilled out of the registers, 5000 x 6000 float 285).
+template <typename T, int FORM> __global__ void __launch_bounds__(THREADS) norm_columns_kernel(NormArgs a, Partials to)
+{
+    constexpr int VALUES = Piece<T>::VALUES;
+    constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS && FORM != GATED_GAINS, GATED = FORM == GATED_GAINS || FORM == GATED_ALL;
+    const int64_t col = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * VALUES;
+    if (col >= a.width) return;
+    const RowAt<T> vectors(a, blockIdx.z, 0);
+    const auto vector = [&](const T *p, float other, float (&v)[VALUES]) {
+        Piece<T> x;
+        if (p) {
+            x = fetch_piece(p, col, a.width);
+            settle_piece(x, col, a.width);
+        }
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) v[e] = p ? x.get(e) : other;
+    };
+    float g1[VALUES], b1[VALUES], g2[VALUES], q[VALUES], gate[VALUES], slope[VALUES];
+    vector(vectors.g2, 1.0f, g2);
+    if constexpr (BLOCK) {
+        vector(vectors.g1, 1.0f, g1);
+        if constexpr (BIASES) vector(vectors.b1, 0.0f, b1);
+        if constexpr (!GATED) {
+            vector(vectors.q, 1.0f, q);
+#pragma unroll
+            for (int e = 0; e < VALUES; ++e) gate_of(vectors.q ? a.act : GATE_NONE, q[e], gate[e], slope[e]);
+        }
+    }
+    float sums[SUMS][VALUES] = {};
+    const auto fetch = [&](const Span &s, int64_t t) {
+        Piece<T> x;
+        x.v = decltype(x.v){};
+        return s.p ? fetch_piece(RowAt<T>::at(s, blockIdx.z, t), col, a.width) : x;
+    };
+#pragma unroll 2
+    for (int64_t t = blockIdx.y; t < a.rows; t += gridDim.y) {
+        Piece<T> x = fetch(a.x, t), f, p, dy = fetch(a.dy, t), dh = fetch(a.dh, t);
+        if constexpr (BLOCK) f = fetch(a.f, t);
+        if constexpr (GATED) p = fetch(a.gate, t);
+        const RowSums row = to.rows[blockIdx.z * a.rows + t];
+        settle_piece(x, col, a.width);
+        settle_piece(dy, col, a.width);
+        settle_piece(dh, col, a.width);
+        if constexpr (BLOCK) settle_piece(f, col, a.width);
+        if constexpr (GATED) settle_piece(p, col, a.width);
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) {
+            float fn = 0.0f, u = 0.0f, h = a.x_scale * x.get(e), value = 0.0f, D = dh.get(e);
+            if constexpr (BLOCK) {
+                fn = a.post ? unit_of(row.post, f.get(e)) : f.get(e);
+                u = BIASES ? fmaf(fn, g1[e], b1[e]) : fn * g1[e];
+                if constexpr (GATED) gate_of(a.act, p.get(e), value, slope[e]);
+                else value = gate[e];
+                value *= a.f_scale;
+                h = fmaf(value, u, h);
+            }
+            if (a.pre) {
+                const float hn = unit_of(row.pre, h), v = dy.get(e);
+                D += row.pre.r * fmaf(-hn, row.mean_eh, v * g2[e] - row.mean_e);
+                sums[2][e] = fmaf(v, hn, sums[2][e]);
+                sums[3][e] += v;
+            }
+            if constexpr (BLOCK) {
+                const float du = value * D;
+                sums[0][e] = fmaf(du, fn, sums[0][e]);
+                sums[1][e] += du;
+                sums[4][e] = fmaf(u, D, sums[4][e]);
+            }
+        }
+    }
+    if constexpr (BLOCK && !GATED)
+#pragma unroll
+        for (int e = 0; e < VALUES; ++e) sums[4][e] *= a.f_scale * slope[e];
+    float *mine = to.p + (blockIdx.z * to.workgroups + blockIdx.y) * to.sums * to.padded + col;
+#pragma unroll
+    for (int s = 0; s < SUMS; ++s)
+        if (to.place[s] >= 0)
+#pragma unroll
+            for (int e = 0; e < VALUES; e += 4) *reinterpret_cast<f32x4 *>(mine + to.place[s] * to.padded + e) = f32x4{sums[s][e], sums[s][e + 1], sums[s][e + 2], sums[s][e + 3]};
+}
+
 // ---- launches --------------------------------------------------------------------------------------------------------
 
 template <typename T> static int64_t pieces_of(int64_t width) { return (width + Piece<T>::VALUES - 1) / Piece<T>::VALUES; }
@@ -862,19 +951,28 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
     else stream();
 }
 
-// Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes.
-template <class Go, class Long> static void with_row_grad(int64_t n, const Go &go, const Long &stream)
+// Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes.  Of longer rows the sums have a kernel of their own; float's still
+// fit with two pieces (3662 x 8192 with a gate for all rows 161 us, by two kernels 259; with a gate of rows and biases 282 and 360).
+template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
+template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
 {
+    const int64_t n = pieces_of<T>(a.width);
     if (n <= 1) stream();                          // rows of no more than a piece
-    else if (n <= 8) go(Held<8, 1>());
-    else if (n <= 16) go(Held<16, 1>());
-    else if (n <= 32) go(Held<32, 1>());
-    else if (n <= 64) go(Held<64, 1>());
-    else if (n <= 128) go(Held<128, 1>());
-    else if (n <= 256) go(Held<256, 1>());
-    else if (n <= 512) go(Held<512, 1>());
-    else if (n <= 1024) go(Held<1024, 1>());
-    else if (n <= 2048) go(Held<1024, 2>());
+    else if (n <= 8) go(HeldGrad<8, 1, true>());
+    else if (n <= 16) go(HeldGrad<16, 1, true>());
+    else if (n <= 32) go(HeldGrad<32, 1, true>());
+    else if (n <= 64) go(HeldGrad<64, 1, true>());
+    else if (n <= 128) go(HeldGrad<128, 1, true>());
+    else if (n <= 256) go(HeldGrad<256, 1, true>());
+    else if (n <= 512) go(HeldGrad<512, 1, true>());
+    else if (n <= 1024) go(HeldGrad<1024, 1, true>());
+    else if constexpr (sizeof(T) == 4) {
+        if (n <= 2048) go(HeldGrad<1024, 2, true>());
+        else if (n <= 4096) go(HeldGrad<1024, 4, false>());
+        else stream();
+    } else if (n <= 2048) {
+        go(HeldGrad<1024, 2, false>());
+    }
     else stream();
 }
 
@@ -897,44 +995,65 @@ void launch_block_norm(hipStream_t s, const NormArgs &a)
     else block_norm_of<float>(s, a);
 }
 
-static Partials partials_of(const NormArgs &a, void *work)
+// Whether rows are written over rows that are read.
+static bool in_place(const NormArgs &a)
 {
-    Partials to{};
+    for (const Span *o : {&a.dx, &a.df, &a.dgate})
+        for (const Span *i : {&a.dy, &a.dh, &a.x, &a.f, &a.gate})
+            if (o->p && o->p == i->p) return true;
+    return false;
+}
+
+struct GradPlan { Partials to; bool summed, twice; int64_t workgroups; };      // sums held by the rows' kernel; that one run twice; its workgroups for each of the batch
+
+template <typename T> static GradPlan grad_plan(const NormArgs &a, void *work)
+{
+    GradPlan plan{};
+    Partials &to = plan.to;
     const Span *const outs[SUMS] = {&a.dpost_gain, &a.dpost_bias, &a.dpre_gain, &a.dpre_bias, &a.dgate};
     for (int s = 0; s < SUMS; ++s) {
         const bool there = outs[s]->p && !(s == 4 && a.gate_rows);
         to.place[s] = there ? to.sums : -1;
         if (there) to.out[to.sums++] = *outs[s];
     }
-    to.p = (float *)work;
     to.padded = up_to(a.width, 8);
     int64_t rows = 1, threads = THREADS;           // rows of a workgroup at once
-    with_row_grad(a.bf16 ? pieces_of<uint16_t>(a.width) : pieces_of<float>(a.width), [&](auto held) {
+    with_row_grad<T>(a, [&](auto held) {
         threads = threads_of(decltype(held)::LANES);
         rows = threads / decltype(held)::LANES;
+        plan.summed = decltype(held)::SUMMED;
     }, []() { });
     // as many as the card holds at once, if each has two turns
     const int64_t places = 256 * (1024 / threads), most = a.batch * 8 < places ? places / a.batch : 8, turns = (a.rows + rows - 1) / rows, all = (turns + 1) / 2;
-    to.workgroups = all < most ? all : most;
-    // behind the sums, for results that nobody wants: a row for each of a workgroup's groups of lanes
-    const bool all_wanted = a.dx.p && (!a.f.p || a.df.p) && (!a.f.p || !a.gate_rows || !a.gate.p || a.dgate.p);
-    to.bytes = up_to(4 * a.batch * to.workgroups * to.sums * to.padded, 256);
-    to.unwanted = (char *)work + to.bytes;
-    if (!all_wanted) to.bytes += (a.bf16 ? 2 : 4) * a.batch * to.workgroups * rows * to.padded;
-    return to;
+    plan.workgroups = all < most ? all : most;
+    to.workgroups = plan.workgroups;
+    if (!plan.summed) {                            // eight workgroups of the columns' kernel on every compute unit
+        const int64_t slabs = (pieces_of<T>(a.width) + THREADS - 1) / THREADS, blocks = 2048 / (slabs * a.batch);
+        to.workgroups = blocks < 1 ? 1 : blocks < a.rows ? blocks : a.rows;
+    }
+    // the rows' kernel leaves the means for the columns' kernel, which needs the operands as they were
+    plan.twice = !plan.summed && to.sums > 0 && in_place(a);
+    const bool all_wanted = !plan.twice && a.dx.p && (!a.f.p || a.df.p) && (!a.f.p || !a.gate_rows || !a.gate.p || a.dgate.p);
+    char *at = (char *)work;
+    const auto take = [&](int64_t n) { char *p = at; at += up_to(n, 256); return p; };
+    to.p = (float *)take(4 * a.batch * to.workgroups * to.sums * to.padded);
+    to.rows = (RowSums *)take(!plan.summed && to.sums > 0 ? (int64_t)sizeof(RowSums) * a.batch * a.rows : 0);
+    to.unwanted = take(all_wanted ? 0 : (int64_t)sizeof(T) * a.batch * plan.workgroups * rows * to.padded);
+    if (plan.summed || to.sums == 0) to.rows = nullptr;
+    to.bytes = at - (char *)work;
+    return plan;
 }
 
 int64_t block_norm_grad_workspace(const NormArgs &a)
 {
     if (a.batch == 0) return 0;
-    return partials_of(a, nullptr).bytes;
+    return a.bf16 ? grad_plan<uint16_t>(a, nullptr).to.bytes : grad_plan<float>(a, nullptr).to.bytes;
 }
 
-template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
+// go(form): what kind of block it is.
+template <class Go> static void with_form(const NormArgs &a, const Partials &to, const Go &go)
 {
-    const dim3 grid((uint32_t)to.workgroups, (uint32_t)a.batch);
     const bool gated = a.gate_rows && a.gate.p, biases = a.post_bias.p || to.place[1] >= 0 || to.place[3] >= 0;
-    const auto go = [&](auto form) { norm_grad_kernel<T, LANES, PIECES, LAYER, form()><<<grid, threads_of(LANES), 0, s>>>(a, to); };
     if (!a.f.p) go(std::integral_constant<int, NORM_ALONE>());
     else if (gated && biases) go(std::integral_constant<int, GATED_ALL>());
     else if (gated) go(std::integral_constant<int, GATED_GAINS>());
@@ -942,24 +1061,47 @@ template <typename T, int LANES, int PIECES, bool LAYER> static void norm_grad_o
     else go(std::integral_constant<int, BLOCK_GAINS>());
 }
 
-template <typename T> static void block_norm_grad_of(hipStream_t s, const NormArgs &a, const Partials &to)
+template <typename T> static void launch_rows(hipStream_t s, const NormArgs &a, const GradPlan &plan)
 {
-    if (to.workgroups > 0) with_row_grad(pieces_of<T>(a.width), [&](auto held) {
+    if (plan.workgroups == 0) return;
+    const dim3 grid((uint32_t)plan.workgroups, (uint32_t)a.batch);
+    with_row_grad<T>(a, [&](auto held) {
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
-        if (a.layer) norm_grad_of<T, LANES, PIECES, true>(s, a, to);
-        else norm_grad_of<T, LANES, PIECES, false>(s, a, to);
+        constexpr bool SUMMED = decltype(held)::SUMMED;
+        with_form(a, plan.to, [&](auto form) {
+            if (a.layer) norm_grad_kernel<T, LANES, PIECES, true, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
+            else norm_grad_kernel<T, LANES, PIECES, false, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
+        });
     }, [&]() {
-        long_norm_grad_kernel<T><<<dim3((uint32_t)to.workgroups, (uint32_t)a.batch), THREADS, 0, s>>>(a, to);
+        long_norm_grad_kernel<T><<<grid, THREADS, 0, s>>>(a, plan.to);
     });
+}
+
+template <typename T> static void block_norm_grad_of(hipStream_t s, const NormArgs &a, void *work)
+{
+    const GradPlan plan = grad_plan<T>(a, work);
+    const Partials &to = plan.to;
+    if (plan.twice) {
+        NormArgs means = a;
+        means.dx.p = means.df.p = nullptr;
+        if (a.gate_rows) means.dgate.p = nullptr;
+        launch_rows<T>(s, means, plan);
+    } else {
+        launch_rows<T>(s, a, plan);
+    }
+    if (!plan.summed && to.sums > 0 && a.rows > 0) {
+        const dim3 grid((uint32_t)((pieces_of<T>(a.width) + THREADS - 1) / THREADS), (uint32_t)to.workgroups, (uint32_t)a.batch);
+        with_form(a, to, [&](auto form) { norm_columns_kernel<T, form()><<<grid, THREADS, 0, s>>>(a, to); });
+    }
     if (to.sums > 0) join_sums_kernel<T><<<dim3((uint32_t)((a.width + JOIN_COLUMNS - 1) / JOIN_COLUMNS), to.sums, (uint32_t)a.batch), JOIN_COLUMNS * JOIN_TURNS, 0, s>>>(a, to);
+    if (plan.twice) launch_rows<T>(s, a, plan);
 }
 
 void launch_block_norm_grad(hipStream_t s, const NormArgs &a, void *work)
 {
     if (a.batch == 0) return;
-    const Partials to = partials_of(a, work);
-    if (a.bf16) block_norm_grad_of<uint16_t>(s, a, to);
-    else block_norm_grad_of<float>(s, a, to);
+    if (a.bf16) block_norm_grad_of<uint16_t>(s, a, work);
+    else block_norm_grad_of<float>(s, a, work);
 }
 
 }  // namespace netmax

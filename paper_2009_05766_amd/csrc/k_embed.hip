@@ -124,28 +124,28 @@ template <typename T> __device__ __forceinline__ void zero_rows(const EmbedArgs 
 
 // ---- gradient for few tokens -------------------------------------------------------------------------------------------
 
-constexpr int FEW = 2048, FEW_ROWS = 16;           // tokens (64 words of 64 bits hold their places twice over); rows of the table that a workgroup looks whether to clear
-constexpr uint32_t AHEAD = 8;                      // rows that a lane has under way at once
+constexpr int FEW = 2048;                          // tokens
+constexpr uint32_t AHEAD = 16;                     // rows that a lane has under way at once
 
 // Clears rows of the table that no token has.
-template <typename T> __device__ __forceinline__ void clear_few(const EmbedArgs &a, const int32_t *ids, T *table, int64_t first)
+template <typename T> __device__ __forceinline__ void clear_few(const EmbedArgs &a, const int32_t *ids, T *table, int64_t first, int count)
 {
-    __shared__ uint32_t hits;
+    __shared__ unsigned long long hits;
     if (first >= a.vocab) return;
     if (threadIdx.x == 0) hits = 0;
     int32_t seen[FEW / THREADS];
 #pragma unroll
     for (int i = 0; i < FEW / THREADS; ++i) seen[i] = i * THREADS + threadIdx.x < a.tokens ? ids[i * THREADS + threadIdx.x] : -1;
     __syncthreads();
-    uint32_t hit = 0;
+    unsigned long long hit = 0;
 #pragma unroll
     for (int i = 0; i < FEW / THREADS; ++i) {
         const int64_t r = (int64_t)seen[i] - first;
-        if (r >= 0 && r < FEW_ROWS) hit |= 1u << r;
+        if (r >= 0 && r < count) hit |= 1ull << r;
     }
     if (hit) atomicOr(&hits, hit);
     __syncthreads();
-    zero_rows(a, table, first, a.vocab - first < FEW_ROWS ? (int)(a.vocab - first) : FEW_ROWS, hits);
+    zero_rows(a, table, first, a.vocab - first < count ? (int)(a.vocab - first) : count, hits);
 }
 
 // The sum over `all` rows of dy of a piece from column col on: those of turn share, share + SHARES, ...
@@ -169,7 +169,7 @@ template <typename T, int SHARES> __device__ __forceinline__ void sum_rows(const
 
 // Narrow rows: a wave for each token, LANES lanes for a row, the others take turns with them.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a, uint32_t sums)
+__global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a, uint32_t sums, int rows_to_clear)
 {
     constexpr int VALUES = Piece<T>::VALUES, SHARES = 64 / LANES, ROUNDS = 8;
     __shared__ uint16_t places[THREADS / 64][FEW];
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a,
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens, lane = threadIdx.x & 63;
     if (id >= sums) {
-        clear_few(a, ids, table, (int64_t)(id - sums) * FEW_ROWS);
+        clear_few(a, ids, table, (int64_t)(id - sums) * rows_to_clear, rows_to_clear);
         return;
     }
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = id * (THREADS / 64) + wave;
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a,
 
 // Others: a workgroup for each token and slab of LANES pieces, whose lanes take turns at the token's rows.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, uint32_t slabs, uint32_t sums)
+__global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, uint32_t slabs, uint32_t sums, int rows_to_clear)
 {
     constexpr int VALUES = Piece<T>::VALUES, SHARES = THREADS / LANES;
     __shared__ uint64_t place[FEW / 64];
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens;
     if (id >= sums) {
-        clear_few(a, ids, table, (int64_t)(id - sums) * FEW_ROWS);
+        clear_few(a, ids, table, (int64_t)(id - sums) * rows_to_clear, rows_to_clear);
         return;
     }
     int32_t seen[FEW / THREADS];                   // a share of the ids, all under way at once
@@ -586,13 +586,15 @@ template <typename T> static void embed_grad_of(hipStream_t s, const EmbedArgs &
         constexpr int LANES = lanes(), GROUPS = THREADS / LANES;
         const int64_t slabs = (pieces_of<T>(a.width) + LANES - 1) / LANES;
         if (a.tokens <= FEW) {
-            const int64_t zeros = a.accumulate ? 0 : (a.vocab + FEW_ROWS - 1) / FEW_ROWS;
+            // rows that a workgroup looks whether to clear: 64 while they are short
+            const int rows_to_clear = a.width * (int64_t)sizeof(T) <= 1024 ? 64 : 16;
+            const int64_t zeros = a.accumulate ? 0 : (a.vocab + rows_to_clear - 1) / rows_to_clear;
             if constexpr (LANES <= 64) {
                 const int64_t sums = (a.tokens + THREADS / 64 - 1) / (THREADS / 64);
-                if (sums + zeros > 0) embed_grad_narrow_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)sums);
+                if (sums + zeros > 0) embed_grad_narrow_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)sums, rows_to_clear);
             } else {
                 const int64_t sums = a.tokens * slabs;
-                if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, (uint32_t)sums);
+                if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, (uint32_t)sums, rows_to_clear);
             }
             return;
         }
