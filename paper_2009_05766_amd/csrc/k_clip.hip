@@ -169,9 +169,9 @@ template <bool DENSE> __global__ void __launch_bounds__(THREADS) scale_kernel(It
     }
 }
 
-// Models of few units: norm and scaling by one workgroup, whose every THREADS threads take units in turn, in one launch (a gradient of 256 values 10.4 -> 6.9 us).
+// Models of few units: norm and scaling by one workgroup, whose every THREADS threads take units in turn, in one launch (a gradient of 256 values 10.4 -> 6.7 us).
 constexpr int SMALL_THREADS = 1024;
-constexpr uint32_t SMALL_UNITS = 16;
+constexpr uint32_t SMALL_UNITS = 4;                // one for each THREADS threads (with 12, 90000 bfloat16 values in four padded tensors took 23 us, by two launches 11)
 template <bool DENSE> __global__ void __launch_bounds__(SMALL_THREADS) clip_small_kernel(Items<DENSE> items, int scale, float max_norm, float *norm)
 {
     __shared__ double room[SMALL_THREADS / 64][1];

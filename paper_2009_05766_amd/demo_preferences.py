@@ -2,11 +2,12 @@
 
 Each of M workers holds a model of the next token (embedding, a residual block d -> f -> d with GELU, projection onto the vocabulary) and its own data.  First
 the workers learn from pairs of sequences, one written by a hidden teacher and one at random (`netmax_preference_loss`); then they write sequences
-themselves and are rewarded for the teacher's choices (`netmax_policy_loss`, with a KL term to the model that the second phase began with).  The layers run as one batch over the
-workers (`netmax_linear`, `netmax_linear_grad`), weight matrices are updated by orthogonalised momentum (`netmax_orthogonalize`), and
-`netmax_mix` takes those updates as the gradient of a context without momentum.
+themselves and are rewarded for the teacher's choices (`netmax_policy_loss`, with a KL term to the model that the second phase began with).  Embeddings and layers run as one batch over the
+workers (`netmax_embed`, `netmax_linear` and their gradients), weight matrices are updated by orthogonalised momentum (`netmax_orthogonalize`), and
+`netmax_mix` takes those updates as the gradient of a context without momentum.  With --norms the residual block has norms before and after it and a gate for each channel
+(`netmax_block_norm`); with --clip every worker's gradients are scaled down to a largest norm (`netmax_clip_grads`).
 
-    python -m paper_2009_05766_amd.demo_preferences [--workers 8] [--steps 60]
+    python -m paper_2009_05766_amd.demo_preferences [--workers 8] [--steps 60] [--norms] [--clip 1.0]
 """
 from __future__ import annotations
 
@@ -22,69 +23,89 @@ PAIRS, LENGTH = 8, 24                                   # per worker: pairs of a
 LR, MU = 0.02, 0.9
 
 
-def _layout():
+MATRICES = ("embed", "w1", "w2", "out")
+NORMS = ("first_gain", "post_gain", "gate", "pre_gain")                     # gains of the norms before, after and behind the block; the block's gate
+
+
+def _layout(norms: bool):
     """Where each parameter lies in a worker's row: name -> (offset, shape)."""
     places, at = {}, 0
-    for name, shape in (("embed", (VOCAB, WIDTH)), ("w1", (WIDTH, HIDDEN)), ("b1", (HIDDEN,)), ("w2", (HIDDEN, WIDTH)), ("b2", (WIDTH,)), ("out", (WIDTH, VOCAB))):
+    for name, shape in (("embed", (VOCAB, WIDTH)), ("w1", (WIDTH, HIDDEN)), ("b1", (HIDDEN,)), ("w2", (HIDDEN, WIDTH)), ("b2", (WIDTH,)), ("out", (WIDTH, VOCAB)),
+                        *((n, (WIDTH,)) for n in NORMS if norms)):
         places[name] = (at, shape)
         at += int(np.prod(shape))
     return places, at
 
 
-PLACES, D = _layout()
-
-
-def cut(rows, name):
-    """A parameter of all workers as a view of their rows [M, D]."""
-    at, shape = PLACES[name]
-    return rows[:, at:at + int(np.prod(shape))].view(rows.shape[0], *shape)
-
-
 class Workers:
-    def __init__(self, M: int, seed: int = 0):
-        self.M = M
+    def __init__(self, M: int, seed: int = 0, norms: bool = False, clip: float = 0.0):
+        self.M, self.norms, self.clip = M, norms, clip
+        self.places, D = _layout(norms)
+        self.D = D
         self.g = torch.Generator(device="cuda").manual_seed(seed)
         x0 = torch.zeros(M, D, device="cuda")
         for name, scale in (("embed", 1.0), ("w1", WIDTH ** -0.5), ("w2", HIDDEN ** -0.5), ("out", 0.02)):
-            shape = PLACES[name][1]
-            cut(x0, name).copy_(torch.randn(shape, generator=self.g, device="cuda") * scale)        # the same start for all
+            shape = self.places[name][1]
+            self.cut(x0, name).copy_(torch.randn(shape, generator=self.g, device="cuda") * scale)   # the same start for all
+        for name in NORMS if norms else ():
+            self.cut(x0, name).fill_(1.0)
         P = (np.ones((M, M)) - np.eye(M)) / (M - 1)
         self.run = nm.NetMax(M=M, D=D, ld=-(-D // nm.NETMAX_TILE) * nm.NETMAX_TILE, model=nm.NETMAX_FLAT, lr=LR, momentum=0.0, rho=float(P.max()) / (4 * LR),
                              seed=seed, P=P)
         self.run.set("x", x0)
         self.params, self.grads, self.moments = x0, torch.zeros(M, D, device="cuda"), torch.zeros(M, D, device="cuda")
+        self.clipped = nm.Gradients([self.cut(self.grads, n) for n in self.places], batch=True)
         self.iteration = 0
+
+    def cut(self, rows, name):
+        """A parameter of all workers as a view of their rows [M, D]."""
+        at, shape = self.places[name]
+        return rows[:, at:at + int(np.prod(shape))].view(rows.shape[0], *shape)
 
     def forward(self, tokens):
         """Logits [M, T, VOCAB] of what follows each of tokens [M, T], and what the backward pass needs."""
-        p = self.params
-        e = cut(p, "embed").gather(1, tokens.long()[..., None].expand(-1, -1, WIDTH))
-        a, z = nm.netmax_linear(e, cut(p, "w1"), cut(p, "b1"), act="gelu", keep_preact=True)
-        h = nm.netmax_linear(a, cut(p, "w2"), cut(p, "b2"), e)                                      # onto the residual stream
-        return nm.netmax_linear(h, cut(p, "out")), (tokens, e, a, z, h)
+        p = lambda name: self.cut(self.params, name)  # noqa: E731
+        ids = tokens.to(torch.int32)
+        e = nm.netmax_embed(ids, p("embed"))
+        n = nm.netmax_block_norm(e, pre_gain=p("first_gain"))[1] if self.norms else e
+        a, z = nm.netmax_linear(n, p("w1"), p("b1"), act="gelu", keep_preact=True)
+        f = None
+        if self.norms:
+            f = nm.netmax_linear(a, p("w2"), p("b2"))
+            h = nm.netmax_block_norm(e, f, p("gate"), p("post_gain"), None, p("pre_gain"), need_h=False)[1]
+        else:
+            h = nm.netmax_linear(a, p("w2"), p("b2"), e)                                            # onto the residual stream
+        return nm.netmax_linear(h, p("out")), (ids, e, n, a, z, f, h)
 
     def backward(self, dlogits, kept):
         """Gradients of all parameters into the workers' rows."""
-        tokens, e, a, z, h = kept
-        p, g = self.params, self.grads
-        dh, _, _ = nm.netmax_linear_grad(dlogits, h, cut(p, "out"), dw=cut(g, "out"), need_bias=False)
-        da, _, _ = nm.netmax_linear_grad(dh, a, cut(p, "w2"), dw=cut(g, "w2"), db=cut(g, "b2"))
-        de, _, _ = nm.netmax_linear_grad(da, e, cut(p, "w1"), z, act="gelu", dw=cut(g, "w1"), db=cut(g, "b1"))
-        cut(g, "embed").zero_().scatter_add_(1, tokens.long()[..., None].expand(-1, -1, WIDTH), dh + de)
+        ids, e, n, a, z, f, h = kept
+        p, g = (lambda name: self.cut(self.params, name)), (lambda name: self.cut(self.grads, name))  # noqa: E731
+        dh, _, _ = nm.netmax_linear_grad(dlogits, h, p("out"), dw=g("out"), need_bias=False)
+        df = dh
+        if self.norms:
+            dh, df = nm.netmax_block_norm_grad(dh, None, e, f, p("gate"), p("post_gain"), None, p("pre_gain"), dgate=g("gate"), dpost_gain=g("post_gain"), dpre_gain=g("pre_gain"))[:2]
+        da, _, _ = nm.netmax_linear_grad(df, a, p("w2"), dw=g("w2"), db=g("b2"))
+        dn, _, _ = nm.netmax_linear_grad(da, n, p("w1"), z, act="gelu", dw=g("w1"), db=g("b1"))
+        de = nm.netmax_block_norm_grad(dn, dh, e, pre_gain=p("first_gain"), dpre_gain=g("first_gain")).dx if self.norms else dh + dn
+        nm.netmax_embed_grad(de, ids, dtable=g("embed"))
 
     def update(self):
-        """One NetMax iteration: orthogonalised momentum of the matrices, momentum of the biases, second step of the update with a drawn peer's copy."""
+        """One NetMax iteration: orthogonalised momentum of the matrices, momentum of the vectors, second step of the update with a drawn peer's copy."""
         g, m = self.grads, self.moments
-        for name in ("embed", "w1", "w2", "out"):
-            rows, cols = PLACES[name][1]
-            nm.netmax_orthogonalize(cut(g, name), cut(m, name), mu=MU, out=cut(g, name), scale=0.2 * max(rows, cols) ** 0.5)
-        for name in ("b1", "b2"):
-            g_, m_ = cut(g, name), cut(m, name)
-            g_.copy_(m_.mul_(MU).add_(g_))
+        if self.clip:
+            nm.netmax_clip_grads(self.clipped, self.clip)
+        for name in self.places:
+            g_, m_ = self.cut(g, name), self.cut(m, name)
+            if name in MATRICES:
+                rows, cols = self.places[name][1]
+                nm.netmax_orthogonalize(g_, m_, mu=MU, out=g_, scale=0.2 * max(rows, cols) ** 0.5)
+            else:
+                g_.copy_(m_.mul_(MU).add_(g_))
         self.run.sample_peers(self.iteration)
         self.run.set("g", g)
         self.run.mix(self.iteration)
-        self.params = self.run.get("x", D)
+        self.params = self.run.get("x", self.D)
         self.iteration += 1
 
 
@@ -144,8 +165,10 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--workers", type=int, default=8)
     ap.add_argument("--steps", type=int, default=60, help="iterations of each phase")
+    ap.add_argument("--norms", action="store_true", help="norms before and after the residual block, and a gate for each channel")
+    ap.add_argument("--clip", type=float, default=0.0, help="largest norm of a worker's gradients (0: any)")
     a = ap.parse_args(argv)
-    w, rules, seen = Workers(a.workers), teacher(), []
+    w, rules, seen = Workers(a.workers, norms=a.norms, clip=a.clip), teacher(), []
     for k in range(a.steps):
         seen.append(preference_step(w, rules))
         if k % 10 == 0 or k + 1 == a.steps:
