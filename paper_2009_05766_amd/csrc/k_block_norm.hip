@@ -407,12 +407,12 @@ template <typename T, int LANES> struct Lane {
     }
 };
 
-// 1 / sqrt(v), v > 0: the hardware's in float on a mantissa, one step of Newton's iteration, to 1.5 units in the last place.
+// 1 / sqrt(v), v > 0: the hardware's in float on a mantissa, one step of Newton's iteration, to 1.5 units in the last place; 0 for inf.
 __device__ __forceinline__ float inverse_root(double v)
 {
     const int twice = __builtin_amdgcn_frexp_exp(v) & ~1;
     const float m = (float)__builtin_amdgcn_ldexp(v, -twice), r = __builtin_amdgcn_rsqf(m);
-    return __builtin_amdgcn_ldexpf(fmaf(r * 0.5f, fmaf(-m * r, r, 1.0f), r), -twice / 2);
+    return __builtin_amdgcn_ldexpf(r > 0.0f ? fmaf(r * 0.5f, fmaf(-m * r, r, 1.0f), r) : r, -twice / 2);
 }
 
 // get(k, v): the values of the lane's piece k, of which lane.once() leaves those that count.
@@ -475,9 +475,9 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
 {
     constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES;
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
-    const int64_t t = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
-    if (GROUPS > 1 && t >= a.rows) return;                          // whole groups, and no barriers
-    const RowAt<T> row(a, blockIdx.y, t);
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * GROUPS + threadIdx.x / LANES;
+    if (t >= a.rows) return;                       // whole groups; with barriers a whole workgroup
+    const RowAt<T> row(a, blockIdx.z, t);
     const Lane<T, LANES> lane(a.width);
     const double share = a.share;
     Piece<T> x[PIECES], f[PIECES], q[PIECES], g1[PIECES], b1[PIECES], g2[PIECES], b2[PIECES];
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_kernel(NormArgs a)
             for (int e = 0; e < VALUES; ++e) h[k][e] = fmaf(gate[e], u[e], h[k][e]);
         }
     }
-    T *to_h = RowAt<T>::at(a.h, blockIdx.y, t), *to_y = RowAt<T>::at(a.y, blockIdx.y, t);
+    T *to_h = RowAt<T>::at(a.h, blockIdx.z, t), *to_y = RowAt<T>::at(a.y, blockIdx.z, t);
     if (to_h)
 #pragma unroll
         for (int k = 0; k < PIECES; ++k) lane.store(to_h, k, h[k]);
@@ -980,7 +980,9 @@ template <typename T> static void block_norm_of(hipStream_t s, const NormArgs &a
 {
     with_row(pieces_of<T>(a.width), [&](auto held) {
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES, GROUPS = threads_of(LANES) / LANES;
-        const dim3 grid((uint32_t)((a.rows + GROUPS - 1) / GROUPS), (uint32_t)a.batch);
+        // threads along a dimension of a launch have to be fewer than 2^32
+        const int64_t n = (a.rows + GROUPS - 1) / GROUPS, across = n < (1 << 20) ? n : 1 << 20;
+        const dim3 grid((uint32_t)across, (uint32_t)((n + across - 1) / across), (uint32_t)a.batch);
         if (a.layer) norm_kernel<T, LANES, PIECES, true><<<grid, threads_of(LANES), 0, s>>>(a);
         else norm_kernel<T, LANES, PIECES, false><<<grid, threads_of(LANES), 0, s>>>(a);
     }, [&]() {

@@ -385,6 +385,8 @@ def test_norm_rows_of_zeros_and_not_finite(dtype):
     for norm in ("rms", "layer"):
         y = nm.netmax_block_norm(x, norm=norm)[1]
         assert not bool(y[1].any()) and bool(y[3].isnan().any()) and bool(y[4].isnan().all()) and bool(y[[0, 2, 5]].isfinite().all())
+        if norm == "rms":                          # an infinite mean square leaves 0 of what is finite
+            assert bool(y[3, 7].isnan()) and not bool(y[3, :7].any()) and not bool(y[3, 8:].any())
     assert torch.equal(nm.netmax_block_norm(x)[1][[0, 2, 5]], clean[[0, 2, 5]])
     got = nm.netmax_block_norm_grad(torch.ones_like(x), None, x, pre_gain=torch.ones(200, device="cuda", dtype=dtype))
     assert bool(got.dx[[0, 1, 2, 5]].isfinite().all()) and bool(got.dx[4].isnan().all())
@@ -607,6 +609,18 @@ def test_many_rows_and_tokens():
     size = torch.zeros(50, 4, dtype=torch.float64, device="cuda").index_add_(0, tokens.clamp(min=0).long(), dy.double().abs())
     # chunks of 32, then 16000 partial sums of them in shares: far fewer than 2^14 roundings of each sum
     within(nm.netmax_embed_grad(dy, tokens, 50), want, 2.0 ** 14 * E * size, "dtable")
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """Rows that a workgroup each works on, more of them than threads along one dimension of a launch allow."""
+    n, width = 16_777_300, 1032
+    x = torch.empty(n, width, device="cuda", dtype=BF16)
+    parts = [slice(0, 3), slice((1 << 20) - 2, (1 << 20) + 2), slice((1 << 24) - 2, n)]
+    for p in parts:
+        x[p] = normal(gen(p.start), *x[p].shape, dtype=BF16)
+    y = nm.netmax_block_norm(x)[1]
+    for p in parts:
+        assert torch.equal(y[p], nm.netmax_block_norm(x[p].clone())[1])
 
 
 def everything(g):
