@@ -934,7 +934,8 @@ template <typename T, int FORM> __global__ void __launch_bounds__(THREADS) norm_
 
 template <typename T> static int64_t pieces_of(int64_t width) { return (width + Piece<T>::VALUES - 1) / Piece<T>::VALUES; }
 
-// Lanes and pieces for a row of n pieces; longer ones than any of them hold are streamed.
+// Lanes and pieces for a row of n pieces; longer ones than any of them hold are streamed.  Two pieces for a lane while a wave's registers allow it: what a row's sums cost is shared by more
+// values.  768 lanes: 6000 x 5000 float 103 us, with 1024 of them 150; 384 would be slower than 512 (6000 x 5000 bfloat16 60 us and 52).
 template <int LANES_, int PIECES_> struct Held { static constexpr int LANES = LANES_, PIECES = PIECES_; };
 template <class Go, class Long> static void with_row(int64_t n, const Go &go, const Long &stream)
 {
@@ -947,11 +948,13 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
     else if (n <= 256) go(Held<256, 1>());
     else if (n <= 512) go(Held<256, 2>());
     else if (n <= 1024) go(Held<512, 2>());
+    else if (n <= 1536) go(Held<768, 2>());
     else if (n <= 2048) go(Held<1024, 2>());
     else stream();
 }
 
-// Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes.  Of longer rows the sums have a kernel of their own; float's still
+// Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes, as few idle ones as whole waves allow (6000 x 5000 bfloat16 with a gate of rows: 181 us by 768
+// lanes, 233 by 1024; 20000 x 1500: 152 by 192, 165 by 256).  Of longer rows the sums have a kernel of their own; float's still
 // fit with two pieces (3662 x 8192 with a gate for all rows 161 us, by two kernels 259; with a gate of rows and biases 282 and 360).
 template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
 template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
@@ -963,8 +966,11 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
     else if (n <= 32) go(HeldGrad<32, 1, true>());
     else if (n <= 64) go(HeldGrad<64, 1, true>());
     else if (n <= 128) go(HeldGrad<128, 1, true>());
+    else if (n <= 192) go(HeldGrad<192, 1, true>());
     else if (n <= 256) go(HeldGrad<256, 1, true>());
+    else if (n <= 384) go(HeldGrad<384, 1, true>());
     else if (n <= 512) go(HeldGrad<512, 1, true>());
+    else if (n <= 768) go(HeldGrad<768, 1, true>());
     else if (n <= 1024) go(HeldGrad<1024, 1, true>());
     else if constexpr (sizeof(T) == 4) {
         if (n <= 2048) go(HeldGrad<1024, 2, true>());

@@ -71,16 +71,37 @@ template <typename T> __device__ __forceinline__ void settle_piece(Piece<T> &x, 
     constexpr int VALUES = Piece<T>::VALUES;
     if (cols >= VALUES && col > cols - VALUES) shift_down(x, (int)(col - (cols - VALUES)));
 }
+// A row's last values in as few writes as their number has bits.
+__device__ __forceinline__ void store_some(float *p, Piece<float> x, int left)
+{
+    typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+    if (left & 2) {
+        *reinterpret_cast<f32x2_any *>(p) = f32x2_any{x.v[0], x.v[1]};
+        p += 2;
+        x.v[0] = x.v[2];
+    }
+    if (left & 1) *p = x.v[0];
+}
+__device__ __forceinline__ void store_some(uint16_t *p, Piece<uint16_t> x, int left)
+{
+    typedef uint32_t u32_any __attribute__((aligned(2)));
+    if (left & 4) {
+        *reinterpret_cast<u32x2_any *>(p) = u32x2{x.v[0], x.v[1]};
+        p += 4;
+        x.v[0] = x.v[2];
+        x.v[1] = x.v[3];
+    }
+    if (left & 2) {
+        *reinterpret_cast<u32_any *>(p) = x.v[0];
+        p += 2;
+        x.v[0] = x.v[1];
+    }
+    if (left & 1) *p = (uint16_t)x.v[0];
+}
 template <typename T> __device__ __forceinline__ void store_piece(T *p, int64_t left, const Piece<T> &x)
 {
-    constexpr int VALUES = Piece<T>::VALUES;
-    if (left >= VALUES) {
-        *reinterpret_cast<typename Piece<T>::Memory *>(p) = x.v;
-    } else {
-#pragma unroll
-        for (int k = 0; k < VALUES; ++k)
-            if (k < left) store_value(p + k, x.get(k));
-    }
+    if (left >= Piece<T>::VALUES) *reinterpret_cast<typename Piece<T>::Memory *>(p) = x.v;
+    else store_some(p, x, (int)left);
 }
 
 // Sums over LANES neighbouring lanes (a power of two, 64 at most), each of which gets them: the lanes of a row of 16 exchange values on their way into the addition.
@@ -114,7 +135,7 @@ template <int LANES, typename S> __device__ __forceinline__ S lanes_sum(S v)
     return v;
 }
 
-// Sums over the LANES lanes that work on one row: part of a wave, or a workgroup of so many threads, through `room`, with one barrier; before a `room` is used again there is
+// Sums over the LANES lanes that work on one row: part of a wave, or a workgroup of so many threads (whole waves), through `room`, with one barrier; before a `room` is used again there is
 // another one (of another sum, or the caller's).
 template <int LANES, int N, typename S> __device__ __forceinline__ void row_sum(S (&v)[N], S (*room)[N])
 {
@@ -126,7 +147,12 @@ template <int LANES, int N, typename S> __device__ __forceinline__ void row_sum(
             for (int k = 0; k < N; ++k) room[threadIdx.x >> 6][k] = v[k];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = lanes_sum<LANES / 64>(room[threadIdx.x & (LANES / 64 - 1)][k]);
+        for (int k = 0; k < N; ++k) {
+            constexpr int WAVES = LANES / 64, EVEN = WAVES <= 2 ? 2 : WAVES <= 4 ? 4 : WAVES <= 8 ? 8 : 16;      // the power of two from there on
+            const int w = threadIdx.x & (EVEN - 1);
+            const S part = room[w < WAVES ? w : 0][k];
+            v[k] = lanes_sum<EVEN>(w < WAVES ? part : S(0));
+        }
     }
 }
 
