@@ -1,7 +1,8 @@
 // The calls of the operators around a language model's layers on torch's tensors, as an extension module of Python.
 //
-// Small calls are bound by what the host does before a kernel starts.  Reading sixteen tensors and filling a C structure took Python 40 us for the gradients of a block's norms, and 13 us
-// for its forward call; here it is 3 and 2.  The module checks tensors and allocates outputs and workspaces; everything else is checked by the C entry points, whose addresses it is given.
+// Small calls are bound by what the host does before a kernel starts.  Through ctypes the host took 40 us for the gradients of a block's norms (sixteen operands, two launches of 3.7 us each),
+// 17.5 for its forward call and 9.5 for a lookup; here 14, 5.9 and 4.3.  The module checks tensors and allocates outputs and workspaces; everything else is checked by the C entry points, whose
+// addresses it is given.
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
