@@ -956,6 +956,8 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
 // Gradients hold sums over the rows as well: one piece for a lane as long as there are lanes, as few idle ones as whole waves allow (6000 x 5000 bfloat16 with a gate of rows: 181 us by 768
 // lanes, 233 by 1024; 20000 x 1500: 152 by 192, 165 by 256).  Of longer rows the sums have a kernel of their own; float's still
 // fit with two pieces (3662 x 8192 with a gate for all rows 161 us, by two kernels 259; with a gate of rows and biases 282 and 360).
+// A norm alone has fewer sums, and two pieces for a lane pay where they keep the row in one wave (42857 x 700 bfloat16 49 us, one piece 74; 30000 x 1000 43 and 56) or in one kernel with
+// few idle lanes (3333 x 9000 bfloat16 65 us, by two kernels 101; 6000 x 5000 float 93, by 1024 lanes 101); between the two, one piece is as fast or faster (7324 x 4096 bfloat16 51 and 53).
 template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
 template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
 {
@@ -965,6 +967,7 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
     else if (n <= 16) go(HeldGrad<16, 1, true>());
     else if (n <= 32) go(HeldGrad<32, 1, true>());
     else if (n <= 64) go(HeldGrad<64, 1, true>());
+    else if (!a.f.p && n <= 128) go(HeldGrad<64, 2, true>());
     else if (n <= 128) go(HeldGrad<128, 1, true>());
     else if (n <= 192) go(HeldGrad<192, 1, true>());
     else if (n <= 256) go(HeldGrad<256, 1, true>());
@@ -972,6 +975,7 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
     else if (n <= 512) go(HeldGrad<512, 1, true>());
     else if (n <= 768) go(HeldGrad<768, 1, true>());
     else if (n <= 1024) go(HeldGrad<1024, 1, true>());
+    else if (!a.f.p && n <= 1536) go(HeldGrad<768, 2, true>());
     else if constexpr (sizeof(T) == 4) {
         if (n <= 2048) go(HeldGrad<1024, 2, true>());
         else if (n <= 4096) go(HeldGrad<1024, 4, false>());
@@ -1077,8 +1081,11 @@ template <typename T> static void launch_rows(hipStream_t s, const NormArgs &a, 
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
         constexpr bool SUMMED = decltype(held)::SUMMED;
         with_form(a, plan.to, [&](auto form) {
-            if (a.layer) norm_grad_kernel<T, LANES, PIECES, true, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
-            else norm_grad_kernel<T, LANES, PIECES, false, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
+            // two pieces with sums by fewer lanes are a norm's alone, and two waves with one a block's
+            if constexpr (form() == NORM_ALONE ? LANES != 128 : PIECES == 1 || !SUMMED || LANES == 1024) {
+                if (a.layer) norm_grad_kernel<T, LANES, PIECES, true, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
+                else norm_grad_kernel<T, LANES, PIECES, false, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
+            }
         });
     }, [&]() {
         long_norm_grad_kernel<T><<<grid, THREADS, 0, s>>>(a, plan.to);

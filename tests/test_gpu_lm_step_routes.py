@@ -11,7 +11,7 @@ FORMS = [dict(block=False), dict(gate="channel"), dict(gate="channel", bias=True
 
 @ops.BOTH
 @pytest.mark.parametrize("norm", ["rms", "layer"])
-@pytest.mark.parametrize("rows,width", [(60, 30), (35, 100), (70, 300), (9, 600), (11, 900), (8, 1400), (6, 1800), (7, 2500), (5, 3500), (5, 6000), (4, 7000), (3, 11000)])
+@pytest.mark.parametrize("rows,width", [(60, 30), (35, 100), (70, 300), (9, 600), (11, 900), (8, 1400), (6, 1800), (7, 2500), (5, 3500), (5, 6000), (4, 7000), (3, 11000), (3, 13000)])
 def test_norms(rows, width, norm, dtype):
     for k, form in enumerate(FORMS):
         ops.check_norm(rows, width, dtype, norm, seed=k + width, **form)
