@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
 {
     constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES, MEANS = LAYER ? 2 : 1;
     constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS && FORM != GATED_GAINS, GATED = FORM == GATED_GAINS || FORM == GATED_ALL;
-    constexpr bool AHEAD = LANES < 1024 || (PIECES == 1 && (!BLOCK || FORM == BLOCK_GAINS)) || (PIECES == 2 && !BLOCK);       // as far as registers go
+    constexpr bool AHEAD = LANES < 1024 ? PIECES == 1 || !GATED : PIECES == 1 ? !BLOCK || FORM == BLOCK_GAINS : PIECES == 2 && !BLOCK;      // as far as registers go
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
     __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][MEANS];
     __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
@@ -935,10 +935,12 @@ template <typename T, int FORM> __global__ void __launch_bounds__(THREADS) norm_
 template <typename T> static int64_t pieces_of(int64_t width) { return (width + Piece<T>::VALUES - 1) / Piece<T>::VALUES; }
 
 // Lanes and pieces for a row of n pieces; longer ones than any of them hold are streamed.  Two pieces for a lane while a wave's registers allow it: what a row's sums cost is shared by more
-// values.  768 lanes: 6000 x 5000 float 103 us, with 1024 of them 150; 384 would be slower than 512 (6000 x 5000 bfloat16 60 us and 52).
+// values.  768 lanes: 6000 x 5000 float 103 us, with 1024 of them 150; 384 would be slower than 512 (6000 x 5000 bfloat16 60 us and 52).  Three and four pieces of float against rows read
+// again: 2500 x 12000 113 us and 157, with a gate of rows and layer norms 168 and 280, a norm alone 55 and 72; 1831 x 16384 128 and 185, a norm alone 90 and 82.
 template <int LANES_, int PIECES_> struct Held { static constexpr int LANES = LANES_, PIECES = PIECES_; };
-template <class Go, class Long> static void with_row(int64_t n, const Go &go, const Long &stream)
+template <typename T, class Go, class Long> static void with_row(const NormArgs &a, const Go &go, const Long &stream)
 {
+    const int64_t n = pieces_of<T>(a.width);
     if (n <= 1) stream();                          // rows of no more than a piece
     else if (n <= 8) go(Held<8, 1>());
     else if (n <= 16) go(Held<16, 1>());
@@ -950,6 +952,11 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
     else if (n <= 1024) go(Held<512, 2>());
     else if (n <= 1536) go(Held<768, 2>());
     else if (n <= 2048) go(Held<1024, 2>());
+    else if constexpr (sizeof(T) == 4) {
+        if (n <= 3 * 1024) go(Held<1024, 3>());
+        else if (a.f.p && n <= 4096) go(Held<1024, 4>());
+        else stream();
+    }
     else stream();
 }
 
@@ -958,6 +965,8 @@ template <class Go, class Long> static void with_row(int64_t n, const Go &go, co
 // fit with two pieces (3662 x 8192 with a gate for all rows 161 us, by two kernels 259; with a gate of rows and biases 282 and 360).
 // A norm alone has fewer sums, and two pieces for a lane pay where they keep the row in one wave (42857 x 700 bfloat16 49 us, one piece 74; 30000 x 1000 43 and 56) or in one kernel with
 // few idle lanes (3333 x 9000 bfloat16 65 us, by two kernels 101; 6000 x 5000 float 93, by 1024 lanes 101); between the two, one piece is as fast or faster (7324 x 4096 bfloat16 51 and 53).
+// Without the sums, lanes that fill a row and hold it without spills: 3333 x 9000 float 283 us with three pieces and 411 with four (layer norms, a gate of rows and biases 441 and 661); bfloat16
+// 172 us by 768 lanes and 197 by 1024 (286 and 391).
 template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
 template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
 {
@@ -978,8 +987,11 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
     else if (!a.f.p && n <= 1536) go(HeldGrad<768, 2, true>());
     else if constexpr (sizeof(T) == 4) {
         if (n <= 2048) go(HeldGrad<1024, 2, true>());
+        else if (n <= 3 * 1024) go(HeldGrad<1024, 3, false>());
         else if (n <= 4096) go(HeldGrad<1024, 4, false>());
         else stream();
+    } else if (n <= 1536) {
+        go(HeldGrad<768, 2, false>());
     } else if (n <= 2048) {
         go(HeldGrad<1024, 2, false>());
     }
@@ -988,7 +1000,7 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
 
 template <typename T> static void block_norm_of(hipStream_t s, const NormArgs &a)
 {
-    with_row(pieces_of<T>(a.width), [&](auto held) {
+    with_row<T>(a, [&](auto held) {
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES, GROUPS = threads_of(LANES) / LANES;
         // threads along a dimension of a launch have to be fewer than 2^32
         const int64_t n = (a.rows + GROUPS - 1) / GROUPS, across = n < (1 << 20) ? n : 1 << 20;
@@ -1082,7 +1094,7 @@ template <typename T> static void launch_rows(hipStream_t s, const NormArgs &a, 
         constexpr bool SUMMED = decltype(held)::SUMMED;
         with_form(a, plan.to, [&](auto form) {
             // two pieces with sums by fewer lanes are a norm's alone, and two waves with one a block's
-            if constexpr (form() == NORM_ALONE ? LANES != 128 : PIECES == 1 || !SUMMED || LANES == 1024) {
+            if constexpr (form() == NORM_ALONE ? LANES != 128 && (LANES != 768 || PIECES == 1 || SUMMED) : PIECES == 1 || !SUMMED || LANES == 1024) {
                 if (a.layer) norm_grad_kernel<T, LANES, PIECES, true, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
                 else norm_grad_kernel<T, LANES, PIECES, false, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
             }
