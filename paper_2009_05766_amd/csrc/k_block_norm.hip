@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
 {
     constexpr int VALUES = Piece<T>::VALUES, GROUPS = threads_of(LANES) / LANES, MEANS = LAYER ? 2 : 1;
     constexpr bool BLOCK = FORM != NORM_ALONE, BIASES = FORM != BLOCK_GAINS && FORM != GATED_GAINS, GATED = FORM == GATED_GAINS || FORM == GATED_ALL;
-    constexpr bool AHEAD = LANES < 1024 ? PIECES == 1 || !GATED : PIECES == 1 ? !BLOCK || FORM == BLOCK_GAINS : PIECES == 2 && !BLOCK;      // as far as registers go
+    constexpr bool AHEAD = LANES < 1024 ? PIECES == 1 || !GATED : PIECES == 1 ? !BLOCK || FORM == BLOCK_GAINS : PIECES == 2 && !BLOCK && (sizeof(T) == 4 || !HELD);      // as far as registers go
     __shared__ double room[4][LANES > 64 ? LANES / 64 : 1][1];
     __shared__ float pairs[2][LANES > 64 ? LANES / 64 : 1][MEANS];
     __shared__ float shared_sums[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? LANES * PIECES * VALUES : 1];
@@ -966,7 +966,8 @@ template <typename T, class Go, class Long> static void with_row(const NormArgs 
 // A norm alone has fewer sums, and two pieces for a lane pay where they keep the row in one wave (42857 x 700 bfloat16 49 us, one piece 74; 30000 x 1000 43 and 56) or in one kernel with
 // few idle lanes (3333 x 9000 bfloat16 65 us, by two kernels 101; 6000 x 5000 float 93, by 1024 lanes 101); between the two, one piece is as fast or faster (7324 x 4096 bfloat16 51 and 53).
 // Without the sums, lanes that fill a row and hold it without spills: 3333 x 9000 float 283 us with three pieces and 411 with four (layer norms, a gate of rows and biases 441 and 661); bfloat16
-// 172 us by 768 lanes and 197 by 1024 (286 and 391).
+// 172 us by 768 lanes and 197 by 1024 (286 and 391).  A norm alone has room for its sums here too (3333 x 9000 float 105 us, without them 137; 1831 x 16384 bfloat16 69 and 80), but for
+// float in four pieces (2142 x 14000 165 us, without them 134).
 template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
 template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
 {
@@ -987,11 +988,14 @@ template <typename T, class Go, class Long> static void with_row_grad(const Norm
     else if (!a.f.p && n <= 1536) go(HeldGrad<768, 2, true>());
     else if constexpr (sizeof(T) == 4) {
         if (n <= 2048) go(HeldGrad<1024, 2, true>());
+        else if (!a.f.p && n <= 3 * 1024) go(HeldGrad<1024, 3, true>());
         else if (n <= 3 * 1024) go(HeldGrad<1024, 3, false>());
         else if (n <= 4096) go(HeldGrad<1024, 4, false>());
         else stream();
     } else if (n <= 1536) {
         go(HeldGrad<768, 2, false>());
+    } else if (!a.f.p && n <= 2048) {
+        go(HeldGrad<1024, 2, true>());
     } else if (n <= 2048) {
         go(HeldGrad<1024, 2, false>());
     }
@@ -1093,8 +1097,8 @@ template <typename T> static void launch_rows(hipStream_t s, const NormArgs &a, 
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
         constexpr bool SUMMED = decltype(held)::SUMMED;
         with_form(a, plan.to, [&](auto form) {
-            // two pieces with sums by fewer lanes are a norm's alone, and two waves with one a block's
-            if constexpr (form() == NORM_ALONE ? LANES != 128 && (LANES != 768 || PIECES == 1 || SUMMED) : PIECES == 1 || !SUMMED || LANES == 1024) {
+            // what with_row_grad asks for of a norm alone, and of a block
+            if constexpr (form() == NORM_ALONE ? LANES != 128 && (SUMMED || PIECES == 4) : PIECES == 1 || !SUMMED || (sizeof(T) == 4 && LANES == 1024 && PIECES == 2)) {
                 if (a.layer) norm_grad_kernel<T, LANES, PIECES, true, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
                 else norm_grad_kernel<T, LANES, PIECES, false, form(), SUMMED><<<grid, threads_of(LANES), 0, s>>>(a, plan.to);
             }
