@@ -22,7 +22,6 @@ constexpr int THREADS = 256;
 
 // ---- a row -----------------------------------------------------------------------------------------------------------
 
-struct Unit { float mean, rest, r; };              // N(v) = ((v - mean) - rest) r
 __device__ __forceinline__ float unit_of(const Unit &n, float v) { return ((v - n.mean) - n.rest) * n.r; }
 
 // act(q) and act'(q).  With w = exp(-|z|), 1 / (1 + exp(-z)) is d = 1 / (1 + w) or w d and its slope w d^2: nothing cancels far out.  tanh q is the same with z = 2 q: (1 - w) d, which cancels near 0,
@@ -204,16 +203,6 @@ template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_kerne
         }
     }
 }
-
-// Sums over the rows, in order: dg1, db1, dg2, db2, dq.  A workgroup's rows leave their sums in its own row of partial sums [SUMS][padded].
-constexpr int SUMS = 5;
-struct Partials {
-    float *p; int64_t padded, workgroups; int32_t place[SUMS]; int32_t sums; Span out[SUMS];  // place: which of the rows that are there, -1: none
-    struct RowSums *rows;                          // [batch][rows], where the sums are taken by a kernel of their own
-    void *unwanted; int64_t bytes;                 // room for results that nobody wants; of the whole workspace
-};
-// What a row's gradients at one column need to know of all others.
-struct RowSums { Unit post, pre; float mean_e, mean_eh; };
 
 template <typename T> __global__ void __launch_bounds__(THREADS) long_norm_grad_kernel(NormArgs a, Partials to)
 {
@@ -614,7 +603,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
     const Window<T, LANES, PIECES> lane(a.width);
     const float share = (float)a.share;
     const RowAt<T> vectors(a, blockIdx.y, 0);
-    T *const unwanted = (T *)to.unwanted + (blockIdx.y * to.workgroups + blockIdx.x) * GROUPS * to.padded + (threadIdx.x / LANES) * to.padded;
+    T *const unwanted = (T *)to.unwanted + to.unwanted_row(blockIdx.y, blockIdx.x, threadIdx.x / LANES, GROUPS);
     Piece<T> g1[PIECES], b1[PIECES], g2[PIECES];
     float gate[BLOCK ? PIECES : 1][VALUES];        // b act(q)
     lane.fetch_or(vectors.g2, g2, 1.0f);
@@ -1032,7 +1021,7 @@ static bool in_place(const NormArgs &a)
     return false;
 }
 
-struct GradPlan { Partials to; bool summed, twice; int64_t workgroups; };      // sums held by the rows' kernel; that one run twice; its workgroups for each of the batch
+struct GradPlan { Partials to; bool summed, twice; };               // sums held by the rows' kernel; that one run twice
 
 template <typename T> static GradPlan grad_plan(const NormArgs &a, void *work)
 {
@@ -1053,8 +1042,7 @@ template <typename T> static GradPlan grad_plan(const NormArgs &a, void *work)
     }, []() { });
     // as many as the card holds at once, if each has two turns
     const int64_t places = 256 * (1024 / threads), most = a.batch * 8 < places ? places / a.batch : 8, turns = (a.rows + rows - 1) / rows, all = (turns + 1) / 2;
-    plan.workgroups = all < most ? all : most;
-    to.workgroups = plan.workgroups;
+    to.workgroups = to.row_workgroups = all < most ? all : most;
     if (!plan.summed) {                            // eight workgroups of the columns' kernel on every compute unit
         const int64_t slabs = (pieces_of<T>(a.width) + THREADS - 1) / THREADS, blocks = 2048 / (slabs * a.batch);
         to.workgroups = blocks < 1 ? 1 : blocks < a.rows ? blocks : a.rows;
@@ -1066,7 +1054,7 @@ template <typename T> static GradPlan grad_plan(const NormArgs &a, void *work)
     const auto take = [&](int64_t n) { char *p = at; at += up_to(n, 256); return p; };
     to.p = (float *)take(4 * a.batch * to.workgroups * to.sums * to.padded);
     to.rows = (RowSums *)take(!plan.summed && to.sums > 0 ? (int64_t)sizeof(RowSums) * a.batch * a.rows : 0);
-    to.unwanted = take(all_wanted ? 0 : (int64_t)sizeof(T) * a.batch * plan.workgroups * rows * to.padded);
+    to.unwanted = take(all_wanted ? 0 : (int64_t)sizeof(T) * a.batch * to.row_workgroups * rows * to.padded);
     if (plan.summed || to.sums == 0) to.rows = nullptr;
     to.bytes = at - (char *)work;
     return plan;
@@ -1091,8 +1079,8 @@ template <class Go> static void with_form(const NormArgs &a, const Partials &to,
 
 template <typename T> static void launch_rows(hipStream_t s, const NormArgs &a, const GradPlan &plan)
 {
-    if (plan.workgroups == 0) return;
-    const dim3 grid((uint32_t)plan.workgroups, (uint32_t)a.batch);
+    if (plan.to.row_workgroups == 0) return;
+    const dim3 grid((uint32_t)plan.to.row_workgroups, (uint32_t)a.batch);
     with_row_grad<T>(a, [&](auto held) {
         constexpr int LANES = decltype(held)::LANES, PIECES = decltype(held)::PIECES;
         constexpr bool SUMMED = decltype(held)::SUMMED;

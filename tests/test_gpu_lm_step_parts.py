@@ -1,0 +1,51 @@
+"""Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
+their own.  (Where their kernels work is looked at without a GPU: test_lm_step_places.py.)"""
+import pytest
+import torch
+
+import paper_2009_05766_amd as nm
+import test_gpu_lm_step_ops as ops
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(3, 5, 40), (2, 33, 300), (2, 64, 700), (2, 20, 1500), (3, 7, 6000), (2, 10, 8200), (2, 64, 9000), (4, 64, 12000), (8, 20, 16384), (2, 6, 20000)]
+
+
+def operands(g, batch, rows, width, dtype, block=True, gate=None):
+    x, f, q, dy, dh = (ops.normal(g, batch, rows, width, dtype=dtype) for _ in range(5))
+    v = [ops.normal(g, batch, width, dtype=dtype, mean=1.0) for _ in range(5)]
+    if not block:
+        return dy, dh, [x, None, None, None, None, v[0], v[1]]
+    return dy, dh, [x, f, {"rows": q, "channel": v[4], None: None}[gate], v[0], v[1], v[2], v[3]]
+
+
+@ops.BOTH
+@pytest.mark.parametrize("batch,rows,width", SIZES)
+def test_some_results(batch, rows, width, dtype):
+    g = ops.gen(width)
+    for form in (dict(block=False), dict(gate="channel"), dict(gate="rows")):
+        dy, dh, t = operands(g, batch, rows, width, dtype, **form)
+        options = dict(norm="layer", gate_act="sigmoid")
+        want = nm.netmax_block_norm_grad(dy, dh, *t, **options)
+        same = lambda got, names: all((torch.equal(a, b) if n in names else a is None) for n, a, b in zip(want._fields, got, want) if b is not None)  # noqa: E731
+        of_rows = [n for n, w in want._asdict().items() if w is not None and w.dim() == 3]
+        others = [n for n, w in want._asdict().items() if w is not None and w.dim() == 2]
+        assert same(nm.netmax_block_norm_grad(dy, dh, *t, need_input=False, **options), others), form
+        assert same(nm.netmax_block_norm_grad(dy, dh, *t, need_params=False, **options), of_rows), form
+        for n in of_rows:
+            got = nm.netmax_block_norm_grad(dy, dh, *t, need_input=False, **options, **{n: torch.empty_like(dy)})
+            assert same(got, [n, *others]), (form, n)
+
+
+@ops.BOTH
+@pytest.mark.parametrize("batch,rows,width", SIZES)
+def test_results_over_what_is_read(batch, rows, width, dtype):
+    g = ops.gen(width + 1)
+    for gate in (None, "rows"):
+        dy, dh, t = operands(g, batch, rows, width, dtype, gate=gate)
+        want = nm.netmax_block_norm_grad(dy, dh, *t)
+        for order in (dict(dx=0, df=1), dict(dx=1, df=3), dict(dx=3), dict(df=2)):
+            c = [v if v is None else v.clone() for v in t]
+            rows_of = [dy.clone(), dh.clone(), *c[:3]]
+            got = nm.netmax_block_norm_grad(rows_of[0], rows_of[1], *c, **{n: rows_of[k] for n, k in order.items()})
+            assert all(torch.equal(a, b) for a, b in zip(got, want) if b is not None), (gate, order)
