@@ -131,7 +131,6 @@ constexpr uint32_t AHEAD = 16;                     // rows that a lane has under
 template <typename T> __device__ __forceinline__ void clear_few(const EmbedArgs &a, const int32_t *ids, T *table, int64_t first, int count)
 {
     __shared__ unsigned long long hits;
-    if (first >= a.vocab) return;
     if (threadIdx.x == 0) hits = 0;
     int32_t seen[FEW / THREADS];
 #pragma unroll
@@ -169,15 +168,15 @@ template <typename T, int SHARES> __device__ __forceinline__ void sum_rows(const
 
 // Narrow rows: a wave for each token, LANES lanes for a row, the others take turns with them.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a, uint32_t sums, int rows_to_clear)
+__global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a, GradTurns turns, int rows_to_clear)
 {
     constexpr int VALUES = Piece<T>::VALUES, SHARES = 64 / LANES, ROUNDS = 8;
     __shared__ uint16_t places[THREADS / 64][FEW];
     const int32_t *ids = a.ids + blockIdx.z * a.s_ids;
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens, lane = threadIdx.x & 63;
-    if (id >= sums) {
-        clear_few(a, ids, table, (int64_t)(id - sums) * rows_to_clear, rows_to_clear);
+    if (id >= turns.sums) {
+        if (turns.clears(id)) clear_few(a, ids, table, (int64_t)(id - turns.sums) * rows_to_clear, rows_to_clear);
         return;
     }
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = id * (THREADS / 64) + wave;
@@ -213,7 +212,7 @@ __global__ void __launch_bounds__(THREADS) embed_grad_narrow_kernel(EmbedArgs a,
 
 // Others: a workgroup for each token and slab of LANES pieces, whose lanes take turns at the token's rows.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, uint32_t slabs, uint32_t sums, int rows_to_clear)
+__global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, uint32_t slabs, GradTurns turns, int rows_to_clear)
 {
     constexpr int VALUES = Piece<T>::VALUES, SHARES = THREADS / LANES;
     __shared__ uint64_t place[FEW / 64];
@@ -223,8 +222,8 @@ __global__ void __launch_bounds__(THREADS) embed_grad_few_kernel(EmbedArgs a, ui
     const int32_t *ids = a.ids + blockIdx.z * a.s_ids;
     T *table = (T *)a.table + blockIdx.z * a.st;
     const uint32_t id = workgroup(), tokens = (uint32_t)a.tokens;
-    if (id >= sums) {
-        clear_few(a, ids, table, (int64_t)(id - sums) * rows_to_clear, rows_to_clear);
+    if (id >= turns.sums) {
+        if (turns.clears(id)) clear_few(a, ids, table, (int64_t)(id - turns.sums) * rows_to_clear, rows_to_clear);
         return;
     }
     int32_t seen[FEW / THREADS];                   // a share of the ids, all under way at once
@@ -416,16 +415,16 @@ struct Sorted {
 };
 
 template <typename T, int LANES>
-__global__ void __launch_bounds__(THREADS) embed_sum_kernel(EmbedArgs a, Sorted s, uint32_t slabs, uint32_t sums)
+__global__ void __launch_bounds__(THREADS) embed_sum_kernel(EmbedArgs a, Sorted s, uint32_t slabs, GradTurns turns)
 {
     constexpr int VALUES = Piece<T>::VALUES, GROUPS = THREADS / LANES, DEEP = 8;
     __shared__ uint32_t token[GROUPS][CHUNK + 2], place[GROUPS][CHUNK];
     const uint32_t id = workgroup();
     const int64_t tokens = a.tokens, row = blockIdx.z * tokens;
     T *table = (T *)a.table + blockIdx.z * a.st;
-    if (id >= sums) {
-        const int64_t first = (int64_t)(id - sums) * MANY_ROWS, v = first + (threadIdx.x & 63);
-        if (first >= a.vocab) return;
+    if (id >= turns.sums) {
+        if (!turns.clears(id)) return;
+        const int64_t first = (int64_t)(id - turns.sums) * MANY_ROWS, v = first + (threadIdx.x & 63);
         int64_t lo = 0, hi = tokens;               // the first token that is not less than v
         while (lo < hi) {
             const int64_t mid = (lo + hi) >> 1;
@@ -591,10 +590,10 @@ template <typename T> static void embed_grad_of(hipStream_t s, const EmbedArgs &
             const int64_t zeros = a.accumulate ? 0 : (a.vocab + rows_to_clear - 1) / rows_to_clear;
             if constexpr (LANES <= 64) {
                 const int64_t sums = (a.tokens + THREADS / 64 - 1) / (THREADS / 64);
-                if (sums + zeros > 0) embed_grad_narrow_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)sums, rows_to_clear);
+                if (sums + zeros > 0) embed_grad_narrow_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, GradTurns{(uint32_t)sums, (uint32_t)zeros}, rows_to_clear);
             } else {
                 const int64_t sums = a.tokens * slabs;
-                if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, (uint32_t)sums, rows_to_clear);
+                if (sums + zeros > 0) embed_grad_few_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, (uint32_t)slabs, GradTurns{(uint32_t)sums, (uint32_t)zeros}, rows_to_clear);
             }
             return;
         }
@@ -604,7 +603,7 @@ template <typename T> static void embed_grad_of(hipStream_t s, const EmbedArgs &
         embed_sort_kernel<false><<<tiles, THREADS, 0, s>>>(plan.sorting);
         if (plan.sorting.passes == 2) embed_sort_kernel<true><<<tiles, THREADS, 0, s>>>(plan.sorting);
         const int64_t sums = (plan.sorted.chunks + GROUPS - 1) / GROUPS * slabs, zeros = a.accumulate ? 0 : (a.vocab + MANY_ROWS - 1) / MANY_ROWS;
-        embed_sum_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)slabs, (uint32_t)sums);
+        embed_sum_kernel<T, LANES><<<grid_of(sums + zeros, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)slabs, GradTurns{(uint32_t)sums, (uint32_t)zeros});
         const int64_t join = (pieces_of<T>(a.width) + JOIN_LANES - 1) / JOIN_LANES;
         embed_join_kernel<T><<<grid_of((plan.sorted.chunks + JOIN_CHUNKS - 1) / JOIN_CHUNKS * join, a.batch), THREADS, 0, s>>>(a, plan.sorted, (uint32_t)join);
     });

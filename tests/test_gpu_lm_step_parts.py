@@ -1,4 +1,4 @@
-"""Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
+"""Results that a call leaves alone.  Rows of an embedding's gradient that are added to.  Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
 their own.  (Where their kernels work is looked at without a GPU: test_lm_step_places.py.)"""
 import pytest
 import torch
@@ -49,3 +49,17 @@ def test_results_over_what_is_read(batch, rows, width, dtype):
             rows_of = [dy.clone(), dh.clone(), *c[:3]]
             got = nm.netmax_block_norm_grad(rows_of[0], rows_of[1], *c, **{n: rows_of[k] for n, k in order.items()})
             assert all(torch.equal(a, b) for a, b in zip(got, want) if b is not None), (gate, order)
+
+
+def test_rows_of_other_tokens_are_kept_by_the_widest_calls():
+    """A launch of more workgroups than go along one dimension, to which its shape adds some: they clear nothing of what is added to, and what they should of what is not."""
+    n, vocab, width = 513, 12, (1 << 22) - 4
+    dy = torch.ones(n, width, device="cuda")
+    tokens = (torch.arange(n, device="cuda") % 3 * 4).to(torch.int32)                   # 0, 4 and 8, 171 times each
+    table = torch.full((vocab, width), 5.0, device="cuda")
+    nm.netmax_embed_grad(dy, tokens, accumulate=True, dtable=table)
+    want = torch.full((vocab,), 5.0, device="cuda")
+    want[::4] += 171.0
+    assert torch.equal(table, want[:, None].expand(vocab, width))
+    nm.netmax_embed_grad(dy, tokens, dtable=table)
+    assert torch.equal(table, (want - 5.0)[:, None].expand(vocab, width))

@@ -8,7 +8,7 @@ import pytest
 import paper_2009_05766_amd as nm
 from lm_calls import BF16, F32, ROOT
 from paper_2009_05766_amd.build import LIB, build
-from test_lm_step_routes import norm
+from test_lm_step_routes import embed, norm
 
 pytestmark = pytest.mark.skipif(shutil.which("g++") is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"), reason="needs g++ and the HIP headers")
 
@@ -33,7 +33,7 @@ def call(tmp_path_factory):
     return run
 
 
-WRONG = ("behind_the_workspace",)
+WRONG = ("behind_the_workspace", "clears_kept_rows", "clears_behind_the_table")
 
 
 def wrong(call, calls):
@@ -64,4 +64,15 @@ def test_gradients_of_norms_stay_in_their_workspace(call, dtype, batch):
                 calls.append(("norm_grad", dict(v, dx=v["x"])))
                 if "df" in v:
                     calls.append(("norm_grad", dict(v, dx=v["dh"], df=v["x"])))
+    assert wrong(call, calls) == []
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_of_embeddings_clear_what_they_may(call, dtype):
+    """Launches of more workgroups than go along one dimension are rounded up: what is added clears nothing."""
+    sizes = [(1, 10, 8), (300, 90, 100), (2048, 33, 2000), (2049, 17, 40), (5000, 6000, 100), (40000, 131072, 64)]
+    wide = ((1 << 22) - 4) // (1 + dtype)
+    sizes += [(513 * (1 + 3 * dtype), 20, wide), (2048, 20, wide), (2048, 60000, wide // 8), (1 << 24, 100, 16384), (1 << 25, 1000, 8200), (1 << 30, 5, 7)]
+    calls = [c for n, vocab, width in sizes for c in embed(n, vocab, width, dtype=dtype, table=1 << 47, y=1 << 48, work=1 << 49)]
+    assert all(launches for launches in call(*calls))
     assert wrong(call, calls) == []
