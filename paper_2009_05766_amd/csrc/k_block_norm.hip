@@ -14,6 +14,7 @@
 #include "block_norm.h"
 #include "piece.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace netmax {
@@ -1045,7 +1046,7 @@ template <typename T> static GradPlan grad_plan(const NormArgs &a, void *work)
     to.workgroups = to.row_workgroups = all < most ? all : most;
     if (!plan.summed) {                            // eight workgroups of the columns' kernel on every compute unit
         const int64_t slabs = (pieces_of<T>(a.width) + THREADS - 1) / THREADS, blocks = 2048 / (slabs * a.batch);
-        to.workgroups = blocks < 1 ? 1 : blocks < a.rows ? blocks : a.rows;
+        to.workgroups = std::min(std::max<int64_t>(blocks, 1), a.rows);
     }
     // the rows' kernel leaves the means for the columns' kernel, which needs the operands as they were
     plan.twice = !plan.summed && to.sums > 0 && in_place(a);

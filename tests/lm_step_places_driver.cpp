@@ -1,6 +1,7 @@
 // Where the kernels around a language model's layers work, by the arguments of their launches: lm_step_calls_driver.cpp, which sees each launch's arguments as well.
 // Behind a launch that would do something wrong comes what, in the form of a launch: name@amount.
 //   behind_the_workspace@bytes   a kernel's last row of partial sums, of means or of unwanted results ends so far behind the part of the workspace that it was given
+//   sums_of_no_rows@n            n partial sums are joined that no row has left
 //   clears_kept_rows@workgroups  so many workgroups of a gradient of an embedding that accumulates would clear rows
 //   clears_behind_the_table@row  a workgroup would clear rows from there on, which the table does not have
 #include <hip/hip_runtime.h>
@@ -36,6 +37,7 @@ static void look_at_norm(const std::string &name, dim3 grid, dim3 block, void **
     const int64_t partials = 4 * a.batch * to.workgroups * to.sums * to.padded;
     wrong("behind_the_workspace", start + partials - rows);
     if (to.rows) wrong("behind_the_workspace", (const char *)(to.rows + a.batch * a.rows) - (const char *)to.unwanted);
+    if (name.rfind("join_sums_kernel<", 0) == 0 && a.rows == 0) wrong("sums_of_no_rows", to.workgroups);
     if (name.rfind("norm_grad_kernel<", 0) != 0) return;
     const int64_t groups = block.x / std::stoi(argument(name, 1));
     const bool block_form = argument(name, 4) != "0", gated = argument(name, 4) >= "3";

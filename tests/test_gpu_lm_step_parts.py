@@ -1,4 +1,4 @@
-"""Results that a call leaves alone.  Rows of an embedding's gradient that are added to.  Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
+"""Sums over no rows.  Rows of an embedding's gradient that are added to.  Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
 their own.  (Where their kernels work is looked at without a GPU: test_lm_step_places.py.)"""
 import pytest
 import torch
@@ -63,3 +63,14 @@ def test_rows_of_other_tokens_are_kept_by_the_widest_calls():
     assert torch.equal(table, want[:, None].expand(vocab, width))
     nm.netmax_embed_grad(dy, tokens, dtable=table)
     assert torch.equal(table, (want - 5.0)[:, None].expand(vocab, width))
+
+
+@ops.BOTH
+@pytest.mark.parametrize("batch,width", [(300, 16384), (3000, 3), (5000, 8200), (2, 20000)])
+def test_sums_over_no_rows(batch, width, dtype):
+    x, v = torch.empty(batch, 0, width, device="cuda", dtype=dtype), torch.ones(batch, width, device="cuda", dtype=dtype)
+    for _ in range(2):
+        memory = torch.full((1 << 28,), float("nan"), device="cuda")                    # what workspaces may come from
+        del memory
+        got = nm.netmax_block_norm_grad(x, x, x, x, v, v, v, v, v)
+        assert all(t.shape == (batch, width) and not bool(t.any()) for t in got[2:])

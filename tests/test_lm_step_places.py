@@ -33,7 +33,7 @@ def call(tmp_path_factory):
     return run
 
 
-WRONG = ("behind_the_workspace", "clears_kept_rows", "clears_behind_the_table")
+WRONG = ("behind_the_workspace", "sums_of_no_rows", "clears_kept_rows", "clears_behind_the_table")
 
 
 def wrong(call, calls):
@@ -65,6 +65,12 @@ def test_gradients_of_norms_stay_in_their_workspace(call, dtype, batch):
                 if "df" in v:
                     calls.append(("norm_grad", dict(v, dx=v["dh"], df=v["x"])))
     assert wrong(call, calls) == []
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_of_no_rows_join_nothing(call, dtype):
+    calls = [norm(0, width, dtype, batch=batch, **form, **{n + ".s": width for n in ("dx", "df", "dgate")})[1] for batch in (1, 2, 300, 3000, 65535) for width in (3, 100, 5000, 9000, 16384, 40000) for form in FORMS]
+    assert wrong(call, calls) == [] and all(launches for launches in call(*calls))
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
