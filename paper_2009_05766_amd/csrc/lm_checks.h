@@ -36,7 +36,7 @@ inline bool strides_ok(int64_t batch, int64_t rows, int64_t cols, int64_t ld, in
     return (rows <= 1 || ld >= cols) && ld >= 0 && ld <= MOST && step >= 0 && step <= MOST && (rows == 0 || product_fits(rows, ld, 1)) && product_fits(batch, step, 1);
 }
 
-// `written`: results of a batch need memory of their own each.
+// `written`: results of a batch need memory of their own each, if there are any.
 inline int check_matrix(const char *name, const void *p, bool needed, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t step, bool written = false)
 {
     char buf[160];
@@ -46,7 +46,7 @@ inline int check_matrix(const char *name, const void *p, bool needed, int32_t dt
         return netmax_fail(NETMAX_EINVAL, buf);
     }
     if (aligned(p, dtype) && strides_ok(batch, rows, cols, ld, step) &&
-        !(written && batch > 1 && (step == 0 || batch_overlaps(Place(p, size_of(dtype), batch, rows, cols, ld, step))))) return NETMAX_OK;
+        !(written && batch > 1 && rows > 0 && cols > 0 && (step == 0 || batch_overlaps(Place(p, size_of(dtype), batch, rows, cols, ld, step))))) return NETMAX_OK;
     snprintf(buf, sizeof buf, "%s: misaligned, or rows closer together than they are long, or a negative stride, or results in the same place", name);
     return netmax_fail(NETMAX_EINVAL, buf);
 }

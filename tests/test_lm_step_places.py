@@ -73,6 +73,12 @@ def test_gradients_of_no_rows_join_nothing(call, dtype):
     assert wrong(call, calls) == [] and all(launches for launches in call(*calls))
 
 
+def test_results_without_rows_have_any_distance(call):
+    """Matrices of no rows lie 0 apart where they lie next to each other: they share no memory, and the sums over their rows are 0."""
+    calls = [norm(0, 40, batch=3, **form)[1] for form in FORMS]
+    assert all(c[1]["dx.s"] == 0 for c in calls) and all(launches for launches in call(*calls))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_gradients_of_embeddings_clear_what_they_may(call, dtype):
     """Launches of more workgroups than go along one dimension are rounded up: what is added clears nothing."""
