@@ -780,7 +780,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) norm_grad_kernel(NormArgs a
 #pragma unroll
                 for (int e = 0; e < VALUES; ++e) {
                     const float fn = unit_held_of<LAYER>(post, row.f[k].get(e));
-                    v[e] = post.r * fmaf(-fn, mean_cf, LAYER ? d[k][e] - mean_c : d[k][e]);
+                    v[e] = a.post ? post.r * fmaf(-fn, mean_cf, LAYER ? d[k][e] - mean_c : d[k][e]) : d[k][e];      // without a norm c itself, wherever f is infinite
                 }
                 out[k].set(v);
             }
