@@ -1,5 +1,4 @@
-"""Values at which the operators around a language model's layers went wrong once: infinities that nothing norms, products beside the middle of two bfloat16 values, outputs made in inference
-mode.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
+"""Values at which the operators around a language model's layers went wrong once: infinities that nothing norms, products beside the middle of two bfloat16 values.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
 import pytest
 import torch
 
@@ -26,3 +25,39 @@ def test_infinities_of_a_block_without_norms(width, gate, dtype):
         want = 1.5 * dh.double() * (1.0 if gates is None else gates.double())
         ops.within(got.df, want, (3 * E + ULP[dtype]) * want.abs() + 1e-37, f"df {norm}")
         ops.within(got.dx, 0.5 * dh.double(), (E + ULP[dtype]) * dh.double().abs(), f"dx {norm}")
+
+
+def nearest_bf16(v):
+    """Doubles rounded to bfloat16 once, ties to even, by their bits (no value here is subnormal or past the range)."""
+    bits = v.view(torch.int64)
+    return ((bits + (1 << 44) - 1 + (bits >> 45 & 1)) & -(1 << 45)).view(torch.float64)
+
+
+def test_clipping_rounds_bfloat16_once():
+    """g max / norm in double, rounded once: not to float, which may end in the middle of two bfloat16 values, before.  The values' squares have 14 bits behind the point and their
+    sum is exact, so that norm and factor are those of any order; 128 products for each of 40000 norms, one in 2^17 of which float would round to the wrong side."""
+    g = ops.gen(3)
+    t = (1.0 + torch.randint(0, 128, (40000, 512), generator=g, device="cuda") / 128.0).to(BF16)
+    norm = (t.double() ** 2).sum(1).sqrt()
+    want = nearest_bf16(t.double() * (float(torch.tensor(0.7, dtype=ops.F32)) / norm)[:, None])
+    through_float = (t.double() * (float(torch.tensor(0.7, dtype=ops.F32)) / norm)[:, None]).float().to(BF16)
+    assert int((through_float.double() != want).sum()) > 0          # such products are among them
+    nm.netmax_clip_grads([t], 0.7, batch=True)
+    assert torch.equal(t.double(), want)
+
+
+def test_clipping_rounds_bfloat16_at_the_ends_of_the_range():
+    """Subnormal results are rounded once, too, and what is past the range or no number stays what it is."""
+    t = torch.tensor([3.0 * 2.0 ** -133, 2.0 ** -133, 5.0 * 2.0 ** -133, 3.3895e38, -3.3895e38], device="cuda", dtype=BF16)
+    big = t.clone()
+    assert float(nm.netmax_clip_grads([big], 2.0 ** 127)) > 2.0 ** 127
+    factor = 2.0 ** 127 / float((t.double() ** 2).sum().sqrt())
+    ops.within(big, t.double() * factor, 2.0 ** -8 * t.double().abs() + 2.0 ** -134, "scaled")
+    whole = t.clone()
+    nm.netmax_clip_grads([whole], float("inf"), out=[out := torch.zeros_like(t)])
+    assert torch.equal(out, t)
+    odd = torch.tensor([float("nan"), 1.0, float("inf"), -float("inf")], device="cuda", dtype=BF16)
+    nm.netmax_clip_grads([odd[2:]], float("inf"), out=[out := torch.zeros(2, device="cuda", dtype=BF16)])
+    assert out.tolist() == [float("inf"), -float("inf")]
+    nm.netmax_clip_grads([odd[:2]], 1.0)
+    assert bool(odd[:2].isnan().all())
