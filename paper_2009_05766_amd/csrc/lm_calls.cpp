@@ -331,22 +331,36 @@ PyObject *block_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 // ---- clipping --------------------------------------------------------------------------------------------------------
 
-// tensors, outputs, their addresses as bytes; entries (address of netmax_gradient[]), models, whether there is a batch; max_norm or None
+// Whether a tensor lies as it did when its list was laid out, from `at` on: address, type, dimensions, sizes and strides.  What is behind is that of the next one.
+void check_laid_out(const at::Tensor &t, const int64_t *&at, const int64_t *end)
+{
+    constexpr const char *CHANGED = "a gradient has changed its sizes, strides or type since the list was laid out";
+    if (end - at < 3 || end - at - 3 < 2 * at[2]) refuse("a list of gradients that was not laid out");
+    if ((int64_t)t.data_ptr() != at[0]) refuse("a gradient has moved since the list was laid out");
+    const int64_t n = t.dim();
+    if ((t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) || dtype_of(t) != at[1] || n != at[2]) refuse("%s", CHANGED);
+    at += 3;
+    if (t.sizes() != at::IntArrayRef(at, n) || t.strides() != at::IntArrayRef(at + n, n)) refuse("%s", CHANGED);
+    at += 2 * n;
+}
+
+// tensors, outputs, how they lie as bytes; entries (address of netmax_gradient[]), models, whether there is a batch; max_norm or None
 PyObject *clip(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded(n, 7, [&] {
         if (!PyTuple_Check(a[0]) || !PyTuple_Check(a[1]) || !PyBytes_Check(a[2])) refuse("a list of gradients that was not laid out");
         const Py_ssize_t count = PyTuple_GET_SIZE(a[0]);
-        if (count < 1 || PyTuple_GET_SIZE(a[1]) != count || PyBytes_GET_SIZE(a[2]) != 2 * count * (Py_ssize_t)sizeof(void *)) refuse("a list of gradients that has changed since it was laid out");
-        const void *const *at = (const void *const *)PyBytes_AS_STRING(a[2]);
+        if (count < 1 || PyTuple_GET_SIZE(a[1]) != count) refuse("a list of gradients that has changed since it was laid out");
+        const int64_t *at = (const int64_t *)PyBytes_AS_STRING(a[2]), *const end = at + PyBytes_GET_SIZE(a[2]) / (Py_ssize_t)sizeof(int64_t);
         for (int side = 0; side < 2; ++side)
             for (Py_ssize_t k = 0; k < count; ++k) {
                 PyObject *o = PyTuple_GET_ITEM(a[side], k);
                 if (!THPVariable_Check(o)) refuse("a gradient must be a tensor");
                 const at::Tensor &t = THPVariable_Unpack(o);
-                if (t.data_ptr() != at[side * count + k]) refuse("a gradient has moved since the list was laid out");
+                check_laid_out(t, at, end);
                 no_graph("a gradient", t);
             }
+        if (at != end) refuse("a list of gradients that has changed since it was laid out");
         const at::Tensor &first = THPVariable_Unpack(PyTuple_GET_ITEM(a[0], 0));
         const netmax_gradient *entries = (const netmax_gradient *)PyLong_AsVoidPtr(a[3]);
         const int64_t models = whole(a[4]);

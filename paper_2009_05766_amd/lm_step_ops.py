@@ -7,7 +7,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
-import struct
+from array import array
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -87,12 +87,17 @@ def netmax_block_norm_grad(dy, dh, x, f=None, gate=None, post_gain=None, post_bi
 
 # ---- clipping ------------------------------------------------------------------------------------------------------------
 
+def _laid_out(tensors) -> bytes:
+    """Address, type, dimensions, sizes and strides of each tensor, for the extension module to compare with."""
+    return array("q", [n for t in tensors for n in (t.data_ptr(), _DTYPES[t.dtype], t.dim(), *t.shape, *t.stride())]).tobytes()
+
+
 class Gradients:
     """Where a model's gradients lie, for `netmax_grad_norm` and `netmax_clip_grads`: a program whose gradients stay in the same memory lays the list out once.
 
     tensors: float32 or bfloat16, of any shapes, rows at one distance, on one GPU; batch: their first dimension counts models (workers), which have a norm each.  out: where the scaled
-    gradients go, of the same shapes and types; None: in place.  The tensors are kept alive; one that is moved to other memory is noticed
-    and refused."""
+    gradients go, of the same shapes and types; None: in place.  The tensors are kept alive; one that has other memory, sizes, strides or
+    another type than when the list was laid out is refused."""
 
     def __init__(self, tensors: Sequence[torch.Tensor], *, out: Optional[Sequence[torch.Tensor]] = None, batch: bool = False):
         self.tensors = tuple(tensors)
@@ -116,7 +121,7 @@ class Gradients:
                     _refuse("an output must be a tensor of its gradient's shape and type")
             e.ldo, e.so = self._place(o, "an output")[2:]
             e.g, e.out, e.rows, e.cols, e.dtype = g.data_ptr(), o.data_ptr(), rows, cols, _DTYPES[g.dtype]
-        self._at = struct.pack(f"{2 * len(self.tensors)}P", *(t.data_ptr() for t in self.tensors), *(t.data_ptr() for t in self.out))
+        self._laid = _laid_out(self.tensors + self.out)
         self._entries_at = C.addressof(self.entries)
 
     def _place(self, t, name):
@@ -149,7 +154,7 @@ class Gradients:
         return rows, shape[-1], ld, step
 
     def _run(self, max_norm: Optional[float]):
-        return (_calls or _load_calls()).clip(self.tensors, self.out, self._at, self._entries_at, self.models, self.batch, max_norm)
+        return (_calls or _load_calls()).clip(self.tensors, self.out, self._laid, self._entries_at, self.models, self.batch, max_norm)
 
 
 def _gradients(gradients, out, batch) -> Gradients:

@@ -1,4 +1,4 @@
-"""Sums over no rows.  Rows of an embedding's gradient that are added to.  Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
+"""Lists of gradients whose tensors have changed.  Sums over no rows.  Rows of an embedding's gradient that are added to.  Gradients of a block's norms of which only some are wanted, or that are written over what is read, in batches of rows of every kind of kernel: the same bits as all of them in memory of
 their own.  (Where their kernels work is looked at without a GPU: test_lm_step_places.py.)"""
 import pytest
 import torch
@@ -74,3 +74,21 @@ def test_sums_over_no_rows(batch, width, dtype):
         del memory
         got = nm.netmax_block_norm_grad(x, x, x, x, v, v, v, v, v)
         assert all(t.shape == (batch, width) and not bool(t.any()) for t in got[2:])
+
+
+def test_a_list_whose_tensors_have_changed():
+    """Neither read nor written by the sizes that a tensor had, whichever of the two sides it is on; what has changed back, or only its values, is fine."""
+    g = ops.gen(2)
+    room, out = ops.normal(g, 50, 40), torch.full((50, 40), 5.0, device="cuda")
+    laid = nm.Gradients([room], out=[out])
+    want = nm.netmax_clip_grads(laid, 1.0)
+    for t in (room, out):
+        for change in (lambda: t.resize_(20, 40), lambda: t.resize_(40, 50), lambda: t.as_strided_((50, 30), (40, 1))):
+            change()
+            for call in (lambda: nm.netmax_grad_norm(laid), lambda: nm.netmax_clip_grads(laid, 1.0)):
+                with pytest.raises(nm.NetmaxError, match="has changed") as e:
+                    call()
+                assert e.value.code == nm.NETMAX_EINVAL
+            t.as_strided_((50, 40), (40, 1))
+    room.mul_(2.0)
+    assert torch.equal(nm.netmax_clip_grads(laid, 1.0), 2 * want) and float(nm.netmax_grad_norm([out])) == pytest.approx(1.0, rel=1e-5)
