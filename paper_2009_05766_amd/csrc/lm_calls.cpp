@@ -85,9 +85,10 @@ const at::Tensor &checked(const char *name, PyObject *o, const at::Tensor &like,
     return t;
 }
 
+// Tensors made in inference mode have no version.
 void changed(PyObject *o)
 {
-    if (o && o != Py_None) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+    if (o && o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
 }
 
 int64_t row_distance(const at::Tensor &t) { return t.stride(t.dim() - 2); }

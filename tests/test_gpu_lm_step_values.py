@@ -1,4 +1,5 @@
-"""Values at which the operators around a language model's layers went wrong once: infinities that nothing norms, products beside the middle of two bfloat16 values.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
+"""Values at which the operators around a language model's layers went wrong once: infinities that nothing norms, products beside the middle of two bfloat16 values, outputs made in inference
+mode.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
 import pytest
 import torch
 
@@ -61,3 +62,24 @@ def test_clipping_rounds_bfloat16_at_the_ends_of_the_range():
     assert out.tolist() == [float("inf"), -float("inf")]
     nm.netmax_clip_grads([odd[:2]], 1.0)
     assert bool(odd[:2].isnan().all())
+
+
+def test_outputs_made_in_inference_mode():
+    """They have no count of changes to raise; a call writes them as any other memory."""
+    x, v, tokens = torch.ones(4, 8, device="cuda"), torch.ones(8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    with torch.inference_mode():
+        rows = [torch.full((4, 8), 5.0, device="cuda") for _ in range(8)]
+        vectors = [torch.full((8,), 5.0, device="cuda") for _ in range(4)]
+        w = torch.ones(8, 8, device="cuda")
+    assert nm.netmax_linear(x, w, y=rows[0]) is rows[0] and bool((rows[0] == 8).all())
+    assert nm.netmax_embed(tokens, x, scale=2.0, y=rows[0]) is rows[0] and bool((rows[0] == 2).all())
+    assert nm.netmax_embed_grad(x, tokens, dtable=rows[1]) is rows[1] and bool((rows[1][0] == 4).all()) and not bool(rows[1][1:].any())
+    h, y = nm.netmax_block_norm(x, x, h=rows[2], y=rows[3], post=False)
+    assert h is rows[2] and y is rows[3] and bool((h == 2).all()) and bool((y - 1 < 1e-6).all())
+    got = nm.netmax_block_norm_grad(x, x, x, x, x, v, v, v, v, dx=rows[4], df=rows[5], dgate=rows[6], dpost_gain=vectors[0], dpost_bias=vectors[1], dpre_gain=vectors[2], dpre_bias=vectors[3])
+    assert all(a is b for a, b in zip(got, rows[4:7] + vectors)) and not bool(got.dx.eq(5).any())
+    # the root of 32 is no float: rounded once, by at most 2^-24 of itself; the largest norm here is 1/16 of that float, exactly, the factor 1/16 to 2^-24 and its product with 1 rounded once more
+    norm = float(nm.netmax_clip_grads([x], float(torch.tensor(32.0).sqrt()) / 16, out=[rows[7]]))
+    assert norm == pytest.approx(32 ** 0.5, rel=E) and bool(((rows[7] * 16 - 1).abs() <= 2.5 * E).all())
+    with torch.inference_mode():
+        nm.netmax_clip_grads([rows[7]], 1.0)
