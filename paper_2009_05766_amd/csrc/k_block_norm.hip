@@ -927,11 +927,13 @@ template <typename T> static int64_t pieces_of(int64_t width) { return (width + 
 // Lanes and pieces for a row of n pieces; longer ones than any of them hold are streamed.  Two pieces for a lane while a wave's registers allow it: what a row's sums cost is shared by more
 // values.  768 lanes: 6000 x 5000 float 103 us, with 1024 of them 150; 384 would be slower than 512 (6000 x 5000 bfloat16 60 us and 52).  Three and four pieces of float against rows read
 // again: 2500 x 12000 113 us and 157, with a gate of rows and layer norms 168 and 280, a norm alone 55 and 72; 1831 x 16384 128 and 185, a norm alone 90 and 82.
+// Rows of no more than a piece (4 float or 8 bfloat16 values) are too short to be read in whole pieces from their ends: they are streamed, by one thread of a workgroup, and slow where there are
+// many (1000000 x 8 of a norm alone: bfloat16 1585 us and 3893 for the gradients, float, two pieces, 37 and 37; 1000 x 8 4.5 and 3.8 us, gradients 18 and 9.8).
 template <int LANES_, int PIECES_> struct Held { static constexpr int LANES = LANES_, PIECES = PIECES_; };
 template <typename T, class Go, class Long> static void with_row(const NormArgs &a, const Go &go, const Long &stream)
 {
     const int64_t n = pieces_of<T>(a.width);
-    if (n <= 1) stream();                          // rows of no more than a piece
+    if (n <= 1) stream();
     else if (n <= 8) go(Held<8, 1>());
     else if (n <= 16) go(Held<16, 1>());
     else if (n <= 32) go(Held<32, 1>());
@@ -955,14 +957,14 @@ template <typename T, class Go, class Long> static void with_row(const NormArgs 
 // fit with two pieces (3662 x 8192 with a gate for all rows 161 us, by two kernels 259; with a gate of rows and biases 282 and 360).
 // A norm alone has fewer sums, and two pieces for a lane pay where they keep the row in one wave (42857 x 700 bfloat16 49 us, one piece 74; 30000 x 1000 43 and 56) or in one kernel with
 // few idle lanes (3333 x 9000 bfloat16 65 us, by two kernels 101; 6000 x 5000 float 93, by 1024 lanes 101); between the two, one piece is as fast or faster (7324 x 4096 bfloat16 51 and 53).
-// Without the sums, lanes that fill a row and hold it without spills: 3333 x 9000 float 283 us with three pieces and 411 with four (layer norms, a gate of rows and biases 441 and 661); bfloat16
-// 172 us by 768 lanes and 197 by 1024 (286 and 391).  A norm alone has room for its sums here too (3333 x 9000 float 105 us, without them 137; 1831 x 16384 bfloat16 69 and 80), but for
-// float in four pieces (2142 x 14000 165 us, without them 134).
+// Without the sums, lanes that fill a row: 3333 x 9000 float 283 us with three pieces (2 to 17 registers spilled) and 411 with four (27 to 131 spilled; layer norms, a gate of rows and biases 441
+// and 661); bfloat16 172 us by 768 lanes (none spilled) and 197 by 1024 (286 and 391).  A norm alone has room for its sums here too (3333 x 9000 float 105 us, without them 137; 1831 x 16384
+// bfloat16 69 and 80), but for float in four pieces (2142 x 14000 165 us, without them 134).  With sums, float rows in two pieces and biases spill 18 to 23 registers.
 template <int LANES_, int PIECES_, bool SUMMED_> struct HeldGrad { static constexpr int LANES = LANES_, PIECES = PIECES_; static constexpr bool SUMMED = SUMMED_; };
 template <typename T, class Go, class Long> static void with_row_grad(const NormArgs &a, const Go &go, const Long &stream)
 {
     const int64_t n = pieces_of<T>(a.width);
-    if (n <= 1) stream();                          // rows of no more than a piece
+    if (n <= 1) stream();
     else if (n <= 8) go(HeldGrad<8, 1, true>());
     else if (n <= 16) go(HeldGrad<16, 1, true>());
     else if (n <= 32) go(HeldGrad<32, 1, true>());

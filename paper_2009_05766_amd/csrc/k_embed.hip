@@ -6,8 +6,8 @@
 // a fixed order, so that a gradient's bits do not change from run to run.
 //
 // Few tokens: a wave or a workgroup for each token looks through all of them and, if its token is the first of its kind, sums the rows of the others; one launch.
-// Many tokens: they are sorted (stable, by two digits), the sorted ones are cut into chunks of equal length, so that a frequent token is no longer a chain than a rare
-// one, and tokens whose rows end in another chunk than they begin leave partial sums, which are joined in order.
+// Many tokens: they are sorted (stable, by two digits) and the sorted ones cut into chunks of equal length, so that a frequent token's rows are read by as many workgroups as rare ones'; tokens
+// whose rows end in another chunk than they begin leave partial sums, which are joined in order by four groups of lanes: n equal tokens are chains of 32 and of n / 128 additions.
 #include "embed.h"
 #include "piece.h"
 

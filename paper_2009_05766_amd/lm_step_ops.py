@@ -93,7 +93,8 @@ def _laid_out(tensors) -> bytes:
 
 
 class Gradients:
-    """Where a model's gradients lie, for `netmax_grad_norm` and `netmax_clip_grads`: a program whose gradients stay in the same memory lays the list out once.
+    """Where a model's gradients lie, for `netmax_grad_norm` and `netmax_clip_grads`: a program whose gradients stay in the same memory lays the list out once (a sequence of tensors is laid out
+    in every call, 3 us for each: 96 small ones 300 us a call, laid out before 16).
 
     tensors: float32 or bfloat16, of any shapes, rows at one distance, on one GPU; batch: their first dimension counts models (workers), which have a norm each.  out: where the scaled
     gradients go, of the same shapes and types; None: in place.  The tensors are kept alive; one that has other memory, sizes, strides or

@@ -1,5 +1,5 @@
 """Values at which the operators around a language model's layers went wrong once: infinities that nothing norms, products beside the middle of two bfloat16 values, outputs made in inference
-mode.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
+mode; sums of very many rows.  Tolerances as in test_gpu_lm_step_ops.py, where they are not bits."""
 import pytest
 import torch
 
@@ -83,3 +83,20 @@ def test_outputs_made_in_inference_mode():
     assert norm == pytest.approx(32 ** 0.5, rel=E) and bool(((rows[7] * 16 - 1).abs() <= 2.5 * E).all())
     with torch.inference_mode():
         nm.netmax_clip_grads([rows[7]], 1.0)
+
+
+@ops.BOTH
+@pytest.mark.parametrize("n", [2049, 33000, 600000])
+def test_gradient_of_one_frequent_token(n, dtype):
+    """A chunk's 32 rows take at most 31 roundings, a fourth of the chunks n / 128 and one, three more join the fourths and one scales; where a chunk begins or ends with others it is no more."""
+    g = ops.gen(n)
+    dy = ops.normal(g, n, 24, dtype=dtype, mean=1.0)
+    tokens = torch.full((n,), 2, dtype=torch.int32, device="cuda")
+    tokens[5::1000] = 1
+    got = nm.netmax_embed_grad(dy, tokens, 4, scale=1.7)
+    scale = float(torch.tensor(1.7, dtype=ops.F32))
+    for v in (1, 2):
+        rows = dy.double()[tokens == v] * scale
+        want = rows.sum(0)
+        ops.within(got[v], want, (n / 128 + 36) * E * rows.abs().sum(0) + ULP[dtype] * want.abs(), f"token {v}")
+    assert not bool(got[[0, 3]].any())
